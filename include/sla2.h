@@ -233,6 +233,114 @@ int sla2_backward(const sla2_params* params, const void* q, const void* k, const
 int sla2_dense_forward(const sla2_params* params, const void* q, const void* k, const void* v,
                        void* out, void* hip_stream);
 
+/* ---- The steps around the attention in a layer of a diffusion transformer ------------------------------------------------
+ * Rotary positions of q and k on their way into sla2_forward or sla2_dense_forward, and the norms before and after a block
+ * (attention or feed-forward) with its modulation, gate and residual.  Conventions, status codes and streams as above; one
+ * kernel for a forward call, two at most for a backward call, nothing allocated, no atomics: two calls on the same data give
+ * the same bits.  Everything between the stored types is fp32 and rounded once; angles are fp64.  Vectors of channels
+ * (weights, gate, scale, shift) are DEVICE float, 16-byte aligned.  What is NaN or infinite stays in its row, and in the
+ * gradients that are sums over rows.  These entry points are not stages of the profile below. */
+
+/* Pair j of a head: channels (2 j, 2 j + 1), or (j, j + d / 2). */
+typedef enum { SLA2_ROPE_INTERLEAVED = 0, SLA2_ROPE_HALVES = 1 } sla2_rope_pairing;
+/* RMS norm in front of the rotation: x / sqrt(mean(x^2) + eps) (.) weight, the mean over the d channels of a head (weight [d],
+ * the same for all heads) or over the H d channels of a token (weight [H, d]). */
+typedef enum { SLA2_ROPE_NORM_NONE = 0, SLA2_ROPE_NORM_HEAD = 1, SLA2_ROPE_NORM_TOKEN = 2 } sla2_rope_norm;
+
+typedef struct sla2_rope_params {
+  int B, H, N, d;          /* as in sla2_params; d in {64, 128}; SLA2_ROPE_NORM_TOKEN: H d <= 8192 */
+  int dtype;               /* sla2_dtype of q, k, the results and their gradients */
+  int pairing;             /* sla2_rope_pairing */
+  int norm;                /* sla2_rope_norm */
+  float eps;               /* > 0 with a norm */
+  int axis_pairs[3];       /* pairs that turn with the first, second and third axis (time, height, width), in this order;
+                              d / 2 at most in all, the pairs behind them are not rotated.  One axis: {d / 2, 0, 0} */
+  int grid[3];             /* T, Y, X >= 1 (T Y X < 2^31): token n is at origin + (n / (Y X), n / X % Y, n % X), tokens from
+                              T Y X on are not rotated.  All zero: positions are given */
+  int origin[3];           /* of the grid: a later stretch of a stream starts at its own frame.  Zero without a grid */
+  int positions_per_batch; /* given positions: 0: [N, 3], shared; 1: [B, N, 3] */
+  long long in_stride[3];  /* (batch, head, token) element strides of q, k and their gradients; all zero: [B, H, N, d].  As in */
+  long long out_stride[3]; /* sla2_params.  out_stride: of the results and their gradients */
+} sla2_rope_params;
+
+/* Pure host functions.  Bytes of the workspace of sla2_rope_backward (0: params are invalid); and theta^(-i / n) for the i-th
+ * of the n pairs of each axis, 0 for the pairs behind them, into the HOST array freq[d / 2]: the usual frequencies, for the
+ * caller to change as its model wants and to upload.  theta > 0. */
+size_t sla2_rope_workspace_bytes(const sla2_rope_params* params);
+int sla2_rope_frequencies(const sla2_rope_params* params, double theta, double* freq);
+
+/* q_out, k_out = rotated (normed) q, k: the angle of pair j is position[axis of j] freq[j], and
+ * (m1, m2) -> (m1 cos - m2 sin, m1 sin + m2 cos).
+ *   k, k_out              both NULL: q alone (k with another number of heads takes a call of its own)
+ *   freq                  DEVICE double [d / 2], radians per position
+ *   positions             DEVICE int32, see positions_per_batch; NULL with a grid
+ *   q_weight, k_weight    of the norm; NULL: ones.  NULL without a norm
+ *   q_out, k_out          written; may be q, k themselves where in_stride and out_stride are the same (the slices of a packed
+ *                         projection, in place); otherwise they must share no element with an input or each other */
+int sla2_rope_forward(const sla2_rope_params* params, const void* q, const void* k, const double* freq, const int32_t* positions,
+                      const float* q_weight, const float* k_weight, void* q_out, void* k_out, void* hip_stream);
+
+/* Gradients of q, k and the weights from those of q_out, k_out.
+ *   q, k                      as in the forward call, not overwritten since; not read without a norm (may be NULL then)
+ *   dq_out, dk_out            layout out_stride;  dk_out, dk both NULL: q alone
+ *   dq, dk                    layout in_stride, written; may be dq_out, dk_out or q, k themselves where the strides are the same
+ *   dq_weight, dk_weight      DEVICE float [d] or [H, d], written; NULL: not wanted.  NULL without a norm
+ *   workspace                 sla2_rope_workspace_bytes(), 256-byte aligned; NULL where neither is wanted */
+int sla2_rope_backward(const sla2_rope_params* params, const void* q, const void* k, const double* freq, const int32_t* positions,
+                       const float* q_weight, const float* k_weight, const void* dq_out, const void* dk_out, void* dq, void* dk,
+                       float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* norm(v) = (v - mean(v)) / sqrt(var(v) + eps) (layer), v / sqrt(mean(v^2) + eps) (rms), v (none), over the C channels of a token. */
+typedef enum { SLA2_NORM_NONE = 0, SLA2_NORM_RMS = 1, SLA2_NORM_LAYER = 2 } sla2_norm_kind;
+/* gate, scale and shift: one vector of C channels for each batch, for each token, or one in all. */
+typedef enum { SLA2_MOD_BATCH = 0, SLA2_MOD_TOKEN = 1, SLA2_MOD_SHARED = 2 } sla2_mod_layout;
+
+typedef struct sla2_norm_params {
+  int B, N, C;             /* x, y, h are [B, N, C]; B <= 65535; C a multiple of 8, at most 8192 */
+  int dtype_x;             /* sla2_dtype of the residual stream (x, x_out and their gradients) */
+  int dtype_h;             /* of the block's output y and input h (and their gradients); SLA2_F32 only with an fp32 stream */
+  int norm_in, norm_out;   /* sla2_norm_kind before the block (of the stream) and after it (of y) */
+  float eps;               /* > 0 with a norm */
+  float residual_scale;    /* rho; finite */
+  int mod_layout;          /* sla2_mod_layout */
+  /* (batch, token) element strides of x, x_out, dx_out, dx and of y, h, dh, dy; both zero: contiguous.  Positive, multiples of
+   * 16 bytes, the token stride at least C; the caller guarantees that they describe memory it owns. */
+  long long x_stride[2];
+  long long h_stride[2];
+  /* of gate, scale, shift and their gradients: the slices of a [B, 6, C] modulation have (6 C, 0), those of [B, N, 6, C]
+   * (6 N C, 6 C).  Both zero: contiguous [B, C] or [B, N, C].  Multiples of 4, at least C; SLA2_MOD_SHARED: zero */
+  long long mod_stride[2];
+} sla2_norm_params;
+
+/* Bytes of the workspace of sla2_norm_backward; 0: params are invalid.  Pure host function. */
+size_t sla2_norm_workspace_bytes(const sla2_norm_params* params);
+
+/* The step between two blocks:
+ *   x_out = residual_scale x + gate (.) norm_out(y) (.) out_weight          (after a block)
+ *   h     = norm_in(x_out) (.) in_weight (.) (1 + scale) + shift             (before the next)
+ *   y, x_out     both NULL: nothing comes before (h is taken of x, which is not written; gate and out_weight NULL)
+ *   h            NULL: nothing follows (in_weight, scale and shift NULL)
+ *   gate, scale, shift, out_weight, in_weight      NULL: 1, 0, 0, 1, 1
+ * x_out may be x and h may be y (in place); otherwise they share no element with an input.  h is taken of x_out as stored:
+ * the one call gives the bits of the two. */
+int sla2_norm_forward(const sla2_norm_params* params, const void* x, const void* y, const float* gate, const float* out_weight,
+                      void* x_out, const float* in_weight, const float* scale, const float* shift, void* h, void* hip_stream);
+
+/* Gradients of that step.
+ *   x            what norm_in was taken of in the forward call: x_out, or x where there was no y.  Not read where dh is NULL
+ *   y            as in the forward call (NULL, with dy, where there was none)
+ *   dh           gradient of h; NULL where there was no h
+ *   dx_out       gradient that x_out (x where there was no y) has besides, from where else it is read: the residual; NULL: none
+ *   dx, dy       written.  dx may be dx_out or x, dy may be dh or y (in place)
+ *   dgate, dscale, dshift          in mod_layout, written; for SLA2_MOD_BATCH and _SHARED summed over what shares them
+ *   dout_weight, din_weight        DEVICE float [C], written
+ * Each of these five may be NULL (not wanted); one without its input (dgate without gate, ...; dshift without dh) is refused.
+ *   workspace    sla2_norm_workspace_bytes(), 256-byte aligned; NULL where none of the five is wanted */
+int sla2_norm_backward(const sla2_norm_params* params, const void* x, const void* y, const float* gate, const float* out_weight,
+                       const float* in_weight, const float* scale, const void* dh, const void* dx_out, void* dx, void* dy,
+                       float* dgate, float* dout_weight, float* din_weight, float* dscale, float* dshift, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
 /* Per-kernel timing for benchmarks (not part of the operator).  While no profile is open the other entry
  * points share no mutable host state and may be called from several threads; between sla2_profile_begin
  * and sla2_profile_end all calls must come from one thread.

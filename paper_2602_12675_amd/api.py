@@ -8,6 +8,7 @@ import of this module fails: there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -21,11 +22,17 @@ QUANT_MODES = {"none": SLA2_QUANT_NONE, "fp8": SLA2_QUANT_FP8, "int8": SLA2_QUAN
                "fp8v": SLA2_QUANT_FP8_V}   # workload name -> sla2_quant
 SLA2_FLAG_NO_SMOOTH_K = 1
 SLA2_FLAG_SAVE_FOR_BACKWARD = 2
+SLA2_ROPE_INTERLEAVED, SLA2_ROPE_HALVES = 0, 1
+SLA2_ROPE_NORM_NONE, SLA2_ROPE_NORM_HEAD, SLA2_ROPE_NORM_TOKEN = 0, 1, 2
+SLA2_NORM_NONE, SLA2_NORM_RMS, SLA2_NORM_LAYER = 0, 1, 2
+SLA2_MOD_BATCH, SLA2_MOD_TOKEN, SLA2_MOD_SHARED = 0, 1, 2
 SLA2_OK, SLA2_EINVAL, SLA2_EUNSUPPORTED, SLA2_EWORKSPACE, SLA2_EALIAS, SLA2_EHIP = 0, -1, -2, -3, -4, -5
 
 SLA2_STATIC_SCRATCH_BYTES = 32 << 20
 EXPORTS = ("sla2_workspace_bytes", "sla2_workspace_layout", "sla2_num_selected", "sla2_router", "sla2_router_static",
-           "sla2_router_soft", "sla2_forward", "sla2_backward", "sla2_dense_forward", "sla2_profile_begin", "sla2_profile_begin_sampled",
+           "sla2_router_soft", "sla2_forward", "sla2_backward", "sla2_dense_forward", "sla2_rope_workspace_bytes",
+           "sla2_rope_frequencies", "sla2_rope_forward", "sla2_rope_backward", "sla2_norm_workspace_bytes", "sla2_norm_forward",
+           "sla2_norm_backward", "sla2_profile_begin", "sla2_profile_begin_sampled",
            "sla2_profile_end",
            "sla2_strerror", "sla2_version")
 
@@ -48,6 +55,22 @@ class WsLayout(ctypes.Structure):
                 ("q_sum", "k_sum", "k_mean", "router_m", "block_idx", "h_total", "z_total",
                  "k_stats", "k_phi", "z_blocks", "k_fp8", "k_scale", "v_fp8", "v_scale", "partial",
                  "o_s", "o_l", "lse", "bwd", "total")]
+
+
+class RopeParams(ctypes.Structure):
+    """struct sla2_rope_params"""
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("N", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("pairing", ctypes.c_int), ("norm", ctypes.c_int), ("eps", ctypes.c_float), ("axis_pairs", ctypes.c_int * 3),
+                ("grid", ctypes.c_int * 3), ("origin", ctypes.c_int * 3), ("positions_per_batch", ctypes.c_int),
+                ("in_stride", ctypes.c_longlong * 3), ("out_stride", ctypes.c_longlong * 3)]
+
+
+class NormParams(ctypes.Structure):
+    """struct sla2_norm_params"""
+    _fields_ = [("B", ctypes.c_int), ("N", ctypes.c_int), ("C", ctypes.c_int), ("dtype_x", ctypes.c_int), ("dtype_h", ctypes.c_int),
+                ("norm_in", ctypes.c_int), ("norm_out", ctypes.c_int), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("mod_layout", ctypes.c_int), ("x_stride", ctypes.c_longlong * 2), ("h_stride", ctypes.c_longlong * 2),
+                ("mod_stride", ctypes.c_longlong * 2)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -73,6 +96,21 @@ _lib.sla2_backward.restype = ctypes.c_int
 _lib.sla2_backward.argtypes = [_pp] + [_vp] * 10 + [ctypes.c_size_t, _vp]
 _lib.sla2_dense_forward.restype = ctypes.c_int
 _lib.sla2_dense_forward.argtypes = [_pp, _vp, _vp, _vp, _vp, _vp]
+_rp, _np = ctypes.POINTER(RopeParams), ctypes.POINTER(NormParams)
+_lib.sla2_rope_workspace_bytes.restype = ctypes.c_size_t
+_lib.sla2_rope_workspace_bytes.argtypes = [_rp]
+_lib.sla2_rope_frequencies.restype = ctypes.c_int
+_lib.sla2_rope_frequencies.argtypes = [_rp, ctypes.c_double, _vp]
+_lib.sla2_rope_forward.restype = ctypes.c_int
+_lib.sla2_rope_forward.argtypes = [_rp] + [_vp] * 9
+_lib.sla2_rope_backward.restype = ctypes.c_int
+_lib.sla2_rope_backward.argtypes = [_rp] + [_vp] * 13 + [ctypes.c_size_t, _vp]
+_lib.sla2_norm_workspace_bytes.restype = ctypes.c_size_t
+_lib.sla2_norm_workspace_bytes.argtypes = [_np]
+_lib.sla2_norm_forward.restype = ctypes.c_int
+_lib.sla2_norm_forward.argtypes = [_np] + [_vp] * 10
+_lib.sla2_norm_backward.restype = ctypes.c_int
+_lib.sla2_norm_backward.argtypes = [_np] + [_vp] * 16 + [ctypes.c_size_t, _vp]
 _lib.sla2_profile_begin.restype = ctypes.c_int
 _lib.sla2_profile_begin.argtypes = [ctypes.c_uint, ctypes.c_int]
 _lib.sla2_profile_begin_sampled.restype = ctypes.c_int
@@ -198,6 +236,171 @@ def sla2_dense_forward(params, q, k, v, out, stream=None, check=True) -> int:
     if check and rc != SLA2_OK:
         raise Sla2Error(rc)
     return rc
+
+
+# ---- the steps around the attention --------------------------------------------------------------------------------
+def make_rope_params(B, H, N, d, axis_pairs, grid=(0, 0, 0), origin=(0, 0, 0), dtype=SLA2_BF16, pairing=SLA2_ROPE_INTERLEAVED,
+                     norm=SLA2_ROPE_NORM_NONE, eps=1e-6, positions_per_batch=0, in_stride=None, out_stride=None) -> RopeParams:
+    """axis_pairs: pairs of channels that turn with the time, height and width axis.  in_stride / out_stride: (batch, head, token)
+    element strides of q, k and their gradients / of the results and theirs; None = contiguous [B, H, N, d]."""
+    p = RopeParams(B, H, N, d, dtype, pairing, norm, eps)
+    p.axis_pairs[:], p.grid[:], p.origin[:] = axis_pairs, grid, origin
+    p.positions_per_batch = positions_per_batch
+    if in_stride is not None:
+        p.in_stride[:] = [int(x) for x in in_stride]
+    if out_stride is not None:
+        p.out_stride[:] = [int(x) for x in out_stride]
+    return p
+
+
+def make_norm_params(B, N, C, dtype_x=SLA2_BF16, dtype_h=SLA2_BF16, norm_in=SLA2_NORM_LAYER, norm_out=SLA2_NORM_NONE, eps=1e-6,
+                     residual_scale=1.0, mod_layout=SLA2_MOD_BATCH, x_stride=None, h_stride=None, mod_stride=None) -> NormParams:
+    """x_stride, h_stride, mod_stride: (batch, token) element strides of the residual stream, of the block's input and output, and of
+    gate, scale and shift; None = contiguous."""
+    p = NormParams(B, N, C, dtype_x, dtype_h, norm_in, norm_out, eps, residual_scale, mod_layout)
+    for dst, src in ((p.x_stride, x_stride), (p.h_stride, h_stride), (p.mod_stride, mod_stride)):
+        if src is not None:
+            dst[:] = [int(x) for x in src]
+    return p
+
+
+_TYPES = {SLA2_F32: torch.float32, SLA2_BF16: torch.bfloat16}
+
+
+def _held(t, dtype, count):
+    """The address of t, once it is seen to have the element type and at least the number of elements that the kernels will
+    take it to have: a tensor that has not would be read or written out of bounds.  (Its strides are the caller's to state.)"""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype != dtype or t.numel() < count:
+        raise Sla2Error(SLA2_EINVAL)
+    return t.data_ptr()
+
+
+def _vector(t):
+    """A vector of channels, frequencies or positions: contiguous besides."""
+    if t is not None and not isinstance(t, int) and not t.is_contiguous():
+        raise Sla2Error(SLA2_EINVAL)
+    return t
+
+
+def _one_device(tensors):
+    """The device of the tensors, which is one for all."""
+    dev = None
+    for t in tensors:
+        if t is not None and not isinstance(t, int):
+            if dev is None:
+                dev = t.device
+            elif t.device != dev:
+                raise Sla2Error(SLA2_EINVAL)
+    return dev
+
+
+def _launch(fn, args, tensors, stream, check):
+    """Calls fn on the tensors' device, on `stream` or that device's current one."""
+    dev = _one_device(tensors)
+    if dev is None or dev.type != "cuda" or dev.index == torch.cuda.current_device():
+        rc = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _stream(stream))
+    if check and rc != SLA2_OK:
+        raise Sla2Error(rc)
+    return rc
+
+
+def _entry(fn):
+    """check=False: a refusal of the binding's own comes back as a status, as the library's do."""
+    @functools.wraps(fn)
+    def call(*args, check=True, **kw):
+        try:
+            return fn(*args, check=check, **kw)
+        except Sla2Error as e:
+            if check:
+                raise
+            return e.status
+    return call
+
+
+def _bytes(workspace, ws_bytes):
+    if ws_bytes is not None:                           # a raw address needs its size spelled out
+        return ws_bytes
+    return workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def sla2_rope_workspace_bytes(params: RopeParams) -> int:
+    return _lib.sla2_rope_workspace_bytes(ctypes.byref(params))
+
+
+def sla2_rope_frequencies(params: RopeParams, theta: float = 10000.0) -> torch.Tensor:
+    """-> float64 [d / 2] on the host"""
+    out = torch.empty(max(params.d, 2) // 2, dtype=torch.float64)
+    rc = _lib.sla2_rope_frequencies(ctypes.byref(params), float(theta), out.data_ptr())
+    if rc != SLA2_OK:
+        raise Sla2Error(rc)
+    return out
+
+
+def _rope_sizes(p):
+    """(elements of q, of a weight, of the positions; element type)"""
+    return (p.B * p.H * p.N * p.d, p.H * p.d if p.norm == SLA2_ROPE_NORM_TOKEN else p.d, 3 * p.N * (p.B if p.positions_per_batch else 1),
+            _TYPES.get(p.dtype))
+
+
+@_entry
+def sla2_rope_forward(params, q, k, freq, q_out, k_out, q_weight=None, k_weight=None, positions=None, stream=None, check=True) -> int:
+    n, w, np_, dt = _rope_sizes(params)
+    args = (ctypes.byref(params), _held(q, dt, n), _held(k, dt, n), _held(_vector(freq), torch.float64, params.d // 2),
+            _held(_vector(positions), torch.int32, np_), _held(_vector(q_weight), torch.float32, w),
+            _held(_vector(k_weight), torch.float32, w), _held(q_out, dt, n), _held(k_out, dt, n))
+    return _launch(_lib.sla2_rope_forward, args, (q, k, freq, positions, q_weight, k_weight, q_out, k_out), stream, check)
+
+
+@_entry
+def sla2_rope_backward(params, q, k, freq, dq_out, dk_out, dq, dk, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
+                       positions=None, workspace=None, stream=None, check=True, ws_bytes=None) -> int:
+    n, w, np_, dt = _rope_sizes(params)
+    args = (ctypes.byref(params), _held(q, dt, n), _held(k, dt, n), _held(_vector(freq), torch.float64, params.d // 2),
+            _held(_vector(positions), torch.int32, np_), _held(_vector(q_weight), torch.float32, w),
+            _held(_vector(k_weight), torch.float32, w), _held(dq_out, dt, n), _held(dk_out, dt, n), _held(dq, dt, n), _held(dk, dt, n),
+            _held(_vector(dq_weight), torch.float32, w), _held(_vector(dk_weight), torch.float32, w), _ptr(workspace),
+            _bytes(workspace, ws_bytes))
+    return _launch(_lib.sla2_rope_backward, args, (q, k, freq, positions, q_weight, k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight,
+                                                   workspace), stream, check)
+
+
+def sla2_norm_workspace_bytes(params: NormParams) -> int:
+    return _lib.sla2_norm_workspace_bytes(ctypes.byref(params))
+
+
+def _norm_sizes(p):
+    """(elements of x, of a modulation; element types of x and of h)"""
+    rows = {SLA2_MOD_BATCH: p.B, SLA2_MOD_TOKEN: p.B * p.N}.get(p.mod_layout, 1)
+    return p.B * p.N * p.C, rows * p.C, _TYPES.get(p.dtype_x), _TYPES.get(p.dtype_h)
+
+
+@_entry
+def sla2_norm_forward(params, x, h, y=None, x_out=None, gate=None, out_weight=None, in_weight=None, scale=None, shift=None, stream=None,
+                      check=True) -> int:
+    n, m, tx, th = _norm_sizes(params)
+    f32, c = torch.float32, params.C
+    args = (ctypes.byref(params), _held(x, tx, n), _held(y, th, n), _held(gate, f32, m), _held(_vector(out_weight), f32, c),
+            _held(x_out, tx, n), _held(_vector(in_weight), f32, c), _held(scale, f32, m), _held(shift, f32, m), _held(h, th, n))
+    return _launch(_lib.sla2_norm_forward, args, (x, y, gate, out_weight, x_out, in_weight, scale, shift, h), stream, check)
+
+
+@_entry
+def sla2_norm_backward(params, x, dh, dx_out, dx, y=None, gate=None, out_weight=None, in_weight=None, scale=None, dy=None, dgate=None,
+                       dout_weight=None, din_weight=None, dscale=None, dshift=None, workspace=None, stream=None, check=True,
+                       ws_bytes=None) -> int:
+    n, m, tx, th = _norm_sizes(params)
+    f32, c = torch.float32, params.C
+    args = (ctypes.byref(params), _held(x, tx, n), _held(y, th, n), _held(gate, f32, m), _held(_vector(out_weight), f32, c),
+            _held(_vector(in_weight), f32, c), _held(scale, f32, m), _held(dh, th, n), _held(dx_out, tx, n), _held(dx, tx, n),
+            _held(dy, th, n), _held(dgate, f32, m), _held(_vector(dout_weight), f32, c), _held(_vector(din_weight), f32, c),
+            _held(dscale, f32, m), _held(dshift, f32, m), _ptr(workspace), _bytes(workspace, ws_bytes))
+    return _launch(_lib.sla2_norm_backward, args, (x, y, gate, out_weight, in_weight, scale, dh, dx_out, dx, dy, dgate, dout_weight,
+                                                   din_weight, dscale, dshift, workspace), stream, check)
 
 
 def sla2_profile_begin(stages, max_calls: int) -> None:

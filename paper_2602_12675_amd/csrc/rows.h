@@ -1,0 +1,228 @@
+// Rows of channels in registers: what the kernels around the attention share (sla2_rope.hip, sla2_norm.hip).
+//
+// A row (the channels of a token, or of some of its heads) is read once, in chunks of 8 channels, by a team: `lanes` neighbouring lanes
+// of a wave (8, 16, 32 or 64), or several whole waves, each thread holding V chunks, chunk l + v T being thread l's of T.  Everything
+// these kernels do is bound by memory, so a row stays in registers from its load to the store of what is made of it, and a workgroup
+// goes on with other rows of the same batch, whose modulation, gate or weights it then holds already.  The sums of a row are kept in
+// fp32; within a wave they are vector instructions only, and where a team has several waves these exchange all sums of a step through
+// LDS at once, behind one barrier.
+#pragma once
+#include "common.h"
+
+namespace sla2 {
+
+constexpr int kChunk = 8;                    // channels: 16 bytes of bf16
+constexpr int kMaxRow = 8192;                // channels of a row: 8 waves of 2 chunks a lane
+constexpr int kTeamThreads = 512;            // most threads of a workgroup
+
+// How a row of `chunks` chunks is spread over threads.
+struct RowTeam {
+  int lanes, waves, vec;                     // lanes of a wave, whole waves (1 where lanes < 64), chunks a thread
+  __host__ __device__ int threads() const { return lanes * waves; }
+};
+// The fewest places without a chunk; of two ways that leave equally many the one with fewer waves.
+inline RowTeam row_team(int chunks) {
+  RowTeam t{64, 1, 1};
+  if (chunks <= 64) {
+    while (t.lanes > 8 && t.lanes / 2 >= chunks) t.lanes /= 2;
+    return t;
+  }
+  const int rounds = (chunks + 63) / 64;     // of a whole wave
+  t.vec = rounds % 2 == 0 || rounds > kTeamThreads / 64 ? 2 : 1;
+  t.waves = (rounds + t.vec - 1) / t.vec;
+  return t;
+}
+
+// 8 neighbouring elements as they are stored, and as fp32.
+template <bool BF16> struct Raw {
+  u32x4 a[BF16 ? 1 : 2];
+};
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+template <bool BF16> __device__ __forceinline__ size_t elem_bytes() { return BF16 ? 2 : 4; }
+template <bool BF16> __device__ __forceinline__ Raw<BF16> load8(const void* p, size_t elem) {
+  const u32x4* a = (const u32x4*)((const char*)p + elem * elem_bytes<BF16>());
+  Raw<BF16> r;
+  r.a[0] = a[0];
+  if constexpr (!BF16) r.a[1] = a[1];
+  return r;
+}
+template <bool BF16> __device__ __forceinline__ Raw<BF16> zero8() {
+  Raw<BF16> r;
+  r.a[0] = u32x4{0, 0, 0, 0};
+  if constexpr (!BF16) r.a[1] = u32x4{0, 0, 0, 0};
+  return r;
+}
+template <bool BF16> __device__ __forceinline__ void store8(void* p, size_t elem, const Raw<BF16>& r) {
+  u32x4* a = (u32x4*)((char*)p + elem * elem_bytes<BF16>());
+  a[0] = r.a[0];
+  if constexpr (!BF16) a[1] = r.a[1];
+}
+template <bool BF16> __device__ __forceinline__ void unpack8(const Raw<BF16>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const unsigned u = BF16 ? r.a[0][i / 2] : r.a[i / 4 % (BF16 ? 1 : 2)][i % 4];
+    x[i] = __builtin_bit_cast(float, !BF16 ? u : i % 2 ? u & 0xffff0000u : u << 16);
+  }
+}
+template <bool BF16> __device__ __forceinline__ Raw<BF16> pack8(const float (&x)[8]) {   // bf16: to the nearest, ties to even
+  Raw<BF16> r;
+  if constexpr (BF16) {
+    const f32x8 f = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+    r.a[0] = __builtin_bit_cast(u32x4, __builtin_convertvector(f, bf16x8));
+  } else {
+    r.a[0] = __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]});
+    r.a[1] = __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]});
+  }
+  return r;
+}
+// 8 fp32 values of a vector of channels that may be absent
+__device__ __forceinline__ void load_vector8(const float* p, size_t elem, float absent, float (&x)[8]) {
+  if (p) {
+    unpack8<false>(load8<false>(p, elem), x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = absent;
+  }
+}
+
+// Sum over `lanes` neighbouring lanes (8, 16, 32, 64; the same for the whole launch), on all of them.
+__device__ __forceinline__ float lanes_sum(float x, int lanes) {
+  x = row_sum<8>(x);
+  if (lanes > 8) x += dpp_move<0x140>(x);              // row_mirror
+  if (lanes > 16) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+  }
+  if (lanes > 32) x = swap_halves_sum(x);
+  return x;
+}
+
+// A thread's place in its team.  Every thread of a workgroup takes part in every exchange, so all its teams make equally many steps.
+constexpr int kExchange = 4;                 // sums that a step exchanges at most
+constexpr int kExchangeFloats = 2 * (kTeamThreads / kWave) * kExchange;
+struct Team {
+  RowTeam t;
+  int team, lane;                            // which team of the workgroup; thread of the team
+  float* lds;                                // kExchangeFloats floats
+  int flip = 0;
+  __device__ Team(const RowTeam& t_, float* lds_) : t(t_), lds(lds_) {
+    team = (int)threadIdx.x / t.threads();
+    lane = (int)threadIdx.x - team * t.threads();
+  }
+  // x[k] of every wave of the team -> f(wave of the team, its x).  Two buffers in turn: the next exchange but one writes over this one's,
+  // behind the barrier of the next, which every wave reaches after its reads.
+  template <int K, class F> __device__ __forceinline__ void exchange(const float (&x)[K], F f) {
+    static_assert(K <= kExchange, "");
+    float* m = lds + flip * (kExchangeFloats / 2);
+    flip ^= 1;
+    const int wave = (int)threadIdx.x / kWave;
+    if ((int)threadIdx.x % kWave == 0) {
+#pragma unroll
+      for (int k = 0; k < K; k++) m[wave * K + k] = x[k];
+    }
+    __syncthreads();
+    const float* first = m + team * t.waves * K;
+    for (int w = 0; w < t.waves; w++) f(w, first + w * K);
+  }
+  // what the waves of the team gave the last exchange, of K
+  template <int K> __device__ __forceinline__ const float* last() const { return lds + (flip ^ 1) * (kExchangeFloats / 2) + team * t.waves * K; }
+  // sums over the team
+  template <int K> __device__ __forceinline__ void sum(float (&x)[K]) {
+#pragma unroll
+    for (int k = 0; k < K; k++) x[k] = lanes_sum(x[k], t.lanes);
+    if (t.waves == 1) return;
+    float s[K];
+#pragma unroll
+    for (int k = 0; k < K; k++) s[k] = 0.f;
+    exchange(x, [&](int, const float* o) {
+#pragma unroll
+      for (int k = 0; k < K; k++) s[k] += o[k];
+    });
+#pragma unroll
+    for (int k = 0; k < K; k++) x[k] = s[k];
+  }
+  // channels that wave w of the team holds of a row of `chunks` chunks
+  __device__ __forceinline__ float channels(int w, int chunks) const {
+    int n = 0;
+    for (int v = 0; v < t.vec; v++) {
+      const int left = chunks - v * t.threads() - w * kWave;
+      n += left < 0 ? 0 : left > t.lanes ? t.lanes : left;
+    }
+    return (float)(n * kChunk);
+  }
+};
+
+// ---- sums of the columns of a matrix, as both backward passes end: out[c] = factor[c] * sum over rows of (plus + weight[row][c]) rows[row][c] ----
+struct ColumnJob {
+  const float* rows;                         // [batches][count][columns]
+  int batches, count;
+  const float* factor;                       // [columns], or null: 1
+  const float* weight;                       // a vector of channels for every `per_weight` rows, weight_stride apart; null: 1
+  float plus;
+  int per_weight;
+  long long weight_stride;
+  float* out;                                // [batches], out_stride apart
+  long long out_stride;
+};
+constexpr int kMaxJobs = 5;
+struct ColumnJobs {
+  ColumnJob job[kMaxJobs];
+  int jobs, columns;
+};
+hipError_t launch_column_sums(const ColumnJobs& j, hipStream_t stream);
+
+// ---- q and k: RMS norm and rotation ----
+struct HeadStrides {
+  long long b, h, n;
+};
+struct RopeArgs {
+  const void* x[2];                          // q, k (k: null where there is none)
+  const void* dy[2];                         // backward: gradients of the results
+  void* y[2];                                // results; backward: gradients of x
+  const float* weight[2];                    // [d] or [H, d], or null
+  const double* freq;                        // [d / 2]
+  const int32_t* positions;                  // [N, 3] or [B, N, 3], or null: the grid
+  float* partial;                            // backward with a norm: [2][workgroups][d or H d], or null: no gradient of the weights
+  float* dweight[2];
+  int tensors, B, H, N, d;
+  int pairs_end[3];                          // of the axes, one behind the last pair of each
+  int grid[3], origin[3];
+  long long positions_stride;                // of a batch
+  HeadStrides sin, sout;                     // of x (and its gradient); of the results (and their gradients)
+  float eps;
+  int norm;                                  // sla2_rope_norm
+  bool bf16, halves;
+  float sign;                                // of the angles
+  // launch
+  RowTeam team;
+  int teams, heads, groups, walkers;         // teams of a workgroup; heads of a row, rows of a token; workgroups of a (batch, group)
+};
+void plan_rope(RopeArgs* a);                 // fills in the launch from the sizes
+size_t rope_partial_floats(const RopeArgs& a);
+hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
+hipError_t launch_rope_bwd(const RopeArgs& a, hipStream_t stream);
+
+// ---- norms around a block ----
+struct NormArgs {
+  const void *x, *y;                         // backward: x is what norm_in was taken of
+  const float *gate, *out_weight, *in_weight, *scale, *shift;
+  void *x_out, *h;
+  // backward
+  const void *dh, *dx_out;
+  void *dx, *dy;
+  float *dgate, *dout_weight, *din_weight, *dscale, *dshift;
+  float* partial;                            // [3][B * walkers][C]: sums for scale, shift, gate of the rows of a workgroup
+  int B, N, C;
+  long long x_b, x_n, h_b, h_n, mod_b, mod_n;
+  int norm_in, norm_out, mods;               // sla2_norm_kind, sla2_mod_layout
+  float eps, rho;
+  bool x_bf16, h_bf16;
+  RowTeam team;
+  int teams, walkers;                        // teams of a workgroup; workgroups of a batch
+};
+void plan_norm(NormArgs* a, bool backward);
+hipError_t launch_norm(const NormArgs& a, hipStream_t stream);
+hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream);
+
+}  // namespace sla2

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "common.h"
+#include "host_checks.h"
 #include "masked_sums.h"
 
 namespace sla2 {
@@ -216,12 +217,6 @@ static size_t span_bytes(const Shape& s, const Strides& st) {
                        (size_t)(s.N - 1) * (size_t)st.n + (size_t)s.d;
   return elems * (s.bf16 ? 2 : 4);
 }
-static bool misaligned16(const void* p) { return ((uintptr_t)p & 15u) != 0; }
-
-static bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + nb && y < x + na;
-}
 
 // Two tensors of the same strides whose address ranges interleave (slices of one packed projection,
 // [.., N, x, H, d]): they are disjoint when every token period holds each of them in its own stretch.
@@ -230,11 +225,7 @@ static bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
 static bool interleaved_disjoint(const Shape& s, const Strides& st, const void* a, const void* b) {
   const long long esz = s.bf16 ? 2 : 4, period = st.n;
   if (st.h < s.d || (s.B > 1 && st.b % period != 0)) return false;
-  const long long extent = (long long)(s.H - 1) * st.h + s.d;
-  if (extent > period) return false;
-  const long long delta = ((long long)(intptr_t)b - (long long)(intptr_t)a) / esz;
-  const long long r = ((delta % period) + period) % period;
-  return r >= extent && r <= period - extent;
+  return stretches_disjoint(a, b, esz, period, (long long)(s.H - 1) * st.h + s.d);
 }
 
 static int check_workspace(size_t need, const void* ws, size_t bytes) {

@@ -1,0 +1,369 @@
+// q and k on their way into the attention: RMS norm over a head or over all heads of a token, then rotary positions of up to three axes.
+//   m = x r w,  r = 1 / sqrt(mean(x^2) + eps);   pair j of a head, of axis a(j):  angle = p_a(j)(token) f_j,
+//   (m_1, m_2) -> (m_1 cos - m_2 sin, m_1 sin + m_2 cos)
+// and backward, with g = the gradient turned back by the angle, n = x r, t = g w:  dw = sum g n,  dx = r (t - n mean(t n)).
+//
+// A row is a token with all its heads (as many as kMaxRow channels hold, where no sum goes over them), of q and of k: one reading of
+// each, one writing, and the angles are formed once for all heads of both.  A thread's chunks all lie at the same channels of their
+// heads, so it needs 4 angles (pairs of neighbours) or 8 (halves: the partner's channels come from a lane 4 or 8 further, by vector
+// instructions).  Angles are products in fp64, taken as fractions of a turn with the whole turns off before the rounding to fp32: a
+// position of 2^31 is as exact as fp64 has it.
+#include "rows.h"
+
+namespace sla2 {
+
+// x of the lane that holds the other channel of each pair of a head of LANES lanes
+template <int LANES> __device__ __forceinline__ float half_head_away(float x) {
+  if constexpr (LANES == 16) return rotate16<8>(x);
+  else return dpp_move<0x1B>(dpp_move<0x141>(x));           // row_half_mirror (l ^ 7), quad_perm 3 2 1 0 (l ^ 3)
+}
+
+// The angles of a thread: cos and sin of those of a token.
+template <bool BF16, bool HALVES> struct Angles {
+  static constexpr int kPairs = HALVES ? 8 : 4;
+  double turns[kPairs];                      // of a pair per position
+  int axis[kPairs];
+  float c[kPairs], s[kPairs];
+  __device__ __forceinline__ void init(const RopeArgs& a, int chunk) {
+    const int first = HALVES ? chunk * kChunk % (a.d / 2) : chunk % (a.d / kChunk) * 4;
+#pragma unroll
+    for (int i = 0; i < kPairs; i++) {
+      const int j = first + i;
+      turns[i] = j < a.pairs_end[2] ? a.freq[j] * 0.15915494309189533577 : 0.0;       // 1 / (2 pi)
+      axis[i] = j < a.pairs_end[0] ? 0 : j < a.pairs_end[1] ? 1 : 2;
+    }
+  }
+  // bf16 results: the hardware's sine and cosine of a fraction of a turn, whose error is far below half a step of bf16
+  __device__ __forceinline__ void at(int p0, int p1, int p2, float sign) {
+#pragma unroll
+    for (int i = 0; i < kPairs; i++) {
+      const int p = axis[i] == 0 ? p0 : axis[i] == 1 ? p1 : p2;
+      const double t = (double)p * turns[i];
+      const float f = (float)(t - rint(t));
+      if constexpr (BF16) {
+        s[i] = __builtin_amdgcn_sinf(f);
+        c[i] = __builtin_amdgcn_cosf(f);
+      } else {
+        sincospif(2.f * f, &s[i], &c[i]);
+      }
+      s[i] *= sign;
+    }
+  }
+};
+
+// Where token n of batch b is.
+__device__ __forceinline__ void position(const RopeArgs& a, int b, int n, int& p0, int& p1, int& p2) {
+  if (a.positions) {
+    const int32_t* p = a.positions + b * a.positions_stride + 3ll * n;
+    p0 = p[0]; p1 = p[1]; p2 = p[2];
+  } else {
+    const unsigned x = (unsigned)a.grid[2], yx = (unsigned)a.grid[1] * x, t = (unsigned)n / yx, r = (unsigned)n - t * yx;
+    const bool in = t < (unsigned)a.grid[0];
+    p0 = in ? a.origin[0] + (int)t : 0;
+    p1 = in ? a.origin[1] + (int)(r / x) : 0;
+    p2 = in ? a.origin[2] + (int)(r % x) : 0;
+  }
+}
+
+template <bool BF16, bool HALVES>
+__device__ __forceinline__ void turn(const RopeArgs& a, const Angles<BF16, HALVES>& an, bool second, float (&x)[8]) {
+  if constexpr (HALVES) {
+    float o[8];
+    if (a.d == 128) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) o[i] = half_head_away<16>(x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) o[i] = half_head_away<8>(x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = x[i] * an.c[i] + (second ? o[i] : -o[i]) * an.s[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float p = x[2 * i], q = x[2 * i + 1];
+      x[2 * i] = p * an.c[i] - q * an.s[i];
+      x[2 * i + 1] = p * an.s[i] + q * an.c[i];
+    }
+  }
+}
+
+__device__ __forceinline__ float head_sum(float x, int d) { return d == 128 ? row_sum<16>(x) : row_sum<8>(x); }
+
+// What a thread holds of its rows: V chunks of heads.
+template <int V> struct Place {
+  bool has[V];
+  size_t in[V], out[V];                      // offsets from the token
+  int col[V];                                // channel among all heads
+  int channel;                               // of its chunks in their heads
+  __device__ __forceinline__ Place(const RopeArgs& a, const Team& tm, int group) {
+    const int per_head = a.d / kChunk;
+    channel = tm.lane % per_head * kChunk;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const int c = tm.lane + v * a.team.threads(), head = group * a.heads + c / per_head;
+      has[v] = tm.team < a.teams && c < a.heads * per_head && head < a.H;
+      const int h = has[v] ? head : 0;
+      in[v] = (size_t)h * a.sin.h + channel;
+      out[v] = (size_t)h * a.sout.h + channel;
+      col[v] = has[v] ? h * a.d + channel : 0;
+    }
+  }
+};
+
+template <int V, bool BF16, bool HALVES, int NORM>
+__global__ __launch_bounds__(kTeamThreads) void rope_kernel(RopeArgs a) {
+  __shared__ float lds[kExchangeFloats];
+  constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
+  Team tm(a.team, lds);
+  const int part = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers, b = part / a.groups;
+  const Place<V> at(a, tm, part % a.groups);
+  const bool second = at.channel >= a.d / 2;
+  Angles<BF16, HALVES> an;
+  an.init(a, tm.lane);
+  float w[2][W][8];
+  if (NORM != SLA2_ROPE_NORM_NONE) {
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int v = 0; v < W; v++) load_vector8(a.weight[t], NORM == SLA2_ROPE_NORM_TOKEN ? at.col[v] : at.channel, 1.f, w[t][v]);
+  }
+  for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += (long long)a.walkers * a.teams) {
+    const bool row = n0 + tm.team < a.N;
+    const int n = row ? (int)(n0 + tm.team) : 0;
+    const size_t xo = (size_t)b * a.sin.b + (size_t)n * a.sin.n, yo = (size_t)b * a.sout.b + (size_t)n * a.sout.n;
+    Raw<BF16> raw[2][V];
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int v = 0; v < V; v++) raw[t][v] = row && at.has[v] && t < a.tensors ? load8<BF16>(a.x[t], xo + at.in[v]) : zero8<BF16>();
+    int p0, p1, p2;
+    position(a, b, n, p0, p1, p2);
+    an.at(p0, p1, p2, a.sign);
+    float s[2] = {0.f, 0.f};
+    if (NORM == SLA2_ROPE_NORM_TOKEN) {
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+          float x[8];
+          unpack8<BF16>(raw[t][v], x);
+#pragma unroll
+          for (int i = 0; i < 8; i++) s[t] += x[i] * x[i];
+        }
+      tm.sum(s);
+#pragma unroll
+      for (int t = 0; t < 2; t++) s[t] = 1.f / sqrtf(s[t] / (float)(a.H * a.d) + a.eps);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+      if (t >= a.tensors) break;
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        float x[8];
+        unpack8<BF16>(raw[t][v], x);
+        if (NORM == SLA2_ROPE_NORM_HEAD) {
+          float q = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; i++) q += x[i] * x[i];
+          s[t] = 1.f / sqrtf(head_sum(q, a.d) / (float)a.d + a.eps);
+        }
+        if (NORM != SLA2_ROPE_NORM_NONE) {
+#pragma unroll
+          for (int i = 0; i < 8; i++) x[i] = x[i] * s[t] * w[t][v % W][i];
+        }
+        turn<BF16, HALVES>(a, an, second, x);
+        if (row && at.has[v]) store8<BF16>(a.y[t], yo + at.out[v], pack8<BF16>(x));
+      }
+    }
+  }
+}
+
+// Gradients of x and, where there are partial sums, of the weights.
+template <int V, bool BF16, bool HALVES, int NORM>
+__global__ __launch_bounds__(kTeamThreads) void rope_bwd_kernel(RopeArgs a) {
+  __shared__ float lds[kExchangeFloats];
+  constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
+  __shared__ f32x4 sums[kTeamThreads * 2 * W];            // 8 W floats of every thread
+  Team tm(a.team, lds);
+  const int part = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers, b = part / a.groups;
+  const Place<V> at(a, tm, part % a.groups);
+  const bool second = at.channel >= a.d / 2;
+  Angles<BF16, HALVES> an;
+  an.init(a, tm.lane);
+  float w[2][W][8], acc[2][W][8];
+#pragma unroll
+  for (int t = 0; t < 2; t++)
+#pragma unroll
+    for (int v = 0; v < W; v++) {
+      load_vector8(a.weight[t], NORM == SLA2_ROPE_NORM_TOKEN ? at.col[v] : at.channel, 1.f, w[t][v]);
+#pragma unroll
+      for (int i = 0; i < 8; i++) acc[t][v][i] = 0.f;
+    }
+  const float count = (float)(NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
+  for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += (long long)a.walkers * a.teams) {
+    const bool row = n0 + tm.team < a.N;
+    const int n = row ? (int)(n0 + tm.team) : 0;
+    const size_t xo = (size_t)b * a.sin.b + (size_t)n * a.sin.n, yo = (size_t)b * a.sout.b + (size_t)n * a.sout.n;
+    Raw<BF16> rx[2][V], rg[2][V];
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        const bool on = row && at.has[v] && t < a.tensors;
+        rx[t][v] = on ? load8<BF16>(a.x[t], xo + at.in[v]) : zero8<BF16>();
+        rg[t][v] = on ? load8<BF16>(a.dy[t], yo + at.out[v]) : zero8<BF16>();
+      }
+    int p0, p1, p2;
+    position(a, b, n, p0, p1, p2);
+    an.at(p0, p1, p2, a.sign);
+    float g[2][V][8], s[4] = {0.f, 0.f, 0.f, 0.f};       // sum x^2, sum t x: of q, of k
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        float x[8];
+        unpack8<BF16>(rx[t][v], x);
+        unpack8<BF16>(rg[t][v], g[t][v]);
+        turn<BF16, HALVES>(a, an, second, g[t][v]);
+        if (NORM == SLA2_ROPE_NORM_TOKEN) {
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            s[2 * t] += x[i] * x[i];
+            s[2 * t + 1] += g[t][v][i] * w[t][v % W][i] * x[i];
+          }
+        }
+      }
+    if (NORM == SLA2_ROPE_NORM_TOKEN) tm.sum(s);
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+      if (t >= a.tensors) break;
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        float x[8];
+        unpack8<BF16>(rx[t][v], x);
+        float xx = s[2 * t], tx = s[2 * t + 1];
+        if (NORM == SLA2_ROPE_NORM_HEAD) {
+          xx = tx = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            xx += x[i] * x[i];
+            tx += g[t][v][i] * w[t][0][i] * x[i];
+          }
+          xx = head_sum(xx, a.d);
+          tx = head_sum(tx, a.d);
+        }
+        const float r = 1.f / sqrtf(xx / count + a.eps), mean = tx * r / count;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          const float nx = x[i] * r;
+          acc[t][v % W][i] += g[t][v][i] * nx;
+          x[i] = r * (g[t][v][i] * w[t][v % W][i] - nx * mean);
+        }
+        if (row && at.has[v]) store8<BF16>(a.y[t], xo + at.in[v], pack8<BF16>(x));
+      }
+    }
+  }
+  if (!a.partial) return;
+  const int cols = NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d;
+#pragma unroll
+  for (int t = 0; t < 2; t++) {
+    if (!a.dweight[t]) continue;
+    float* to = a.partial + ((size_t)t * gridDim.x + blockIdx.x) * cols;
+    if (NORM == SLA2_ROPE_NORM_TOKEN) {
+      float* m = (float*)sums;               // [teams - 1][H d]
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < W; v++)
+        if (tm.team > 0 && at.has[v]) store8<false>(m, (size_t)(tm.team - 1) * cols + at.col[v], pack8<false>(acc[t][v]));
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < W; v++)
+        if (tm.team == 0 && at.has[v]) {
+          for (int k = 1; k < a.teams; k++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) acc[t][v][i] += m[(size_t)(k - 1) * cols + at.col[v] + i];
+          store8<false>(to, at.col[v], pack8<false>(acc[t][v]));
+        }
+    } else {
+      // every thread's sums; those of one place in a head are a head's lanes apart
+      const int per_head = a.d / kChunk;
+      __syncthreads();
+      store8<false>(sums, (size_t)threadIdx.x * 8, pack8<false>(acc[t][0]));
+      __syncthreads();
+      if ((int)threadIdx.x < a.d) {
+        float x = 0.f;
+        for (int k = (int)threadIdx.x / 8; k < (int)blockDim.x; k += per_head) x += ((const float*)sums)[k * 8 + threadIdx.x % 8];
+        to[threadIdx.x] = x;
+      }
+    }
+  }
+}
+
+void plan_rope(RopeArgs* a) {
+  const int most = kMaxRow / a->d;           // heads of a row
+  a->groups = (a->H + most - 1) / most;
+  a->heads = (a->H + a->groups - 1) / a->groups;
+  a->team = row_team(a->heads * a->d / kChunk);
+  a->teams = kTeamThreads / a->team.threads();
+  if (a->teams > a->N) a->teams = a->N;
+  const int resident = 512;                  // two workgroups of 8 waves a CU
+  long long walkers = resident / ((long long)a->B * a->groups);
+  const long long needed = ((long long)a->N + a->teams - 1) / a->teams;
+  if (walkers < 1) walkers = 1;
+  a->walkers = (int)(walkers < needed ? walkers : needed);
+}
+
+static int workgroups(const RopeArgs& a) { return a.B * a.groups * a.walkers; }
+size_t rope_partial_floats(const RopeArgs& a) {
+  return a.norm == SLA2_ROPE_NORM_NONE ? 0 : (size_t)2 * workgroups(a) * (a.norm == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
+}
+
+template <int V, bool BF16, bool HALVES>
+static hipError_t launch_norms(const RopeArgs& a, bool backward, hipStream_t stream) {
+  // whole waves; the sums of the weights want a thread for every channel of a head
+  int threads = (a.teams * a.team.threads() + kWave - 1) / kWave * kWave;
+  if (backward && threads < a.d) threads = a.d;
+  const dim3 grid((unsigned)workgroups(a)), block(threads);
+  if (backward) {
+    if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
+    else rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
+  } else {
+    if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
+    else if (a.norm == SLA2_ROPE_NORM_HEAD) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
+    else rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_NONE><<<grid, block, 0, stream>>>(a);
+  }
+  return hipGetLastError();
+}
+template <int V>
+static hipError_t launch_vec(const RopeArgs& a, bool backward, hipStream_t stream) {
+  if (a.bf16) return a.halves ? launch_norms<V, true, true>(a, backward, stream) : launch_norms<V, true, false>(a, backward, stream);
+  return a.halves ? launch_norms<V, false, true>(a, backward, stream) : launch_norms<V, false, false>(a, backward, stream);
+}
+static hipError_t launch_any(const RopeArgs& a, bool backward, hipStream_t stream) {
+  return a.team.vec == 1 ? launch_vec<1>(a, backward, stream) : launch_vec<2>(a, backward, stream);
+}
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t stream) { return launch_any(a, false, stream); }
+
+hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
+  RopeArgs a = args;
+  a.sign = -1.f;
+  if (a.norm == SLA2_ROPE_NORM_NONE) {       // the rotation back, from the layout of the results to that of x
+    for (int t = 0; t < 2; t++) a.x[t] = a.dy[t];
+    const HeadStrides s = a.sin;
+    a.sin = a.sout;
+    a.sout = s;
+    return launch_any(a, false, stream);
+  }
+  if (hipError_t e = launch_any(a, true, stream); e != hipSuccess) return e;
+  ColumnJobs js{};
+  js.columns = a.norm == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d;
+  const int rows = workgroups(a);
+  for (int t = 0; t < 2; t++)
+    if (a.dweight[t])
+      js.job[js.jobs++] = ColumnJob{a.partial + (size_t)t * rows * js.columns, 1, rows, nullptr, nullptr, 0.f, 1, 0, a.dweight[t], 0};
+  return launch_column_sums(js, stream);
+}
+
+}  // namespace sla2
