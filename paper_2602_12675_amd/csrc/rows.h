@@ -14,23 +14,41 @@ namespace sla2 {
 constexpr int kChunk = 8;                    // channels: 16 bytes of bf16
 constexpr int kMaxRow = 8192;                // channels of a row: 8 waves of 2 chunks a lane
 constexpr int kTeamThreads = 512;            // most threads of a workgroup
+constexpr int kCus = 256;
+// Waves of a SIMD that a kernel leaves registers for: 4 (two workgroups a CU), or 2 where a row takes more than 128 registers a thread.
+constexpr int waves_of(bool many_registers) { return many_registers ? 2 : 4; }
+constexpr int threads_of(bool many_registers) { return 4 * kWave * waves_of(many_registers); }
 
 // How a row of `chunks` chunks is spread over threads.
 struct RowTeam {
   int lanes, waves, vec;                     // lanes of a wave, whole waves (1 where lanes < 64), chunks a thread
   __host__ __device__ int threads() const { return lanes * waves; }
 };
-// The fewest places without a chunk; of two ways that leave equally many the one with fewer waves.
-inline RowTeam row_team(int chunks) {
+// The fewest waves with at most `most` chunks a thread (with more where a workgroup has not that many waves), and then the fewest chunks.
+inline RowTeam row_team(int chunks, int most) {
   RowTeam t{64, 1, 1};
   if (chunks <= 64) {
     while (t.lanes > 8 && t.lanes / 2 >= chunks) t.lanes /= 2;
     return t;
   }
-  const int rounds = (chunks + 63) / 64;     // of a whole wave
-  t.vec = rounds % 2 == 0 || rounds > kTeamThreads / 64 ? 2 : 1;
-  t.waves = (rounds + t.vec - 1) / t.vec;
+  const int rounds = (chunks + 63) / 64, waves = (rounds + most - 1) / most;      // rounds: of a whole wave
+  t.waves = waves < kTeamThreads / 64 ? waves : kTeamThreads / 64;
+  t.vec = (rounds + t.waves - 1) / t.waves;
   return t;
+}
+// Teams of a workgroup, of 8 waves where there are rows enough.
+inline int block_threads() {
+  return kTeamThreads;
+}
+inline int block_teams(const RowTeam& t, int rows) {
+  const int n = t.threads() < block_threads() ? block_threads() / t.threads() : 1;
+  return n < rows ? n : rows;
+}
+// Workgroups of a launch: those that are resident at once, with `threads` threads a CU.  Each goes through its rows side by side with the
+// others, so that all read and write one stretch of memory; more of them than fit, or runs of rows for each, cost 5 to 25 %.
+inline int resident_workgroups(const RowTeam& t, int teams, int threads) {
+  const int block = (teams * t.threads() + kWave - 1) / kWave * kWave, n = threads / block;
+  return kCus * (n < 1 ? 1 : n);
 }
 
 // 8 neighbouring elements as they are stored, and as fp32.
@@ -38,9 +56,13 @@ template <bool BF16> struct Raw {
   u32x4 a[BF16 ? 1 : 2];
 };
 typedef __attribute__((ext_vector_type(8))) float f32x8;
-template <bool BF16> __device__ __forceinline__ size_t elem_bytes() { return BF16 ? 2 : 4; }
-template <bool BF16> __device__ __forceinline__ Raw<BF16> load8(const void* p, size_t elem) {
-  const u32x4* a = (const u32x4*)((const char*)p + elem * elem_bytes<BF16>());
+template <bool BF16> constexpr size_t elem_bytes() { return BF16 ? 2 : 4; }
+// element `elem` of a tensor
+template <bool BF16, class T> __device__ __forceinline__ T* at_elem(T* p, long long elem) {
+  return (T*)((const char*)p + elem * (long long)elem_bytes<BF16>());
+}
+template <bool BF16, class Offset> __device__ __forceinline__ Raw<BF16> load8(const void* p, Offset elem) {     // unsigned: 32 bits beside a scalar address
+  const u32x4* a = (const u32x4*)((const char*)p + elem * (Offset)elem_bytes<BF16>());
   Raw<BF16> r;
   r.a[0] = a[0];
   if constexpr (!BF16) r.a[1] = a[1];
@@ -52,10 +74,15 @@ template <bool BF16> __device__ __forceinline__ Raw<BF16> zero8() {
   if constexpr (!BF16) r.a[1] = u32x4{0, 0, 0, 0};
   return r;
 }
-template <bool BF16> __device__ __forceinline__ void store8(void* p, size_t elem, const Raw<BF16>& r) {
-  u32x4* a = (u32x4*)((char*)p + elem * elem_bytes<BF16>());
+template <bool BF16, class Offset> __device__ __forceinline__ void store8(void* p, Offset elem, const Raw<BF16>& r) {
+  u32x4* a = (u32x4*)((char*)p + elem * (Offset)elem_bytes<BF16>());
   a[0] = r.a[0];
   if constexpr (!BF16) a[1] = r.a[1];
+}
+// Results.  bf16: past the caches, in whole cache lines a wave.  fp32: a wave's two stores share their lines, which the cache has to join.
+template <bool BF16, class Offset> __device__ __forceinline__ void put8(void* p, Offset elem, const Raw<BF16>& r) {
+  if constexpr (BF16) store_streamed((u32x4*)((char*)p + elem * (Offset)2), r.a[0]);
+  else store8<false>(p, elem, r);
 }
 template <bool BF16> __device__ __forceinline__ void unpack8(const Raw<BF16>& r, float (&x)[8]) {
 #pragma unroll
@@ -76,7 +103,7 @@ template <bool BF16> __device__ __forceinline__ Raw<BF16> pack8(const float (&x)
   return r;
 }
 // 8 fp32 values of a vector of channels that may be absent
-__device__ __forceinline__ void load_vector8(const float* p, size_t elem, float absent, float (&x)[8]) {
+__device__ __forceinline__ void load_vector8(const float* p, unsigned elem, float absent, float (&x)[8]) {
   if (p) {
     unpack8<false>(load8<false>(p, elem), x);
   } else {
@@ -98,58 +125,60 @@ __device__ __forceinline__ float lanes_sum(float x, int lanes) {
   return x;
 }
 
-// A thread's place in its team.  Every thread of a workgroup takes part in every exchange, so all its teams make equally many steps.
+// 1 / sqrt(x) to a step of fp32; x is at least a normal number (eps is)
+__device__ __forceinline__ float inv_sqrt(float x) { return __builtin_amdgcn_rsqf(x); }
+
+// A thread's place in its team, and its team's among those of the workgroup.  Every thread of a workgroup takes part in every exchange, so
+// all its teams make equally many steps.  What is the same for a wave is in scalar registers: the rows' addresses above all.
 constexpr int kExchange = 4;                 // sums that a step exchanges at most
 constexpr int kExchangeFloats = 2 * (kTeamThreads / kWave) * kExchange;
 struct Team {
   RowTeam t;
-  int team, lane;                            // which team of the workgroup; thread of the team
+  int team, lane;                            // team of the workgroup; thread of the team
+  int first, sub;                            // the first team of the wave; how far behind it this thread's is
   float* lds;                                // kExchangeFloats floats
   int flip = 0;
   __device__ Team(const RowTeam& t_, float* lds_) : t(t_), lds(lds_) {
     team = (int)threadIdx.x / t.threads();
     lane = (int)threadIdx.x - team * t.threads();
+    first = __builtin_amdgcn_readfirstlane(team);
+    sub = team - first;
   }
-  // x[k] of every wave of the team -> f(wave of the team, its x).  Two buffers in turn: the next exchange but one writes over this one's,
+  // x[k] of every wave of the team, [wave][K], behind a barrier.  Two buffers in turn: the next exchange but one writes over this one's,
   // behind the barrier of the next, which every wave reaches after its reads.
-  template <int K, class F> __device__ __forceinline__ void exchange(const float (&x)[K], F f) {
+  template <int K> __device__ __forceinline__ const float* exchange(const float (&x)[K]) {
     static_assert(K <= kExchange, "");
-    float* m = lds + flip * (kExchangeFloats / 2);
-    flip ^= 1;
+    float* m = lds + flip;
+    flip ^= kExchangeFloats / 2;
     const int wave = (int)threadIdx.x / kWave;
     if ((int)threadIdx.x % kWave == 0) {
 #pragma unroll
       for (int k = 0; k < K; k++) m[wave * K + k] = x[k];
     }
     __syncthreads();
-    const float* first = m + team * t.waves * K;
-    for (int w = 0; w < t.waves; w++) f(w, first + w * K);
+    return m + first * t.waves * K;
   }
-  // what the waves of the team gave the last exchange, of K
-  template <int K> __device__ __forceinline__ const float* last() const { return lds + (flip ^ 1) * (kExchangeFloats / 2) + team * t.waves * K; }
   // sums over the team
   template <int K> __device__ __forceinline__ void sum(float (&x)[K]) {
 #pragma unroll
     for (int k = 0; k < K; k++) x[k] = lanes_sum(x[k], t.lanes);
     if (t.waves == 1) return;
-    float s[K];
+    const float* o = exchange(x);
 #pragma unroll
-    for (int k = 0; k < K; k++) s[k] = 0.f;
-    exchange(x, [&](int, const float* o) {
+    for (int k = 0; k < K; k++) x[k] = o[k];
+    for (int w = 1; w < t.waves; w++) {
 #pragma unroll
-      for (int k = 0; k < K; k++) s[k] += o[k];
-    });
-#pragma unroll
-    for (int k = 0; k < K; k++) x[k] = s[k];
+      for (int k = 0; k < K; k++) x[k] += o[w * K + k];
+    }
   }
   // channels that wave w of the team holds of a row of `chunks` chunks
-  __device__ __forceinline__ float channels(int w, int chunks) const {
+  __device__ __forceinline__ int channels(int w, int chunks) const {
     int n = 0;
     for (int v = 0; v < t.vec; v++) {
       const int left = chunks - v * t.threads() - w * kWave;
-      n += left < 0 ? 0 : left > t.lanes ? t.lanes : left;
+      n += left < 0 ? 0 : left > kWave ? kWave : left;
     }
-    return (float)(n * kChunk);
+    return n * kChunk;
   }
 };
 
@@ -193,12 +222,12 @@ struct RopeArgs {
   float eps;
   int norm;                                  // sla2_rope_norm
   bool bf16, halves;
-  float sign;                                // of the angles
+  double sign;                               // of the angles
   // launch
   RowTeam team;
   int teams, heads, groups, walkers;         // teams of a workgroup; heads of a row, rows of a token; workgroups of a (batch, group)
 };
-void plan_rope(RopeArgs* a);                 // fills in the launch from the sizes
+void plan_rope(RopeArgs* a, bool backward);                 // fills in the launch from the sizes
 size_t rope_partial_floats(const RopeArgs& a);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 hipError_t launch_rope_bwd(const RopeArgs& a, hipStream_t stream);

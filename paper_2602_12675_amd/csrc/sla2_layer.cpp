@@ -77,7 +77,7 @@ static bool extent_ok(int dims, const long long* count, const long long* stride,
   return n < ((__int128)1 << 60);
 }
 
-static int make_rope(const sla2_rope_params* p, RopeArgs* a) {
+static int make_rope(const sla2_rope_params* p, bool backward, RopeArgs* a) {
   if (!p) return SLA2_EINVAL;
   if (p->B < 1 || p->H < 1 || p->N < 1) return SLA2_EINVAL;
   if (p->dtype != SLA2_F32 && p->dtype != SLA2_BF16) return SLA2_EINVAL;
@@ -126,9 +126,9 @@ static int make_rope(const sla2_rope_params* p, RopeArgs* a) {
   a->norm = p->norm;
   a->bf16 = p->dtype == SLA2_BF16;
   a->halves = p->pairing == SLA2_ROPE_HALVES;
-  a->sign = 1.f;
+  a->sign = 1.0;
   a->positions_stride = p->positions_per_batch ? 3ll * p->N : 0;
-  plan_rope(a);
+  plan_rope(a, backward);
   return SLA2_OK;
 }
 
@@ -208,14 +208,14 @@ extern "C" {
 
 size_t sla2_rope_workspace_bytes(const sla2_rope_params* params) {
   RopeArgs a;
-  if (make_rope(params, &a) != SLA2_OK) return 0;
+  if (make_rope(params, true, &a) != SLA2_OK) return 0;
   const size_t n = align256(rope_partial_floats(a) * sizeof(float));
   return n ? n : 256;
 }
 
 int sla2_rope_frequencies(const sla2_rope_params* params, double theta, double* freq) {
   RopeArgs a;
-  const int rc = make_rope(params, &a);
+  const int rc = make_rope(params, false, &a);
   if (rc != SLA2_OK) return rc;
   if (!freq || !(theta > 0.0 && theta < INFINITY)) return SLA2_EINVAL;
   for (int j = 0, first = 0, axis = 0; j < a.d / 2; j++) {
@@ -228,7 +228,7 @@ int sla2_rope_frequencies(const sla2_rope_params* params, double theta, double* 
 int sla2_rope_forward(const sla2_rope_params* params, const void* q, const void* k, const double* freq, const int32_t* positions,
                       const float* q_weight, const float* k_weight, void* q_out, void* k_out, void* hip_stream) {
   RopeArgs a;
-  const int rc = make_rope(params, &a);
+  const int rc = make_rope(params, false, &a);
   if (rc != SLA2_OK) return rc;
   if (!q || !q_out || !k != !k_out || (!k && k_weight)) return SLA2_EINVAL;
   if (misaligned16(q) || misaligned16(k) || misaligned16(q_out) || misaligned16(k_out)) return SLA2_EINVAL;
@@ -251,7 +251,7 @@ int sla2_rope_backward(const sla2_rope_params* params, const void* q, const void
                        const float* q_weight, const float* k_weight, const void* dq_out, const void* dk_out, void* dq, void* dk,
                        float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes, void* hip_stream) {
   RopeArgs a;
-  int rc = make_rope(params, &a);
+  int rc = make_rope(params, true, &a);
   if (rc != SLA2_OK) return rc;
   const bool normed = a.norm != SLA2_ROPE_NORM_NONE;
   if (!dq_out || !dq || !dk_out != !dk) return SLA2_EINVAL;

@@ -12,6 +12,8 @@
 
 namespace sla2 {
 
+constexpr bool large_forward(int vec, int norm) { return vec == 3 && norm == SLA2_ROPE_NORM_TOKEN; }
+
 // x of the lane that holds the other channel of each pair of a head of LANES lanes
 template <int LANES> __device__ __forceinline__ float half_head_away(float x) {
   if constexpr (LANES == 16) return rotate16<8>(x);
@@ -24,17 +26,17 @@ template <bool BF16, bool HALVES> struct Angles {
   double turns[kPairs];                      // of a pair per position
   int axis[kPairs];
   float c[kPairs], s[kPairs];
-  __device__ __forceinline__ void init(const RopeArgs& a, int chunk) {
+  __device__ __forceinline__ void init(const RopeArgs& a, int chunk) {         // backward: turned the other way round
     const int first = HALVES ? chunk * kChunk % (a.d / 2) : chunk % (a.d / kChunk) * 4;
 #pragma unroll
     for (int i = 0; i < kPairs; i++) {
       const int j = first + i;
-      turns[i] = j < a.pairs_end[2] ? a.freq[j] * 0.15915494309189533577 : 0.0;       // 1 / (2 pi)
+      turns[i] = j < a.pairs_end[2] ? a.freq[j] * (a.sign * 0.15915494309189533577) : 0.0;       // 1 / (2 pi)
       axis[i] = j < a.pairs_end[0] ? 0 : j < a.pairs_end[1] ? 1 : 2;
     }
   }
   // bf16 results: the hardware's sine and cosine of a fraction of a turn, whose error is far below half a step of bf16
-  __device__ __forceinline__ void at(int p0, int p1, int p2, float sign) {
+  __device__ __forceinline__ void at(int p0, int p1, int p2) {
 #pragma unroll
     for (int i = 0; i < kPairs; i++) {
       const int p = axis[i] == 0 ? p0 : axis[i] == 1 ? p1 : p2;
@@ -46,7 +48,6 @@ template <bool BF16, bool HALVES> struct Angles {
       } else {
         sincospif(2.f * f, &s[i], &c[i]);
       }
-      s[i] *= sign;
     }
   }
 };
@@ -93,7 +94,7 @@ __device__ __forceinline__ float head_sum(float x, int d) { return d == 128 ? ro
 // What a thread holds of its rows: V chunks of heads.
 template <int V> struct Place {
   bool has[V];
-  size_t in[V], out[V];                      // offsets from the token
+  size_t in[V], out[V];                      // offsets from the first token of the wave
   int col[V];                                // channel among all heads
   int channel;                               // of its chunks in their heads
   __device__ __forceinline__ Place(const RopeArgs& a, const Team& tm, int group) {
@@ -104,15 +105,15 @@ template <int V> struct Place {
       const int c = tm.lane + v * a.team.threads(), head = group * a.heads + c / per_head;
       has[v] = tm.team < a.teams && c < a.heads * per_head && head < a.H;
       const int h = has[v] ? head : 0;
-      in[v] = (size_t)h * a.sin.h + channel;
-      out[v] = (size_t)h * a.sout.h + channel;
+      in[v] = (size_t)tm.sub * a.sin.n + (size_t)h * a.sin.h + channel;
+      out[v] = (size_t)tm.sub * a.sout.n + (size_t)h * a.sout.h + channel;
       col[v] = has[v] ? h * a.d + channel : 0;
     }
   }
 };
 
 template <int V, bool BF16, bool HALVES, int NORM>
-__global__ __launch_bounds__(kTeamThreads) void rope_kernel(RopeArgs a) {
+__global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) void rope_kernel(RopeArgs a) {
   __shared__ float lds[kExchangeFloats];
   constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
   Team tm(a.team, lds);
@@ -121,6 +122,7 @@ __global__ __launch_bounds__(kTeamThreads) void rope_kernel(RopeArgs a) {
   const bool second = at.channel >= a.d / 2;
   Angles<BF16, HALVES> an;
   an.init(a, tm.lane);
+  const float share = 1.f / (float)(NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
   float w[2][W][8];
   if (NORM != SLA2_ROPE_NORM_NONE) {
 #pragma unroll
@@ -128,18 +130,31 @@ __global__ __launch_bounds__(kTeamThreads) void rope_kernel(RopeArgs a) {
 #pragma unroll
       for (int v = 0; v < W; v++) load_vector8(a.weight[t], NORM == SLA2_ROPE_NORM_TOKEN ? at.col[v] : at.channel, 1.f, w[t][v]);
   }
-  for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += (long long)a.walkers * a.teams) {
-    const bool row = n0 + tm.team < a.N;
-    const int n = row ? (int)(n0 + tm.team) : 0;
-    const size_t xo = (size_t)b * a.sin.b + (size_t)n * a.sin.n, yo = (size_t)b * a.sout.b + (size_t)n * a.sout.n;
-    Raw<BF16> raw[2][V];
-#pragma unroll
-    for (int t = 0; t < 2; t++)
-#pragma unroll
-      for (int v = 0; v < V; v++) raw[t][v] = row && at.has[v] && t < a.tensors ? load8<BF16>(a.x[t], xo + at.in[v]) : zero8<BF16>();
+  struct Row {
+    Raw<BF16> x[2][V];
     int p0, p1, p2;
-    position(a, b, n, p0, p1, p2);
-    an.at(p0, p1, p2, a.sign);
+  };
+  auto load = [&](long long n0) {
+    const long long n = n0 + tm.first;
+    const bool row = n + tm.sub < a.N;
+    Row r;
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+      const void* px = at_elem<BF16>(a.x[t], b * a.sin.b + n * a.sin.n);
+#pragma unroll
+      for (int v = 0; v < V; v++) r.x[t][v] = row && at.has[v] && t < a.tensors ? load8<BF16>(px, at.in[v]) : zero8<BF16>();
+    }
+    position(a, b, row ? (int)(n + tm.sub) : 0, r.p0, r.p1, r.p2);
+    return r;
+  };
+  const long long step = (long long)a.walkers * a.teams;
+  for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += step) {
+    const long long n = n0 + tm.first;
+    const bool row = n + tm.sub < a.N;
+    const long long yo = b * a.sout.b + n * a.sout.n;
+    Row cur = load(n0);
+    Raw<BF16> (&raw)[2][V] = cur.x;
+    an.at(cur.p0, cur.p1, cur.p2);
     float s[2] = {0.f, 0.f};
     if (NORM == SLA2_ROPE_NORM_TOKEN) {
 #pragma unroll
@@ -153,7 +168,7 @@ __global__ __launch_bounds__(kTeamThreads) void rope_kernel(RopeArgs a) {
         }
       tm.sum(s);
 #pragma unroll
-      for (int t = 0; t < 2; t++) s[t] = 1.f / sqrtf(s[t] / (float)(a.H * a.d) + a.eps);
+      for (int t = 0; t < 2; t++) s[t] = inv_sqrt(s[t] * share + a.eps);
     }
 #pragma unroll
     for (int t = 0; t < 2; t++) {
@@ -166,14 +181,14 @@ __global__ __launch_bounds__(kTeamThreads) void rope_kernel(RopeArgs a) {
           float q = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; i++) q += x[i] * x[i];
-          s[t] = 1.f / sqrtf(head_sum(q, a.d) / (float)a.d + a.eps);
+          s[t] = inv_sqrt(head_sum(q, a.d) * share + a.eps);
         }
         if (NORM != SLA2_ROPE_NORM_NONE) {
 #pragma unroll
           for (int i = 0; i < 8; i++) x[i] = x[i] * s[t] * w[t][v % W][i];
         }
         turn<BF16, HALVES>(a, an, second, x);
-        if (row && at.has[v]) store8<BF16>(a.y[t], yo + at.out[v], pack8<BF16>(x));
+        if (row && at.has[v]) put8<BF16>(at_elem<BF16>(a.y[t], yo), at.out[v], pack8<BF16>(x));
       }
     }
   }
@@ -181,7 +196,7 @@ __global__ __launch_bounds__(kTeamThreads) void rope_kernel(RopeArgs a) {
 
 // Gradients of x and, where there are partial sums, of the weights.
 template <int V, bool BF16, bool HALVES, int NORM>
-__global__ __launch_bounds__(kTeamThreads) void rope_bwd_kernel(RopeArgs a) {
+__global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void rope_bwd_kernel(RopeArgs a) {
   __shared__ float lds[kExchangeFloats];
   constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
   __shared__ f32x4 sums[kTeamThreads * 2 * W];            // 8 W floats of every thread
@@ -191,6 +206,7 @@ __global__ __launch_bounds__(kTeamThreads) void rope_bwd_kernel(RopeArgs a) {
   const bool second = at.channel >= a.d / 2;
   Angles<BF16, HALVES> an;
   an.init(a, tm.lane);
+  const float share = 1.f / (float)(NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
   float w[2][W][8], acc[2][W][8];
 #pragma unroll
   for (int t = 0; t < 2; t++)
@@ -200,67 +216,82 @@ __global__ __launch_bounds__(kTeamThreads) void rope_bwd_kernel(RopeArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; i++) acc[t][v][i] = 0.f;
     }
-  const float count = (float)(NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
-  for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += (long long)a.walkers * a.teams) {
-    const bool row = n0 + tm.team < a.N;
-    const int n = row ? (int)(n0 + tm.team) : 0;
-    const size_t xo = (size_t)b * a.sin.b + (size_t)n * a.sin.n, yo = (size_t)b * a.sout.b + (size_t)n * a.sout.n;
-    Raw<BF16> rx[2][V], rg[2][V];
+  struct Row {
+    Raw<BF16> x[2][V], g[2][V];
+    int p0, p1, p2;
+  };
+  auto load = [&](long long n0) {
+    const long long n = n0 + tm.first;
+    const bool row = n + tm.sub < a.N;
+    Row r;
 #pragma unroll
-    for (int t = 0; t < 2; t++)
+    for (int t = 0; t < 2; t++) {
+      const void *px = at_elem<BF16>(a.x[t], b * a.sin.b + n * a.sin.n), *pg = at_elem<BF16>(a.dy[t], b * a.sout.b + n * a.sout.n);
 #pragma unroll
       for (int v = 0; v < V; v++) {
         const bool on = row && at.has[v] && t < a.tensors;
-        rx[t][v] = on ? load8<BF16>(a.x[t], xo + at.in[v]) : zero8<BF16>();
-        rg[t][v] = on ? load8<BF16>(a.dy[t], yo + at.out[v]) : zero8<BF16>();
+        r.x[t][v] = on ? load8<BF16>(px, at.in[v]) : zero8<BF16>();
+        r.g[t][v] = on ? load8<BF16>(pg, at.out[v]) : zero8<BF16>();
       }
-    int p0, p1, p2;
-    position(a, b, n, p0, p1, p2);
-    an.at(p0, p1, p2, a.sign);
-    float g[2][V][8], s[4] = {0.f, 0.f, 0.f, 0.f};       // sum x^2, sum t x: of q, of k
+    }
+    position(a, b, row ? (int)(n + tm.sub) : 0, r.p0, r.p1, r.p2);
+    return r;
+  };
+  const long long step = (long long)a.walkers * a.teams;
+  for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += step) {
+    const long long n = n0 + tm.first;
+    const bool row = n + tm.sub < a.N;
+    const long long xo = b * a.sin.b + n * a.sin.n;
+    Row cur = load(n0);
+    an.at(cur.p0, cur.p1, cur.p2);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};                   // over all heads: sum x^2, sum t x of q, of k
+    float g[2][W][8];
+    if (NORM == SLA2_ROPE_NORM_TOKEN) {
 #pragma unroll
-    for (int t = 0; t < 2; t++)
+      for (int t = 0; t < 2; t++)
 #pragma unroll
-      for (int v = 0; v < V; v++) {
-        float x[8];
-        unpack8<BF16>(rx[t][v], x);
-        unpack8<BF16>(rg[t][v], g[t][v]);
-        turn<BF16, HALVES>(a, an, second, g[t][v]);
-        if (NORM == SLA2_ROPE_NORM_TOKEN) {
+        for (int v = 0; v < W; v++) {
+          float x[8];
+          unpack8<BF16>(cur.x[t][v], x);
+          unpack8<BF16>(cur.g[t][v], g[t][v]);
+          turn<BF16, HALVES>(a, an, second, g[t][v]);
 #pragma unroll
           for (int i = 0; i < 8; i++) {
             s[2 * t] += x[i] * x[i];
-            s[2 * t + 1] += g[t][v][i] * w[t][v % W][i] * x[i];
+            s[2 * t + 1] += g[t][v][i] * w[t][v][i] * x[i];
           }
         }
-      }
-    if (NORM == SLA2_ROPE_NORM_TOKEN) tm.sum(s);
+      tm.sum(s);
+    }
 #pragma unroll
     for (int t = 0; t < 2; t++) {
       if (t >= a.tensors) break;
 #pragma unroll
       for (int v = 0; v < V; v++) {
-        float x[8];
-        unpack8<BF16>(rx[t][v], x);
+        constexpr bool kToken = NORM == SLA2_ROPE_NORM_TOKEN;
+        float x[8], (&gv)[8] = g[t][kToken ? v : 0], (&wv)[8] = w[t][kToken ? v : 0], (&av)[8] = acc[t][kToken ? v : 0];
+        unpack8<BF16>(cur.x[t][v], x);
         float xx = s[2 * t], tx = s[2 * t + 1];
-        if (NORM == SLA2_ROPE_NORM_HEAD) {
+        if (!kToken) {
+          unpack8<BF16>(cur.g[t][v], gv);
+          turn<BF16, HALVES>(a, an, second, gv);
           xx = tx = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; i++) {
             xx += x[i] * x[i];
-            tx += g[t][v][i] * w[t][0][i] * x[i];
+            tx += gv[i] * wv[i] * x[i];
           }
           xx = head_sum(xx, a.d);
           tx = head_sum(tx, a.d);
         }
-        const float r = 1.f / sqrtf(xx / count + a.eps), mean = tx * r / count;
+        const float r = inv_sqrt(xx * share + a.eps), mean = tx * share * r;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
           const float nx = x[i] * r;
-          acc[t][v % W][i] += g[t][v][i] * nx;
-          x[i] = r * (g[t][v][i] * w[t][v % W][i] - nx * mean);
+          av[i] += gv[i] * nx;
+          x[i] = r * (gv[i] * wv[i] - nx * mean);
         }
-        if (row && at.has[v]) store8<BF16>(a.y[t], xo + at.in[v], pack8<BF16>(x));
+        if (row && at.has[v]) put8<BF16>(at_elem<BF16>(a.y[t], xo), at.in[v], pack8<BF16>(x));
       }
     }
   }
@@ -275,7 +306,7 @@ __global__ __launch_bounds__(kTeamThreads) void rope_bwd_kernel(RopeArgs a) {
       __syncthreads();
 #pragma unroll
       for (int v = 0; v < W; v++)
-        if (tm.team > 0 && at.has[v]) store8<false>(m, (size_t)(tm.team - 1) * cols + at.col[v], pack8<false>(acc[t][v]));
+        if (tm.team > 0 && at.has[v]) store8<false>(m, (unsigned)((tm.team - 1) * cols) + at.col[v], pack8<false>(acc[t][v]));
       __syncthreads();
 #pragma unroll
       for (int v = 0; v < W; v++)
@@ -283,13 +314,13 @@ __global__ __launch_bounds__(kTeamThreads) void rope_bwd_kernel(RopeArgs a) {
           for (int k = 1; k < a.teams; k++)
 #pragma unroll
             for (int i = 0; i < 8; i++) acc[t][v][i] += m[(size_t)(k - 1) * cols + at.col[v] + i];
-          store8<false>(to, at.col[v], pack8<false>(acc[t][v]));
+          store8<false>(to, (unsigned)at.col[v], pack8<false>(acc[t][v]));
         }
     } else {
       // every thread's sums; those of one place in a head are a head's lanes apart
       const int per_head = a.d / kChunk;
       __syncthreads();
-      store8<false>(sums, (size_t)threadIdx.x * 8, pack8<false>(acc[t][0]));
+      store8<false>(sums, threadIdx.x * 8, pack8<false>(acc[t][0]));
       __syncthreads();
       if ((int)threadIdx.x < a.d) {
         float x = 0.f;
@@ -300,18 +331,16 @@ __global__ __launch_bounds__(kTeamThreads) void rope_bwd_kernel(RopeArgs a) {
   }
 }
 
-void plan_rope(RopeArgs* a) {
+void plan_rope(RopeArgs* a, bool backward) {
   const int most = kMaxRow / a->d;           // heads of a row
   a->groups = (a->H + most - 1) / most;
   a->heads = (a->H + a->groups - 1) / a->groups;
-  a->team = row_team(a->heads * a->d / kChunk);
-  a->teams = kTeamThreads / a->team.threads();
-  if (a->teams > a->N) a->teams = a->N;
-  const int resident = 512;                  // two workgroups of 8 waves a CU
-  long long walkers = resident / ((long long)a->B * a->groups);
-  const long long needed = ((long long)a->N + a->teams - 1) / a->teams;
-  if (walkers < 1) walkers = 1;
-  a->walkers = (int)(walkers < needed ? walkers : needed);
+  a->team = row_team(a->heads * a->d / kChunk, backward ? 1 : 3);
+  a->teams = block_teams(a->team, a->N);
+  const bool large = backward ? a->team.vec > 1 : large_forward(a->team.vec, a->norm);
+  const int walkers = resident_workgroups(a->team, a->teams, threads_of(large)) / (a->B * a->groups);
+  const int needed = (int)(((long long)a->N + a->teams - 1) / a->teams);
+  a->walkers = walkers < 1 ? 1 : walkers < needed ? walkers : needed;
 }
 
 static int workgroups(const RopeArgs& a) { return a.B * a.groups * a.walkers; }
@@ -326,8 +355,11 @@ static hipError_t launch_norms(const RopeArgs& a, bool backward, hipStream_t str
   if (backward && threads < a.d) threads = a.d;
   const dim3 grid((unsigned)workgroups(a)), block(threads);
   if (backward) {
-    if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
-    else rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
+    if (a.norm == SLA2_ROPE_NORM_TOKEN) {
+      if constexpr (V <= 2) rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
+    } else {
+      if constexpr (V <= 2) rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
+    }
   } else {
     if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
     else if (a.norm == SLA2_ROPE_NORM_HEAD) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
@@ -341,14 +373,14 @@ static hipError_t launch_vec(const RopeArgs& a, bool backward, hipStream_t strea
   return a.halves ? launch_norms<V, false, true>(a, backward, stream) : launch_norms<V, false, false>(a, backward, stream);
 }
 static hipError_t launch_any(const RopeArgs& a, bool backward, hipStream_t stream) {
-  return a.team.vec == 1 ? launch_vec<1>(a, backward, stream) : launch_vec<2>(a, backward, stream);
+  return a.team.vec == 1 ? launch_vec<1>(a, backward, stream) : a.team.vec == 2 ? launch_vec<2>(a, backward, stream) : launch_vec<3>(a, backward, stream);
 }
 
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream) { return launch_any(a, false, stream); }
 
 hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
   RopeArgs a = args;
-  a.sign = -1.f;
+  a.sign = -1.0;
   if (a.norm == SLA2_ROPE_NORM_NONE) {       // the rotation back, from the layout of the results to that of x
     for (int t = 0; t < 2; t++) a.x[t] = a.dy[t];
     const HeadStrides s = a.sin;
