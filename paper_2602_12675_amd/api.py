@@ -8,7 +8,6 @@ import of this module fails: there is no fallback.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 
 import torch
@@ -267,65 +266,46 @@ def make_norm_params(B, N, C, dtype_x=SLA2_BF16, dtype_h=SLA2_BF16, norm_in=SLA2
 _TYPES = {SLA2_F32: torch.float32, SLA2_BF16: torch.bfloat16}
 
 
-def _held(t, dtype, count):
-    """The address of t, once it is seen to have the element type and at least the number of elements that the kernels will
-    take it to have: a tensor that has not would be read or written out of bounds.  (Its strides are the caller's to state.)"""
-    if t is None or isinstance(t, int):
-        return t
-    if t.dtype != dtype or t.numel() < count:
-        raise Sla2Error(SLA2_EINVAL)
-    return t.data_ptr()
-
-
-def _vector(t):
-    """A vector of channels, frequencies or positions: contiguous besides."""
-    if t is not None and not isinstance(t, int) and not t.is_contiguous():
-        raise Sla2Error(SLA2_EINVAL)
-    return t
-
-
-def _one_device(tensors):
-    """The device of the tensors, which is one for all."""
-    dev = None
-    for t in tensors:
-        if t is not None and not isinstance(t, int):
-            if dev is None:
-                dev = t.device
-            elif t.device != dev:
-                raise Sla2Error(SLA2_EINVAL)
-    return dev
-
-
-def _launch(fn, args, tensors, stream, check):
-    """Calls fn on the tensors' device, on `stream` or that device's current one."""
-    dev = _one_device(tensors)
-    if dev is None or dev.type != "cuda" or dev.index == torch.cuda.current_device():
-        rc = fn(*args, _stream(stream))
-    else:
-        with torch.cuda.device(dev):
-            rc = fn(*args, _stream(stream))
+def _call(fn, params, tensors, stream, check, *tail) -> int:
+    """fn(params, addresses, *tail, stream) on the device of the tensors, on `stream` or that device's current one.
+    tensors: (tensor, element type, elements, whether it is a vector).  A tensor of another element type, with fewer elements than the
+    kernels will take it to have, on the host or on another device than the others, or a vector that is not contiguous, is refused: it
+    would be read or written out of bounds.  Strides of the others are the caller's to state; addresses (int) are taken as they are."""
+    out, dev, rc = [ctypes.byref(params)], None, SLA2_OK
+    for t, dtype, count, vector in tensors:
+        if t is None or t.__class__ is int:
+            out.append(t)
+            continue
+        d = t.get_device()
+        if dev is None:
+            dev = d
+        if t.dtype is not dtype or t.numel() < count or d != dev or d < 0 or (vector and not t.is_contiguous()):
+            rc = SLA2_EINVAL
+            break
+        out.append(t.data_ptr())
+    if rc == SLA2_OK:
+        if dev is None:
+            rc = fn(*out, *tail, _stream(stream))
+        else:
+            st = torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+            if dev == torch.cuda.current_device():
+                rc = fn(*out, *tail, st)
+            else:
+                with torch.cuda.device(dev):
+                    rc = fn(*out, *tail, st)
     if check and rc != SLA2_OK:
         raise Sla2Error(rc)
     return rc
-
-
-def _entry(fn):
-    """check=False: a refusal of the binding's own comes back as a status, as the library's do."""
-    @functools.wraps(fn)
-    def call(*args, check=True, **kw):
-        try:
-            return fn(*args, check=check, **kw)
-        except Sla2Error as e:
-            if check:
-                raise
-            return e.status
-    return call
 
 
 def _bytes(workspace, ws_bytes):
     if ws_bytes is not None:                           # a raw address needs its size spelled out
         return ws_bytes
     return workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def _scratch(workspace):
+    return workspace, getattr(workspace, "dtype", None), 0, True
 
 
 def sla2_rope_workspace_bytes(params: RopeParams) -> int:
@@ -347,26 +327,23 @@ def _rope_sizes(p):
             _TYPES.get(p.dtype))
 
 
-@_entry
 def sla2_rope_forward(params, q, k, freq, q_out, k_out, q_weight=None, k_weight=None, positions=None, stream=None, check=True) -> int:
     n, w, np_, dt = _rope_sizes(params)
-    args = (ctypes.byref(params), _held(q, dt, n), _held(k, dt, n), _held(_vector(freq), torch.float64, params.d // 2),
-            _held(_vector(positions), torch.int32, np_), _held(_vector(q_weight), torch.float32, w),
-            _held(_vector(k_weight), torch.float32, w), _held(q_out, dt, n), _held(k_out, dt, n))
-    return _launch(_lib.sla2_rope_forward, args, (q, k, freq, positions, q_weight, k_weight, q_out, k_out), stream, check)
+    f32 = torch.float32
+    return _call(_lib.sla2_rope_forward, params, (
+        (q, dt, n, False), (k, dt, n, False), (freq, torch.float64, params.d // 2, True), (positions, torch.int32, np_, True),
+        (q_weight, f32, w, True), (k_weight, f32, w, True), (q_out, dt, n, False), (k_out, dt, n, False)), stream, check)
 
 
-@_entry
 def sla2_rope_backward(params, q, k, freq, dq_out, dk_out, dq, dk, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
                        positions=None, workspace=None, stream=None, check=True, ws_bytes=None) -> int:
     n, w, np_, dt = _rope_sizes(params)
-    args = (ctypes.byref(params), _held(q, dt, n), _held(k, dt, n), _held(_vector(freq), torch.float64, params.d // 2),
-            _held(_vector(positions), torch.int32, np_), _held(_vector(q_weight), torch.float32, w),
-            _held(_vector(k_weight), torch.float32, w), _held(dq_out, dt, n), _held(dk_out, dt, n), _held(dq, dt, n), _held(dk, dt, n),
-            _held(_vector(dq_weight), torch.float32, w), _held(_vector(dk_weight), torch.float32, w), _ptr(workspace),
-            _bytes(workspace, ws_bytes))
-    return _launch(_lib.sla2_rope_backward, args, (q, k, freq, positions, q_weight, k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight,
-                                                   workspace), stream, check)
+    f32 = torch.float32
+    return _call(_lib.sla2_rope_backward, params, (
+        (q, dt, n, False), (k, dt, n, False), (freq, torch.float64, params.d // 2, True), (positions, torch.int32, np_, True),
+        (q_weight, f32, w, True), (k_weight, f32, w, True), (dq_out, dt, n, False), (dk_out, dt, n, False), (dq, dt, n, False),
+        (dk, dt, n, False), (dq_weight, f32, w, True), (dk_weight, f32, w, True), _scratch(workspace)), stream, check,
+        _bytes(workspace, ws_bytes))
 
 
 def sla2_norm_workspace_bytes(params: NormParams) -> int:
@@ -379,28 +356,25 @@ def _norm_sizes(p):
     return p.B * p.N * p.C, rows * p.C, _TYPES.get(p.dtype_x), _TYPES.get(p.dtype_h)
 
 
-@_entry
 def sla2_norm_forward(params, x, h, y=None, x_out=None, gate=None, out_weight=None, in_weight=None, scale=None, shift=None, stream=None,
                       check=True) -> int:
     n, m, tx, th = _norm_sizes(params)
     f32, c = torch.float32, params.C
-    args = (ctypes.byref(params), _held(x, tx, n), _held(y, th, n), _held(gate, f32, m), _held(_vector(out_weight), f32, c),
-            _held(x_out, tx, n), _held(_vector(in_weight), f32, c), _held(scale, f32, m), _held(shift, f32, m), _held(h, th, n))
-    return _launch(_lib.sla2_norm_forward, args, (x, y, gate, out_weight, x_out, in_weight, scale, shift, h), stream, check)
+    return _call(_lib.sla2_norm_forward, params, (
+        (x, tx, n, False), (y, th, n, False), (gate, f32, m, False), (out_weight, f32, c, True), (x_out, tx, n, False),
+        (in_weight, f32, c, True), (scale, f32, m, False), (shift, f32, m, False), (h, th, n, False)), stream, check)
 
 
-@_entry
 def sla2_norm_backward(params, x, dh, dx_out, dx, y=None, gate=None, out_weight=None, in_weight=None, scale=None, dy=None, dgate=None,
                        dout_weight=None, din_weight=None, dscale=None, dshift=None, workspace=None, stream=None, check=True,
                        ws_bytes=None) -> int:
     n, m, tx, th = _norm_sizes(params)
     f32, c = torch.float32, params.C
-    args = (ctypes.byref(params), _held(x, tx, n), _held(y, th, n), _held(gate, f32, m), _held(_vector(out_weight), f32, c),
-            _held(_vector(in_weight), f32, c), _held(scale, f32, m), _held(dh, th, n), _held(dx_out, tx, n), _held(dx, tx, n),
-            _held(dy, th, n), _held(dgate, f32, m), _held(_vector(dout_weight), f32, c), _held(_vector(din_weight), f32, c),
-            _held(dscale, f32, m), _held(dshift, f32, m), _ptr(workspace), _bytes(workspace, ws_bytes))
-    return _launch(_lib.sla2_norm_backward, args, (x, y, gate, out_weight, in_weight, scale, dh, dx_out, dx, dy, dgate, dout_weight,
-                                                   din_weight, dscale, dshift, workspace), stream, check)
+    return _call(_lib.sla2_norm_backward, params, (
+        (x, tx, n, False), (y, th, n, False), (gate, f32, m, False), (out_weight, f32, c, True), (in_weight, f32, c, True),
+        (scale, f32, m, False), (dh, th, n, False), (dx_out, tx, n, False), (dx, tx, n, False), (dy, th, n, False), (dgate, f32, m, False),
+        (dout_weight, f32, c, True), (din_weight, f32, c, True), (dscale, f32, m, False), (dshift, f32, m, False), _scratch(workspace)),
+        stream, check, _bytes(workspace, ws_bytes))
 
 
 def sla2_profile_begin(stages, max_calls: int) -> None:

@@ -182,13 +182,15 @@ struct Team {
   }
 };
 
-// ---- sums of the columns of a matrix, as both backward passes end: out[c] = factor[c] * sum over rows of (plus + weight[row][c]) rows[row][c] ----
+// ---- sums of the columns of a matrix, as both backward passes end:
+//      out[c] = (factor_plus + factor[c]) * sum over rows of (weight_plus + weight[row][c]) rows[row][c] ----
 struct ColumnJob {
   const float* rows;                         // [batches][count][columns]
   int batches, count;
   const float* factor;                       // [columns], or null: 1
+  float factor_plus;
   const float* weight;                       // a vector of channels for every `per_weight` rows, weight_stride apart; null: 1
-  float plus;
+  float weight_plus;
   int per_weight;
   long long weight_stride;
   float* out;                                // [batches], out_stride apart

@@ -435,11 +435,18 @@ __global__ __launch_bounds__(kSumRows * 8) void column_sums_kernel(ColumnJobs js
   const bool on = c < js.columns;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (on) {
-    const float* p = j.rows + ((size_t)y * j.count) * js.columns + c;
-    for (int r = r0; r < j.count; r += kSumRows) {
-      f32x4 x = *(const f32x4*)(p + (size_t)r * js.columns);
-      if (j.weight) x *= *(const f32x4*)(j.weight + (size_t)(r / j.per_weight) * j.weight_stride + c) + j.plus;
-      s += x;
+    const float* p = j.rows + (size_t)y * j.count * js.columns + c;
+    // 8 rows on their way at a time: one after the other, 512 rows took as long as 8 trips to memory
+    for (int r = r0; r < j.count; r += 8 * kSumRows) {
+      f32x4 x[8];
+#pragma unroll
+      for (int k = 0; k < 8; k++) {
+        const int at = r + k * kSumRows;
+        x[k] = at < j.count ? *(const f32x4*)(p + (size_t)at * js.columns) : f32x4{0.f, 0.f, 0.f, 0.f};
+        if (j.weight && at < j.count) x[k] *= *(const f32x4*)(j.weight + (size_t)(at / j.per_weight) * j.weight_stride + c) + j.weight_plus;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; k++) s += x[k];
     }
   }
   lds[r0][quad] = s;
@@ -449,7 +456,7 @@ __global__ __launch_bounds__(kSumRows * 8) void column_sums_kernel(ColumnJobs js
   }
   if (r0 == 0 && on) {
     s = lds[0][quad];
-    if (j.factor) s *= *(const f32x4*)(j.factor + c);
+    if (j.factor) s *= *(const f32x4*)(j.factor + c) + j.factor_plus;
     *(f32x4*)(j.out + (size_t)y * j.out_stride + c) = s;
   }
 }
@@ -520,11 +527,14 @@ hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
   js.columns = a.C;
   // the sum over the rows of each batch, or of all
   auto add = [&](const float* from, const float* factor, float* out) {
-    if (out) js.job[js.jobs++] = ColumnJob{from, batch ? a.B : 1, batch ? a.walkers : rows, factor, nullptr, 0.f, 1, 0, out, a.mod_b};
+    if (out) js.job[js.jobs++] = ColumnJob{from, batch ? a.B : 1, batch ? a.walkers : rows, factor, 0.f, nullptr, 0.f, 1, 0, out, a.mod_b};
   };
-  // a weight's: over all rows, each with the modulation of its batch (1 + s or g), which a token's own has in it already
+  // a weight's: over all rows, each with the modulation of its batch (1 + s or g); one that is the same for all rows comes behind the sum,
+  // and that of a token is in it already
   auto add_weight = [&](const float* from, const float* modulation, float plus, float* out) {
-    if (out) js.job[js.jobs++] = ColumnJob{from, 1, rows, nullptr, token ? nullptr : modulation, plus, a.walkers, a.mod_b, out, 0};
+    const bool by_row = batch && a.B > 1;
+    const float *factor = by_row || token ? nullptr : modulation, *weight = by_row ? modulation : nullptr;
+    if (out) js.job[js.jobs++] = ColumnJob{from, 1, rows, factor, plus, weight, plus, a.walkers, a.mod_b, out, 0};
   };
   if (a.dh) {
     if (!token) add(p, a.in_weight, a.dscale);

@@ -20,54 +20,92 @@ template <int LANES> __device__ __forceinline__ float half_head_away(float x) {
   else return dpp_move<0x1B>(dpp_move<0x141>(x));           // row_half_mirror (l ^ 7), quad_perm 3 2 1 0 (l ^ 3)
 }
 
-// The angles of a thread: cos and sin of those of a token.
+// Where the tokens of a thread's rows are, one step of the workgroup after the other.
+struct Position {
+  unsigned t, y, x;                          // of the grid
+  unsigned dt, dy, dx;                       // a step
+  __device__ __forceinline__ Position(const RopeArgs& a, long long first, long long step) : t(0), y(0), x(0), dt(0), dy(0), dx(0) {
+    if (a.positions) return;
+    const unsigned cols = (unsigned)a.grid[2], rows = (unsigned)a.grid[1], n = (unsigned)first, s = (unsigned)step;
+    x = n % cols; y = n / cols % rows; t = n / cols / rows;
+    dx = s % cols; dy = s / cols % rows; dt = s / cols / rows;
+  }
+  __device__ __forceinline__ void advance(const RopeArgs& a) {
+    x += dx; y += dy; t += dt;
+    if (x >= (unsigned)a.grid[2]) { x -= (unsigned)a.grid[2]; y++; }
+    if (y >= (unsigned)a.grid[1]) { y -= (unsigned)a.grid[1]; t++; }
+  }
+  // of token n of batch b, which is where the steps are
+  __device__ __forceinline__ void at(const RopeArgs& a, int b, long long n, bool row, int& p0, int& p1, int& p2) const {
+    if (a.positions) {
+      const int32_t* q = a.positions + b * a.positions_stride + (row ? 3 * n : 0);
+      p0 = q[0]; p1 = q[1]; p2 = q[2];
+    } else {
+      const bool in = t < (unsigned)a.grid[0];
+      p0 = in ? a.origin[0] + (int)t : 0;
+      p1 = in ? a.origin[1] + (int)y : 0;
+      p2 = in ? a.origin[2] + (int)x : 0;
+    }
+  }
+};
+
+// The cosines and sines of the pairs of a thread's channels.  A token has d / 2 angles in all: each lane of a wave forms those of one
+// pair, or as many as there are tokens in the wave more, and all take theirs from LDS, where a wave has a place of its own.  Each lane
+// forming its own 4 or 8, most of them again in other lanes, was up to half of the instructions of a row.
+constexpr int kAngleFloats = 512;            // of a wave: 8 tokens of 64 channels, 4 of 128: cosines, then sines, of the pairs of each
+struct AngleLds {
+  double turns[64];                          // of a pair per position
+  float of[kTeamThreads / kWave * kAngleFloats];
+};
 template <bool BF16, bool HALVES> struct Angles {
   static constexpr int kPairs = HALVES ? 8 : 4;
-  double turns[kPairs];                      // of a pair per position
-  int axis[kPairs];
+  const double* turns;
+  int end0, end1, lanes, pair, half;         // of the axes; lanes of a token in the wave; the first pair that this one forms; d / 2
+  float *token, *from;
+  float other;                               // halves: which way the other channel of a pair goes into this one
   float c[kPairs], s[kPairs];
-  __device__ __forceinline__ void init(const RopeArgs& a, int chunk) {         // backward: turned the other way round
-    const int first = HALVES ? chunk * kChunk % (a.d / 2) : chunk % (a.d / kChunk) * 4;
-#pragma unroll
-    for (int i = 0; i < kPairs; i++) {
-      const int j = first + i;
-      turns[i] = j < a.pairs_end[2] ? a.freq[j] * (a.sign * 0.15915494309189533577) : 0.0;       // 1 / (2 pi)
-      axis[i] = j < a.pairs_end[0] ? 0 : j < a.pairs_end[1] ? 1 : 2;
-    }
+  __device__ __forceinline__ Angles(const RopeArgs& a, const Team& tm, AngleLds& lds) : turns(lds.turns), end0(a.pairs_end[0]), end1(a.pairs_end[1]) {
+    lanes = tm.t.lanes;
+    half = a.d / 2;
+    pair = tm.lane % lanes;
+    for (int j = (int)threadIdx.x; j < half; j += (int)blockDim.x)
+      lds.turns[j] = j < a.pairs_end[2] ? a.freq[j] * (a.sign * 0.15915494309189533577) : 0.0;     // 1 / (2 pi); backward: the other way round
+    __syncthreads();
+    token = lds.of + (int)threadIdx.x / kWave * kAngleFloats + (int)threadIdx.x % kWave / lanes * a.d;
+    other = HALVES && tm.lane % (a.d / kChunk) < a.d / kChunk / 2 ? -1.f : 1.f;
+    from = token + (HALVES ? tm.lane * kChunk % half : tm.lane % (a.d / kChunk) * 4);
   }
   // bf16 results: the hardware's sine and cosine of a fraction of a turn, whose error is far below half a step of bf16
   __device__ __forceinline__ void at(int p0, int p1, int p2) {
-#pragma unroll
-    for (int i = 0; i < kPairs; i++) {
-      const int p = axis[i] == 0 ? p0 : axis[i] == 1 ? p1 : p2;
-      const double t = (double)p * turns[i];
+    wave_lds_fence();
+    for (int j = pair; j < half; j += lanes) {
+      const double t = (double)(j < end0 ? p0 : j < end1 ? p1 : p2) * turns[j];
       const float f = (float)(t - rint(t));
+      float si, co;
       if constexpr (BF16) {
-        s[i] = __builtin_amdgcn_sinf(f);
-        c[i] = __builtin_amdgcn_cosf(f);
+        si = __builtin_amdgcn_sinf(f);
+        co = __builtin_amdgcn_cosf(f);
       } else {
-        sincospif(2.f * f, &s[i], &c[i]);
+        sincospif(2.f * f, &si, &co);
+      }
+      token[j] = co;
+      token[half + j] = si;
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < kPairs; i += 4) {
+      const f32x4 co = *(const f32x4*)(from + i), si = *(const f32x4*)(from + half + i);
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        c[i + k] = co[k];
+        s[i + k] = HALVES ? other * si[k] : si[k];
       }
     }
   }
 };
 
-// Where token n of batch b is.
-__device__ __forceinline__ void position(const RopeArgs& a, int b, int n, int& p0, int& p1, int& p2) {
-  if (a.positions) {
-    const int32_t* p = a.positions + b * a.positions_stride + 3ll * n;
-    p0 = p[0]; p1 = p[1]; p2 = p[2];
-  } else {
-    const unsigned x = (unsigned)a.grid[2], yx = (unsigned)a.grid[1] * x, t = (unsigned)n / yx, r = (unsigned)n - t * yx;
-    const bool in = t < (unsigned)a.grid[0];
-    p0 = in ? a.origin[0] + (int)t : 0;
-    p1 = in ? a.origin[1] + (int)(r / x) : 0;
-    p2 = in ? a.origin[2] + (int)(r % x) : 0;
-  }
-}
-
 template <bool BF16, bool HALVES>
-__device__ __forceinline__ void turn(const RopeArgs& a, const Angles<BF16, HALVES>& an, bool second, float (&x)[8]) {
+__device__ __forceinline__ void turn(const RopeArgs& a, const Angles<BF16, HALVES>& an, float (&x)[8]) {
   if constexpr (HALVES) {
     float o[8];
     if (a.d == 128) {
@@ -78,7 +116,7 @@ __device__ __forceinline__ void turn(const RopeArgs& a, const Angles<BF16, HALVE
       for (int i = 0; i < 8; i++) o[i] = half_head_away<8>(x[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = x[i] * an.c[i] + (second ? o[i] : -o[i]) * an.s[i];
+    for (int i = 0; i < 8; i++) x[i] = x[i] * an.c[i] + o[i] * an.s[i];
   } else {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -115,13 +153,12 @@ template <int V> struct Place {
 template <int V, bool BF16, bool HALVES, int NORM>
 __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) void rope_kernel(RopeArgs a) {
   __shared__ float lds[kExchangeFloats];
+  __shared__ AngleLds angles;
   constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
   Team tm(a.team, lds);
   const int part = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers, b = part / a.groups;
   const Place<V> at(a, tm, part % a.groups);
-  const bool second = at.channel >= a.d / 2;
-  Angles<BF16, HALVES> an;
-  an.init(a, tm.lane);
+  Angles<BF16, HALVES> an(a, tm, angles);
   const float share = 1.f / (float)(NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
   float w[2][W][8];
   if (NORM != SLA2_ROPE_NORM_NONE) {
@@ -130,6 +167,8 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
 #pragma unroll
       for (int v = 0; v < W; v++) load_vector8(a.weight[t], NORM == SLA2_ROPE_NORM_TOKEN ? at.col[v] : at.channel, 1.f, w[t][v]);
   }
+  const long long step = (long long)a.walkers * a.teams;
+  Position where(a, (long long)walker * a.teams + tm.team, step);
   struct Row {
     Raw<BF16> x[2][V];
     int p0, p1, p2;
@@ -144,16 +183,16 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
 #pragma unroll
       for (int v = 0; v < V; v++) r.x[t][v] = row && at.has[v] && t < a.tensors ? load8<BF16>(px, at.in[v]) : zero8<BF16>();
     }
-    position(a, b, row ? (int)(n + tm.sub) : 0, r.p0, r.p1, r.p2);
+    where.at(a, b, n + tm.sub, row, r.p0, r.p1, r.p2);
     return r;
   };
-  const long long step = (long long)a.walkers * a.teams;
   for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += step) {
     const long long n = n0 + tm.first;
     const bool row = n + tm.sub < a.N;
     const long long yo = b * a.sout.b + n * a.sout.n;
     Row cur = load(n0);
     Raw<BF16> (&raw)[2][V] = cur.x;
+    where.advance(a);
     an.at(cur.p0, cur.p1, cur.p2);
     float s[2] = {0.f, 0.f};
     if (NORM == SLA2_ROPE_NORM_TOKEN) {
@@ -187,7 +226,7 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
 #pragma unroll
           for (int i = 0; i < 8; i++) x[i] = x[i] * s[t] * w[t][v % W][i];
         }
-        turn<BF16, HALVES>(a, an, second, x);
+        turn<BF16, HALVES>(a, an, x);
         if (row && at.has[v]) put8<BF16>(at_elem<BF16>(a.y[t], yo), at.out[v], pack8<BF16>(x));
       }
     }
@@ -198,14 +237,13 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
 template <int V, bool BF16, bool HALVES, int NORM>
 __global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void rope_bwd_kernel(RopeArgs a) {
   __shared__ float lds[kExchangeFloats];
+  __shared__ AngleLds angles;
   constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
   __shared__ f32x4 sums[kTeamThreads * 2 * W];            // 8 W floats of every thread
   Team tm(a.team, lds);
   const int part = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers, b = part / a.groups;
   const Place<V> at(a, tm, part % a.groups);
-  const bool second = at.channel >= a.d / 2;
-  Angles<BF16, HALVES> an;
-  an.init(a, tm.lane);
+  Angles<BF16, HALVES> an(a, tm, angles);
   const float share = 1.f / (float)(NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
   float w[2][W][8], acc[2][W][8];
 #pragma unroll
@@ -216,6 +254,8 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void rope_bwd_kernel
 #pragma unroll
       for (int i = 0; i < 8; i++) acc[t][v][i] = 0.f;
     }
+  const long long step = (long long)a.walkers * a.teams;
+  Position where(a, (long long)walker * a.teams + tm.team, step);
   struct Row {
     Raw<BF16> x[2][V], g[2][V];
     int p0, p1, p2;
@@ -234,15 +274,15 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void rope_bwd_kernel
         r.g[t][v] = on ? load8<BF16>(pg, at.out[v]) : zero8<BF16>();
       }
     }
-    position(a, b, row ? (int)(n + tm.sub) : 0, r.p0, r.p1, r.p2);
+    where.at(a, b, n + tm.sub, row, r.p0, r.p1, r.p2);
     return r;
   };
-  const long long step = (long long)a.walkers * a.teams;
   for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += step) {
     const long long n = n0 + tm.first;
     const bool row = n + tm.sub < a.N;
     const long long xo = b * a.sin.b + n * a.sin.n;
     Row cur = load(n0);
+    where.advance(a);
     an.at(cur.p0, cur.p1, cur.p2);
     float s[4] = {0.f, 0.f, 0.f, 0.f};                   // over all heads: sum x^2, sum t x of q, of k
     float g[2][W][8];
@@ -254,7 +294,7 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void rope_bwd_kernel
           float x[8];
           unpack8<BF16>(cur.x[t][v], x);
           unpack8<BF16>(cur.g[t][v], g[t][v]);
-          turn<BF16, HALVES>(a, an, second, g[t][v]);
+          turn<BF16, HALVES>(a, an, g[t][v]);
 #pragma unroll
           for (int i = 0; i < 8; i++) {
             s[2 * t] += x[i] * x[i];
@@ -274,7 +314,7 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void rope_bwd_kernel
         float xx = s[2 * t], tx = s[2 * t + 1];
         if (!kToken) {
           unpack8<BF16>(cur.g[t][v], gv);
-          turn<BF16, HALVES>(a, an, second, gv);
+          turn<BF16, HALVES>(a, an, gv);
           xx = tx = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; i++) {
@@ -394,7 +434,7 @@ hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
   const int rows = workgroups(a);
   for (int t = 0; t < 2; t++)
     if (a.dweight[t])
-      js.job[js.jobs++] = ColumnJob{a.partial + (size_t)t * rows * js.columns, 1, rows, nullptr, nullptr, 0.f, 1, 0, a.dweight[t], 0};
+      js.job[js.jobs++] = ColumnJob{a.partial + (size_t)t * rows * js.columns, 1, rows, nullptr, 0.f, nullptr, 0.f, 1, 0, a.dweight[t], 0};
   return launch_column_sums(js, stream);
 }
 
