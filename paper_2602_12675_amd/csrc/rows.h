@@ -13,7 +13,8 @@ namespace sla2 {
 
 constexpr int kChunk = 8;                    // channels: 16 bytes of bf16
 constexpr int kMaxRow = 8192;                // channels of a row: 8 waves of 2 chunks a lane
-constexpr int kTeamThreads = 512;            // most threads of a workgroup
+constexpr int kTeamThreads = 512;            // threads of a workgroup
+constexpr int kMaxThreads = 1024;
 constexpr int kCus = 256;
 // Waves of a SIMD that a kernel leaves registers for: 4 (two workgroups a CU), or 2 where a row takes more than 128 registers a thread.
 constexpr int waves_of(bool many_registers) { return many_registers ? 2 : 4; }
@@ -24,24 +25,23 @@ struct RowTeam {
   int lanes, waves, vec;                     // lanes of a wave, whole waves (1 where lanes < 64), chunks a thread
   __host__ __device__ int threads() const { return lanes * waves; }
 };
-// The fewest waves with at most `most` chunks a thread (with more where a workgroup has not that many waves), and then the fewest chunks.
-inline RowTeam row_team(int chunks, int most) {
+// The fewest waves with at most `most` chunks a thread (with more where a workgroup of `threads` threads has not that many waves), and then the
+// fewest chunks.
+inline RowTeam row_team(int chunks, int most, int threads = kTeamThreads) {
   RowTeam t{64, 1, 1};
   if (chunks <= 64) {
     while (t.lanes > 8 && t.lanes / 2 >= chunks) t.lanes /= 2;
     return t;
   }
   const int rounds = (chunks + 63) / 64, waves = (rounds + most - 1) / most;      // rounds: of a whole wave
-  t.waves = waves < kTeamThreads / 64 ? waves : kTeamThreads / 64;
+  t.waves = waves < threads / kWave ? waves : threads / kWave;
   t.vec = (rounds + t.waves - 1) / t.waves;
+  t.waves = (rounds + t.vec - 1) / t.vec;
   return t;
 }
-// Teams of a workgroup, of 8 waves where there are rows enough.
-inline int block_threads() {
-  return kTeamThreads;
-}
-inline int block_teams(const RowTeam& t, int rows) {
-  const int n = t.threads() < block_threads() ? block_threads() / t.threads() : 1;
+// Teams of a workgroup of `threads` threads, where there are rows enough.
+inline int block_teams(const RowTeam& t, int rows, int threads = kTeamThreads) {
+  const int n = t.threads() < threads ? threads / t.threads() : 1;
   return n < rows ? n : rows;
 }
 // Workgroups of a launch: those that are resident at once, with `threads` threads a CU.  Each goes through its rows side by side with the
@@ -102,6 +102,10 @@ template <bool BF16> __device__ __forceinline__ Raw<BF16> pack8(const float (&x)
   }
   return r;
 }
+// The compiler takes r to be another value from here on, so that what is unpacked from it is unpacked again rather than kept.
+template <bool BF16> __device__ __forceinline__ void unpack_again(Raw<BF16>& r) {
+  if constexpr (BF16) asm volatile("" : "+v"(r.a[0]));
+}
 // 8 fp32 values of a vector of channels that may be absent
 __device__ __forceinline__ void load_vector8(const float* p, unsigned elem, float absent, float (&x)[8]) {
   if (p) {
@@ -112,10 +116,17 @@ __device__ __forceinline__ void load_vector8(const float* p, unsigned elem, floa
   }
 }
 
+// x and that of another lane of its 16, added in one instruction: every lane of these patterns has a source, so what an absent one would
+// give does not matter, and the compiler may put the move into the addition.
+template <int CTRL> __device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum8(float x) { return dpp_add<0x141>(dpp_add<0x4E>(dpp_add<0xB1>(x))); }      // quad_perm 1 0 3 2, 2 3 0 1, row_half_mirror
+__device__ __forceinline__ float sum16(float x) { return dpp_add<0x140>(sum8(x)); }                               // row_mirror
 // Sum over `lanes` neighbouring lanes (8, 16, 32, 64; the same for the whole launch), on all of them.
 __device__ __forceinline__ float lanes_sum(float x, int lanes) {
-  x = row_sum<8>(x);
-  if (lanes > 8) x += dpp_move<0x140>(x);              // row_mirror
+  x = sum8(x);
+  if (lanes > 8) x = dpp_add<0x140>(x);
   if (lanes > 16) {
     const unsigned u = __builtin_bit_cast(unsigned, x);
     const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
@@ -131,7 +142,7 @@ __device__ __forceinline__ float inv_sqrt(float x) { return __builtin_amdgcn_rsq
 // A thread's place in its team, and its team's among those of the workgroup.  Every thread of a workgroup takes part in every exchange, so
 // all its teams make equally many steps.  What is the same for a wave is in scalar registers: the rows' addresses above all.
 constexpr int kExchange = 4;                 // sums that a step exchanges at most
-constexpr int kExchangeFloats = 2 * (kTeamThreads / kWave) * kExchange;
+constexpr int kExchangeFloats = 2 * (kMaxThreads / kWave) * kExchange;
 struct Team {
   RowTeam t;
   int team, lane;                            // team of the workgroup; thread of the team
@@ -144,32 +155,31 @@ struct Team {
     first = __builtin_amdgcn_readfirstlane(team);
     sub = team - first;
   }
-  // x[k] of every wave of the team, [wave][K], behind a barrier.  Two buffers in turn: the next exchange but one writes over this one's,
-  // behind the barrier of the next, which every wave reaches after its reads.
-  template <int K> __device__ __forceinline__ const float* exchange(const float (&x)[K]) {
+  // x[k] of wave l % 16 of the team on lane l (0 where there is no such wave), behind a barrier: one read of LDS, and what is done with the
+  // waves' values is done by 16 lanes side by side.  Two buffers in turn: the next exchange but one writes over this one's, behind the barrier
+  // of the next, which every wave reaches after its reads.
+  template <int K> __device__ __forceinline__ void exchange(float (&x)[K]) {
     static_assert(K <= kExchange, "");
     float* m = lds + flip;
     flip ^= kExchangeFloats / 2;
-    const int wave = (int)threadIdx.x / kWave;
+    const int wave = (int)threadIdx.x / kWave, other = (int)threadIdx.x % 16;
     if ((int)threadIdx.x % kWave == 0) {
 #pragma unroll
-      for (int k = 0; k < K; k++) m[wave * K + k] = x[k];
+      for (int k = 0; k < K; k++) m[wave * kExchange + k] = x[k];
     }
     __syncthreads();
-    return m + first * t.waves * K;
+    const float* o = m + (first * t.waves + (other < t.waves ? other : 0)) * kExchange;
+#pragma unroll
+    for (int k = 0; k < K; k++) x[k] = other < t.waves ? o[k] : 0.f;
   }
   // sums over the team
   template <int K> __device__ __forceinline__ void sum(float (&x)[K]) {
 #pragma unroll
     for (int k = 0; k < K; k++) x[k] = lanes_sum(x[k], t.lanes);
     if (t.waves == 1) return;
-    const float* o = exchange(x);
+    exchange(x);
 #pragma unroll
-    for (int k = 0; k < K; k++) x[k] = o[k];
-    for (int w = 1; w < t.waves; w++) {
-#pragma unroll
-      for (int k = 0; k < K; k++) x[k] += o[w * K + k];
-    }
+    for (int k = 0; k < K; k++) x[k] = sum16(x[k]);
   }
   // channels that wave w of the team holds of a row of `chunks` chunks
   __device__ __forceinline__ int channels(int w, int chunks) const {

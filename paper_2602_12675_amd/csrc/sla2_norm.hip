@@ -23,17 +23,17 @@ constexpr bool large_forward(int vec, int part, bool token) {
   return vec == 3 ? both || token : vec == 2 && both && token;
 }
 
-// What the statistics of a row need of the team: 1 / C, 1 / channels of this wave, and in LDS the channels of every wave.
+// What the statistics of a row need of the team: 1 / C, 1 / channels of this wave, and the channels of wave l % 16 on lane l.
 struct Counts {
-  float all, mine;
-  const float* of;
-  __device__ __forceinline__ Counts(const Team& tm, int chunks, float* lds) : of(lds) {
+  float all, mine, other;
+  __device__ __forceinline__ Counts(const Team& tm, int chunks) {
     all = 1.f / (float)(chunks * kChunk);
     mine = all;
+    other = 0.f;
     if (tm.t.waves == 1) return;
-    const int own = tm.channels(tm.lane / kWave, chunks);
+    const int own = tm.channels(tm.lane / kWave, chunks), w = (int)threadIdx.x % 16;
     mine = own ? 1.f / (float)own : 0.f;
-    if ((int)threadIdx.x < tm.t.waves) lds[threadIdx.x] = (float)tm.channels((int)threadIdx.x, chunks);    // read behind an exchange's barrier
+    other = w < tm.t.waves ? (float)tm.channels(w, chunks) : 0.f;
   }
 };
 
@@ -68,70 +68,60 @@ __device__ __forceinline__ Moments moments(Team& tm, const Counts& n, int kind, 
   }
   m2 = lanes_sum(m2, tm.t.lanes);
   if (tm.t.waves > 1) {
-    const float own[2] = {mu, m2};
-    const float* o = tm.exchange(own);
-    mu = m2 = 0.f;
-    for (int w = 0; w < tm.t.waves; w++) mu += n.of[w] * o[2 * w];
-    mu *= n.all;
-    for (int w = 0; w < tm.t.waves; w++) m2 += o[2 * w + 1] + n.of[w] * (o[2 * w] - mu) * (o[2 * w] - mu);
+    float o[2] = {mu, m2};
+    tm.exchange(o);
+    mu = sum16(n.other * o[0]) * n.all;
+    const float d = o[0] - mu;
+    m2 = sum16(o[1] + n.other * d * d);
   }
   return {mu, inv_sqrt(m2 * n.all + eps)};
 }
 
-// The same with mean(t) and mean(t n), n = (x - mu) r, for the gradient t behind the norm: all sums in one exchange.
+// The same with mean(t) and mean(t n), n = (x - mu) r, for the gradient t behind the norm: all sums in one exchange.  value(x) and
+// gradient(t) give a thread's chunk of either.
 struct BackMoments {
   float mu, r, t, tn;
 };
-template <int V>
-__device__ __forceinline__ BackMoments back_moments(Team& tm, const Counts& n, int kind, const float (&x)[V][8], const float (&t)[V][8],
-                                                    const bool (&has)[V], float eps) {
+template <class Value, class Gradient>
+__device__ __forceinline__ BackMoments back_moments(Team& tm, const Counts& n, int kind, Value value, Gradient gradient, bool has, float eps) {
+  float x[8], t[8];
+  value(x);
   if (kind == SLA2_NORM_RMS) {
     float s[2] = {0.f, 0.f};
+    gradient(t);
 #pragma unroll
-    for (int v = 0; v < V; v++)
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        s[0] += x[v][i] * x[v][i];
-        s[1] += t[v][i] * x[v][i];
-      }
+    for (int i = 0; i < 8; i++) {
+      s[0] += x[i] * x[i];
+      s[1] += t[i] * x[i];
+    }
     tm.sum(s);
     const float r = inv_sqrt(s[0] * n.all + eps);
     return {0.f, r, 0.f, s[1] * n.all * r};
   }
   float mu = 0.f, m2 = 0.f, st = 0.f, stx = 0.f;
 #pragma unroll
-  for (int v = 0; v < V; v++)
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      mu += x[v][i];
-      st += t[v][i];
-    }
+  for (int i = 0; i < 8; i++) mu += x[i];
   mu = lanes_sum(mu, tm.t.lanes) * n.mine;
+  const float m = has ? mu : 0.f;
+  gradient(t);
 #pragma unroll
-  for (int v = 0; v < V; v++) {
-    const float m = has[v] ? mu : 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const float c = x[v][i] - m;
-      m2 += c * c;
-      stx += t[v][i] * c;
-    }
+  for (int i = 0; i < 8; i++) {
+    const float c = x[i] - m;
+    m2 += c * c;
+    st += t[i];
+    stx += t[i] * c;
   }
   m2 = lanes_sum(m2, tm.t.lanes);
   st = lanes_sum(st, tm.t.lanes);
   stx = lanes_sum(stx, tm.t.lanes);
   if (tm.t.waves > 1) {
-    const float own[4] = {mu, m2, st, stx};
-    const float* o = tm.exchange(own);
-    mu = m2 = st = stx = 0.f;
-    for (int w = 0; w < tm.t.waves; w++) mu += n.of[w] * o[4 * w];
-    mu *= n.all;
-    for (int w = 0; w < tm.t.waves; w++) {
-      const float d = o[4 * w] - mu;
-      m2 += o[4 * w + 1] + n.of[w] * d * d;
-      st += o[4 * w + 2];
-      stx += o[4 * w + 3] + d * o[4 * w + 2];
-    }
+    float o[4] = {mu, m2, st, stx};
+    tm.exchange(o);
+    mu = sum16(n.other * o[0]) * n.all;
+    const float d = o[0] - mu;
+    m2 = sum16(o[1] + n.other * d * d);
+    st = sum16(o[2]);
+    stx = sum16(o[3] + d * o[2]);
   }
   const float r = inv_sqrt(m2 * n.all + eps);
   return {mu, r, st * n.all, stx * n.all * r};
@@ -157,10 +147,10 @@ template <int V> struct Columns {
 // x' and h
 template <int V, bool XB, bool HB, int PART, bool TOKEN>
 __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, PART, TOKEN))) void norm_kernel(NormArgs a) {
-  __shared__ float lds[kExchangeFloats], counts[kTeamThreads / kWave];
+  __shared__ float lds[kExchangeFloats];
   Team tm(a.team, lds);
   const int b = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers;
-  const Counts n_of(tm, a.C / kChunk, counts);
+  const Counts n_of(tm, a.C / kChunk);
   const Columns<V> at(a, tm);
   float g[V][8], w[V][8], sh[V][8], wo[V][8], wi[V][8];   // g w_out; w_in (1 + s); b.  TOKEN: row by row, of w_out and w_in
   auto vectors = [&](long long mod, const unsigned (&off)[V]) {
@@ -233,194 +223,202 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, PART, TOKEN
   }
 }
 
-// One of the sums of a workgroup: its teams' in order, through LDS, into row `at` of the partial sums.
-template <int V>
-__device__ __forceinline__ void store_partial(const Team& tm, int teams, float* lds, const float (&acc)[V][8], const bool (&has)[V],
-                                              const unsigned (&col)[V], int C, float* to) {
+// One of the sums of a workgroup: its teams' in order, through LDS, into its row of the partial sums.
+__device__ __forceinline__ void store_partial(const Team& tm, int teams, float* lds, const float (&acc)[8], bool has, unsigned col, int C,
+                                              float* to) {
   if (teams > 1) {
     __syncthreads();
-    if (tm.team > 0 && tm.team < teams) {
-#pragma unroll
-      for (int v = 0; v < V; v++)
-        if (has[v]) {
-          float* p = lds + (size_t)(tm.team - 1) * C + col[v];
-          *(f32x4*)p = f32x4{acc[v][0], acc[v][1], acc[v][2], acc[v][3]};
-          *(f32x4*)(p + 4) = f32x4{acc[v][4], acc[v][5], acc[v][6], acc[v][7]};
-        }
-    }
+    if (tm.team > 0 && has) store8<false>(lds, (unsigned)((tm.team - 1) * C) + col, pack8<false>(acc));
     __syncthreads();
   }
-  if (tm.team == 0) {
+  if (tm.team > 0 || !has) return;
+  float s[8];
 #pragma unroll
-    for (int v = 0; v < V; v++)
-      if (has[v]) {
-        float s[8];
+  for (int i = 0; i < 8; i++) s[i] = acc[i];
+  for (int t = 1; t < teams; t++) {
+    float o[8];
+    load_vector8(lds, (unsigned)((t - 1) * C) + col, 0.f, o);
 #pragma unroll
-        for (int i = 0; i < 8; i++) s[i] = acc[v][i];
-        for (int t = 1; t < teams; t++) {
-          const float* p = lds + (size_t)(t - 1) * C + col[v];
-#pragma unroll
-          for (int i = 0; i < 8; i++) s[i] += p[i];
-        }
-        store8<false>(to, col[v], pack8<false>(s));
-      }
+    for (int i = 0; i < 8; i++) s[i] += o[i];
   }
+  store8<false>(to, col, pack8<false>(s));
 }
 
-template <int V, bool XB, bool HB, int PART, bool TOKEN>
-__global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void norm_bwd_kernel(NormArgs a) {
-  __shared__ float lds[kExchangeFloats], counts[kTeamThreads / kWave];
-  extern __shared__ float teams_lds[];       // [teams - 1][C]
+// A thread has one chunk, and nothing is kept in fp32 across the sums of a row: the values are unpacked again behind them, and the vectors of
+// the batch are read from LDS.  What stays from row to row are the sums for the column gradients.  The time hangs on the waves that
+// registers leave room for: with the vectors in registers, two chunks a thread from 4,096 channels on (its second workgroup finding no place
+// on the CU) 7,180 rows of 4,976 bf16 channels took 205 us, layer norms on both sides, and 20,000 of 5,120 with an fp32 stream 411 us;
+// so 140 and 344 us.  The next row fetched ahead cost more in registers than it gave.
+template <bool XB, bool HB, int PART, bool TOKEN>
+__global__ __launch_bounds__(kMaxThreads, 4) void norm_bwd_kernel(NormArgs a) {
+  __shared__ float lds[kExchangeFloats];
+  // g w_out and w_in (1 + s) of the batch, [2][C + 8], the last 8 being 0 for threads without a channel; at the end the sums of the teams,
+  // [teams - 1][C]
+  extern __shared__ float shared[];
   Team tm(a.team, lds);
   const int b = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers;
-  const Counts n_of(tm, a.C / kChunk, counts);
-  const Columns<V> at(a, tm);
-  float g[V][8], w[V][8], wo[V][8], wi[V][8];             // as in norm_kernel; TOKEN: g, 1 + s, w_out, w_in
-  float p_sum[V][8], s_sum[V][8], q_sum[V][8];            // TOKEN: of d w_in, nothing, of d w_out
-  auto vectors = [&](long long mod, const unsigned (&off)[V]) {
+  const Counts n_of(tm, a.C / kChunk);
+  const Columns<1> columns(a, tm);
+  const bool has = columns.has[0];
+  const unsigned col = columns.col[0], at_x = columns.x[0], at_h = columns.h[0], at_mod = columns.mod[0], place = has ? col : (unsigned)a.C;
+  float p_sum[8], s_sum[8], q_sum[8];                     // TOKEN: of d w_in, nothing, of d w_out
 #pragma unroll
-    for (int v = 0; v < V; v++) {
-      if (PART & kAfter) load_vector8(a.gate ? a.gate + mod : nullptr, off[v], 1.f, g[v]);
-      if (PART & kBefore) {
-        load_vector8(a.scale ? a.scale + mod : nullptr, off[v], 0.f, w[v]);
-#pragma unroll
-        for (int i = 0; i < 8; i++) w[v][i] += 1.f;
-      }
-    }
-  };
-#pragma unroll
-  for (int v = 0; v < V; v++) {
-#pragma unroll
-    for (int i = 0; i < 8; i++) g[v][i] = w[v][i] = p_sum[v][i] = s_sum[v][i] = q_sum[v][i] = 0.f;
-    if (PART & kAfter) load_vector8(a.out_weight, at.col[v], 1.f, wo[v]);
-    if (PART & kBefore) load_vector8(a.in_weight, at.col[v], 1.f, wi[v]);
-  }
+  for (int i = 0; i < 8; i++) p_sum[i] = s_sum[i] = q_sum[i] = 0.f;
+  float* const scales_lds = shared + a.C + kChunk;
   if (!TOKEN) {
-    vectors(b * a.mod_b, at.col);
-#pragma unroll
-    for (int v = 0; v < V; v++)
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        if (PART & kBefore) w[v][i] *= wi[v][i];
-        if (PART & kAfter) g[v][i] = at.has[v] ? g[v][i] * wo[v][i] : 0.f;
-      }
+    if ((int)threadIdx.x < kChunk) shared[a.C + threadIdx.x] = scales_lds[a.C + threadIdx.x] = 0.f;
+    for (int c = (int)threadIdx.x * 4; c < a.C; c += (int)blockDim.x * 4) {
+      const f32x4 one = {1.f, 1.f, 1.f, 1.f};
+      const long long mod = b * a.mod_b + c;
+      if (PART & kAfter) *(f32x4*)(shared + c) = (a.gate ? *(const f32x4*)(a.gate + mod) : one) * (a.out_weight ? *(const f32x4*)(a.out_weight + c) : one);
+      if (PART & kBefore) *(f32x4*)(scales_lds + c) = (a.scale ? *(const f32x4*)(a.scale + mod) + one : one) * (a.in_weight ? *(const f32x4*)(a.in_weight + c) : one);
+    }
+    __syncthreads();
   }
   for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += (long long)a.walkers * a.teams) {
     const long long n = n0 + tm.first;
-    const bool row = n + tm.sub < a.N;
+    const bool row = n + tm.sub < a.N, on = row && has;
     const long long xo = b * a.x_b + n * a.x_n, ho = b * a.h_b + n * a.h_n, mo = b * a.mod_b + n * a.mod_n;
-    const void *px = at_elem<XB>(a.x, xo), *pu = at_elem<XB>(a.dx_out, xo), *ph = at_elem<HB>(a.dh, ho), *py = at_elem<HB>(a.y, ho);
-    Raw<XB> rx[V], ru[V];
-    Raw<HB> ry[V], rh[V];
-#pragma unroll
-    for (int v = 0; v < V; v++) {
-      const bool on = row && at.has[v];
-      if (PART & kBefore) {
-        rx[v] = on ? load8<XB>(px, at.x[v]) : zero8<XB>();
-        rh[v] = on ? load8<HB>(ph, at.h[v]) : zero8<HB>();
-      }
-      ru[v] = on && a.dx_out ? load8<XB>(pu, at.x[v]) : zero8<XB>();
-      if (PART & kAfter) ry[v] = on ? load8<HB>(py, at.h[v]) : zero8<HB>();
+    Raw<XB> rx, ru = on && a.dx_out ? load8<XB>(at_elem<XB>(a.dx_out, xo), at_x) : zero8<XB>();
+    Raw<HB> ry, rh;
+    if (PART & kBefore) {
+      rx = on ? load8<XB>(at_elem<XB>(a.x, xo), at_x) : zero8<XB>();
+      rh = on ? load8<HB>(at_elem<HB>(a.dh, ho), at_h) : zero8<HB>();
     }
-    if (TOKEN && row) vectors(mo, at.mod);
-    float u[V][8];
+    if (PART & kAfter) ry = on ? load8<HB>(at_elem<HB>(a.y, ho), at_h) : zero8<HB>();
+    // the gate and 1 + s: with their weights, or of a token without them; 0 where there is no value
+    auto gates = [&](float (&g)[8]) {
+      if (TOKEN) {
+        load_vector8(a.gate && row ? a.gate + mo : nullptr, at_mod, 1.f, g);
 #pragma unroll
-    for (int v = 0; v < V; v++) unpack8<XB>(ru[v], u[v]);
-    // Behind a norm: grad[] += the gradient in front of it from t, of the value x; each(v, i, n) with the normalised value
-    auto through = [&](int kind, const float (&x)[V][8], const float (&t)[V][8], float (&grad)[V][8], auto each) {
+        for (int i = 0; i < 8; i++) g[i] = on ? g[i] : 0.f;
+      } else {
+        load_vector8(shared, place, 0.f, g);
+      }
+    };
+    auto scales = [&](float (&w)[8]) {
+      if (TOKEN) {
+        load_vector8(a.scale && row ? a.scale + mo : nullptr, at_mod, 0.f, w);
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = on ? w[i] + 1.f : 0.f;
+      } else {
+        load_vector8(scales_lds, place, 0.f, w);
+      }
+    };
+    // Behind a norm of the value with the gradient: each(n, g) with the normalised values and the gradient in front of it
+    auto through = [&](int kind, auto value, auto gradient, auto again, auto each) {
+      float x[8], t[8];
       if (kind == SLA2_NORM_NONE) {
-#pragma unroll
-        for (int v = 0; v < V; v++)
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            each(v, i, x[v][i]);
-            grad[v][i] += t[v][i];
-          }
+        value(x);
+        gradient(t);
+        each(x, t);
         return;
       }
-      const BackMoments m = back_moments<V>(tm, n_of, kind, x, t, at.has, a.eps);
+      const BackMoments m = back_moments(tm, n_of, kind, value, gradient, has, a.eps);
       const float rt = -m.r * m.t, rtn = -m.r * m.tn;
+      again();
+      value(x);
+      gradient(t);
 #pragma unroll
-      for (int v = 0; v < V; v++)
+      for (int i = 0; i < 8; i++) {
+        x[i] = (x[i] - m.mu) * m.r;
+        t[i] = m.r * t[i] + (x[i] * rtn + rt);
+      }
+      each(x, t);
+    };
+    float u[8];
+    if (!(PART & kBefore)) {
+      unpack8<XB>(ru, u);
+    } else {
+      auto value = [&](float (&x)[8]) { unpack8<XB>(rx, x); };
+      auto gradient = [&](float (&t)[8]) {
+        float w[8];
+        unpack8<HB>(rh, t);
+        scales(w);
+        if (TOKEN) {
+          float wi[8];
+          load_vector8(a.in_weight, col, 1.f, wi);
+#pragma unroll
+          for (int i = 0; i < 8; i++) w[i] *= wi[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) t[i] *= w[i];
+      };
+      auto again = [&]() {
+        unpack_again(rx);
+        unpack_again(rh);
+      };
+      through(a.norm_in, value, gradient, again, [&](const float (&nv)[8], const float (&grad)[8]) {
+        float dh[8];
+        unpack8<HB>(rh, dh);
+        unpack8<XB>(ru, u);
+        if (TOKEN) {
+          float w[8], wi[8], ds[8];
+          scales(w);
+          load_vector8(a.in_weight, col, 1.f, wi);
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            ds[i] = dh[i] * nv[i];
+            p_sum[i] += ds[i] * w[i];
+            ds[i] *= wi[i];
+          }
+          if (on && a.dscale) put8<false>(a.dscale + mo, at_mod, pack8<false>(ds));
+          if (on && a.dshift) put8<false>(a.dshift + mo, at_mod, pack8<false>(dh));
+        }
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-          const float nv = (x[v][i] - m.mu) * m.r;
-          each(v, i, nv);
-          grad[v][i] += m.r * t[v][i] + (nv * rtn + rt);
-        }
-    };
-    if (PART & kBefore) {
-      float x[V][8], t[V][8], dh[V][8], ds[V][8];
-#pragma unroll
-      for (int v = 0; v < V; v++) {
-        unpack8<XB>(rx[v], x[v]);
-        unpack8<HB>(rh[v], dh[v]);
-#pragma unroll
-        for (int i = 0; i < 8; i++) t[v][i] = dh[v][i] * (TOKEN ? wi[v][i] * w[v][i] : w[v][i]);
-      }
-      through(a.norm_in, x, t, u, [&](int v, int i, float nv) {
-        if (TOKEN) {
-          ds[v][i] = dh[v][i] * nv;
-          p_sum[v][i] += row ? ds[v][i] * w[v][i] : 0.f;
-          ds[v][i] *= wi[v][i];
-        } else {
-          p_sum[v][i] += dh[v][i] * nv;
-          s_sum[v][i] += dh[v][i];
+          if (!TOKEN) {
+            p_sum[i] += dh[i] * nv[i];
+            s_sum[i] += dh[i];
+          }
+          u[i] += grad[i];
         }
       });
-      if (TOKEN) {
-        float *pds = a.dscale + mo, *pdb = a.dshift + mo;
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-          if (row && at.has[v] && a.dscale) put8<false>(pds, at.mod[v], pack8<false>(ds[v]));
-          if (row && at.has[v] && a.dshift) put8<false>(pdb, at.mod[v], pack8<false>(dh[v]));
-        }
-      }
     }
     if (PART & kAfter) {
-      float y[V][8], t[V][8], dy[V][8], dg[V][8];
-#pragma unroll
-      for (int v = 0; v < V; v++) {
-        unpack8<HB>(ry[v], y[v]);
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-          if (TOKEN) t[v][i] = row && at.has[v] ? u[v][i] * (wo[v][i] * g[v][i]) : 0.f;
-          else t[v][i] = u[v][i] * g[v][i];
-          dy[v][i] = 0.f;
-        }
-      }
-      through(a.norm_out, y, t, dy, [&](int v, int i, float nv) {
+      auto value = [&](float (&x)[8]) { unpack8<HB>(ry, x); };
+      auto gradient = [&](float (&t)[8]) {
+        gates(t);
         if (TOKEN) {
-          dg[v][i] = u[v][i] * nv;
-          q_sum[v][i] += row ? dg[v][i] * g[v][i] : 0.f;
-          dg[v][i] *= wo[v][i];
-        } else {
-          q_sum[v][i] += u[v][i] * nv;
+          float wo[8];
+          load_vector8(a.out_weight, col, 1.f, wo);
+#pragma unroll
+          for (int i = 0; i < 8; i++) t[i] *= wo[i];
         }
+#pragma unroll
+        for (int i = 0; i < 8; i++) t[i] *= u[i];
+      };
+      auto again = [&]() { unpack_again(ry); };
+      through(a.norm_out, value, gradient, again, [&](const float (&nv)[8], const float (&grad)[8]) {
+        if (TOKEN) {
+          float g[8], wo[8], dg[8];
+          gates(g);
+          load_vector8(a.out_weight, col, 1.f, wo);
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            dg[i] = u[i] * nv[i];
+            q_sum[i] += dg[i] * g[i];
+            dg[i] *= wo[i];
+          }
+          if (on && a.dgate) put8<false>(a.dgate + mo, at_mod, pack8<false>(dg));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; i++) q_sum[i] += u[i] * nv[i];
+        }
+        if (on) put8<HB>(at_elem<HB>(a.dy, ho), at_h, pack8<HB>(grad));
+#pragma unroll
+        for (int i = 0; i < 8; i++) u[i] *= a.rho;
       });
-      void* pdy = at_elem<HB>(a.dy, ho);
-      float* pdg = a.dgate + mo;
-#pragma unroll
-      for (int v = 0; v < V; v++) {
-        const bool on = row && at.has[v];
-        if (on) put8<HB>(pdy, at.h[v], pack8<HB>(dy[v]));
-        if (TOKEN && on && a.dgate) put8<false>(pdg, at.mod[v], pack8<false>(dg[v]));
-#pragma unroll
-        for (int i = 0; i < 8; i++) u[v][i] *= a.rho;
-      }
     }
-    void* pdx = at_elem<XB>(a.dx, xo);
-#pragma unroll
-    for (int v = 0; v < V; v++)
-      if (row && at.has[v]) put8<XB>(pdx, at.x[v], pack8<XB>(u[v]));
+    if (on) put8<XB>(at_elem<XB>(a.dx, xo), at_x, pack8<XB>(u));
   }
   const size_t rows = (size_t)a.B * a.walkers, first = (size_t)blockIdx.x * a.C;
   if (PART & kBefore) {
-    if (a.dscale || a.din_weight) store_partial<V>(tm, a.teams, teams_lds, p_sum, at.has, at.col, a.C, a.partial + first);
-    if (!TOKEN && a.dshift) store_partial<V>(tm, a.teams, teams_lds, s_sum, at.has, at.col, a.C, a.partial + rows * a.C + first);
+    if (a.dscale || a.din_weight) store_partial(tm, a.teams, shared, p_sum, has, col, a.C, a.partial + first);
+    if (!TOKEN && a.dshift) store_partial(tm, a.teams, shared, s_sum, has, col, a.C, a.partial + rows * a.C + first);
   }
   if ((PART & kAfter) && (a.dgate || a.dout_weight))
-    store_partial<V>(tm, a.teams, teams_lds, q_sum, at.has, at.col, a.C, a.partial + 2 * rows * a.C + first);
+    store_partial(tm, a.teams, shared, q_sum, has, col, a.C, a.partial + 2 * rows * a.C + first);
 }
 
 // 32 columns (8 lanes of 4) by 64 rows at a time per workgroup; the 64 partial sums in order through LDS.
@@ -472,54 +470,53 @@ hipError_t launch_column_sums(const ColumnJobs& j, hipStream_t stream) {
 static int part_of(const NormArgs& a, bool backward) { return ((backward ? a.dh : a.h) ? kBefore : 0) | (a.y ? kAfter : 0); }
 
 void plan_norm(NormArgs* a, bool backward) {
-  a->team = row_team(a->C / kChunk, backward ? 1 : 3);
+  a->team = backward ? row_team(a->C / kChunk, 1, kMaxThreads) : row_team(a->C / kChunk, 3, kTeamThreads);
   // the rows of a wave lie within 2 GB of its first; where strides are longer than that it has one
   const long long x_n = a->x_n > a->h_n ? a->x_n : a->h_n, widest = x_n > a->mod_n ? x_n : a->mod_n;
   if (widest >= (1ll << 29) / (kWave / a->team.lanes)) a->team.lanes = kWave;
-  a->teams = block_teams(a->team, a->N);
-  const bool large = backward ? a->team.vec > 1 : large_forward(a->team.vec, part_of(*a, false), false);
+  const bool large = !backward && large_forward(a->team.vec, part_of(*a, false), false);
+  a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);
   const int walkers = resident_workgroups(a->team, a->teams, threads_of(large)) / a->B, most = (int)(((long long)a->N + a->teams - 1) / a->teams);
   a->walkers = walkers < 1 ? 1 : walkers < most ? walkers : most;
 }
 
-template <int V, bool XB, bool HB, int PART>
-static hipError_t launch_part(const NormArgs& a, bool backward, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.B * a.walkers)), block((a.teams * a.team.threads() + kWave - 1) / kWave * kWave);
-  const size_t lds = backward ? (size_t)(a.teams - 1) * a.C * sizeof(float) : 0;
-  const bool token = a.mods == SLA2_MOD_TOKEN;
-  if (backward) {
-    if constexpr (V <= 2) {
-      if (token) norm_bwd_kernel<V, XB, HB, PART, true><<<grid, block, lds, stream>>>(a);
-      else norm_bwd_kernel<V, XB, HB, PART, false><<<grid, block, lds, stream>>>(a);
-    }
-  } else {
-    if (token) norm_kernel<V, XB, HB, PART, true><<<grid, block, 0, stream>>>(a);
-    else norm_kernel<V, XB, HB, PART, false><<<grid, block, 0, stream>>>(a);
-  }
-  return hipGetLastError();
+// f(types, part, modulation of every token) with the constants of a call
+template <class F> static void with_types(const NormArgs& a, int part, F f) {
+  auto with_part = [&](auto xb, auto hb) {
+    auto with_token = [&](auto p) {
+      if (a.mods == SLA2_MOD_TOKEN) f(xb, hb, p, std::true_type());
+      else f(xb, hb, p, std::false_type());
+    };
+    if (part == kBefore) with_token(std::integral_constant<int, kBefore>());
+    else if (part == kAfter) with_token(std::integral_constant<int, kAfter>());
+    else with_token(std::integral_constant<int, kBefore | kAfter>());
+  };
+  if (a.x_bf16) with_part(std::true_type(), std::true_type());
+  else if (a.h_bf16) with_part(std::false_type(), std::true_type());
+  else with_part(std::false_type(), std::false_type());
 }
-template <int V, bool XB, bool HB>
-static hipError_t launch_types(const NormArgs& a, int part, bool backward, hipStream_t stream) {
-  if (part == kBefore) return launch_part<V, XB, HB, kBefore>(a, backward, stream);
-  if (part == kAfter) return launch_part<V, XB, HB, kAfter>(a, backward, stream);
-  return launch_part<V, XB, HB, kBefore | kAfter>(a, backward, stream);
-}
-template <int V>
-static hipError_t launch_vec(const NormArgs& a, int part, bool backward, hipStream_t stream) {
-  if (a.x_bf16) return launch_types<V, true, true>(a, part, backward, stream);
-  if (a.h_bf16) return launch_types<V, false, true>(a, part, backward, stream);
-  return launch_types<V, false, false>(a, part, backward, stream);
-}
-static hipError_t launch_any(const NormArgs& a, int part, bool backward, hipStream_t stream) {
-  return a.team.vec == 1 ? launch_vec<1>(a, part, backward, stream) : a.team.vec == 2 ? launch_vec<2>(a, part, backward, stream) : launch_vec<3>(a, part, backward, stream);
-}
+static dim3 norm_block(const NormArgs& a) { return dim3((a.teams * a.team.threads() + kWave - 1) / kWave * kWave); }
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
-  return launch_any(a, part_of(a, false), false, stream);
+  const dim3 grid((unsigned)(a.B * a.walkers)), block = norm_block(a);
+  with_types(a, part_of(a, false), [&](auto xb, auto hb, auto part, auto token) {
+    constexpr bool XB = decltype(xb)::value, HB = decltype(hb)::value, TOKEN = decltype(token)::value;
+    constexpr int PART = decltype(part)::value;
+    if (a.team.vec == 1) norm_kernel<1, XB, HB, PART, TOKEN><<<grid, block, 0, stream>>>(a);
+    else if (a.team.vec == 2) norm_kernel<2, XB, HB, PART, TOKEN><<<grid, block, 0, stream>>>(a);
+    else norm_kernel<3, XB, HB, PART, TOKEN><<<grid, block, 0, stream>>>(a);
+  });
+  return hipGetLastError();
 }
 
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
-  if (hipError_t e = launch_any(a, part_of(a, true), true, stream); e != hipSuccess) return e;
+  const dim3 grid((unsigned)(a.B * a.walkers)), block = norm_block(a);
+  const int vectors = 2 * (a.C + kChunk), sums = (a.teams - 1) * a.C;
+  const size_t lds = (size_t)(vectors > sums ? vectors : sums) * sizeof(float);
+  with_types(a, part_of(a, true), [&](auto xb, auto hb, auto part, auto token) {
+    norm_bwd_kernel<decltype(xb)::value, decltype(hb)::value, decltype(part)::value, decltype(token)::value><<<grid, block, lds, stream>>>(a);
+  });
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const int rows = a.B * a.walkers;
   const float *p = a.partial, *s = p + (size_t)rows * a.C, *q = s + (size_t)rows * a.C;
   const bool batch = a.mods == SLA2_MOD_BATCH, token = a.mods == SLA2_MOD_TOKEN;

@@ -55,8 +55,9 @@ struct Position {
 constexpr int kAngleFloats = 512;            // of a wave: 8 tokens of 64 channels, 4 of 128: cosines, then sines, of the pairs of each
 struct AngleLds {
   double turns[64];                          // of a pair per position
-  float of[kTeamThreads / kWave * kAngleFloats];
+  float of[kMaxThreads / kWave * kAngleFloats];            // at the end of the backward kernel: 8 floats of every thread
 };
+static_assert(kAngleFloats >= kWave * kChunk, "");
 template <bool BF16, bool HALVES> struct Angles {
   static constexpr int kPairs = HALVES ? 8 : 4;
   const double* turns;
@@ -127,7 +128,7 @@ __device__ __forceinline__ void turn(const RopeArgs& a, const Angles<BF16, HALVE
   }
 }
 
-__device__ __forceinline__ float head_sum(float x, int d) { return d == 128 ? row_sum<16>(x) : row_sum<8>(x); }
+__device__ __forceinline__ float head_sum(float x, int d) { return d == 128 ? sum16(x) : sum8(x); }
 
 // What a thread holds of its rows: V chunks of heads.
 template <int V> struct Place {
@@ -233,140 +234,104 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
   }
 }
 
-// Gradients of x and, where there are partial sums, of the weights.
-template <int V, bool BF16, bool HALVES, int NORM>
-__global__ __launch_bounds__(kTeamThreads, waves_of(V > 1)) void rope_bwd_kernel(RopeArgs a) {
+// Gradients of x and, where there are partial sums, of the weights.  A thread has one chunk of q and of k; with two it would need more
+// registers than leave a CU 16 waves (12 heads of 32,760 tokens 139 us, with one 117).
+template <bool BF16, bool HALVES, bool TOKEN>
+__global__ __launch_bounds__(kMaxThreads, 4) void rope_bwd_kernel(RopeArgs a) {
   __shared__ float lds[kExchangeFloats];
   __shared__ AngleLds angles;
-  constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
-  __shared__ f32x4 sums[kTeamThreads * 2 * W];            // 8 W floats of every thread
   Team tm(a.team, lds);
   const int part = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers, b = part / a.groups;
-  const Place<V> at(a, tm, part % a.groups);
+  const Place<1> at(a, tm, part % a.groups);
   Angles<BF16, HALVES> an(a, tm, angles);
-  const float share = 1.f / (float)(NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
-  float w[2][W][8], acc[2][W][8];
+  const float share = 1.f / (float)(TOKEN ? a.H * a.d : a.d);
+  float w[2][8], acc[2][8];
 #pragma unroll
-  for (int t = 0; t < 2; t++)
+  for (int t = 0; t < 2; t++) {
+    load_vector8(a.weight[t], TOKEN ? at.col[0] : at.channel, 1.f, w[t]);
 #pragma unroll
-    for (int v = 0; v < W; v++) {
-      load_vector8(a.weight[t], NORM == SLA2_ROPE_NORM_TOKEN ? at.col[v] : at.channel, 1.f, w[t][v]);
-#pragma unroll
-      for (int i = 0; i < 8; i++) acc[t][v][i] = 0.f;
-    }
+    for (int i = 0; i < 8; i++) acc[t][i] = 0.f;
+  }
   const long long step = (long long)a.walkers * a.teams;
   Position where(a, (long long)walker * a.teams + tm.team, step);
-  struct Row {
-    Raw<BF16> x[2][V], g[2][V];
-    int p0, p1, p2;
-  };
-  auto load = [&](long long n0) {
-    const long long n = n0 + tm.first;
-    const bool row = n + tm.sub < a.N;
-    Row r;
-#pragma unroll
-    for (int t = 0; t < 2; t++) {
-      const void *px = at_elem<BF16>(a.x[t], b * a.sin.b + n * a.sin.n), *pg = at_elem<BF16>(a.dy[t], b * a.sout.b + n * a.sout.n);
-#pragma unroll
-      for (int v = 0; v < V; v++) {
-        const bool on = row && at.has[v] && t < a.tensors;
-        r.x[t][v] = on ? load8<BF16>(px, at.in[v]) : zero8<BF16>();
-        r.g[t][v] = on ? load8<BF16>(pg, at.out[v]) : zero8<BF16>();
-      }
-    }
-    where.at(a, b, n + tm.sub, row, r.p0, r.p1, r.p2);
-    return r;
-  };
   for (long long n0 = (long long)walker * a.teams; n0 < a.N; n0 += step) {
-    const long long n = n0 + tm.first;
-    const bool row = n + tm.sub < a.N;
-    const long long xo = b * a.sin.b + n * a.sin.n;
-    Row cur = load(n0);
-    where.advance(a);
-    an.at(cur.p0, cur.p1, cur.p2);
-    float s[4] = {0.f, 0.f, 0.f, 0.f};                   // over all heads: sum x^2, sum t x of q, of k
-    float g[2][W][8];
-    if (NORM == SLA2_ROPE_NORM_TOKEN) {
-#pragma unroll
-      for (int t = 0; t < 2; t++)
-#pragma unroll
-        for (int v = 0; v < W; v++) {
-          float x[8];
-          unpack8<BF16>(cur.x[t][v], x);
-          unpack8<BF16>(cur.g[t][v], g[t][v]);
-          turn<BF16, HALVES>(a, an, g[t][v]);
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            s[2 * t] += x[i] * x[i];
-            s[2 * t + 1] += g[t][v][i] * w[t][v][i] * x[i];
-          }
-        }
-      tm.sum(s);
-    }
+    const long long n = n0 + tm.first, xo = b * a.sin.b + n * a.sin.n, yo = b * a.sout.b + n * a.sout.n;
+    const bool row = n + tm.sub < a.N, on = row && at.has[0];
+    Raw<BF16> rx[2], rg[2];
 #pragma unroll
     for (int t = 0; t < 2; t++) {
-      if (t >= a.tensors) break;
+      rx[t] = on && t < a.tensors ? load8<BF16>(at_elem<BF16>(a.x[t], xo), at.in[0]) : zero8<BF16>();
+      rg[t] = on && t < a.tensors ? load8<BF16>(at_elem<BF16>(a.dy[t], yo), at.out[0]) : zero8<BF16>();
+    }
+    int p0, p1, p2;
+    where.at(a, b, n + tm.sub, row, p0, p1, p2);
+    where.advance(a);
+    an.at(p0, p1, p2);
+    float g[2][8], s[4];                     // sum x^2, sum t x: of q, of k
+    auto sums = [&](int t) {
+      float x[8];
+      unpack8<BF16>(rx[t], x);
+      unpack8<BF16>(rg[t], g[t]);
+      turn<BF16, HALVES>(a, an, g[t]);
+      s[2 * t] = s[2 * t + 1] = 0.f;
 #pragma unroll
-      for (int v = 0; v < V; v++) {
-        constexpr bool kToken = NORM == SLA2_ROPE_NORM_TOKEN;
-        float x[8], (&gv)[8] = g[t][kToken ? v : 0], (&wv)[8] = w[t][kToken ? v : 0], (&av)[8] = acc[t][kToken ? v : 0];
-        unpack8<BF16>(cur.x[t][v], x);
-        float xx = s[2 * t], tx = s[2 * t + 1];
-        if (!kToken) {
-          unpack8<BF16>(cur.g[t][v], gv);
-          turn<BF16, HALVES>(a, an, gv);
-          xx = tx = 0.f;
+      for (int i = 0; i < 8; i++) {
+        s[2 * t] += x[i] * x[i];
+        s[2 * t + 1] += g[t][i] * w[t][i] * x[i];
+      }
+    };
+    auto finish = [&](int t) {
+      float x[8];
+      unpack8<BF16>(rx[t], x);
+      const float r = inv_sqrt(s[2 * t] * share + a.eps), mean = s[2 * t + 1] * share * r;
 #pragma unroll
-          for (int i = 0; i < 8; i++) {
-            xx += x[i] * x[i];
-            tx += gv[i] * wv[i] * x[i];
-          }
-          xx = head_sum(xx, a.d);
-          tx = head_sum(tx, a.d);
-        }
-        const float r = inv_sqrt(xx * share + a.eps), mean = tx * share * r;
+      for (int i = 0; i < 8; i++) {
+        const float nx = x[i] * r;
+        acc[t][i] += g[t][i] * nx;
+        x[i] = r * (g[t][i] * w[t][i] - nx * mean);
+      }
+      if (on) put8<BF16>(at_elem<BF16>(a.y[t], xo), at.in[0], pack8<BF16>(x));
+    };
+    if constexpr (TOKEN) {                   // both in one exchange
+      sums(0);
+      sums(1);
+      tm.sum(s);
+      finish(0);
+      if (a.tensors > 1) finish(1);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-          const float nx = x[i] * r;
-          av[i] += gv[i] * nx;
-          x[i] = r * (gv[i] * wv[i] - nx * mean);
-        }
-        if (row && at.has[v]) put8<BF16>(at_elem<BF16>(a.y[t], xo), at.in[v], pack8<BF16>(x));
+      for (int t = 0; t < 2; t++) {
+        if (t >= a.tensors) break;
+        sums(t);
+        s[2 * t] = head_sum(s[2 * t], a.d);
+        s[2 * t + 1] = head_sum(s[2 * t + 1], a.d);
+        finish(t);
       }
     }
   }
   if (!a.partial) return;
-  const int cols = NORM == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d;
+  const int cols = TOKEN ? a.H * a.d : a.d;
 #pragma unroll
   for (int t = 0; t < 2; t++) {
     if (!a.dweight[t]) continue;
     float* to = a.partial + ((size_t)t * gridDim.x + blockIdx.x) * cols;
-    if (NORM == SLA2_ROPE_NORM_TOKEN) {
-      float* m = (float*)sums;               // [teams - 1][H d]
-      __syncthreads();
+    __syncthreads();
+    store8<false>(angles.of, threadIdx.x * 8, pack8<false>(acc[t]));
+    __syncthreads();
+    if constexpr (TOKEN) {                   // those of the teams, in order
+      if (tm.team == 0 && at.has[0]) {
+        for (int k = 1; k < a.teams; k++) {
+          float o[8];
+          load_vector8(angles.of, (unsigned)(k * a.team.threads() + tm.lane) * 8, 0.f, o);
 #pragma unroll
-      for (int v = 0; v < W; v++)
-        if (tm.team > 0 && at.has[v]) store8<false>(m, (unsigned)((tm.team - 1) * cols) + at.col[v], pack8<false>(acc[t][v]));
-      __syncthreads();
-#pragma unroll
-      for (int v = 0; v < W; v++)
-        if (tm.team == 0 && at.has[v]) {
-          for (int k = 1; k < a.teams; k++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) acc[t][v][i] += m[(size_t)(k - 1) * cols + at.col[v] + i];
-          store8<false>(to, (unsigned)at.col[v], pack8<false>(acc[t][v]));
+          for (int i = 0; i < 8; i++) acc[t][i] += o[i];
         }
-    } else {
-      // every thread's sums; those of one place in a head are a head's lanes apart
-      const int per_head = a.d / kChunk;
-      __syncthreads();
-      store8<false>(sums, threadIdx.x * 8, pack8<false>(acc[t][0]));
-      __syncthreads();
-      if ((int)threadIdx.x < a.d) {
-        float x = 0.f;
-        for (int k = (int)threadIdx.x / 8; k < (int)blockDim.x; k += per_head) x += ((const float*)sums)[k * 8 + threadIdx.x % 8];
-        to[threadIdx.x] = x;
+        store8<false>(to, (unsigned)at.col[0], pack8<false>(acc[t]));
       }
+    } else if ((int)threadIdx.x < a.d) {     // those of one place in a head, which are a head's lanes apart
+      float x = 0.f;
+      for (int k = (int)threadIdx.x / 8; k < (int)blockDim.x; k += a.d / kChunk) x += angles.of[k * 8 + threadIdx.x % 8];
+      to[threadIdx.x] = x;
     }
   }
 }
@@ -375,10 +340,11 @@ void plan_rope(RopeArgs* a, bool backward) {
   const int most = kMaxRow / a->d;           // heads of a row
   a->groups = (a->H + most - 1) / most;
   a->heads = (a->H + a->groups - 1) / a->groups;
-  a->team = row_team(a->heads * a->d / kChunk, backward ? 1 : 3);
-  a->teams = block_teams(a->team, a->N);
-  const bool large = backward ? a->team.vec > 1 : large_forward(a->team.vec, a->norm);
-  const int walkers = resident_workgroups(a->team, a->teams, threads_of(large)) / (a->B * a->groups);
+  const int chunks = a->heads * a->d / kChunk;
+  a->team = backward ? row_team(chunks, 1, kMaxThreads) : row_team(chunks, 3, kTeamThreads);
+  a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);
+  const int threads = threads_of(!backward && large_forward(a->team.vec, a->norm));
+  const int walkers = resident_workgroups(a->team, a->teams, threads) / (a->B * a->groups);
   const int needed = (int)(((long long)a->N + a->teams - 1) / a->teams);
   a->walkers = walkers < 1 ? 1 : walkers < needed ? walkers : needed;
 }
@@ -388,35 +354,32 @@ size_t rope_partial_floats(const RopeArgs& a) {
   return a.norm == SLA2_ROPE_NORM_NONE ? 0 : (size_t)2 * workgroups(a) * (a.norm == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
 }
 
-template <int V, bool BF16, bool HALVES>
-static hipError_t launch_norms(const RopeArgs& a, bool backward, hipStream_t stream) {
-  // whole waves; the sums of the weights want a thread for every channel of a head
-  int threads = (a.teams * a.team.threads() + kWave - 1) / kWave * kWave;
-  if (backward && threads < a.d) threads = a.d;
-  const dim3 grid((unsigned)workgroups(a)), block(threads);
-  if (backward) {
-    if (a.norm == SLA2_ROPE_NORM_TOKEN) {
-      if constexpr (V <= 2) rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
-    } else {
-      if constexpr (V <= 2) rope_bwd_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
-    }
-  } else {
-    if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
-    else if (a.norm == SLA2_ROPE_NORM_HEAD) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
-    else rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_NONE><<<grid, block, 0, stream>>>(a);
-  }
+// f(element type, pairing) with the constants of a call
+template <class F> static void with_types(const RopeArgs& a, F f) {
+  auto with_pairs = [&](auto bf16) {
+    if (a.halves) f(bf16, std::true_type());
+    else f(bf16, std::false_type());
+  };
+  if (a.bf16) with_pairs(std::true_type());
+  else with_pairs(std::false_type());
+}
+static int whole_waves(const RopeArgs& a) { return (a.teams * a.team.threads() + kWave - 1) / kWave * kWave; }
+
+template <int V, bool BF16, bool HALVES> static void launch_forward(const RopeArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)workgroups(a)), block(whole_waves(a));
+  if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_TOKEN><<<grid, block, 0, stream>>>(a);
+  else if (a.norm == SLA2_ROPE_NORM_HEAD) rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_HEAD><<<grid, block, 0, stream>>>(a);
+  else rope_kernel<V, BF16, HALVES, SLA2_ROPE_NORM_NONE><<<grid, block, 0, stream>>>(a);
+}
+hipError_t launch_rope(const RopeArgs& a, hipStream_t stream) {
+  with_types(a, [&](auto bf16, auto halves) {
+    constexpr bool BF16 = decltype(bf16)::value, HALVES = decltype(halves)::value;
+    if (a.team.vec == 1) launch_forward<1, BF16, HALVES>(a, stream);
+    else if (a.team.vec == 2) launch_forward<2, BF16, HALVES>(a, stream);
+    else launch_forward<3, BF16, HALVES>(a, stream);
+  });
   return hipGetLastError();
 }
-template <int V>
-static hipError_t launch_vec(const RopeArgs& a, bool backward, hipStream_t stream) {
-  if (a.bf16) return a.halves ? launch_norms<V, true, true>(a, backward, stream) : launch_norms<V, true, false>(a, backward, stream);
-  return a.halves ? launch_norms<V, false, true>(a, backward, stream) : launch_norms<V, false, false>(a, backward, stream);
-}
-static hipError_t launch_any(const RopeArgs& a, bool backward, hipStream_t stream) {
-  return a.team.vec == 1 ? launch_vec<1>(a, backward, stream) : a.team.vec == 2 ? launch_vec<2>(a, backward, stream) : launch_vec<3>(a, backward, stream);
-}
-
-hipError_t launch_rope(const RopeArgs& a, hipStream_t stream) { return launch_any(a, false, stream); }
 
 hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
   RopeArgs a = args;
@@ -426,9 +389,18 @@ hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
     const HeadStrides s = a.sin;
     a.sin = a.sout;
     a.sout = s;
-    return launch_any(a, false, stream);
+    plan_rope(&a, false);
+    return launch_rope(a, stream);
   }
-  if (hipError_t e = launch_any(a, true, stream); e != hipSuccess) return e;
+  // the sums of the weights want a thread for every channel of a head
+  const int threads = whole_waves(a) < a.d ? a.d : whole_waves(a);
+  with_types(a, [&](auto bf16, auto halves) {
+    constexpr bool BF16 = decltype(bf16)::value, HALVES = decltype(halves)::value;
+    const dim3 grid((unsigned)workgroups(a)), block(threads);
+    if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_bwd_kernel<BF16, HALVES, true><<<grid, block, 0, stream>>>(a);
+    else rope_bwd_kernel<BF16, HALVES, false><<<grid, block, 0, stream>>>(a);
+  });
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   ColumnJobs js{};
   js.columns = a.norm == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d;
   const int rows = workgroups(a);
