@@ -234,6 +234,7 @@ struct RopeArgs {
   float eps;
   int norm;                                  // sla2_rope_norm
   bool bf16, halves;
+  bool cached;                               // the results stay in the caches
   double sign;                               // of the angles
   // launch
   RowTeam team;

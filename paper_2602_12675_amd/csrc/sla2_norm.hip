@@ -513,10 +513,15 @@ hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)(a.B * a.walkers)), block = norm_block(a);
   const int vectors = 2 * (a.C + kChunk), sums = (a.teams - 1) * a.C;
   const size_t lds = (size_t)(vectors > sums ? vectors : sums) * sizeof(float);
+  hipError_t e = hipSuccess;
   with_types(a, part_of(a, true), [&](auto xb, auto hb, auto part, auto token) {
-    norm_bwd_kernel<decltype(xb)::value, decltype(hb)::value, decltype(part)::value, decltype(token)::value><<<grid, block, lds, stream>>>(a);
+    constexpr auto kernel = norm_bwd_kernel<decltype(xb)::value, decltype(hb)::value, decltype(part)::value, decltype(token)::value>;
+    static OncePerDevice once;
+    e = allow_dynamic_lds(once, (const void*)kernel, 2 * (kMaxRow + kChunk) * (int)sizeof(float));
+    if (e == hipSuccess) kernel<<<grid, block, lds, stream>>>(a);
   });
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (e == hipSuccess) e = hipGetLastError();
+  if (e != hipSuccess) return e;
   const int rows = a.B * a.walkers;
   const float *p = a.partial, *s = p + (size_t)rows * a.C, *q = s + (size_t)rows * a.C;
   const bool batch = a.mods == SLA2_MOD_BATCH, token = a.mods == SLA2_MOD_TOKEN;

@@ -228,7 +228,10 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
           for (int i = 0; i < 8; i++) x[i] = x[i] * s[t] * w[t][v % W][i];
         }
         turn<BF16, HALVES>(a, an, x);
-        if (row && at.has[v]) put8<BF16>(at_elem<BF16>(a.y[t], yo), at.out[v], pack8<BF16>(x));
+        if (row && at.has[v]) {
+          if (a.cached) store8<BF16>(at_elem<BF16>(a.y[t], yo), at.out[v], pack8<BF16>(x));
+          else put8<BF16>(at_elem<BF16>(a.y[t], yo), at.out[v], pack8<BF16>(x));
+        }
       }
     }
   }
@@ -336,11 +339,17 @@ __global__ __launch_bounds__(kMaxThreads, 4) void rope_bwd_kernel(RopeArgs a) {
   }
 }
 
+// Results that fit the 256 MB memory-side cache are left there for the attention, which reads them next: 12 heads of 32,760 tokens (201 MB)
+// with sla2_forward behind them 473 us, past the caches 489 us, though the call alone takes 80.7 and 75.8 us; 2 x 20 heads of 4,096 at
+// d = 64 90.1 / 92.3 us; 40 heads of 75,600 (1.5 GB) 6,347 / 6,300 us.
+constexpr long long kCacheBytes = 256ll << 20;
+
 void plan_rope(RopeArgs* a, bool backward) {
   const int most = kMaxRow / a->d;           // heads of a row
   a->groups = (a->H + most - 1) / most;
   a->heads = (a->H + a->groups - 1) / a->groups;
   const int chunks = a->heads * a->d / kChunk;
+  a->cached = !backward && 2ll * a->B * a->H * a->N * a->d * (a->bf16 ? 2 : 4) <= kCacheBytes;
   a->team = backward ? row_team(chunks, 1, kMaxThreads) : row_team(chunks, 3, kTeamThreads);
   a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);
   const int threads = threads_of(!backward && large_forward(a->team.vec, a->norm));
@@ -390,6 +399,7 @@ hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
     a.sin = a.sout;
     a.sout = s;
     plan_rope(&a, false);
+    a.cached = false;
     return launch_rope(a, stream);
   }
   // the sums of the weights want a thread for every channel of a head
