@@ -239,7 +239,8 @@ int sla2_dense_forward(const sla2_params* params, const void* q, const void* k, 
  * kernel for a forward call, two at most for a backward call, nothing allocated, no atomics: two calls on the same data give
  * the same bits.  Everything between the stored types is fp32 and rounded once; angles are fp64.  Vectors of channels
  * (weights, gate, scale, shift) are DEVICE float, 16-byte aligned.  What is NaN or infinite stays in its row, and in the
- * gradients that are sums over rows.  These entry points are not stages of the profile below. */
+ * gradients that are sums over rows; squares are summed in fp32 (values up to 1e17).  These entry points are not stages of the
+ * profile below: a forward call is one kernel, whose time an event on either side gives. */
 
 /* Pair j of a head: channels (2 j, 2 j + 1), or (j, j + d / 2). */
 typedef enum { SLA2_ROPE_INTERLEAVED = 0, SLA2_ROPE_HALVES = 1 } sla2_rope_pairing;
@@ -252,7 +253,7 @@ typedef struct sla2_rope_params {
   int dtype;               /* sla2_dtype of q, k, the results and their gradients */
   int pairing;             /* sla2_rope_pairing */
   int norm;                /* sla2_rope_norm */
-  float eps;               /* > 0 with a norm */
+  float eps;               /* with a norm: finite, at least the smallest normal number (1.2e-38) */
   int axis_pairs[3];       /* pairs that turn with the first, second and third axis (time, height, width), in this order;
                               d / 2 at most in all, the pairs behind them are not rotated.  One axis: {d / 2, 0, 0} */
   int grid[3];             /* T, Y, X >= 1 (T Y X < 2^31): token n is at origin + (n / (Y X), n / X % Y, n % X), tokens from
@@ -300,7 +301,7 @@ typedef struct sla2_norm_params {
   int dtype_x;             /* sla2_dtype of the residual stream (x, x_out and their gradients) */
   int dtype_h;             /* of the block's output y and input h (and their gradients); SLA2_F32 only with an fp32 stream */
   int norm_in, norm_out;   /* sla2_norm_kind before the block (of the stream) and after it (of y) */
-  float eps;               /* > 0 with a norm */
+  float eps;               /* with a norm: finite, at least the smallest normal number (1.2e-38) */
   float residual_scale;    /* rho; finite */
   int mod_layout;          /* sla2_mod_layout */
   /* (batch, token) element strides of x, x_out, dx_out, dx and of y, h, dh, dy; both zero: contiguous.  Positive, multiples of

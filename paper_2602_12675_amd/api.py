@@ -268,18 +268,19 @@ _TYPES = {SLA2_F32: torch.float32, SLA2_BF16: torch.bfloat16}
 
 def _call(fn, params, tensors, stream, check, *tail) -> int:
     """fn(params, addresses, *tail, stream) on the device of the tensors, on `stream` or that device's current one.
-    tensors: (tensor, element type, elements, whether it is a vector).  A tensor of another element type, with fewer elements than the
-    kernels will take it to have, on the host or on another device than the others, or a vector that is not contiguous, is refused: it
-    would be read or written out of bounds.  Strides of the others are the caller's to state; addresses (int) are taken as they are."""
+    tensors: (tensor, element type, elements, whether it is taken to be contiguous).  A tensor of another element type, with fewer
+    elements than the kernels will take it to have, on the host or on another device than the others, or not contiguous where no
+    strides are stated, is refused: it would be read or written out of bounds.  Strides that are stated are the caller's word, and
+    addresses (int) are taken as they are."""
     out, dev, rc = [ctypes.byref(params)], None, SLA2_OK
-    for t, dtype, count, vector in tensors:
+    for t, dtype, count, dense in tensors:
         if t is None or t.__class__ is int:
             out.append(t)
             continue
         d = t.get_device()
         if dev is None:
             dev = d
-        if t.dtype is not dtype or t.numel() < count or d != dev or d < 0 or (vector and not t.is_contiguous()):
+        if t.dtype is not dtype or t.numel() < count or d != dev or d < 0 or (dense and not t.is_contiguous()):
             rc = SLA2_EINVAL
             break
         out.append(t.data_ptr())
@@ -322,27 +323,27 @@ def sla2_rope_frequencies(params: RopeParams, theta: float = 10000.0) -> torch.T
 
 
 def _rope_sizes(p):
-    """(elements of q, of a weight, of the positions; element type)"""
+    """(elements of q, of a weight, of the positions; element type; whether q and the results are contiguous)"""
     return (p.B * p.H * p.N * p.d, p.H * p.d if p.norm == SLA2_ROPE_NORM_TOKEN else p.d, 3 * p.N * (p.B if p.positions_per_batch else 1),
-            _TYPES.get(p.dtype))
+            _TYPES.get(p.dtype), p.in_stride[2] == 0, p.out_stride[2] == 0)
 
 
 def sla2_rope_forward(params, q, k, freq, q_out, k_out, q_weight=None, k_weight=None, positions=None, stream=None, check=True) -> int:
-    n, w, np_, dt = _rope_sizes(params)
+    n, w, np_, dt, ci, co = _rope_sizes(params)
     f32 = torch.float32
     return _call(_lib.sla2_rope_forward, params, (
-        (q, dt, n, False), (k, dt, n, False), (freq, torch.float64, params.d // 2, True), (positions, torch.int32, np_, True),
-        (q_weight, f32, w, True), (k_weight, f32, w, True), (q_out, dt, n, False), (k_out, dt, n, False)), stream, check)
+        (q, dt, n, ci), (k, dt, n, ci), (freq, torch.float64, params.d // 2, True), (positions, torch.int32, np_, True),
+        (q_weight, f32, w, True), (k_weight, f32, w, True), (q_out, dt, n, co), (k_out, dt, n, co)), stream, check)
 
 
 def sla2_rope_backward(params, q, k, freq, dq_out, dk_out, dq, dk, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
                        positions=None, workspace=None, stream=None, check=True, ws_bytes=None) -> int:
-    n, w, np_, dt = _rope_sizes(params)
+    n, w, np_, dt, ci, co = _rope_sizes(params)
     f32 = torch.float32
     return _call(_lib.sla2_rope_backward, params, (
-        (q, dt, n, False), (k, dt, n, False), (freq, torch.float64, params.d // 2, True), (positions, torch.int32, np_, True),
-        (q_weight, f32, w, True), (k_weight, f32, w, True), (dq_out, dt, n, False), (dk_out, dt, n, False), (dq, dt, n, False),
-        (dk, dt, n, False), (dq_weight, f32, w, True), (dk_weight, f32, w, True), _scratch(workspace)), stream, check,
+        (q, dt, n, ci), (k, dt, n, ci), (freq, torch.float64, params.d // 2, True), (positions, torch.int32, np_, True),
+        (q_weight, f32, w, True), (k_weight, f32, w, True), (dq_out, dt, n, co), (dk_out, dt, n, co), (dq, dt, n, ci),
+        (dk, dt, n, ci), (dq_weight, f32, w, True), (dk_weight, f32, w, True), _scratch(workspace)), stream, check,
         _bytes(workspace, ws_bytes))
 
 
@@ -351,29 +352,30 @@ def sla2_norm_workspace_bytes(params: NormParams) -> int:
 
 
 def _norm_sizes(p):
-    """(elements of x, of a modulation; element types of x and of h)"""
+    """(elements of x, of a modulation; element types of x and of h; whether x, h and a modulation are contiguous)"""
     rows = {SLA2_MOD_BATCH: p.B, SLA2_MOD_TOKEN: p.B * p.N}.get(p.mod_layout, 1)
-    return p.B * p.N * p.C, rows * p.C, _TYPES.get(p.dtype_x), _TYPES.get(p.dtype_h)
+    return (p.B * p.N * p.C, rows * p.C, _TYPES.get(p.dtype_x), _TYPES.get(p.dtype_h), p.x_stride[1] == 0, p.h_stride[1] == 0,
+            p.mod_stride[0] == 0)
 
 
 def sla2_norm_forward(params, x, h, y=None, x_out=None, gate=None, out_weight=None, in_weight=None, scale=None, shift=None, stream=None,
                       check=True) -> int:
-    n, m, tx, th = _norm_sizes(params)
+    n, m, tx, th, cx, ch, cm = _norm_sizes(params)
     f32, c = torch.float32, params.C
     return _call(_lib.sla2_norm_forward, params, (
-        (x, tx, n, False), (y, th, n, False), (gate, f32, m, False), (out_weight, f32, c, True), (x_out, tx, n, False),
-        (in_weight, f32, c, True), (scale, f32, m, False), (shift, f32, m, False), (h, th, n, False)), stream, check)
+        (x, tx, n, cx), (y, th, n, ch), (gate, f32, m, cm), (out_weight, f32, c, True), (x_out, tx, n, cx),
+        (in_weight, f32, c, True), (scale, f32, m, cm), (shift, f32, m, cm), (h, th, n, ch)), stream, check)
 
 
 def sla2_norm_backward(params, x, dh, dx_out, dx, y=None, gate=None, out_weight=None, in_weight=None, scale=None, dy=None, dgate=None,
                        dout_weight=None, din_weight=None, dscale=None, dshift=None, workspace=None, stream=None, check=True,
                        ws_bytes=None) -> int:
-    n, m, tx, th = _norm_sizes(params)
+    n, m, tx, th, cx, ch, cm = _norm_sizes(params)
     f32, c = torch.float32, params.C
     return _call(_lib.sla2_norm_backward, params, (
-        (x, tx, n, False), (y, th, n, False), (gate, f32, m, False), (out_weight, f32, c, True), (in_weight, f32, c, True),
-        (scale, f32, m, False), (dh, th, n, False), (dx_out, tx, n, False), (dx, tx, n, False), (dy, th, n, False), (dgate, f32, m, False),
-        (dout_weight, f32, c, True), (din_weight, f32, c, True), (dscale, f32, m, False), (dshift, f32, m, False), _scratch(workspace)),
+        (x, tx, n, cx), (y, th, n, ch), (gate, f32, m, cm), (out_weight, f32, c, True), (in_weight, f32, c, True),
+        (scale, f32, m, cm), (dh, th, n, ch), (dx_out, tx, n, cx), (dx, tx, n, cx), (dy, th, n, ch), (dgate, f32, m, cm),
+        (dout_weight, f32, c, True), (din_weight, f32, c, True), (dscale, f32, m, cm), (dshift, f32, m, cm), _scratch(workspace)),
         stream, check, _bytes(workspace, ws_bytes))
 
 

@@ -3,16 +3,18 @@
 // A row (the channels of a token, or of some of its heads) is read once, in chunks of 8 channels, by a team: `lanes` neighbouring lanes
 // of a wave (8, 16, 32 or 64), or several whole waves, each thread holding V chunks, chunk l + v T being thread l's of T.  Everything
 // these kernels do is bound by memory, so a row stays in registers from its load to the store of what is made of it, and a workgroup
-// goes on with other rows of the same batch, whose modulation, gate or weights it then holds already.  The sums of a row are kept in
-// fp32; within a wave they are vector instructions only, and where a team has several waves these exchange all sums of a step through
-// LDS at once, behind one barrier.
+// goes on with other rows of the same batch, whose modulation, gate or weights it then holds already, in registers or LDS.  What keeps
+// memory busy is the bytes that a CU's waves have on their way: forward kernels hold up to 3 chunks a thread (32,760 rows of 1,536
+// channels before a block: 92 us as one chunk in three waves, 56 us as three in one), backward kernels, whose sums for the column
+// gradients stay in registers, one.  The sums of a row are kept in fp32; within a wave they are vector instructions only, and where a
+// team has several waves these exchange all sums of a step through LDS at once, behind one barrier.
 #pragma once
 #include "common.h"
 
 namespace sla2 {
 
 constexpr int kChunk = 8;                    // channels: 16 bytes of bf16
-constexpr int kMaxRow = 8192;                // channels of a row: 8 waves of 2 chunks a lane
+constexpr int kMaxRow = 8192;                // channels of a row: 16 waves of a chunk a lane
 constexpr int kTeamThreads = 512;            // threads of a workgroup
 constexpr int kMaxThreads = 1024;
 constexpr int kCus = 256;

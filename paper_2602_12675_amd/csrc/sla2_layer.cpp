@@ -1,5 +1,6 @@
 // Host side of the entry points around the attention (sla2_rope_*, sla2_norm_*): argument validation and launches.
 // Declarations and their contracts are in include/sla2.h.
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 #include <stdint.h>
@@ -68,6 +69,7 @@ static bool aliased(const Output* out, int outs, const View* in, int ins) {
   return false;
 }
 
+static bool eps_ok(float eps) { return eps >= FLT_MIN && eps <= FLT_MAX; }      // not NaN, nothing that the root would take for 0
 static bool vector_ok(const float* p) { return !misaligned16(p); }        // null too
 
 // Sum of (count - 1) stride + inner as 128 bits: whether it can be an extent in memory.
@@ -83,7 +85,7 @@ static int make_rope(const sla2_rope_params* p, bool backward, RopeArgs* a) {
   if (p->dtype != SLA2_F32 && p->dtype != SLA2_BF16) return SLA2_EINVAL;
   if (p->pairing != SLA2_ROPE_INTERLEAVED && p->pairing != SLA2_ROPE_HALVES) return SLA2_EINVAL;
   if (p->norm != SLA2_ROPE_NORM_NONE && p->norm != SLA2_ROPE_NORM_HEAD && p->norm != SLA2_ROPE_NORM_TOKEN) return SLA2_EINVAL;
-  if (p->norm != SLA2_ROPE_NORM_NONE && !(p->eps > 0.f && p->eps < INFINITY)) return SLA2_EINVAL;
+  if (p->norm != SLA2_ROPE_NORM_NONE && !eps_ok(p->eps)) return SLA2_EINVAL;
   if (p->positions_per_batch != 0 && p->positions_per_batch != 1) return SLA2_EINVAL;
   if (p->d != 64 && p->d != 128) return SLA2_EUNSUPPORTED;
   if ((long long)p->B * p->H > 65535) return SLA2_EUNSUPPORTED;
@@ -150,7 +152,7 @@ static int make_norm(const sla2_norm_params* p, NormArgs* a) {
   if ((p->dtype_x != SLA2_F32 && p->dtype_x != SLA2_BF16) || (p->dtype_h != SLA2_F32 && p->dtype_h != SLA2_BF16)) return SLA2_EINVAL;
   for (int k : {p->norm_in, p->norm_out})
     if (k != SLA2_NORM_NONE && k != SLA2_NORM_RMS && k != SLA2_NORM_LAYER) return SLA2_EINVAL;
-  if ((p->norm_in != SLA2_NORM_NONE || p->norm_out != SLA2_NORM_NONE) && !(p->eps > 0.f && p->eps < INFINITY)) return SLA2_EINVAL;
+  if ((p->norm_in != SLA2_NORM_NONE || p->norm_out != SLA2_NORM_NONE) && !eps_ok(p->eps)) return SLA2_EINVAL;
   if (!isfinite(p->residual_scale)) return SLA2_EINVAL;
   if (p->mod_layout != SLA2_MOD_BATCH && p->mod_layout != SLA2_MOD_TOKEN && p->mod_layout != SLA2_MOD_SHARED) return SLA2_EINVAL;
   if (p->C % kChunk || p->C > kMaxRow || p->B > 65535) return SLA2_EUNSUPPORTED;

@@ -175,7 +175,7 @@ def test_absent_vectors(absent, mods):
 
 
 @pytest.mark.parametrize("B,N,C", [(1, 1, 1536), (7, 1, 64), (1, 1, 8), (600, 1, 128), (600, 3, 40), (1, 1300, 8192), (3, 1111, 1032),
-                                   (1, 40000, 8), (2, 700, 5120), (1, 4099, 2048)])
+                                   (1, 40000, 8), (2, 700, 5120), (1, 4099, 2048), (65535, 1, 8)])
 @pytest.mark.parametrize("mods", ["batch", "shared"])
 def test_rows(B, N, C, mods):
     """One row, fewer rows than teams, more batches than workgroups, several rounds of every workgroup with a ragged last one."""

@@ -112,6 +112,13 @@ def test_more_heads_than_a_row_holds(H, d, norm):
     c.check_backward()
 
 
+@pytest.mark.parametrize("norm", NORMS)
+def test_many_sequences_of_one_token(norm):
+    c = Case(65535, 1, 1, 64, norm=norm, layout="tokens")
+    c.check_forward()
+    c.check_backward()
+
+
 @pytest.mark.parametrize("axes", [(32, 0, 0), (0, 0, 32), (8, 12, 12), (0, 7, 3), (0, 0, 0), (1, 1, 1)])
 @pytest.mark.parametrize("halves", [False, True])
 def test_axes_and_channels_left_alone(axes, halves):

@@ -77,6 +77,7 @@ def rope_backward(p, q=Q, k=K, freq=FREQ, dq_out=QO, dk_out=KO, dq=DQ, dk=DK, ws
     (dict(B=0), EINVAL), (dict(H=-1), EINVAL), (dict(N=0), EINVAL), (dict(d=96), EUNSUPPORTED), (dict(d=0), EUNSUPPORTED),
     (dict(dtype=2), EINVAL), (dict(pairing=2), EINVAL), (dict(norm=3), EINVAL), (dict(norm=-1), EINVAL),
     (dict(eps=0.0), EINVAL), (dict(eps=float("nan")), EINVAL), (dict(eps=float("inf")), EINVAL), (dict(positions_per_batch=2), EINVAL),
+    (dict(eps=1e-39), EINVAL), (dict(eps=-1e-6), EINVAL),
     (dict(axis_pairs=(11, 11, 11)), EINVAL), (dict(axis_pairs=(-1, 11, 11)), EINVAL), (dict(axis_pairs=(2 ** 31 - 1, 2 ** 31 - 1, 2)), EINVAL),
     (dict(grid=(0, 2, 5)), EINVAL), (dict(grid=(2, -1, 5)), EINVAL), (dict(grid=(2 ** 16, 2 ** 15, 1)), EUNSUPPORTED),
     (dict(grid=(2, 1, 5), origin=(2 ** 31 - 1, 0, 0)), EINVAL), (dict(origin=(1, 0, 0)), EINVAL),
@@ -157,7 +158,7 @@ def norm_backward(p, x=X, dh=DH, dx_out=DXO, dx=DX, ws_bytes=1 << 19, **kw):
     (dict(B=0), EINVAL), (dict(N=0), EINVAL), (dict(C=0), EINVAL), (dict(C=-8), EINVAL), (dict(C=100), EUNSUPPORTED),
     (dict(C=8200), EUNSUPPORTED), (dict(B=65536), EUNSUPPORTED), (dict(dtype_x=2), EINVAL), (dict(dtype_h=-1), EINVAL),
     (dict(dtype_x=1, dtype_h=0), EUNSUPPORTED), (dict(norm_in=3), EINVAL), (dict(norm_out=-1), EINVAL), (dict(eps=0.0), EINVAL),
-    (dict(eps=float("nan")), EINVAL), (dict(eps=float("inf")), EINVAL), (dict(residual_scale=float("nan")), EINVAL),
+    (dict(eps=float("nan")), EINVAL), (dict(eps=float("inf")), EINVAL), (dict(residual_scale=float("nan")), EINVAL), (dict(eps=1e-39), EINVAL),
     (dict(residual_scale=float("inf")), EINVAL), (dict(mod_layout=3), EINVAL), (dict(x_stride=(0, 64)), EINVAL),
     (dict(x_stride=(640, -64)), EINVAL), (dict(x_stride=(640, 60)), EUNSUPPORTED), (dict(h_stride=(640, 68)), EUNSUPPORTED),
     (dict(h_stride=(644, 64)), EUNSUPPORTED), (dict(x_stride=(1 << 60, 64)), EUNSUPPORTED), (dict(mod_stride=(64, 64)), EINVAL),
@@ -209,6 +210,25 @@ def test_norm_aliases():
     # the gradients of the modulation as slices of one [B, 6, C] buffer are apart; half a slice further they are not
     six = norm(mod_stride=(6 * 64, 0))
     assert norm_backward(six, dgate=DG, dscale=DG + 256, dshift=DG + 384) == EALIAS
+
+
+def test_a_view_without_stated_strides_is_refused():
+    """An expanded or permuted tensor with the default layout would be read beyond its storage or in the wrong order."""
+    class OnGpu(torch.Tensor):                                     # what the binding sees of a tensor on a GPU; never launched
+        def get_device(self):
+            return 0
+
+    def t(x):
+        return x.as_subclass(OnGpu)
+    p, x, h = norm(), torch.zeros(2, 10, 64), torch.zeros(2, 10, 64, dtype=torch.bfloat16)
+    for kw in (dict(x=x[:1].expand(2, 10, 64)), dict(h=h.transpose(0, 1).contiguous().transpose(0, 1)), dict(scale=torch.zeros(64).expand(2, 64)),
+               dict(shift=torch.zeros(2, 6, 64)[:, 1])):
+        kw = {k: t(v) for k, v in dict(dict(x=x, h=h), **kw).items()}
+        assert api.sla2_norm_forward(p, kw.pop("x"), kw.pop("h"), check=False, **kw) == EINVAL
+    p, q = rope(norm=api.SLA2_ROPE_NORM_NONE, grid=(1, 2, 5)), torch.zeros(2, 10, 3, 3, 64, dtype=torch.bfloat16)
+    f = t(torch.zeros(32, dtype=torch.float64))
+    assert api.sla2_rope_forward(p, t(q[:, :, 0].transpose(1, 2)), None, f, t(q[:, :, 1].reshape(2, 3, 10, 64)), None, check=False) == EINVAL
+    assert api.sla2_rope_forward(p, t(q[:, :, 0].reshape(2, 3, 10, 64)), None, f, t(q[:, :, 1]), None, check=False) == EINVAL
 
 
 def test_the_binding_looks_at_tensors():
