@@ -17,7 +17,9 @@
 namespace sla2 {
 
 constexpr int kBefore = 1, kAfter = 2;       // parts of a call: h; x'
-// rows of 3 chunks a thread with both parts, or with a modulation of every token
+// Whether a row takes more than 128 registers a thread, so that one workgroup of 8 waves fills a CU: 3 chunks with both parts (75,600 rows of
+// 5,120 channels 868 us as 256 workgroups, 884 as 512, of which half wait), or with a modulation of every token.  A token's own modulation does
+// not count for the number of workgroups: of 2 x 12,481 rows of 2,048 with one, 185 us as 256, 180 as 512.
 constexpr bool large_forward(int vec, int part, bool token) {
   const bool both = part == (kBefore | kAfter);
   return vec == 3 ? both || token : vec == 2 && both && token;
@@ -475,6 +477,9 @@ void plan_norm(NormArgs* a, bool backward) {
   const long long x_n = a->x_n > a->h_n ? a->x_n : a->h_n, widest = x_n > a->mod_n ? x_n : a->mod_n;
   if (widest >= (1ll << 29) / (kWave / a->team.lanes)) a->team.lanes = kWave;
   const bool large = !backward && large_forward(a->team.vec, part_of(*a, false), false);
+  // backward: one workgroup of up to 16 waves a CU where a team has 5 waves or more - of two with an odd number of waves the second often
+  // finds no place (4 x 3,478 rows of 2,520 channels, 5 waves: 107 us as two, 78 as one) - else two, one of which works while the other waits
+  // (31,201 rows of 1,536: 164 us as two of 6 waves, 172 as one of 15)
   a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);
   const int walkers = resident_workgroups(a->team, a->teams, threads_of(large)) / a->B, most = (int)(((long long)a->N + a->teams - 1) / a->teams);
   a->walkers = walkers < 1 ? 1 : walkers < most ? walkers : most;

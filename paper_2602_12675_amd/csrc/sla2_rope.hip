@@ -12,6 +12,8 @@
 
 namespace sla2 {
 
+// Whether a row takes more than 128 registers a thread: 3 chunks of q and of k behind a sum over all heads (40 heads of 75,601 tokens 566 us as
+// 256 workgroups, 580 as 512).
 constexpr bool large_forward(int vec, int norm) { return vec == 3 && norm == SLA2_ROPE_NORM_TOKEN; }
 
 // x of the lane that holds the other channel of each pair of a head of LANES lanes
@@ -351,6 +353,7 @@ void plan_rope(RopeArgs* a, bool backward) {
   const int chunks = a->heads * a->d / kChunk;
   a->cached = !backward && 2ll * a->B * a->H * a->N * a->d * (a->bf16 ? 2 : 4) <= kCacheBytes;
   a->team = backward ? row_team(chunks, 1, kMaxThreads) : row_team(chunks, 3, kTeamThreads);
+  // backward: one large workgroup a CU where a team has 5 waves or more (sla2_norm.hip: plan_norm)
   a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);
   const int threads = threads_of(!backward && large_forward(a->team.vec, a->norm));
   const int walkers = resident_workgroups(a->team, a->teams, threads) / (a->B * a->groups);
