@@ -194,6 +194,26 @@ struct Team {
   }
 };
 
+// The sum of acc over the parts of a workgroup, one chunk of a part's `width` values a thread, left with part 0: halves of what remains are
+// added through LDS, [parts - 1][width], in the same order every time.  All threads call it, and what was in LDS has been read behind it.
+// 64 parts, two sums (the gradients of a norm of 64 tokens of 64 channels): 6.2 us, with one part after the other 9.5.
+__device__ __forceinline__ void join_parts(float* lds, int part, int parts, int width, unsigned col, bool has, float (&acc)[8]) {
+  if (parts < 2) return;
+  __syncthreads();
+  int half = 1;
+  while (2 * half < parts) half *= 2;
+  for (; half > 0; half /= 2) {
+    if (has && part >= half && part < 2 * half && part < parts) store8<false>(lds, (unsigned)((part - 1) * width) + col, pack8<false>(acc));
+    __syncthreads();
+    if (has && part < half && part + half < parts) {
+      float o[8];
+      load_vector8(lds, (unsigned)((part + half - 1) * width) + col, 0.f, o);
+#pragma unroll
+      for (int i = 0; i < 8; i++) acc[i] += o[i];
+    }
+  }
+}
+
 // ---- sums of the columns of a matrix, as both backward passes end:
 //      out[c] = (factor_plus + factor[c]) * sum over rows of (weight_plus + weight[row][c]) rows[row][c] ----
 struct ColumnJob {
@@ -241,6 +261,7 @@ struct RopeArgs {
   // launch
   RowTeam team;
   int teams, heads, groups, walkers;         // teams of a workgroup; heads of a row, rows of a token; workgroups of a (batch, group)
+  bool direct;                               // backward: one workgroup has all rows and writes the results
 };
 void plan_rope(RopeArgs* a, bool backward);                 // fills in the launch from the sizes
 size_t rope_partial_floats(const RopeArgs& a);
@@ -264,6 +285,7 @@ struct NormArgs {
   bool x_bf16, h_bf16;
   RowTeam team;
   int teams, walkers;                        // teams of a workgroup; workgroups of a batch
+  bool direct;                               // backward: one workgroup has all rows and writes the results
 };
 void plan_norm(NormArgs* a, bool backward);
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream);

@@ -10,7 +10,8 @@
 //   t2 = u g w_out,   dy = r2 (t2 - mean(t2) [layer] - m mean(t2 m))
 // and, over the rows of a batch, P = sum dh n, S = sum dh, Q = sum u m: ds = w_in P, db = S, dw_in = sum over batches of (1 + s) P,
 // dg = w_out Q, dw_out = sum over batches of g Q.  Statistics are formed again from the row, which is in registers anyhow.  A
-// workgroup adds up P, S, Q of its rows in registers, its teams theirs in a fixed order, and a second launch adds up the workgroups'.
+// workgroup adds up P, S, Q of its rows in registers, its teams theirs in a fixed order, and a second launch adds up the workgroups',
+// unless there is but one.
 // A modulation of every token needs no sums but those of the weights.
 #include "rows.h"
 
@@ -225,25 +226,14 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, PART, TOKEN
   }
 }
 
-// One of the sums of a workgroup: its teams' in order, through LDS, into its row of the partial sums.
-__device__ __forceinline__ void store_partial(const Team& tm, int teams, float* lds, const float (&acc)[8], bool has, unsigned col, int C,
-                                              float* to) {
-  if (teams > 1) {
-    __syncthreads();
-    if (tm.team > 0 && has) store8<false>(lds, (unsigned)((tm.team - 1) * C) + col, pack8<false>(acc));
-    __syncthreads();
-  }
-  if (tm.team > 0 || !has) return;
-  float s[8];
+// out = (plus + factor) (.) sum, where out is wanted; factor null: sum
+__device__ __forceinline__ void store_scaled(float* out, const float* factor, float plus, const float (&sum)[8], unsigned col) {
+  if (!out) return;
+  float f[8];
+  load_vector8(factor, col, 1.f - plus, f);
 #pragma unroll
-  for (int i = 0; i < 8; i++) s[i] = acc[i];
-  for (int t = 1; t < teams; t++) {
-    float o[8];
-    load_vector8(lds, (unsigned)((t - 1) * C) + col, 0.f, o);
-#pragma unroll
-    for (int i = 0; i < 8; i++) s[i] += o[i];
-  }
-  store8<false>(to, col, pack8<false>(s));
+  for (int i = 0; i < 8; i++) f[i] = (plus + f[i]) * sum[i];
+  store8<false>(out, col, pack8<false>(f));
 }
 
 // A thread has one chunk, and nothing is kept in fp32 across the sums of a row: the values are unpacked again behind them, and the vectors of
@@ -414,13 +404,34 @@ __global__ __launch_bounds__(kMaxThreads, 4) void norm_bwd_kernel(NormArgs a) {
     }
     if (on) put8<XB>(at_elem<XB>(a.dx, xo), at_x, pack8<XB>(u));
   }
+  auto sum_of = [&](float (&acc)[8]) {       // of the workgroup; whether this thread has some of it
+    join_parts(shared, tm.team, a.teams, a.C, col, has, acc);
+    return tm.team == 0 && has;
+  };
+  // into a row of the partial sums; where this workgroup had all rows, into the results
   const size_t rows = (size_t)a.B * a.walkers, first = (size_t)blockIdx.x * a.C;
+  const long long mod = b * a.mod_b;
+  const float *scale = TOKEN || !a.scale ? nullptr : a.scale + mod, *gate = TOKEN || !a.gate ? nullptr : a.gate + mod;
   if (PART & kBefore) {
-    if (a.dscale || a.din_weight) store_partial(tm, a.teams, shared, p_sum, has, col, a.C, a.partial + first);
-    if (!TOKEN && a.dshift) store_partial(tm, a.teams, shared, s_sum, has, col, a.C, a.partial + rows * a.C + first);
+    if (((!TOKEN && a.dscale) || a.din_weight) && sum_of(p_sum)) {
+      if (a.direct) {
+        if (!TOKEN && a.dscale) store_scaled(a.dscale + mod, a.in_weight, 0.f, p_sum, col);
+        store_scaled(a.din_weight, scale, 1.f, p_sum, col);
+      } else {
+        store8<false>(a.partial + first, col, pack8<false>(p_sum));
+      }
+    }
+    if (!TOKEN && a.dshift && sum_of(s_sum))
+      store8<false>(a.direct ? a.dshift + mod : a.partial + rows * a.C + first, col, pack8<false>(s_sum));
   }
-  if ((PART & kAfter) && (a.dgate || a.dout_weight))
-    store_partial(tm, a.teams, shared, q_sum, has, col, a.C, a.partial + 2 * rows * a.C + first);
+  if ((PART & kAfter) && ((!TOKEN && a.dgate) || a.dout_weight) && sum_of(q_sum)) {
+    if (a.direct) {
+      if (!TOKEN && a.dgate) store_scaled(a.dgate + mod, a.out_weight, 0.f, q_sum, col);
+      store_scaled(a.dout_weight, gate, 0.f, q_sum, col);
+    } else {
+      store8<false>(a.partial + 2 * rows * a.C + first, col, pack8<false>(q_sum));
+    }
+  }
 }
 
 // 32 columns (8 lanes of 4) by 64 rows at a time per workgroup; the 64 partial sums in order through LDS.
@@ -485,6 +496,17 @@ void plan_norm(NormArgs* a, bool backward) {
   a->walkers = walkers < 1 ? 1 : walkers < most ? walkers : most;
 }
 
+// No more rows than one workgroup has teams: it takes them all and writes the gradients of the vectors itself, and the second launch is left
+// out.  LayerNorm with scale and shift, one token of 1,536 channels 4.2 us (two launches 7.0), of 5,120 5.7 (8.4); with two rows a team it is
+// even (8 tokens of 1,536: 7.9, 7.7) or worse (4 of 5,120: 10.2, 8.4).
+static void plan_direct(NormArgs* a) {
+  const int teams = block_teams(a->team, a->N, kMaxThreads);
+  if (a->B > 1 || a->N > teams) return;
+  a->teams = teams;
+  a->walkers = 1;
+  a->direct = true;
+}
+
 // f(types, part, modulation of every token) with the constants of a call
 template <class F> static void with_types(const NormArgs& a, int part, F f) {
   auto with_part = [&](auto xb, auto hb) {
@@ -514,7 +536,9 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
+hipError_t launch_norm_bwd(const NormArgs& args, hipStream_t stream) {
+  NormArgs a = args;
+  plan_direct(&a);
   const dim3 grid((unsigned)(a.B * a.walkers)), block = norm_block(a);
   const int vectors = 2 * (a.C + kChunk), sums = (a.teams - 1) * a.C;
   const size_t lds = (size_t)(vectors > sums ? vectors : sums) * sizeof(float);
@@ -526,7 +550,7 @@ hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
     if (e == hipSuccess) kernel<<<grid, block, lds, stream>>>(a);
   });
   if (e == hipSuccess) e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.direct) return e;
   const int rows = a.B * a.walkers;
   const float *p = a.partial, *s = p + (size_t)rows * a.C, *q = s + (size_t)rows * a.C;
   const bool batch = a.mods == SLA2_MOD_BATCH, token = a.mods == SLA2_MOD_TOKEN;

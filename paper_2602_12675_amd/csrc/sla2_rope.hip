@@ -57,7 +57,7 @@ struct Position {
 constexpr int kAngleFloats = 512;            // of a wave: 8 tokens of 64 channels, 4 of 128: cosines, then sines, of the pairs of each
 struct AngleLds {
   double turns[64];                          // of a pair per position
-  float of[kMaxThreads / kWave * kAngleFloats];            // at the end of the backward kernel: 8 floats of every thread
+  float of[kMaxThreads / kWave * kAngleFloats];            // at the end of the backward kernel: the sums of all threads but the first part's
 };
 static_assert(kAngleFloats >= kWave * kChunk, "");
 template <bool BF16, bool HALVES> struct Angles {
@@ -314,30 +314,17 @@ __global__ __launch_bounds__(kMaxThreads, 4) void rope_bwd_kernel(RopeArgs a) {
       }
     }
   }
-  if (!a.partial) return;
-  const int cols = TOKEN ? a.H * a.d : a.d;
+  if (!a.dweight[0] && !a.dweight[1]) return;
+  // parts: the teams, or the places of a head in a row of any team, which are a head's lanes apart
+  const int cols = TOKEN ? a.H * a.d : a.d, lanes = TOKEN ? a.team.threads() : a.d / kChunk;
+  const int me = (int)threadIdx.x, part_of = me / lanes, parts = TOKEN ? a.teams : (int)blockDim.x / lanes;
 #pragma unroll
   for (int t = 0; t < 2; t++) {
     if (!a.dweight[t]) continue;
-    float* to = a.partial + ((size_t)t * gridDim.x + blockIdx.x) * cols;
-    __syncthreads();
-    store8<false>(angles.of, threadIdx.x * 8, pack8<false>(acc[t]));
-    __syncthreads();
-    if constexpr (TOKEN) {                   // those of the teams, in order
-      if (tm.team == 0 && at.has[0]) {
-        for (int k = 1; k < a.teams; k++) {
-          float o[8];
-          load_vector8(angles.of, (unsigned)(k * a.team.threads() + tm.lane) * 8, 0.f, o);
-#pragma unroll
-          for (int i = 0; i < 8; i++) acc[t][i] += o[i];
-        }
-        store8<false>(to, (unsigned)at.col[0], pack8<false>(acc[t]));
-      }
-    } else if ((int)threadIdx.x < a.d) {     // those of one place in a head, which are a head's lanes apart
-      float x = 0.f;
-      for (int k = (int)threadIdx.x / 8; k < (int)blockDim.x; k += a.d / kChunk) x += angles.of[k * 8 + threadIdx.x % 8];
-      to[threadIdx.x] = x;
-    }
+    join_parts(angles.of, part_of, parts, lanes * kChunk, (unsigned)(me % lanes * kChunk), true, acc[t]);
+    if (part_of != 0 || (TOKEN && !at.has[0])) continue;
+    float* to = a.direct ? a.dweight[t] : a.partial + ((size_t)t * gridDim.x + blockIdx.x) * cols;
+    store8<false>(to, (unsigned)(TOKEN ? at.col[0] : at.channel), pack8<false>(acc[t]));
   }
 }
 
@@ -405,15 +392,21 @@ hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
     a.cached = false;
     return launch_rope(a, stream);
   }
-  // the sums of the weights want a thread for every channel of a head
-  const int threads = whole_waves(a) < a.d ? a.d : whole_waves(a);
+  // few rows: one workgroup takes them all and writes the gradients of the weights itself (sla2_norm.hip: plan_direct); one token of 12 heads
+  // 3.9 us (two launches 7.0), 8 tokens with two rows a team 8.7 (7.8)
+  const int teams = block_teams(a.team, a.N, kMaxThreads);
+  if (a.B * a.groups == 1 && a.N <= teams) {
+    a.teams = teams;
+    a.walkers = 1;
+    a.direct = true;
+  }
   with_types(a, [&](auto bf16, auto halves) {
     constexpr bool BF16 = decltype(bf16)::value, HALVES = decltype(halves)::value;
-    const dim3 grid((unsigned)workgroups(a)), block(threads);
+    const dim3 grid((unsigned)workgroups(a)), block(whole_waves(a));
     if (a.norm == SLA2_ROPE_NORM_TOKEN) rope_bwd_kernel<BF16, HALVES, true><<<grid, block, 0, stream>>>(a);
     else rope_bwd_kernel<BF16, HALVES, false><<<grid, block, 0, stream>>>(a);
   });
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.direct) return e;
   ColumnJobs js{};
   js.columns = a.norm == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d;
   const int rows = workgroups(a);

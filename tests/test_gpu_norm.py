@@ -184,6 +184,20 @@ def test_rows(B, N, C, mods):
     c.check_backward()
 
 
+@pytest.mark.parametrize("N,C", [(127, 8), (128, 8), (129, 8), (3, 72), (33, 136), (16, 264), (17, 264), (5, 1536), (6, 1536), (1, 8192), (2, 8192)])
+@pytest.mark.parametrize("mods", MODS)
+def test_rows_of_one_workgroup(N, C, mods):
+    """As many rows as one workgroup takes side by side, whose sums need no second launch, and one more.  Each gradient alone has the
+    bits that it has with all."""
+    import torch
+    c = Case(1, N, C, norm_in="layer", norm_out="rms", mods=mods)
+    dh, dx_out, want = c.check_backward()
+    for only in [(n,) for n in ("dgate", "dout_weight", "din_weight", "dscale", "dshift")]:
+        got = c.gradients(dh, dx_out, only=only)
+        for name in ("dx", "dy") + only:
+            assert torch.equal(got[name], want[name]), (only, name)
+
+
 @pytest.mark.parametrize("types", TYPES, ids=lambda t: "-".join(t))
 @pytest.mark.parametrize("C", [64, 1032, 2560])
 def test_strides(C, types):

@@ -119,6 +119,15 @@ def test_many_sequences_of_one_token(norm):
     c.check_backward()
 
 
+@pytest.mark.parametrize("H,N,d,norm", [(1, 127, 64, "token"), (1, 128, 64, "token"), (1, 129, 64, "head"), (1, 128, 64, "head"), (1, 64, 128, "head"),
+                                        (3, 32, 64, "head"), (3, 33, 64, "token"), (12, 5, 128, "token"), (12, 6, 128, "head"),
+                                        (64, 1, 128, "token"), (128, 2, 64, "head")])
+@pytest.mark.parametrize("halves", [False, True])
+def test_rows_of_one_workgroup(H, N, d, norm, halves):
+    """As many rows as one workgroup takes side by side, whose sums need no second launch, and one more."""
+    Case(1, H, N, d, norm=norm, halves=halves, dtype="f32" if halves else "bf16", seed=N).check_backward()
+
+
 @pytest.mark.parametrize("axes", [(32, 0, 0), (0, 0, 32), (8, 12, 12), (0, 7, 3), (0, 0, 0), (1, 1, 1)])
 @pytest.mark.parametrize("halves", [False, True])
 def test_axes_and_channels_left_alone(axes, halves):
