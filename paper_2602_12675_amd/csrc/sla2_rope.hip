@@ -6,8 +6,8 @@
 // A row is a token with all its heads (as many as kMaxRow channels hold, where no sum goes over them), of q and of k: one reading of
 // each, one writing, and the angles are formed once for all heads of both.  A thread's chunks all lie at the same channels of their
 // heads, so it needs 4 angles (pairs of neighbours) or 8 (halves: the partner's channels come from a lane 4 or 8 further, by vector
-// instructions).  Angles are products in fp64, taken as fractions of a turn with the whole turns off before the rounding to fp32: a
-// position of 2^31 is as exact as fp64 has it.
+// instructions).  Angles are products in fp64, taken as fractions of a turn with the whole turns off before the rounding to fp32, and for
+// fp32 results what that rounding leaves is put back behind the sine: a position of 2^31 is as exact as fp64 has it.
 #include "rows.h"
 
 namespace sla2 {
@@ -78,18 +78,26 @@ template <bool BF16, bool HALVES> struct Angles {
     other = HALVES && tm.lane % (a.d / kChunk) < a.d / kChunk / 2 ? -1.f : 1.f;
     from = token + (HALVES ? tm.lane * kChunk % half : tm.lane % (a.d / kChunk) * 4);
   }
-  // bf16 results: the hardware's sine and cosine of a fraction of a turn, whose error is far below half a step of bf16
+  // bf16 results: the hardware's sine and cosine of a fraction of a turn, whose error is far below half a step of bf16 (over all fp32
+  // fractions 1.25e-7 at most, with the rounding of the fraction 2.2e-7; half a step at 1 is 3.9e-3)
   __device__ __forceinline__ void at(int p0, int p1, int p2) {
     wave_lds_fence();
     for (int j = pair; j < half; j += lanes) {
       const double t = (double)(j < end0 ? p0 : j < end1 ? p1 : p2) * turns[j];
-      const float f = (float)(t - rint(t));
+      const double fraction = t - rint(t);
+      const float f = (float)fraction;
       float si, co;
       if constexpr (BF16) {
         si = __builtin_amdgcn_sinf(f);
         co = __builtin_amdgcn_cosf(f);
       } else {
-        sincospif(2.f * f, &si, &co);
+        // the rounding of f is up to 2^-26 of a turn, 9.4e-8 in either result: sin (x + r) = sin x + r cos x, cos (x + r) = cos x - r sin x
+        // with r below 2^-23.3, whose square is below 2^-46
+        const float rest = (float)(fraction - (double)f) * 6.28318530717958648f;
+        float s1, c1;
+        sincospif(2.f * f, &s1, &c1);
+        si = s1 + rest * c1;
+        co = c1 - rest * s1;
       }
       token[j] = co;
       token[half + j] = si;
