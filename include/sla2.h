@@ -237,7 +237,8 @@ int sla2_dense_forward(const sla2_params* params, const void* q, const void* k, 
  * Rotary positions of q and k on their way into sla2_forward or sla2_dense_forward, and the norms before and after a block
  * (attention or feed-forward) with its modulation, gate and residual.  Conventions, status codes and streams as above; one
  * kernel for a forward call, two at most for a backward call, nothing allocated, no atomics: two calls on the same data give
- * the same bits.  Everything between the stored types is fp32 and rounded once; angles are fp64.  Vectors of channels
+ * the same bits.  Everything between the stored types is fp32 and rounded once; angles are fp64, their sines and cosines fp32 (good to
+ * 3 units of 2^-24 of themselves; where only bf16 comes of them the hardware's, which are within 2.2e-7).  Vectors of channels
  * (weights, gate, scale, shift) are DEVICE float, 16-byte aligned.  What is NaN or infinite stays in its row, and in the
  * gradients that are sums over rows; squares are summed in fp32 (values up to 1e17).  These entry points are not stages of the
  * profile below: a forward call is one kernel, whose time an event on either side gives. */

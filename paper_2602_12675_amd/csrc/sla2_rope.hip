@@ -6,8 +6,9 @@
 // A row is a token with all its heads (as many as kMaxRow channels hold, where no sum goes over them), of q and of k: one reading of
 // each, one writing, and the angles are formed once for all heads of both.  A thread's chunks all lie at the same channels of their
 // heads, so it needs 4 angles (pairs of neighbours) or 8 (halves: the partner's channels come from a lane 4 or 8 further, by vector
-// instructions).  Angles are products in fp64, taken as fractions of a turn with the whole turns off before the rounding to fp32, and for
-// fp32 results what that rounding leaves is put back behind the sine: a position of 2^31 is as exact as fp64 has it.
+// instructions).  Angles are products in fp64, with the whole turns off before the rounding to fp32: a position of 2^31 is as exact as fp64
+// has it.  What ends in fp32, the gradients of the weights among it, takes sines and cosines that are good to its last places, bf16 results
+// the hardware's.
 #include "rows.h"
 
 namespace sla2 {
@@ -51,16 +52,30 @@ struct Position {
   }
 };
 
+// Sine and cosine of t quarters of a turn, within 3 units of 2^-24 of themselves.  Whole quarters go off in fp64, before the rounding to fp32: the
+// last place of a fraction of a turn in fp32 is 9.4e-8 in either result, however close to zero that is.  1.5 x 2^52 has its last place at 1:
+// added, it leaves the number of quarters there.  Taylor's series over +-pi/4 (what is left out: 2.5e-9 of the sine, 1.5e-10 of the cosine).
+__device__ __forceinline__ void sin_cos_of_quarters(double t, float& s, float& c) {
+  const unsigned q = (unsigned)__builtin_bit_cast(unsigned long long, rint(t) + 6755399441055744.0);
+  const float x = (float)((t - rint(t)) * 1.5707963267948966), z = x * x;
+  const float s0 = x + x * (z * (-1.f / 6 + z * (1.f / 120 + z * (-1.f / 5040 + z * (1.f / 362880)))));
+  const float c0 = 1.f + z * (-0.5f + z * (1.f / 24 + z * (-1.f / 720 + z * (1.f / 40320 + z * (-1.f / 3628800)))));
+  s = q & 1 ? c0 : s0;
+  c = q & 1 ? s0 : c0;
+  if (q & 2) s = -s;
+  if ((q + 1) & 2) c = -c;
+}
+
 // The cosines and sines of the pairs of a thread's channels.  A token has d / 2 angles in all: each lane of a wave forms those of one
 // pair, or as many as there are tokens in the wave more, and all take theirs from LDS, where a wave has a place of its own.  Each lane
 // forming its own 4 or 8, most of them again in other lanes, was up to half of the instructions of a row.
 constexpr int kAngleFloats = 512;            // of a wave: 8 tokens of 64 channels, 4 of 128: cosines, then sines, of the pairs of each
 struct AngleLds {
-  double turns[64];                          // of a pair per position
+  double turns[64];                          // of a pair per position; or quarters of a turn
   float of[kMaxThreads / kWave * kAngleFloats];            // at the end of the backward kernel: the sums of all threads but the first part's
 };
 static_assert(kAngleFloats >= kWave * kChunk, "");
-template <bool BF16, bool HALVES> struct Angles {
+template <bool HARDWARE, bool HALVES> struct Angles {
   static constexpr int kPairs = HALVES ? 8 : 4;
   const double* turns;
   int end0, end1, lanes, pair, half;         // of the axes; lanes of a token in the wave; the first pair that this one forms; d / 2
@@ -72,32 +87,25 @@ template <bool BF16, bool HALVES> struct Angles {
     half = a.d / 2;
     pair = tm.lane % lanes;
     for (int j = (int)threadIdx.x; j < half; j += (int)blockDim.x)
-      lds.turns[j] = j < a.pairs_end[2] ? a.freq[j] * (a.sign * 0.15915494309189533577) : 0.0;     // 1 / (2 pi); backward: the other way round
+      lds.turns[j] = j < a.pairs_end[2] ? a.freq[j] * (a.sign * (HARDWARE ? 1 : 4) * 0.15915494309189533577) : 0.0;     // 1 / (2 pi); backward: the other way round
     __syncthreads();
     token = lds.of + (int)threadIdx.x / kWave * kAngleFloats + (int)threadIdx.x % kWave / lanes * a.d;
     other = HALVES && tm.lane % (a.d / kChunk) < a.d / kChunk / 2 ? -1.f : 1.f;
     from = token + (HALVES ? tm.lane * kChunk % half : tm.lane % (a.d / kChunk) * 4);
   }
-  // bf16 results: the hardware's sine and cosine of a fraction of a turn, whose error is far below half a step of bf16 (over all fp32
-  // fractions 1.25e-7 at most, with the rounding of the fraction 2.2e-7; half a step at 1 is 3.9e-3)
+  // HARDWARE, for bf16 results: the hardware's sine and cosine of a fraction of a turn, whose error is far below half a step of bf16 (over all
+  // fp32 fractions 1.25e-7 at most, with the rounding of the fraction 2.2e-7; half a step at 1 is 3.9e-3)
   __device__ __forceinline__ void at(int p0, int p1, int p2) {
     wave_lds_fence();
     for (int j = pair; j < half; j += lanes) {
       const double t = (double)(j < end0 ? p0 : j < end1 ? p1 : p2) * turns[j];
-      const double fraction = t - rint(t);
-      const float f = (float)fraction;
       float si, co;
-      if constexpr (BF16) {
+      if constexpr (HARDWARE) {
+        const float f = (float)(t - rint(t));
         si = __builtin_amdgcn_sinf(f);
         co = __builtin_amdgcn_cosf(f);
       } else {
-        // the rounding of f is up to 2^-26 of a turn, 9.4e-8 in either result: sin (x + r) = sin x + r cos x, cos (x + r) = cos x - r sin x
-        // with r below 2^-23.3, whose square is below 2^-46
-        const float rest = (float)(fraction - (double)f) * 6.28318530717958648f;
-        float s1, c1;
-        sincospif(2.f * f, &s1, &c1);
-        si = s1 + rest * c1;
-        co = c1 - rest * s1;
+        sin_cos_of_quarters(t, si, co);
       }
       token[j] = co;
       token[half + j] = si;
@@ -115,8 +123,8 @@ template <bool BF16, bool HALVES> struct Angles {
   }
 };
 
-template <bool BF16, bool HALVES>
-__device__ __forceinline__ void turn(const RopeArgs& a, const Angles<BF16, HALVES>& an, float (&x)[8]) {
+template <bool HARDWARE, bool HALVES>
+__device__ __forceinline__ void turn(const RopeArgs& a, const Angles<HARDWARE, HALVES>& an, float (&x)[8]) {
   if constexpr (HALVES) {
     float o[8];
     if (a.d == 128) {
@@ -237,7 +245,7 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
 #pragma unroll
           for (int i = 0; i < 8; i++) x[i] = x[i] * s[t] * w[t][v % W][i];
         }
-        turn<BF16, HALVES>(a, an, x);
+        turn(a, an, x);
         if (row && at.has[v]) {
           if (a.cached) store8<BF16>(at_elem<BF16>(a.y[t], yo), at.out[v], pack8<BF16>(x));
           else put8<BF16>(at_elem<BF16>(a.y[t], yo), at.out[v], pack8<BF16>(x));
@@ -247,7 +255,8 @@ __global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) voi
   }
 }
 
-// Gradients of x and, where there are partial sums, of the weights.  A thread has one chunk of q and of k; with two it would need more
+// Gradients of x and, where there are partial sums, of the weights, which are fp32 whatever x is: its sines and cosines are the exact ones
+// (2 x 20 heads of 4,429 tokens in bf16 35.4 us, with the hardware's 35.0).  A thread has one chunk of q and of k; with two it would need more
 // registers than leave a CU 16 waves (12 heads of 32,760 tokens 139 us, with one 117).
 template <bool BF16, bool HALVES, bool TOKEN>
 __global__ __launch_bounds__(kMaxThreads, 4) void rope_bwd_kernel(RopeArgs a) {
@@ -256,7 +265,7 @@ __global__ __launch_bounds__(kMaxThreads, 4) void rope_bwd_kernel(RopeArgs a) {
   Team tm(a.team, lds);
   const int part = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers, b = part / a.groups;
   const Place<1> at(a, tm, part % a.groups);
-  Angles<BF16, HALVES> an(a, tm, angles);
+  Angles<false, HALVES> an(a, tm, angles);
   const float share = 1.f / (float)(TOKEN ? a.H * a.d : a.d);
   float w[2][8], acc[2][8];
 #pragma unroll
@@ -285,7 +294,7 @@ __global__ __launch_bounds__(kMaxThreads, 4) void rope_bwd_kernel(RopeArgs a) {
       float x[8];
       unpack8<BF16>(rx[t], x);
       unpack8<BF16>(rg[t], g[t]);
-      turn<BF16, HALVES>(a, an, g[t]);
+      turn(a, an, g[t]);
       s[2 * t] = s[2 * t + 1] = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; i++) {
