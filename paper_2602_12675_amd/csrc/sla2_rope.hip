@@ -52,12 +52,20 @@ struct Position {
   }
 };
 
+// t less the whole number next to it.  Of t as it is rounded: contracted with the product that t is, the difference holds that product's own
+// rounding, which past 2^53 is large.
+__device__ __forceinline__ double off_whole(double t) {
+#pragma clang fp contract(off)
+  return t - rint(t);
+}
+
 // Sine and cosine of t quarters of a turn, within 3 units of 2^-24 of themselves.  Whole quarters go off in fp64, before the rounding to fp32: the
 // last place of a fraction of a turn in fp32 is 9.4e-8 in either result, however close to zero that is.  1.5 x 2^52 has its last place at 1:
-// added, it leaves the number of quarters there.  Taylor's series over +-pi/4 (what is left out: 2.5e-9 of the sine, 1.5e-10 of the cosine).
+// added, it leaves the number of quarters there (past 2^51 of them t has no fraction that means anything, and the result is a point of the
+// circle still).  Taylor's series over +-pi/4 (what is left out: 2.5e-9 of the sine, 1.5e-10 of the cosine).
 __device__ __forceinline__ void sin_cos_of_quarters(double t, float& s, float& c) {
   const unsigned q = (unsigned)__builtin_bit_cast(unsigned long long, rint(t) + 6755399441055744.0);
-  const float x = (float)((t - rint(t)) * 1.5707963267948966), z = x * x;
+  const float x = (float)(off_whole(t) * 1.5707963267948966), z = x * x;
   const float s0 = x + x * (z * (-1.f / 6 + z * (1.f / 120 + z * (-1.f / 5040 + z * (1.f / 362880)))));
   const float c0 = 1.f + z * (-0.5f + z * (1.f / 24 + z * (-1.f / 720 + z * (1.f / 40320 + z * (-1.f / 3628800)))));
   s = q & 1 ? c0 : s0;
@@ -101,7 +109,7 @@ template <bool HARDWARE, bool HALVES> struct Angles {
       const double t = (double)(j < end0 ? p0 : j < end1 ? p1 : p2) * turns[j];
       float si, co;
       if constexpr (HARDWARE) {
-        const float f = (float)(t - rint(t));
+        const float f = (float)off_whole(t);
         si = __builtin_amdgcn_sinf(f);
         co = __builtin_amdgcn_cosf(f);
       } else {

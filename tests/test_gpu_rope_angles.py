@@ -93,3 +93,31 @@ def test_gradients_of_the_weights_of_bf16_tensors(d, axes, H, N, norm, halves):
         for value, ref in ((c, r * np.cos(angle)), (s, -r * np.sin(angle))):
             bad = ~(np.abs(value - ref) <= trig_bound(ref, angle, 8))
             assert not bad.any(), (value[bad][:4], ref[bad][:4])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_angles_without_a_fraction_are_rotations_still(dtype):
+    """Angles of 2^53 turns and more, of which fp64 holds no fraction: whatever they are, cos^2 + sin^2 is 1 (each is off by half a step of its
+    type at most, of bf16 2^-8, and by 3 units of 2^-24)."""
+    import torch
+    from paper_2602_12675_amd import api
+    N, d, ty = 40, 64, {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    rng = np.random.default_rng(1)
+    p = api.make_rope_params(1, 1, N, d, (32, 0, 0), dtype=api.SLA2_F32 if dtype == "f32" else api.SLA2_BF16, norm=api.SLA2_ROPE_NORM_HEAD)
+    freq = torch.from_numpy(10.0 ** rng.uniform(10, 60, d // 2)).cuda()
+    at = torch.from_numpy(rng.integers(2 ** 30, 2 ** 31, (N, 3)).astype(np.int32)).cuda()
+    x = ones_and_zeros(torch, N, d, False, ty)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    plain = api.make_rope_params(1, 1, N, d, (32, 0, 0), dtype=p.dtype)
+    half = torch.finfo(ty).eps / 2
+    api.sla2_rope_forward(plain, x, None, freq, y, None, positions=at)
+    api.sla2_rope_backward(plain, None, None, freq, x, None, dx, None, positions=at)
+    for t in (y, dx):
+        c, s = split(f64(t)[0, 0], False)
+        assert np.abs(c * c + s * s - 1).max() <= 2 * (half + 3 * UNIT) * (1 + half)
+    # dy = x: n = sqrt(2) (1, 0), so dw = sqrt(2) cos at the channels of x and 0 at the others, token by token
+    ws = torch.empty(api.sla2_rope_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    dw = torch.empty(d, device="cuda")
+    api.sla2_rope_backward(p, x, None, freq, x, None, dx, None, dq_weight=dw, positions=at, workspace=ws)
+    c, s = split(f64(dw)[None], False)
+    assert not s.any() and np.abs(c).max() <= N * np.sqrt(2) * (1 + 1e-5)
