@@ -230,8 +230,8 @@ struct ColumnJob {
 };
 constexpr int kMaxJobs = 5;
 struct ColumnJobs {
+  int jobs, columns, items;                  // items: workgroups, filled in by the launch
   ColumnJob job[kMaxJobs];
-  int jobs, columns;
 };
 hipError_t launch_column_sums(const ColumnJobs& j, hipStream_t stream);
 

@@ -434,12 +434,15 @@ __global__ __launch_bounds__(kMaxThreads, 4) void norm_bwd_kernel(NormArgs a) {
   }
 }
 
-// 32 columns (8 lanes of 4) by 64 rows at a time per workgroup; the 64 partial sums in order through LDS.
-constexpr int kSumColumns = 32, kSumRows = 64;
+// 32 columns (8 lanes of 4) by 64 rows at a time per workgroup; the 64 partial sums in order through LDS.  A dimension of a launch holds less than
+// 2^32 threads (one of more is dropped without an error): beyond 2^31 of them, with 8,192 channels from 5,461 sequences on, they go on in y.
+constexpr int kSumColumns = 32, kSumRows = 64, kSumGroups = (1u << 31) / (kSumRows * 8);
 __global__ __launch_bounds__(kSumRows * 8) void column_sums_kernel(ColumnJobs js) {
   __shared__ f32x4 lds[kSumRows][kSumColumns / 4];
-  const int tiles = (js.columns + kSumColumns - 1) / kSumColumns, tile = (int)blockIdx.x % tiles;
-  int y = (int)blockIdx.x / tiles, k = 0;
+  const int item = (int)blockIdx.x + kSumGroups * (int)blockIdx.y;
+  if (item >= js.items) return;
+  const int tiles = (js.columns + kSumColumns - 1) / kSumColumns, tile = item % tiles;
+  int y = item / tiles, k = 0;
   while (y >= js.job[k].batches) y -= js.job[k++].batches;
   const ColumnJob& j = js.job[k];
   const int quad = (int)threadIdx.x % 8, r0 = (int)threadIdx.x / 8, c = tile * kSumColumns + 4 * quad;
@@ -472,11 +475,14 @@ __global__ __launch_bounds__(kSumRows * 8) void column_sums_kernel(ColumnJobs js
   }
 }
 
-hipError_t launch_column_sums(const ColumnJobs& j, hipStream_t stream) {
+hipError_t launch_column_sums(const ColumnJobs& jobs, hipStream_t stream) {
+  ColumnJobs j = jobs;
   int batches = 0;
   for (int k = 0; k < j.jobs; k++) batches += j.job[k].batches;
   if (batches == 0) return hipSuccess;
-  column_sums_kernel<<<dim3((unsigned)((j.columns + kSumColumns - 1) / kSumColumns * batches)), kSumRows * 8, 0, stream>>>(j);
+  j.items = (j.columns + kSumColumns - 1) / kSumColumns * batches;               // at most 256 (3 x 65,535 + 2)
+  const dim3 grid((unsigned)(j.items < kSumGroups ? j.items : kSumGroups), (unsigned)((j.items - 1) / kSumGroups + 1));
+  column_sums_kernel<<<grid, kSumRows * 8, 0, stream>>>(j);
   return hipGetLastError();
 }
 
