@@ -287,7 +287,7 @@ int sla2_rope_forward(const sla2_rope_params* params, const void* q, const void*
  *   dq_out, dk_out            layout out_stride;  dk_out, dk both NULL: q alone
  *   dq, dk                    layout in_stride, written; may be dq_out, dk_out or q, k themselves where the strides are the same
  *   dq_weight, dk_weight      DEVICE float [d] or [H, d], written; NULL: not wanted.  NULL without a norm
- *   workspace                 sla2_rope_workspace_bytes(), 256-byte aligned; NULL where neither is wanted */
+ *   workspace                 sla2_rope_workspace_bytes(), 256-byte aligned, apart from every tensor; NULL where neither is wanted */
 int sla2_rope_backward(const sla2_rope_params* params, const void* q, const void* k, const double* freq, const int32_t* positions,
                        const float* q_weight, const float* k_weight, const void* dq_out, const void* dk_out, void* dq, void* dk,
                        float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -337,7 +337,7 @@ int sla2_norm_forward(const sla2_norm_params* params, const void* x, const void*
  *   dgate, dscale, dshift          in mod_layout, written; for SLA2_MOD_BATCH and _SHARED summed over what shares them
  *   dout_weight, din_weight        DEVICE float [C], written
  * Each of these five may be NULL (not wanted); one without its input (dgate without gate, ...; dshift without dh) is refused.
- *   workspace    sla2_norm_workspace_bytes(), 256-byte aligned; NULL where none of the five is wanted */
+ *   workspace    sla2_norm_workspace_bytes(), 256-byte aligned, apart from every tensor; NULL where none of the five is wanted */
 int sla2_norm_backward(const sla2_norm_params* params, const void* x, const void* y, const float* gate, const float* out_weight,
                        const float* in_weight, const float* scale, const void* dh, const void* dx_out, void* dx, void* dy,
                        float* dgate, float* dout_weight, float* din_weight, float* dscale, float* dshift, void* workspace,

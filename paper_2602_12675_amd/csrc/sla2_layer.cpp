@@ -54,7 +54,7 @@ struct Output {
   View v;
   const void* in_place[2];                   // the inputs that it may be, where these have its layout
 };
-// No output on an input, unless it is that input as a whole and may be, and none on another output.
+// No output on an input, unless it is that input as a whole and may be, and none on another output.  A workspace is an output.
 static bool aliased(const Output* out, int outs, const View* in, int ins) {
   for (int i = 0; i < outs; i++) {
     const Output& o = out[i];
@@ -266,11 +266,14 @@ int sla2_rope_backward(const sla2_rope_params* params, const void* q, const void
   const View in[8] = {head_view(a, a.sin, q), head_view(a, a.sin, k), head_view(a, a.sout, dq_out), head_view(a, a.sout, dk_out),
                       flat(freq, 8, a.d / 2), flat(positions, 4, 3ll * a.N * (a.positions_stride ? a.B : 1)),
                       flat(q_weight, 4, weight_count(a)), flat(k_weight, 4, weight_count(a))};
-  const Output out[4] = {{head_view(a, a.sin, dq), {q, dq_out}}, {head_view(a, a.sin, dk), {k, dk_out}},
-                         {flat(dq_weight, 4, weight_count(a)), {}}, {flat(dk_weight, 4, weight_count(a)), {}}};
-  if (aliased(out, 4, in, 8)) return SLA2_EALIAS;
-  if (dq_weight || dk_weight) {
-    if ((rc = check_workspace(rope_partial_floats(a) * sizeof(float), workspace, workspace_bytes)) != SLA2_OK) return rc;
+  const bool sums = dq_weight || dk_weight;
+  const size_t need = rope_partial_floats(a) * sizeof(float);
+  const Output out[5] = {{head_view(a, a.sin, dq), {q, dq_out}}, {head_view(a, a.sin, dk), {k, dk_out}},
+                         {flat(dq_weight, 4, weight_count(a)), {}}, {flat(dk_weight, 4, weight_count(a)), {}},
+                         {flat(sums ? workspace : nullptr, 1, (long long)need), {}}};
+  if (aliased(out, 5, in, 8)) return SLA2_EALIAS;
+  if (sums) {
+    if ((rc = check_workspace(need, workspace, workspace_bytes)) != SLA2_OK) return rc;
     a.partial = (float*)workspace;
   }
   a.x[0] = q; a.x[1] = k;
@@ -329,12 +332,15 @@ int sla2_norm_backward(const sla2_norm_params* params, const void* x, const void
     if (!vector_ok(v)) return SLA2_EINVAL;
   const View in[8] = {x_view(a, x), h_view(a, y), mod_view(a, gate), flat(out_weight, 4, a.C), flat(in_weight, 4, a.C),
                       mod_view(a, scale), h_view(a, dh), x_view(a, dx_out)};
-  const Output out[7] = {{x_view(a, dx), {x, dx_out}}, {h_view(a, dy), {y, dh}}, {mod_view(a, dgate), {}}, {flat(dout_weight, 4, a.C), {}},
-                         {flat(din_weight, 4, a.C), {}}, {mod_view(a, dscale), {}}, {mod_view(a, dshift), {}}};
-  if (aliased(out, 7, in, 8)) return SLA2_EALIAS;
   plan_norm(&a, true);
-  if (dgate || dout_weight || din_weight || dscale || dshift) {
-    if ((rc = check_workspace(norm_partial_bytes(a), workspace, workspace_bytes)) != SLA2_OK) return rc;
+  const bool sums = dgate || dout_weight || din_weight || dscale || dshift;
+  const size_t need = norm_partial_bytes(a);
+  const Output out[8] = {{x_view(a, dx), {x, dx_out}}, {h_view(a, dy), {y, dh}}, {mod_view(a, dgate), {}}, {flat(dout_weight, 4, a.C), {}},
+                         {flat(din_weight, 4, a.C), {}}, {mod_view(a, dscale), {}}, {mod_view(a, dshift), {}},
+                         {flat(sums ? workspace : nullptr, 1, (long long)need), {}}};
+  if (aliased(out, 8, in, 8)) return SLA2_EALIAS;
+  if (sums) {
+    if ((rc = check_workspace(need, workspace, workspace_bytes)) != SLA2_OK) return rc;
     a.partial = (float*)workspace;
   }
   a.x = x; a.y = y; a.gate = gate; a.out_weight = out_weight; a.in_weight = in_weight; a.scale = scale;
