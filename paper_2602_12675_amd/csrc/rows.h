@@ -9,49 +9,9 @@
 // gradients stay in registers, one.  The sums of a row are kept in fp32; within a wave they are vector instructions only, and where a
 // team has several waves these exchange all sums of a step through LDS at once, behind one barrier.
 #pragma once
-#include "common.h"
+#include "row_plan.h"
 
 namespace sla2 {
-
-constexpr int kChunk = 8;                    // channels: 16 bytes of bf16
-constexpr int kMaxRow = 8192;                // channels of a row: 16 waves of a chunk a lane
-constexpr int kTeamThreads = 512;            // threads of a workgroup
-constexpr int kMaxThreads = 1024;
-constexpr int kCus = 256;
-// Waves of a SIMD that a kernel leaves registers for: 4 (two workgroups a CU), or 2 where a row takes more than 128 registers a thread.
-constexpr int waves_of(bool many_registers) { return many_registers ? 2 : 4; }
-constexpr int threads_of(bool many_registers) { return 4 * kWave * waves_of(many_registers); }
-
-// How a row of `chunks` chunks is spread over threads.
-struct RowTeam {
-  int lanes, waves, vec;                     // lanes of a wave, whole waves (1 where lanes < 64), chunks a thread
-  __host__ __device__ int threads() const { return lanes * waves; }
-};
-// The fewest waves with at most `most` chunks a thread (with more where a workgroup of `threads` threads has not that many waves), and then the
-// fewest chunks.
-inline RowTeam row_team(int chunks, int most, int threads = kTeamThreads) {
-  RowTeam t{64, 1, 1};
-  if (chunks <= 64) {
-    while (t.lanes > 8 && t.lanes / 2 >= chunks) t.lanes /= 2;
-    return t;
-  }
-  const int rounds = (chunks + 63) / 64, waves = (rounds + most - 1) / most;      // rounds: of a whole wave
-  t.waves = waves < threads / kWave ? waves : threads / kWave;
-  t.vec = (rounds + t.waves - 1) / t.waves;
-  t.waves = (rounds + t.vec - 1) / t.vec;
-  return t;
-}
-// Teams of a workgroup of `threads` threads, where there are rows enough.
-inline int block_teams(const RowTeam& t, int rows, int threads = kTeamThreads) {
-  const int n = t.threads() < threads ? threads / t.threads() : 1;
-  return n < rows ? n : rows;
-}
-// Workgroups of a launch: those that are resident at once, with `threads` threads a CU.  Each goes through its rows side by side with the
-// others, so that all read and write one stretch of memory; more of them than fit, or runs of rows for each, cost 5 to 25 %.
-inline int resident_workgroups(const RowTeam& t, int teams, int threads) {
-  const int block = (teams * t.threads() + kWave - 1) / kWave * kWave, n = threads / block;
-  return kCus * (n < 1 ? 1 : n);
-}
 
 // 8 neighbouring elements as they are stored, and as fp32.
 template <bool BF16> struct Raw {
@@ -236,58 +196,10 @@ struct ColumnJobs {
 hipError_t launch_column_sums(const ColumnJobs& j, hipStream_t stream);
 
 // ---- q and k: RMS norm and rotation ----
-struct HeadStrides {
-  long long b, h, n;
-};
-struct RopeArgs {
-  const void* x[2];                          // q, k (k: null where there is none)
-  const void* dy[2];                         // backward: gradients of the results
-  void* y[2];                                // results; backward: gradients of x
-  const float* weight[2];                    // [d] or [H, d], or null
-  const double* freq;                        // [d / 2]
-  const int32_t* positions;                  // [N, 3] or [B, N, 3], or null: the grid
-  float* partial;                            // backward with a norm: [2][workgroups][d or H d], or null: no gradient of the weights
-  float* dweight[2];
-  int tensors, B, H, N, d;
-  int pairs_end[3];                          // of the axes, one behind the last pair of each
-  int grid[3], origin[3];
-  long long positions_stride;                // of a batch
-  HeadStrides sin, sout;                     // of x (and its gradient); of the results (and their gradients)
-  float eps;
-  int norm;                                  // sla2_rope_norm
-  bool bf16, halves;
-  bool cached;                               // the results stay in the caches
-  double sign;                               // of the angles
-  // launch
-  RowTeam team;
-  int teams, heads, groups, walkers;         // teams of a workgroup; heads of a row, rows of a token; workgroups of a (batch, group)
-  bool direct;                               // backward: one workgroup has all rows and writes the results
-};
-void plan_rope(RopeArgs* a, bool backward);                 // fills in the launch from the sizes
-size_t rope_partial_floats(const RopeArgs& a);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 hipError_t launch_rope_bwd(const RopeArgs& a, hipStream_t stream);
 
 // ---- norms around a block ----
-struct NormArgs {
-  const void *x, *y;                         // backward: x is what norm_in was taken of
-  const float *gate, *out_weight, *in_weight, *scale, *shift;
-  void *x_out, *h;
-  // backward
-  const void *dh, *dx_out;
-  void *dx, *dy;
-  float *dgate, *dout_weight, *din_weight, *dscale, *dshift;
-  float* partial;                            // [3][B * walkers][C]: sums for scale, shift, gate of the rows of a workgroup
-  int B, N, C;
-  long long x_b, x_n, h_b, h_n, mod_b, mod_n;
-  int norm_in, norm_out, mods;               // sla2_norm_kind, sla2_mod_layout
-  float eps, rho;
-  bool x_bf16, h_bf16;
-  RowTeam team;
-  int teams, walkers;                        // teams of a workgroup; workgroups of a batch
-  bool direct;                               // backward: one workgroup has all rows and writes the results
-};
-void plan_norm(NormArgs* a, bool backward);
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream);
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream);
 

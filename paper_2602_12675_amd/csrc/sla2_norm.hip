@@ -17,15 +17,6 @@
 
 namespace sla2 {
 
-constexpr int kBefore = 1, kAfter = 2;       // parts of a call: h; x'
-// Whether a row takes more than 128 registers a thread, so that one workgroup of 8 waves fills a CU: 3 chunks with both parts (75,600 rows of
-// 5,120 channels 868 us as 256 workgroups, 884 as 512, of which half wait), or with a modulation of every token.  A token's own modulation does
-// not count for the number of workgroups: of 2 x 12,481 rows of 2,048 with one, 185 us as 256, 180 as 512.
-constexpr bool large_forward(int vec, int part, bool token) {
-  const bool both = part == (kBefore | kAfter);
-  return vec == 3 ? both || token : vec == 2 && both && token;
-}
-
 // What the statistics of a row need of the team: 1 / C, 1 / channels of this wave, and the channels of wave l % 16 on lane l.
 struct Counts {
   float all, mine, other;
@@ -149,7 +140,7 @@ template <int V> struct Columns {
 
 // x' and h
 template <int V, bool XB, bool HB, int PART, bool TOKEN>
-__global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, PART, TOKEN))) void norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(kTeamThreads, waves_of(large_norm(V, PART, TOKEN))) void norm_kernel(NormArgs a) {
   __shared__ float lds[kExchangeFloats];
   Team tm(a.team, lds);
   const int b = (int)blockIdx.x / a.walkers, walker = (int)blockIdx.x % a.walkers;
@@ -486,33 +477,6 @@ hipError_t launch_column_sums(const ColumnJobs& jobs, hipStream_t stream) {
   return hipGetLastError();
 }
 
-static int part_of(const NormArgs& a, bool backward) { return ((backward ? a.dh : a.h) ? kBefore : 0) | (a.y ? kAfter : 0); }
-
-void plan_norm(NormArgs* a, bool backward) {
-  a->team = backward ? row_team(a->C / kChunk, 1, kMaxThreads) : row_team(a->C / kChunk, 3, kTeamThreads);
-  // the rows of a wave lie within 2 GB of its first; where strides are longer than that it has one
-  const long long x_n = a->x_n > a->h_n ? a->x_n : a->h_n, widest = x_n > a->mod_n ? x_n : a->mod_n;
-  if (widest >= (1ll << 29) / (kWave / a->team.lanes)) a->team.lanes = kWave;
-  const bool large = !backward && large_forward(a->team.vec, part_of(*a, false), false);
-  // backward: one workgroup of up to 16 waves a CU where a team has 5 waves or more - of two with an odd number of waves the second often
-  // finds no place (4 x 3,478 rows of 2,520 channels, 5 waves: 107 us as two, 78 as one) - else two, one of which works while the other waits
-  // (31,201 rows of 1,536: 164 us as two of 6 waves, 172 as one of 15)
-  a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);
-  const int walkers = resident_workgroups(a->team, a->teams, threads_of(large)) / a->B, most = (int)(((long long)a->N + a->teams - 1) / a->teams);
-  a->walkers = walkers < 1 ? 1 : walkers < most ? walkers : most;
-}
-
-// No more rows than one workgroup has teams: it takes them all and writes the gradients of the vectors itself, and the second launch is left
-// out.  LayerNorm with scale and shift, one token of 1,536 channels 4.2 us (two launches 7.0), of 5,120 5.7 (8.4); with two rows a team it is
-// even (8 tokens of 1,536: 7.9, 7.7) or worse (4 of 5,120: 10.2, 8.4).
-static void plan_direct(NormArgs* a) {
-  const int teams = block_teams(a->team, a->N, kMaxThreads);
-  if (a->B > 1 || a->N > teams) return;
-  a->teams = teams;
-  a->walkers = 1;
-  a->direct = true;
-}
-
 // f(types, part, modulation of every token) with the constants of a call
 template <class F> static void with_types(const NormArgs& a, int part, F f) {
   auto with_part = [&](auto xb, auto hb) {
@@ -544,7 +508,7 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
 
 hipError_t launch_norm_bwd(const NormArgs& args, hipStream_t stream) {
   NormArgs a = args;
-  plan_direct(&a);
+  plan_norm_direct(&a);
   const dim3 grid((unsigned)(a.B * a.walkers)), block = norm_block(a);
   const int vectors = 2 * (a.C + kChunk), sums = (a.teams - 1) * a.C;
   const size_t lds = (size_t)(vectors > sums ? vectors : sums) * sizeof(float);

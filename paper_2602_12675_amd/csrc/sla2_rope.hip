@@ -13,10 +13,6 @@
 
 namespace sla2 {
 
-// Whether a row takes more than 128 registers a thread: 3 chunks of q and of k behind a sum over all heads (40 heads of 75,601 tokens 566 us as
-// 256 workgroups, 580 as 512).
-constexpr bool large_forward(int vec, int norm) { return vec == 3 && norm == SLA2_ROPE_NORM_TOKEN; }
-
 // x of the lane that holds the other channel of each pair of a head of LANES lanes
 template <int LANES> __device__ __forceinline__ float half_head_away(float x) {
   if constexpr (LANES == 16) return rotate16<8>(x);
@@ -178,7 +174,7 @@ template <int V> struct Place {
 };
 
 template <int V, bool BF16, bool HALVES, int NORM>
-__global__ __launch_bounds__(kTeamThreads, waves_of(large_forward(V, NORM))) void rope_kernel(RopeArgs a) {
+__global__ __launch_bounds__(kTeamThreads, waves_of(large_rope(V, NORM))) void rope_kernel(RopeArgs a) {
   __shared__ float lds[kExchangeFloats];
   __shared__ AngleLds angles;
   constexpr int W = NORM == SLA2_ROPE_NORM_TOKEN ? V : 1;
@@ -353,31 +349,6 @@ __global__ __launch_bounds__(kMaxThreads, 4) void rope_bwd_kernel(RopeArgs a) {
   }
 }
 
-// Results that fit the 256 MB memory-side cache are left there for the attention, which reads them next: 12 heads of 32,760 tokens (201 MB)
-// with sla2_forward behind them 473 us, past the caches 489 us, though the call alone takes 80.7 and 75.8 us; 2 x 20 heads of 4,096 at
-// d = 64 90.1 / 92.3 us; 40 heads of 75,600 (1.5 GB) 6,347 / 6,300 us.
-constexpr long long kCacheBytes = 256ll << 20;
-
-void plan_rope(RopeArgs* a, bool backward) {
-  const int most = kMaxRow / a->d;           // heads of a row
-  a->groups = (a->H + most - 1) / most;
-  a->heads = (a->H + a->groups - 1) / a->groups;
-  const int chunks = a->heads * a->d / kChunk;
-  a->cached = !backward && 2ll * a->B * a->H * a->N * a->d * (a->bf16 ? 2 : 4) <= kCacheBytes;
-  a->team = backward ? row_team(chunks, 1, kMaxThreads) : row_team(chunks, 3, kTeamThreads);
-  // backward: one large workgroup a CU where a team has 5 waves or more (sla2_norm.hip: plan_norm)
-  a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);
-  const int threads = threads_of(!backward && large_forward(a->team.vec, a->norm));
-  const int walkers = resident_workgroups(a->team, a->teams, threads) / (a->B * a->groups);
-  const int needed = (int)(((long long)a->N + a->teams - 1) / a->teams);
-  a->walkers = walkers < 1 ? 1 : walkers < needed ? walkers : needed;
-}
-
-static int workgroups(const RopeArgs& a) { return a.B * a.groups * a.walkers; }
-size_t rope_partial_floats(const RopeArgs& a) {
-  return a.norm == SLA2_ROPE_NORM_NONE ? 0 : (size_t)2 * workgroups(a) * (a.norm == SLA2_ROPE_NORM_TOKEN ? a.H * a.d : a.d);
-}
-
 // f(element type, pairing) with the constants of a call
 template <class F> static void with_types(const RopeArgs& a, F f) {
   auto with_pairs = [&](auto bf16) {
@@ -417,14 +388,7 @@ hipError_t launch_rope_bwd(const RopeArgs& args, hipStream_t stream) {
     a.cached = false;
     return launch_rope(a, stream);
   }
-  // few rows: one workgroup takes them all and writes the gradients of the weights itself (sla2_norm.hip: plan_direct); one token of 12 heads
-  // 3.9 us (two launches 7.0), 8 tokens with two rows a team 8.7 (7.8)
-  const int teams = block_teams(a.team, a.N, kMaxThreads);
-  if (a.B * a.groups == 1 && a.N <= teams) {
-    a.teams = teams;
-    a.walkers = 1;
-    a.direct = true;
-  }
+  plan_rope_direct(&a);
   with_types(a, [&](auto bf16, auto halves) {
     constexpr bool BF16 = decltype(bf16)::value, HALVES = decltype(halves)::value;
     const dim3 grid((unsigned)workgroups(a)), block(whole_waves(a));
