@@ -78,17 +78,19 @@ struct RopeArgs {
 // 256 workgroups, 580 as 512).
 constexpr bool large_rope(int vec, int norm) { return vec == 3 && norm == SLA2_ROPE_NORM_TOKEN; }
 
-// Results that fit the 256 MB memory-side cache are left there for the attention, which reads them next: 12 heads of 32,760 tokens (201 MB)
-// with sla2_forward behind them 473 us, past the caches 489 us, though the call alone takes 80.7 and 75.8 us; 2 x 20 heads of 4,096 at
-// d = 64 90.1 / 92.3 us; 40 heads of 75,600 (1.5 GB) 6,347 / 6,300 us.
+// Results - of q and k, or of the one that the call has - that fit the 256 MB memory-side cache are left there for the attention, which reads
+// them next: 12 heads of 32,760 tokens (201 MB) with sla2_forward behind them 473 us, past the caches 489 us, though the call alone takes
+// 80.7 and 75.8 us; 2 x 20 heads of 4,096 at d = 64 90.1 / 92.3 us; 40 heads of 75,600 (1.5 GB) 6,347 / 6,300 us; q alone of 146 and 191 MB
+// the same to 1 %.
 constexpr long long kCacheBytes = 256ll << 20;
 
+// The sizes, types and number of tensors are there.  That number changes nothing but `cached`: a workspace is of the size for both.
 inline void plan_rope(RopeArgs* a, bool backward) {
   const int most = kMaxRow / a->d;           // heads of a row
   a->groups = (a->H + most - 1) / most;
   a->heads = (a->H + a->groups - 1) / a->groups;
   const int chunks = a->heads * a->d / kChunk;
-  a->cached = !backward && 2ll * a->B * a->H * a->N * a->d * (a->bf16 ? 2 : 4) <= kCacheBytes;
+  a->cached = !backward && (long long)a->tensors * a->B * a->H * a->N * a->d * (a->bf16 ? 2 : 4) <= kCacheBytes;
   a->team = backward ? row_team(chunks, 1, kMaxThreads) : row_team(chunks, 3, kTeamThreads);
   // backward: one large workgroup a CU where a team has 5 waves or more (plan_norm)
   a->teams = block_teams(a->team, a->N, backward && a->team.waves > 4 ? kMaxThreads : kTeamThreads);

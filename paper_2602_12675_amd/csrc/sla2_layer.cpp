@@ -79,7 +79,7 @@ static bool extent_ok(int dims, const long long* count, const long long* stride,
   return n < ((__int128)1 << 60);
 }
 
-static int make_rope(const sla2_rope_params* p, bool backward, RopeArgs* a) {
+static int make_rope(const sla2_rope_params* p, bool backward, int tensors, RopeArgs* a) {
   if (!p) return SLA2_EINVAL;
   if (p->B < 1 || p->H < 1 || p->N < 1) return SLA2_EINVAL;
   if (p->dtype != SLA2_F32 && p->dtype != SLA2_BF16) return SLA2_EINVAL;
@@ -123,6 +123,7 @@ static int make_rope(const sla2_rope_params* p, bool backward, RopeArgs* a) {
     if (!extent_ok(3, count, s, p->d)) return SLA2_EUNSUPPORTED;
     *dst[x] = HeadStrides{s[0], s[1], s[2]};
   }
+  a->tensors = tensors;
   a->B = p->B; a->H = p->H; a->N = p->N; a->d = p->d;
   a->eps = p->eps;
   a->norm = p->norm;
@@ -210,14 +211,14 @@ extern "C" {
 
 size_t sla2_rope_workspace_bytes(const sla2_rope_params* params) {
   RopeArgs a;
-  if (make_rope(params, true, &a) != SLA2_OK) return 0;
+  if (make_rope(params, true, 2, &a) != SLA2_OK) return 0;
   const size_t n = align256(rope_partial_floats(a) * sizeof(float));
   return n ? n : 256;
 }
 
 int sla2_rope_frequencies(const sla2_rope_params* params, double theta, double* freq) {
   RopeArgs a;
-  const int rc = make_rope(params, false, &a);
+  const int rc = make_rope(params, false, 2, &a);
   if (rc != SLA2_OK) return rc;
   if (!freq || !(theta > 0.0 && theta < INFINITY)) return SLA2_EINVAL;
   for (int j = 0, first = 0, axis = 0; j < a.d / 2; j++) {
@@ -230,7 +231,7 @@ int sla2_rope_frequencies(const sla2_rope_params* params, double theta, double* 
 int sla2_rope_forward(const sla2_rope_params* params, const void* q, const void* k, const double* freq, const int32_t* positions,
                       const float* q_weight, const float* k_weight, void* q_out, void* k_out, void* hip_stream) {
   RopeArgs a;
-  const int rc = make_rope(params, false, &a);
+  const int rc = make_rope(params, false, k ? 2 : 1, &a);
   if (rc != SLA2_OK) return rc;
   if (!q || !q_out || !k != !k_out || (!k && k_weight)) return SLA2_EINVAL;
   if (misaligned16(q) || misaligned16(k) || misaligned16(q_out) || misaligned16(k_out)) return SLA2_EINVAL;
@@ -245,7 +246,6 @@ int sla2_rope_forward(const sla2_rope_params* params, const void* q, const void*
   a.weight[0] = q_weight; a.weight[1] = k_weight;
   a.freq = freq;
   a.positions = positions;
-  a.tensors = k ? 2 : 1;
   return launch_rope(a, (hipStream_t)hip_stream) == hipSuccess ? SLA2_OK : SLA2_EHIP;
 }
 
@@ -253,7 +253,7 @@ int sla2_rope_backward(const sla2_rope_params* params, const void* q, const void
                        const float* q_weight, const float* k_weight, const void* dq_out, const void* dk_out, void* dq, void* dk,
                        float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes, void* hip_stream) {
   RopeArgs a;
-  int rc = make_rope(params, true, &a);
+  int rc = make_rope(params, true, dk ? 2 : 1, &a);
   if (rc != SLA2_OK) return rc;
   const bool normed = a.norm != SLA2_ROPE_NORM_NONE;
   if (!dq_out || !dq || !dk_out != !dk) return SLA2_EINVAL;
@@ -283,7 +283,6 @@ int sla2_rope_backward(const sla2_rope_params* params, const void* q, const void
   a.dweight[0] = dq_weight; a.dweight[1] = dk_weight;
   a.freq = freq;
   a.positions = positions;
-  a.tensors = dk ? 2 : 1;
   return launch_rope_bwd(a, (hipStream_t)hip_stream) == hipSuccess ? SLA2_OK : SLA2_EHIP;
 }
 

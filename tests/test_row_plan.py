@@ -122,3 +122,15 @@ def test_every_row_once(plans):
             check(p, N, chunks, B * p.groups, 1 if backward else 3, 1024 if backward else 512)
         except AssertionError as e:
             raise AssertionError((line, p)) from e
+
+
+def test_results_that_stay_in_the_memory_side_cache(plans):
+    """Those of a call that come to 256 MB or less: of q and k, or of q alone."""
+    for bf16, esz in ((True, 2), (False, 4)):
+        for B, H, d in ((1, 12, 128), (2, 20, 64)):
+            fits = (256 << 20) // (B * H * d * esz)                          # tokens of one tensor
+            for tensors in (1, 2):
+                n = fits // tensors
+                got = plans([rope(B, H, n, d, "token", bf16, tensors), rope(B, H, n + 1, d, "token", bf16, tensors),
+                             rope(B, H, n, d, "token", bf16, tensors, backward=True)])
+                assert [p.cached for p in got] == [1, 0, 0], (bf16, B, H, d, tensors)
