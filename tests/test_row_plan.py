@@ -134,3 +134,22 @@ def test_results_that_stay_in_the_memory_side_cache(plans):
                 got = plans([rope(B, H, n, d, "token", bf16, tensors), rope(B, H, n + 1, d, "token", bf16, tensors),
                              rope(B, H, n, d, "token", bf16, tensors, backward=True)])
                 assert [p.cached for p in got] == [1, 0, 0], (bf16, B, H, d, tensors)
+
+
+def test_sizes_of_the_gpu_tests_go_round_the_loop(plans):
+    """Of tests/test_gpu_row_loop.py: at least two steps both ways, and for each kernel one size with three and a last one that is not full."""
+    from test_gpu_row_loop import FORMS, NORM, ROPE, WAYS
+    for backward in (False, True):
+        for nm, _, dtype in WAYS:
+            sizes = [s for s in ROPE if nm != "token" or s[1] * s[3] <= 8192]
+            got = plans([rope(*s[:4], nm, dtype == "bf16", 2, backward and nm != "none") for s in sizes])
+            assert all(steps(p, s[2]) >= 2 for p, s in zip(got, sizes)), (nm, backward, [(s, steps(p, s[2]), p) for p, s in zip(got, sizes)])
+            ragged = [p for p, s in zip(got, sizes) if steps(p, s[2]) >= 3 and s[2] % (p.teams * p.walkers)]
+            assert {p.waves > 1 for p in ragged} == {True, False}
+            assert {p.walkers > 1 for p in got} == {True, False}
+        for _, _, _, _, mods, part in FORMS:
+            got = plans([norm(*s, part, mods, backward) for s in NORM])
+            assert all(steps(p, s[1]) >= 2 for p, s in zip(got, NORM)), (part, mods, backward, [(s, steps(p, s[1]), p) for p, s in zip(got, NORM)])
+            ragged = [p for p, s in zip(got, NORM) if steps(p, s[1]) >= 3 and s[1] % (p.teams * p.walkers)]
+            assert {p.waves > 1 for p in ragged} >= ({True, False} if backward else {False})
+            assert {p.walkers > 1 for p in got} == {True, False}
