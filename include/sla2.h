@@ -46,7 +46,7 @@ typedef enum {
   SLA2_EUNSUPPORTED = -2, /* a shape / mode combination the kernels do not cover (see sla2_params) */
   SLA2_EWORKSPACE = -3,   /* workspace null, misaligned or smaller than sla2_workspace_bytes() (sla2_router, sla2_router_soft: than
                              the part that they use) */
-  SLA2_EALIAS = -4,       /* an output overlaps an input (or another output) */
+  SLA2_EALIAS = -4,       /* an output overlaps an input (or another output); sla2_rope_backward, sla2_norm_backward: the workspace too */
   SLA2_EHIP = -5          /* a kernel launch failed */
 } sla2_status;
 

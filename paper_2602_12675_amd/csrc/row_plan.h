@@ -39,7 +39,8 @@ inline int block_teams(const RowTeam& t, int rows, int threads = kTeamThreads) {
   return n < rows ? n : rows;
 }
 // Workgroups of a launch: those that are resident at once, with `threads` threads a CU.  Each goes through its rows side by side with the
-// others, so that all read and write one stretch of memory; more of them than fit, or runs of rows for each, cost 5 to 25 %.
+// others, so that all read and write one stretch of memory.  Two and four times as many take 2 % less to 5 % more time forward, 14 to 57 %
+// more backward (12 heads of 32,760 tokens 78.1 us, 79.5 and 79.0; backward 117, 147 and 142; 2 x 4,096 rows of 1,152 backward 56.8, 64.8, 69.3).
 inline int resident_workgroups(const RowTeam& t, int teams, int threads) {
   const int block = (teams * t.threads() + kWave - 1) / kWave * kWave, n = threads / block;
   return kCus * (n < 1 ? 1 : n);
@@ -138,7 +139,9 @@ struct NormArgs {
 constexpr int kBefore = 1, kAfter = 2;       // parts of a call: h; x'
 // Whether a row takes more than 128 registers a thread, so that one workgroup of 8 waves fills a CU: 3 chunks with both parts (75,600 rows of
 // 5,120 channels 868 us as 256 workgroups, 884 as 512, of which half wait), or with a modulation of every token.  A token's own modulation does
-// not count for the number of workgroups: of 2 x 12,481 rows of 2,048 with one, 185 us as 256, 180 as 512.
+// not count for the number of workgroups, although half of 512 wait: both parts with 2 chunks, 2 x 12,481 rows of 2,048, 185 us as 256, 180 as
+// 512; one part with 3 chunks 124.9 / 124.3 (32,760 rows of 1,536), 84.4 / 82.4 (2 x 12,481 of 1,536, bf16), 265.8 / 262.1 (20,000 of 5,120), and
+// the other way round where there are few rows: 82.7 / 83.8 (7,000 of 5,120, bf16), 14.9 / 15.7 (3,000 of 1,536, fp32 throughout).
 constexpr bool large_norm(int vec, int part, bool token) {
   const bool both = part == (kBefore | kAfter);
   return vec == 3 ? both || token : vec == 2 && both && token;

@@ -590,7 +590,7 @@ const char* sla2_strerror(int status) {
     case SLA2_EINVAL: return "invalid argument";
     case SLA2_EUNSUPPORTED: return "unsupported shape or mode";
     case SLA2_EWORKSPACE: return "workspace missing, misaligned or too small";
-    case SLA2_EALIAS: return "out overlaps an input";
+    case SLA2_EALIAS: return "an output or the workspace overlaps an input or another output";
     case SLA2_EHIP: return "kernel launch failed";
     default: return "unknown status";
   }

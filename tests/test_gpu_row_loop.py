@@ -1,6 +1,10 @@
 """Rows that a team takes one after the other: sizes at which every workgroup of sla2_rope_* and sla2_norm_* goes round its loop several times,
 the last time with rows left for some of its teams only (tests/test_row_plan.py checks that they do, by the plans themselves); and sums over
-rows whose terms are whole numbers, so that they are exact whatever their order and a row that is left out or taken twice shows."""
+rows whose terms are whole numbers, so that they are exact whatever their order and a row that is left out or taken twice shows.
+
+The bounds of values are ROW_UNITS of layer_helpers.  They cover rows of three chunks a thread: a sum has 24 terms in turn in a lane, 6 steps over
+the lanes and 4 over the waves, its mean 2 roundings more, 36 in all, of which a root passes on half, with 3 of its own; a result has fewer
+than 24 of its own."""
 import pytest
 
 import test_gpu_norm as NT
