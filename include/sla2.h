@@ -46,7 +46,8 @@ typedef enum {
   SLA2_EUNSUPPORTED = -2, /* a shape / mode combination the kernels do not cover (see sla2_params) */
   SLA2_EWORKSPACE = -3,   /* workspace null, misaligned or smaller than sla2_workspace_bytes() (sla2_router, sla2_router_soft: than
                              the part that they use) */
-  SLA2_EALIAS = -4,       /* an output overlaps an input (or another output); sla2_rope_backward, sla2_norm_backward: the workspace too */
+  SLA2_EALIAS = -4,       /* an output overlaps an input (or another output); sla2_rope_backward, sla2_norm_backward,
+                             sla2_packed_*, sla2_cache_attention: the workspace too */
   SLA2_EHIP = -5          /* a kernel launch failed */
 } sla2_status;
 
@@ -342,6 +343,97 @@ int sla2_norm_backward(const sla2_norm_params* params, const void* x, const void
                        const float* in_weight, const float* scale, const void* dh, const void* dx_out, void* dx, void* dy,
                        float* dgate, float* dout_weight, float* din_weight, float* dscale, float* dshift, void* workspace,
                        size_t workspace_bytes, void* hip_stream);
+
+/* ---- Attention over packed sequences, and a paged cache of keys and values -------------------------------------------------
+ * softmax(scale Q K^T) V where sequences differ in length: video tokens that read the prompts of a batch, packed training, stretches
+ * of a stream that read what came before them; and the cache that keeps a stream's keys and values.  Conventions, status codes and
+ * streams as above; bf16 tensors, products on the matrix cores with fp32 accumulation, P (and dS) rounded to bf16 between the
+ * products, everything else fp32.  No atomics: two calls on the same data give the same bits.  Offsets, lengths and pages are DEVICE
+ * arrays that the kernels read, so a captured call follows what they hold at each replay; nothing that they hold makes a kernel touch
+ * memory outside the stated tensors.  These entry points are not stages of the profile below. */
+
+typedef struct sla2_packed_params {
+  int sequences;             /* >= 1, at most 65535 */
+  int tokens_q, tokens_k;    /* rows of q, out, dout, dq / of k, v, dk, dv; >= 0 */
+  int H, H_kv, d;            /* H a multiple of H_kv: query head h reads key head h / (H / H_kv).  d in {64, 128} */
+  int dtype;                 /* SLA2_BF16 */
+  int causal;                /* 1: query i of a sequence of n_q queries and n_k keys reads the keys 0 .. i + n_k - n_q (the last query
+                                all of them; one before the first key none); 0: all of its sequence */
+  float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */
+  /* (head, token) element strides of q, dq; of k, v, dk, dv; of out, dout.  Both zero: contiguous [tokens, heads, d].  As in
+   * sla2_params; below 2^24 elements a token */
+  long long q_stride[2];
+  long long kv_stride[2];
+  long long out_stride[2];
+} sla2_packed_params;
+
+/* Bytes of the workspace of sla2_packed_forward (backward = 0) or sla2_packed_backward (1); 0: params are invalid.  Pure host function. */
+size_t sla2_packed_workspace_bytes(const sla2_packed_params* params, int backward);
+
+/* out, lse of every query.  Sequence s has the queries q_start[s] .. q_start[s + 1] - 1 and the keys k_start[s] .. k_start[s + 1] - 1.
+ *   q_start, k_start   DEVICE int32 [sequences + 1], from 0 on, not descending, at most tokens_q / tokens_k.  Rows from q_start[sequences]
+ *                      on belong to no sequence: what is written is left as it was there
+ *   lse_or_null        DEVICE float [H, tokens_q]: logarithm of the sum of the exponentials of the scaled scores
+ *   k, v               NULL where tokens_k is 0;  q, out NULL where tokens_q is 0
+ * A query that reads no key has out = 0 and lse = -inf.  What is NaN or infinite stays in its sequence; in a row of k or v it reaches the
+ * queries that read the row, and with `causal` may reach earlier ones. */
+int sla2_packed_forward(const sla2_packed_params* params, const void* q, const void* k, const void* v, const int32_t* q_start,
+                        const int32_t* k_start, void* out, float* lse_or_null, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of q, k and v from that of out.
+ *   out, lse     of the forward call
+ *   dq, dk, dv   written; they may be slices of one buffer, with other numbers of heads too, that share no element, and share none with
+ *                an input.  A key that no query reads has dk = dv = 0 */
+int sla2_packed_backward(const sla2_packed_params* params, const void* q, const void* k, const void* v, const int32_t* q_start,
+                         const int32_t* k_start, const void* out, const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The cache: `pages` pages of page_size tokens of every key head.  Token t of sequence b is in page page_table[b][t / page_size], at
+ * t % page_size.  SLA2_QUANT_FP8 and SLA2_QUANT_INT8 keep codes with one scale for each token and head, of keys and of values: the rule
+ * of sla2_quant with the d channels of a row in the place of its block (amax = max|x|, code = rne(x * (448 or 127 / amax)), scale =
+ * amax / 448 or 127, both divisions in fp32).  A row whose amax is below 2^-100 has scale 1 and codes 0; one with a NaN or an infinity
+ * has a NaN for its scale and codes 0, and reads back as NaN. */
+typedef struct sla2_cache_params {
+  int B;                     /* sequences, 1 .. 65535 */
+  int H, H_kv, d;            /* as in sla2_packed_params (H: sla2_cache_attention alone) */
+  int pages, page_size;      /* page_size: 16, 32, 64, 128 or 256 */
+  int max_pages;             /* columns of page_table: a sequence has max_pages page_size tokens (< 2^31) at most */
+  int tokens;                /* sla2_cache_write, _read: rows of k and v; >= 0 */
+  int dtype;                 /* SLA2_BF16: of q, k, v, out */
+  int quant_mode;            /* SLA2_QUANT_NONE (the cache is bf16), _FP8 or _INT8 */
+  float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */
+  long long table_stride;    /* elements between the rows of page_table; 0: max_pages */
+  /* (page, head, token) strides of k_cache and v_cache in elements; all zero: [pages, H_kv, page_size, d].  Multiples of 16 bytes */
+  long long cache_stride[3];
+  long long kv_stride[2];    /* (head, token) of k, v; both zero: [tokens, H_kv, d].  As in sla2_packed_params */
+  long long q_stride[2];     /* (head, sequence) of q; both zero: [B, H, d] */
+  long long out_stride[2];   /* of out */
+} sla2_cache_params;
+
+/* New tokens into the cache (quantised on the way), and back out of it (as bf16).
+ *   start         DEVICE int32 [B + 1]: rows start[b] .. start[b + 1] - 1 of k and v are of sequence b (as q_start above).
+ *                 NULL: row b is of sequence b (tokens <= B)
+ *   first         DEVICE int32 [B]: the place in its sequence of the first of them; NULL: 0
+ *   page_table    DEVICE int32 [B, max_pages]
+ *   k_cache, v_cache   uint8 or int8 codes, or bf16;  k_scale, v_scale   DEVICE float [pages, H_kv, page_size], NULL with SLA2_QUANT_NONE
+ * A row whose place is outside its sequence's pages, or whose page is not one of 0 .. pages - 1, is not written; read, it is 0.  Rows
+ * that are written have places of their own: two that share one leave it undefined. */
+int sla2_cache_write(const sla2_cache_params* params, const void* k, const void* v, const int32_t* start, const int32_t* first,
+                     const int32_t* page_table, void* k_cache, void* v_cache, float* k_scale, float* v_scale, void* hip_stream);
+int sla2_cache_read(const sla2_cache_params* params, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                    const int32_t* start, const int32_t* first, const int32_t* page_table, void* k, void* v, void* hip_stream);
+
+/* Bytes of the workspace of sla2_cache_attention; 0: params are invalid.  Pure host function. */
+size_t sla2_cache_workspace_bytes(const sla2_cache_params* params);
+
+/* Attention of one new token of each sequence over the first length[b] tokens of the cache, its own among them if it was written.
+ *   q, out        [B, H, d];  lse_or_null   DEVICE float [B, H]
+ *   length        DEVICE int32 [B]; what is over max_pages page_size is not read.  0 (or less): out = 0, lse = -inf
+ * Tokens in a page that is not one of 0 .. pages - 1 are left out.  What lies behind a sequence's last token is not read.  Codes are
+ * exact in bf16; a token's scales meet its scores and its probability in fp32. */
+int sla2_cache_attention(const sla2_cache_params* params, const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                         const float* v_scale, const int32_t* length, const int32_t* page_table, void* out, float* lse_or_null,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Per-kernel timing for benchmarks (not part of the operator).  While no profile is open the other entry
  * points share no mutable host state and may be called from several threads; between sla2_profile_begin

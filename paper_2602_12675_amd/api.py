@@ -31,7 +31,8 @@ SLA2_STATIC_SCRATCH_BYTES = 32 << 20
 EXPORTS = ("sla2_workspace_bytes", "sla2_workspace_layout", "sla2_num_selected", "sla2_router", "sla2_router_static",
            "sla2_router_soft", "sla2_forward", "sla2_backward", "sla2_dense_forward", "sla2_rope_workspace_bytes",
            "sla2_rope_frequencies", "sla2_rope_forward", "sla2_rope_backward", "sla2_norm_workspace_bytes", "sla2_norm_forward",
-           "sla2_norm_backward", "sla2_profile_begin", "sla2_profile_begin_sampled",
+           "sla2_norm_backward", "sla2_packed_workspace_bytes", "sla2_packed_forward", "sla2_packed_backward", "sla2_cache_write",
+           "sla2_cache_read", "sla2_cache_workspace_bytes", "sla2_cache_attention", "sla2_profile_begin", "sla2_profile_begin_sampled",
            "sla2_profile_end",
            "sla2_strerror", "sla2_version")
 
@@ -72,6 +73,22 @@ class NormParams(ctypes.Structure):
                 ("mod_stride", ctypes.c_longlong * 2)]
 
 
+class PackedParams(ctypes.Structure):
+    """struct sla2_packed_params"""
+    _fields_ = [("sequences", ctypes.c_int), ("tokens_q", ctypes.c_int), ("tokens_k", ctypes.c_int), ("H", ctypes.c_int),
+                ("H_kv", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_longlong * 2), ("kv_stride", ctypes.c_longlong * 2), ("out_stride", ctypes.c_longlong * 2)]
+
+
+class CacheParams(ctypes.Structure):
+    """struct sla2_cache_params"""
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int), ("d", ctypes.c_int), ("pages", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("max_pages", ctypes.c_int), ("tokens", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("quant_mode", ctypes.c_int), ("scale", ctypes.c_float), ("table_stride", ctypes.c_longlong),
+                ("cache_stride", ctypes.c_longlong * 3), ("kv_stride", ctypes.c_longlong * 2), ("q_stride", ctypes.c_longlong * 2),
+                ("out_stride", ctypes.c_longlong * 2)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError("libsla2.so is not built: run `python -m paper_2602_12675_amd.build` "
                       "(there is no CPU fallback)")
@@ -110,6 +127,21 @@ _lib.sla2_norm_forward.restype = ctypes.c_int
 _lib.sla2_norm_forward.argtypes = [_np] + [_vp] * 10
 _lib.sla2_norm_backward.restype = ctypes.c_int
 _lib.sla2_norm_backward.argtypes = [_np] + [_vp] * 16 + [ctypes.c_size_t, _vp]
+_ap, _cp = ctypes.POINTER(PackedParams), ctypes.POINTER(CacheParams)
+_lib.sla2_packed_workspace_bytes.restype = ctypes.c_size_t
+_lib.sla2_packed_workspace_bytes.argtypes = [_ap, ctypes.c_int]
+_lib.sla2_packed_forward.restype = ctypes.c_int
+_lib.sla2_packed_forward.argtypes = [_ap] + [_vp] * 8 + [ctypes.c_size_t, _vp]
+_lib.sla2_packed_backward.restype = ctypes.c_int
+_lib.sla2_packed_backward.argtypes = [_ap] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+_lib.sla2_cache_write.restype = ctypes.c_int
+_lib.sla2_cache_write.argtypes = [_cp] + [_vp] * 10
+_lib.sla2_cache_read.restype = ctypes.c_int
+_lib.sla2_cache_read.argtypes = [_cp] + [_vp] * 10
+_lib.sla2_cache_workspace_bytes.restype = ctypes.c_size_t
+_lib.sla2_cache_workspace_bytes.argtypes = [_cp]
+_lib.sla2_cache_attention.restype = ctypes.c_int
+_lib.sla2_cache_attention.argtypes = [_cp] + [_vp] * 10 + [ctypes.c_size_t, _vp]
 _lib.sla2_profile_begin.restype = ctypes.c_int
 _lib.sla2_profile_begin.argtypes = [ctypes.c_uint, ctypes.c_int]
 _lib.sla2_profile_begin_sampled.restype = ctypes.c_int
@@ -377,6 +409,102 @@ def sla2_norm_backward(params, x, dh, dx_out, dx, y=None, gate=None, out_weight=
         (scale, f32, m, cm), (dh, th, n, ch), (dx_out, tx, n, cx), (dx, tx, n, cx), (dy, th, n, ch), (dgate, f32, m, cm),
         (dout_weight, f32, c, True), (din_weight, f32, c, True), (dscale, f32, m, cm), (dshift, f32, m, cm), _scratch(workspace)),
         stream, check, _bytes(workspace, ws_bytes))
+
+
+# ---- attention over packed sequences, and a paged cache of keys and values ---------------------------------------------
+def make_packed_params(sequences, tokens_q, tokens_k, H, H_kv, d, causal=False, scale=0.0, dtype=SLA2_BF16, q_stride=None, kv_stride=None,
+                       out_stride=None) -> PackedParams:
+    """scale of the scores: 0 = 1 / sqrt(d).  q_stride, kv_stride, out_stride: (head, token) element strides of q and dq, of k, v, dk and
+    dv, of out and dout; None = contiguous [tokens, heads, d]."""
+    p = PackedParams(sequences, tokens_q, tokens_k, H, H_kv, d, dtype, int(causal), scale)
+    for dst, src in ((p.q_stride, q_stride), (p.kv_stride, kv_stride), (p.out_stride, out_stride)):
+        if src is not None:
+            dst[:] = [int(x) for x in src]
+    return p
+
+
+def make_cache_params(B, H, H_kv, d, pages, page_size, max_pages, tokens=0, quant_mode=SLA2_QUANT_NONE, scale=0.0, dtype=SLA2_BF16,
+                      table_stride=0, cache_stride=None, kv_stride=None, q_stride=None, out_stride=None) -> CacheParams:
+    """max_pages: columns of the page table.  tokens: rows of k and v (sla2_cache_write, _read).  cache_stride: (page, head, token) element
+    strides of the cache; kv_stride: (head, token) of k and v; q_stride, out_stride: (head, sequence) of q and out; None = contiguous
+    [pages, H_kv, page_size, d], [tokens, H_kv, d], [B, H, d]."""
+    p = CacheParams(B, H, H_kv, d, pages, page_size, max_pages, tokens, dtype, quant_mode, scale, int(table_stride))
+    for dst, src in ((p.cache_stride, cache_stride), (p.kv_stride, kv_stride), (p.q_stride, q_stride), (p.out_stride, out_stride)):
+        if src is not None:
+            dst[:] = [int(x) for x in src]
+    return p
+
+
+def sla2_packed_workspace_bytes(params: PackedParams, backward=False) -> int:
+    return _lib.sla2_packed_workspace_bytes(ctypes.byref(params), int(backward))
+
+
+def _packed_sizes(p):
+    """(elements of q, of k; element type; elements of q_start; whether q, k and out are contiguous)"""
+    return (p.tokens_q * p.H * p.d, p.tokens_k * p.H_kv * p.d, _TYPES.get(p.dtype), p.sequences + 1, p.q_stride[1] == 0,
+            p.kv_stride[1] == 0, p.out_stride[1] == 0)
+
+
+def sla2_packed_forward(params, q, k, v, q_start, k_start, out, lse=None, workspace=None, stream=None, check=True, ws_bytes=None) -> int:
+    nq, nk, dt, ns, cq, ck, co = _packed_sizes(params)
+    return _call(_lib.sla2_packed_forward, params, (
+        (q, dt, nq, cq), (k, dt, nk, ck), (v, dt, nk, ck), (q_start, torch.int32, ns, True), (k_start, torch.int32, ns, True),
+        (out, dt, nq, co), (lse, torch.float32, params.H * params.tokens_q, True), _scratch(workspace)), stream, check,
+        _bytes(workspace, ws_bytes))
+
+
+def sla2_packed_backward(params, q, k, v, q_start, k_start, out, lse, dout, dq, dk, dv, workspace=None, stream=None, check=True,
+                         ws_bytes=None) -> int:
+    nq, nk, dt, ns, cq, ck, co = _packed_sizes(params)
+    return _call(_lib.sla2_packed_backward, params, (
+        (q, dt, nq, cq), (k, dt, nk, ck), (v, dt, nk, ck), (q_start, torch.int32, ns, True), (k_start, torch.int32, ns, True),
+        (out, dt, nq, co), (lse, torch.float32, params.H * params.tokens_q, True), (dout, dt, nq, co), (dq, dt, nq, cq), (dk, dt, nk, ck),
+        (dv, dt, nk, ck), _scratch(workspace)), stream, check, _bytes(workspace, ws_bytes))
+
+
+_CODES = {SLA2_QUANT_NONE: (torch.bfloat16,), SLA2_QUANT_FP8: (torch.float8_e4m3fn, torch.uint8), SLA2_QUANT_INT8: (torch.int8,)}
+
+
+def _cache_tensors(p, k_cache, v_cache, k_scale, v_scale, page_table):
+    """The arguments of the cache as _call takes them.  Codes of FP8 may be held as uint8."""
+    types = _CODES.get(p.quant_mode, (None,))
+    rows, dense = p.pages * p.H_kv * p.page_size, p.cache_stride[2] == 0
+    table = (p.B - 1) * p.table_stride + p.max_pages if p.table_stride else p.B * p.max_pages
+    kinds = [getattr(t, "dtype", None) if getattr(t, "dtype", None) in types else types[0] for t in (k_cache, v_cache)]
+    return ((k_cache, kinds[0], rows * p.d, dense), (v_cache, kinds[1], rows * p.d, dense), (k_scale, torch.float32, rows, True),
+            (v_scale, torch.float32, rows, True), (page_table, torch.int32, 0 if p.table_stride else table, p.table_stride == 0))
+
+
+def sla2_cache_write(params, k, v, page_table, k_cache, v_cache, k_scale=None, v_scale=None, start=None, first=None, stream=None,
+                     check=True) -> int:
+    n, dense, dt = params.tokens * params.H_kv * params.d, params.kv_stride[1] == 0, _TYPES.get(params.dtype)
+    kc, vc, ks, vs, table = _cache_tensors(params, k_cache, v_cache, k_scale, v_scale, page_table)
+    return _call(_lib.sla2_cache_write, params, (
+        (k, dt, n, dense), (v, dt, n, dense), (start, torch.int32, params.B + 1, True), (first, torch.int32, params.B, True), table, kc, vc,
+        ks, vs), stream, check)
+
+
+def sla2_cache_read(params, k_cache, v_cache, page_table, k, v, k_scale=None, v_scale=None, start=None, first=None, stream=None,
+                    check=True) -> int:
+    n, dense, dt = params.tokens * params.H_kv * params.d, params.kv_stride[1] == 0, _TYPES.get(params.dtype)
+    kc, vc, ks, vs, table = _cache_tensors(params, k_cache, v_cache, k_scale, v_scale, page_table)
+    return _call(_lib.sla2_cache_read, params, (
+        kc, vc, ks, vs, (start, torch.int32, params.B + 1, True), (first, torch.int32, params.B, True), table, (k, dt, n, dense),
+        (v, dt, n, dense)), stream, check)
+
+
+def sla2_cache_workspace_bytes(params: CacheParams) -> int:
+    return _lib.sla2_cache_workspace_bytes(ctypes.byref(params))
+
+
+def sla2_cache_attention(params, q, k_cache, v_cache, page_table, length, out, k_scale=None, v_scale=None, lse=None, workspace=None,
+                         stream=None, check=True, ws_bytes=None) -> int:
+    n, dt, f32 = params.B * params.H * params.d, _TYPES.get(params.dtype), torch.float32
+    kc, vc, ks, vs, table = _cache_tensors(params, k_cache, v_cache, k_scale, v_scale, page_table)
+    return _call(_lib.sla2_cache_attention, params, (
+        (q, dt, n, params.q_stride[1] == 0), kc, vc, ks, vs, (length, torch.int32, params.B, True), table,
+        (out, dt, n, params.out_stride[1] == 0), (lse, f32, params.B * params.H, True), _scratch(workspace)), stream, check,
+        _bytes(workspace, ws_bytes))
 
 
 def sla2_profile_begin(stages, max_calls: int) -> None:

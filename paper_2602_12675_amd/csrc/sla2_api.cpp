@@ -13,7 +13,6 @@
 
 namespace sla2 {
 
-static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // bf16 tensors, d = 128, 128-row blocks: from which k on H_i is formed before the attention kernel (launch_kv_states_bf16: per key
 // block its states written and read, per pair of blocks 96 K products) rather than rebuilt in it (a third of its products per
@@ -228,10 +227,6 @@ static bool interleaved_disjoint(const Shape& s, const Strides& st, const void* 
   return stretches_disjoint(a, b, esz, period, (long long)(s.H - 1) * st.h + s.d);
 }
 
-static int check_workspace(size_t need, const void* ws, size_t bytes) {
-  if (!ws || ((uintptr_t)ws & 255) || bytes < need) return SLA2_EWORKSPACE;
-  return SLA2_OK;
-}
 // What the router touches: all in front of `partial`, and there the pooled keys.
 static size_t router_bytes(const Shape& s, const sla2_ws_layout& L) { return L.partial + pooled_bytes(s); }
 

@@ -1,0 +1,154 @@
+// A paged cache of keys and values: rows of bf16 into it, with one FP8 or INT8 scale for each token and head, and back.
+//
+// A row (the d channels of a token and head) is 8 channels on each of d / 8 neighbouring lanes, read once and written once; its largest
+// magnitude is a maximum over those lanes, taken on the bits of |x|, which order finite numbers, infinities and NaNs alike.  A
+// workgroup has neighbouring tokens of one head, whose codes and scales are neighbours in a page.
+#include "cache.h"
+#include "rows.h"
+
+namespace sla2 {
+
+constexpr int kCacheThreads = 256;
+
+// Where row i of k and v is in the cache: page and slot; page -1: nowhere, -2: the row is of no sequence.  All lanes of the wave take part: the sequence is the
+// number of sequences that end at or in front of the row, counted 64 at a time.
+struct Place {
+  int page, slot;
+};
+__device__ __forceinline__ Place place_of(const CacheArgs& a, int i, int lane) {
+  int b = i;
+  long long at = 0;
+  if (a.start) {
+    b = 0;
+    for (int s0 = 0; s0 < a.B; s0 += kWave) {
+      const int end = s0 + lane < a.B ? a.start[s0 + lane + 1] : INT32_MAX;
+#pragma unroll
+      for (int r = 0; r < kWave / 8; r++) {              // the rows of the wave's teams (8 or 16 lanes each)
+        const int row = __builtin_amdgcn_readlane(i, 8 * r);
+        const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= row));
+        b += lane / 8 == r ? n : 0;
+      }
+    }
+  }
+  if (i >= a.tokens || b >= a.B) return Place{-2, 0};
+  if (a.start) {
+    const int s = a.start[b];
+    if (i < s) return Place{-2, 0};                      // in front of the first sequence
+    at = i - (long long)s;
+  }
+  if (a.first) at += a.first[b];
+  const long long column = at >> a.page_shift;
+  if (at < 0 || column >= a.max_pages) return Place{-1, 0};
+  const int page = a.table[b * a.table_stride + column];
+  return Place{page >= 0 && page < a.pages ? page : -1, (int)(at & ((1 << a.page_shift) - 1))};
+}
+
+// |x| of the largest of a row, an infinity if one of them is not finite
+template <int LANES> __device__ __forceinline__ float row_amax(const Raw<true>& r) {
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; i++) m = max(m, max(r.a[0][i] & 0x7fffu, r.a[0][i] >> 16 & 0x7fffu));
+  float x = __builtin_bit_cast(float, min(m, 0x7f80u) << 16);
+  x = quad_max(x);
+  x = fmaxf(x, dpp_move<0x141>(x));                      // row_half_mirror
+  if (LANES > 8) x = fmaxf(x, dpp_move<0x140>(x));       // row_mirror
+  return x;
+}
+
+// 8 codes of a row whose largest magnitude is amax, and its scale
+template <int QUANT> __device__ __forceinline__ u32x2 codes_of(const Raw<true>& r, float amax, float* scale) {
+  constexpr float top = QUANT == SLA2_QUANT_FP8 ? kE4M3Max : kInt8Max;
+  const bool some = amax >= 0x1p-100f && amax < INFINITY;
+  const float by = some ? top / amax : 0.f;
+  *scale = some ? amax / top : amax < INFINITY ? 1.f : NAN;
+  float x[8];
+  unpack8<true>(r, x);
+  u32x2 c;
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    if constexpr (QUANT == SLA2_QUANT_FP8) {
+      int u = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * by, x[4 * i + 1] * by, 0, false);
+      c[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * by, x[4 * i + 3] * by, u, true);
+    } else {
+      unsigned u = 0;
+#pragma unroll
+      for (int e = 0; e < 4; e++) u |= ((unsigned)(int)rintf(x[4 * i + e] * by) & 255u) << 8 * e;
+      c[i] = u;
+    }
+  }
+  if (!some) c = u32x2{0, 0};                            // NaN x 0 is no code
+  return c;
+}
+
+template <int QUANT> __device__ __forceinline__ Raw<true> values_of(u32x2 c, float scale) {
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    if constexpr (QUANT == SLA2_QUANT_FP8) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], true);
+      x[4 * i] = lo[0], x[4 * i + 1] = lo[1], x[4 * i + 2] = hi[0], x[4 * i + 3] = hi[1];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; e++) x[4 * i + e] = (float)((int)(c[i] << (24 - 8 * e)) >> 24);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i++) x[i] *= scale;
+  return pack8<true>(x);
+}
+
+template <int D, int QUANT, bool WRITE>
+__global__ __launch_bounds__(kCacheThreads) void cache_rows_kernel(CacheArgs a) {
+  constexpr int LANES = D / 8, ROWS = kCacheThreads / LANES, ESZ = QUANT == SLA2_QUANT_NONE ? 2 : 1;
+  const int tid = threadIdx.x, lane = tid % kWave, col = 8 * (tid % LANES), h = blockIdx.y;
+  const bool values = blockIdx.z != 0;
+  const int i = blockIdx.x * ROWS + tid / LANES;
+  uint16_t* rows = values ? a.v : a.k;
+  uint16_t* mine = rows + (size_t)h * a.kv_h + (size_t)min(i, a.tokens - 1) * a.kv_t + col;
+  Raw<true> r;
+  if (WRITE) r = load8<true>(mine, 0u);
+  const Place p = place_of(a, i, lane);
+  if (p.page < -1) return;
+  const long long slot = p.page * a.page_stride + h * a.head_stride + p.slot * a.token_stride + col;
+  char* cache = (char*)(values ? a.vc : a.kc) + slot * ESZ;
+  float* scale = nullptr;
+  if constexpr (QUANT != SLA2_QUANT_NONE)
+    scale = (values ? a.vs : a.ks) + (((long long)p.page * a.Hkv + h) << a.page_shift) + p.slot;
+  if constexpr (WRITE) {
+    if constexpr (QUANT == SLA2_QUANT_NONE) {
+      if (p.page >= 0) *(u32x4*)cache = r.a[0];
+    } else {
+      float s;
+      const u32x2 c = codes_of<QUANT>(r, row_amax<LANES>(r), &s);
+      if (p.page >= 0) {
+        *(u32x2*)cache = c;
+        if (col == 0) *scale = s;
+      }
+    }
+  } else {
+    r = zero8<true>();
+    if (p.page >= 0) {
+      if constexpr (QUANT == SLA2_QUANT_NONE) r.a[0] = *(const u32x4*)cache;
+      else r = values_of<QUANT>(*(const u32x2*)cache, *scale);
+    }
+    store8<true>(mine, 0u, r);
+  }
+}
+
+template <bool WRITE> static hipError_t launch_rows(const CacheArgs& a, hipStream_t stream) {
+  if (!a.tokens) return hipSuccess;
+  const int rows = kCacheThreads / (a.d / 8);
+  const dim3 grid((a.tokens + rows - 1) / rows, a.Hkv, 2);
+#define SLA2_ROWS(D)                                                                                                          \
+  (a.quant == SLA2_QUANT_NONE  ? cache_rows_kernel<D, SLA2_QUANT_NONE, WRITE><<<grid, kCacheThreads, 0, stream>>>(a)          \
+   : a.quant == SLA2_QUANT_FP8 ? cache_rows_kernel<D, SLA2_QUANT_FP8, WRITE><<<grid, kCacheThreads, 0, stream>>>(a)           \
+                               : cache_rows_kernel<D, SLA2_QUANT_INT8, WRITE><<<grid, kCacheThreads, 0, stream>>>(a))
+  if (a.d == 128) SLA2_ROWS(128);
+  else SLA2_ROWS(64);
+#undef SLA2_ROWS
+  return hipGetLastError();
+}
+hipError_t launch_cache_write(const CacheArgs& a, hipStream_t stream) { return launch_rows<true>(a, stream); }
+hipError_t launch_cache_read(const CacheArgs& a, hipStream_t stream) { return launch_rows<false>(a, stream); }
+
+}  // namespace sla2

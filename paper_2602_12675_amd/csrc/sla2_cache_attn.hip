@@ -1,0 +1,319 @@
+// Attention of one new token of each sequence over a paged cache of keys and values.
+//
+// Bound by the bytes of the cache, which are read once: a workgroup has a chunk of a sequence's tokens and a key head, with up to 16
+// query heads of its group as the 16 rows of the matrix products, and each of its waves works on blocks of 32 tokens by itself, from
+// registers alone: no operand passes through LDS, no barrier stands in the loop.
+//   S^T = K Q^T (v_mfma_f32_16x16x32_bf16, 16 tokens a product): lane l feeds the token of row l % 16.  Row m of product t is token
+//   8 (m / 4) + 4 t + m % 4 of the block, so that lane l ends with head l % 16 and the scores of the 8 tokens 8 (l / 16) + 0..7: what it
+//   has to feed as P in O = P V.
+//   V: a lane reads D / 16 neighbouring channels of each of the same 8 tokens, whole rows a quarter wave, and turns its 8 x (D / 16)
+//   block in registers (v_perm_b32, two channels of two tokens at a time) into the operands of D / 16 products, the i-th of which has
+//   the channels D / 16 (l % 16) + i.
+// Codes become bf16 exactly; a token's scales multiply its scores and its probability.  Chunks of a sequence are joined by a second kernel.
+#include "cache.h"
+#include "mfma_tiles.h"
+
+namespace sla2 {
+
+constexpr int kDecodeWaves = 4, kDecodeBlock = 32, kMaxChunk = 1024, kHeadRows = 16;
+
+__device__ __forceinline__ float over_quarters_max(float x) {       // lanes l, l ^ 16, l ^ 32, l ^ 48
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return swap_halves_max(fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])));
+}
+__device__ __forceinline__ float over_quarters_sum(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return swap_halves_sum(__builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]));
+}
+
+// N codes (a multiple of 4, N / 4 registers) as N / 2 registers of bf16 pairs
+template <int QUANT, int N> __device__ __forceinline__ void widen(const unsigned (&c)[N / 4], unsigned (&y)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 4; i++) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    bf16x2 lo, hi;
+    if constexpr (QUANT == SLA2_QUANT_FP8) {
+      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], true);
+      lo = bf16x2{(__bf16)a[0], (__bf16)a[1]};
+      hi = bf16x2{(__bf16)b[0], (__bf16)b[1]};
+    } else {
+      lo = bf16x2{(__bf16)(float)((int)(c[i] << 24) >> 24), (__bf16)(float)((int)(c[i] << 16) >> 24)};
+      hi = bf16x2{(__bf16)(float)((int)(c[i] << 8) >> 24), (__bf16)(float)((int)c[i] >> 24)};
+    }
+    y[2 * i] = __builtin_bit_cast(unsigned, lo);
+    y[2 * i + 1] = __builtin_bit_cast(unsigned, hi);
+  }
+}
+template <int BYTES> __device__ __forceinline__ void load_words(const void* p, unsigned (&w)[BYTES / 4]) {
+  if constexpr (BYTES == 16) {
+    const u32x4 x = *(const u32x4*)p;
+    w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
+  } else if constexpr (BYTES == 8) {
+    const u32x2 x = *(const u32x2*)p;
+    w[0] = x[0], w[1] = x[1];
+  } else {
+    w[0] = *(const unsigned*)p;
+  }
+}
+
+template <int D, int QUANT>
+__global__ __launch_bounds__(kDecodeWaves * kWave) void cache_attention_kernel(CacheArgs a) {
+  constexpr int ESZ = QUANT == SLA2_QUANT_NONE ? 2 : 1;
+  constexpr int KE = QUANT == SLA2_QUANT_NONE ? 8 : 16;            // channels of a 16-byte read of a key
+  constexpr int KL = D / (4 * KE), KS = D / 32;                    // reads and products of a key row
+  constexpr int C = D / 16;                                        // channels of a lane's read of a value row
+  __shared__ float part[kDecodeWaves][kHeadRows][D + 4];           // a wave's O, m and l
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave), g = lane / 16, n = lane % 16;
+  const int tiles = (a.group + kHeadRows - 1) / kHeadRows;         // of query heads
+  const int hk = blockIdx.y / tiles, row0 = blockIdx.y % tiles * kHeadRows, rows = min(kHeadRows, a.group - row0);
+  const int b = blockIdx.z;
+  const long long most = (long long)a.max_pages << a.page_shift;
+  const int len = (int)min((long long)max(a.length[b], 0), most);
+  const int begin = blockIdx.x * a.chunk, end = min(len, begin + a.chunk);
+  if (begin >= end && blockIdx.x) return;
+  const int h0 = hk * a.group + row0;                              // first query head
+  // Q as B operand: lane <- head l % 16, the channels that its reads of a key have
+  bf16x8 qf[KS];
+  {
+    const uint16_t* src = a.q + (size_t)b * a.q_b + (size_t)(h0 + min(n, rows - 1)) * a.q_h;
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) {
+      const int c = KE == 8 ? 32 * ks + 8 * g : 64 * (ks / 2) + 16 * g + 8 * (ks % 2);
+      qf[ks] = *reinterpret_cast<const bf16x8*>(src + c);
+    }
+  }
+  // the pages of the chunk, 16 tokens a lane
+  int id = -1;
+  {
+    const long long column = ((long long)begin + 16 * lane) >> a.page_shift;
+    if (begin + 16 * lane < end) id = a.table[b * a.table_stride + column];
+  }
+  f32x4 oacc[C];
+#pragma unroll
+  for (int i = 0; i < C; i++) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = -1e30f, l_run = 0.f;                               // of head l % 16; l: of this lane's tokens
+  const float c1 = kLog2e * a.scale;
+  const char* kc = (const char*)a.kc + hk * a.head_stride * ESZ;
+  const char* vc = (const char*)a.vc + hk * a.head_stride * ESZ;
+  const int slot_mask = (1 << a.page_shift) - 1;
+  for (int t0 = begin + w * kDecodeBlock; t0 < end; t0 += kDecodeWaves * kDecodeBlock) {
+    const int i0 = (t0 - begin) / 16;
+    int p0 = __builtin_amdgcn_readlane(id, i0), p1 = __builtin_amdgcn_readlane(id, i0 + 1);
+    const bool ok0 = p0 >= 0 && p0 < a.pages, ok1 = p1 >= 0 && p1 < a.pages;
+    const bool whole = ok0 && ok1 && t0 + kDecodeBlock <= end;
+    p0 = ok0 ? p0 : 0;
+    p1 = ok1 ? p1 : p0;
+    const int s0 = t0 & slot_mask, s1 = (t0 + 16) & slot_mask;
+    const long long at0 = p0 * a.page_stride + s0 * a.token_stride, at1 = p1 * a.page_stride + s1 * a.token_stride;
+    // ---- requests ----
+    unsigned kw[2][KL][4], vw[8][C * ESZ / 4];
+    const char* krow = kc + (n < 8 ? at0 : at1) * ESZ + 16 * g;    // tokens 8 (n / 4) + .. of the block: 16 a page at least
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int x = 0; x < KL; x++)
+        load_words<16>(krow + (8 * (n / 4 % 2) + 4 * t + n % 4) * a.token_stride * ESZ + 64 * x, kw[t][x]);
+    const char* vrow = vc + (g < 2 ? at0 : at1) * ESZ + C * ESZ * n;
+#pragma unroll
+    for (int j = 0; j < 8; j++) load_words<C * ESZ>(vrow + (8 * (g % 2) + j) * a.token_stride * ESZ, vw[j]);
+    float ks[8], vs[8];
+    if constexpr (QUANT != SLA2_QUANT_NONE) {
+      const long long at = ((((long long)(g < 2 ? p0 : p1) * a.Hkv + hk)) << a.page_shift) + (g < 2 ? s0 : s1) + 8 * (g % 2);
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const f32x4 k4 = *(const f32x4*)(a.ks + at + 4 * x), v4 = *(const f32x4*)(a.vs + at + 4 * x);
+#pragma unroll
+        for (int e = 0; e < 4; e++) ks[4 * x + e] = k4[e], vs[4 * x + e] = v4[e];
+      }
+    }
+    unsigned dead = 0;                                             // tokens of this lane that have no part
+    if (!whole) {
+#pragma unroll
+      for (int j = 0; j < 8; j++)
+        if (t0 + 8 * g + j >= end || !(g < 2 ? ok0 : ok1)) dead |= 1u << j;
+    }
+    // ---- scores ----
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int x = 0; x < KL; x++) {
+        if constexpr (QUANT == SLA2_QUANT_NONE) {
+          const u32x4 k4 = {kw[t][x][0], kw[t][x][1], kw[t][x][2], kw[t][x][3]};
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k4), qf[x], s[t], 0, 0, 0);
+        } else {
+          unsigned y[8];
+          widen<QUANT, 16>(kw[t][x], y);
+          const u32x4 lo = {y[0], y[1], y[2], y[3]}, hi = {y[4], y[5], y[6], y[7]};
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), qf[2 * x], s[t], 0, 0, 0);
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), qf[2 * x + 1], s[t], 0, 0, 0);
+        }
+      }
+    float sc[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      sc[j] = s[j / 4][j % 4];
+      if constexpr (QUANT != SLA2_QUANT_NONE) sc[j] *= ks[j];
+    }
+    if (!whole) {
+#pragma unroll
+      for (int j = 0; j < 8; j++)
+        if (dead >> j & 1) {
+          sc[j] = -INFINITY;
+          if constexpr (QUANT != SLA2_QUANT_NONE) vs[j] = 0.f;
+#pragma unroll
+          for (int x = 0; x < C * ESZ / 4; x++) vw[j][x] = 0;
+        }
+    }
+    // ---- softmax ----
+    float mx = sc[0];
+#pragma unroll
+    for (int j = 1; j < 8; j++) mx = fmaxf(mx, sc[j]);
+    mx = over_quarters_max(mx) * c1;
+    if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {           // the reference is kept while the maximum stays within 2^8 of it
+      const float m_new = fmaxf(m_run, mx), corr = fast_exp2(m_run - m_new);
+      m_run = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        const float cr = __shfl(corr, 4 * g + r);                  // of the head of this accumulator row
+#pragma unroll
+        for (int i = 0; i < C; i++) oacc[i][r] *= cr;
+      }
+    }
+    bf16x8 pf;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      const float p = fast_exp2(sc[j] * c1 - m_run);
+      l_run += p;
+      if constexpr (QUANT == SLA2_QUANT_NONE) pf[j] = (__bf16)p;
+      else pf[j] = (__bf16)(p * vs[j]);
+    }
+    // ---- O += P V ----
+    unsigned vb[8][C / 2];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      if constexpr (QUANT == SLA2_QUANT_NONE) {
+#pragma unroll
+        for (int x = 0; x < C / 2; x++) vb[j][x] = vw[j][x];
+      } else {
+        widen<QUANT, C>(vw[j], vb[j]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < C; i++) {
+      u32x4 v4;
+#pragma unroll
+      for (int x = 0; x < 4; x++)
+        v4[x] = __builtin_amdgcn_perm(vb[2 * x + 1][i / 2], vb[2 * x][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
+      oacc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf, __builtin_bit_cast(bf16x8, v4), oacc[i], 0, 0, 0);
+    }
+  }
+  // ---- the waves' parts ----
+  l_run = over_quarters_sum(l_run);
+  if (g == 0) {
+    part[w][n][D] = m_run;
+    part[w][n][D + 1] = l_run;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; r++)
+    if (4 * g + r < rows) {
+#pragma unroll
+      for (int i = 0; i < C; i++) part[w][4 * g + r][C * n + i] = oacc[i][r];
+    }
+  __syncthreads();
+  for (int idx = tid; idx < rows * (D / 2); idx += kDecodeWaves * kWave) {
+    const int row = idx / (D / 2), c = idx % (D / 2) * 2, h = h0 + row;
+    float m = part[0][row][D];
+#pragma unroll
+    for (int x = 1; x < kDecodeWaves; x++) m = fmaxf(m, part[x][row][D]);
+    float l = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+    for (int x = 0; x < kDecodeWaves; x++) {
+      const float by = fast_exp2(part[x][row][D] - m);
+      l += by * part[x][row][D + 1];
+      o0 += by * part[x][row][c];
+      o1 += by * part[x][row][c + 1];
+    }
+    if (a.chunks > 1) {
+      const size_t at = ((size_t)b * a.H + h) * a.chunks + blockIdx.x;
+      *(float2*)(a.part_o + at * D + c) = make_float2(o0, o1);
+      if (c == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
+    } else {
+      const bool any = l != 0.f;
+      const float inv = any ? 1.f / l : 0.f;
+      typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+      *(bf16x2*)(a.out + (size_t)b * a.out_b + (size_t)h * a.out_h + c) = bf16x2{(__bf16)(any ? o0 * inv : 0.f), (__bf16)(any ? o1 * inv : 0.f)};
+      if (a.lse && c == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
+    }
+  }
+}
+
+// The chunks of one sequence and head: their O, weighted with e^(m - the largest m), over their l, weighted alike.
+constexpr int kJoinWaves = 8;
+template <int D>
+__global__ __launch_bounds__(kJoinWaves * kWave) void cache_join_kernel(CacheArgs a) {
+  constexpr int E = D / kWave;                                     // channels of a lane
+  __shared__ float part[kJoinWaves][D + 1];
+  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, h = blockIdx.x, b = blockIdx.y;
+  const long long most = (long long)a.max_pages << a.page_shift;
+  const int len = (int)min((long long)max(a.length[b], 0), most);
+  const int n = max(1, (len + a.chunk - 1) / a.chunk);             // the first chunk's part is there in any case
+  const size_t at = ((size_t)b * a.H + h) * a.chunks;
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += kWave) m = fmaxf(m, a.part_ml[2 * (at + i)]);
+  m = wave_max(m);
+  float l = 0.f, o[E] = {};
+  for (int i = w; i < n; i += kJoinWaves) {
+    const float2 ml = *(const float2*)(a.part_ml + 2 * (at + i));
+    const float by = fast_exp2(ml.x - m);
+    l += by * ml.y;
+#pragma unroll
+    for (int e = 0; e < E; e++) o[e] += by * a.part_o[(at + i) * D + E * lane + e];
+  }
+#pragma unroll
+  for (int e = 0; e < E; e++) part[w][E * lane + e] = o[e];
+  if (lane == 0) part[w][D] = l;
+  __syncthreads();
+  if (tid >= D) return;
+  float sum = 0.f, total = 0.f;
+#pragma unroll
+  for (int x = 0; x < kJoinWaves; x++) {
+    sum += part[x][tid];
+    total += part[x][D];
+  }
+  const bool any = total != 0.f;
+  const __bf16 r = (__bf16)(any ? sum / total : 0.f);
+  a.out[(size_t)b * a.out_b + (size_t)h * a.out_h + tid] = __builtin_bit_cast(uint16_t, r);
+  if (a.lse && tid == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(total)) * (1.f / kLog2e) : -INFINITY;
+}
+
+// Chunks: as long as two workgroups a CU allow, in steps of 128 tokens.
+void plan_cache_attention(CacheArgs* a) {
+  const long long most = (long long)a->max_pages << a->page_shift;
+  const long long heads = (long long)a->B * a->Hkv * ((a->group + kHeadRows - 1) / kHeadRows);
+  long long chunk = kMaxChunk;
+  while (chunk > 256 && heads * ((most + chunk - 1) / chunk) < 512) chunk /= 2;
+  a->chunk = (int)chunk;
+  a->chunks = (int)((most + chunk - 1) / chunk);
+}
+
+hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t stream) {
+  const dim3 grid(a.chunks, a.Hkv * ((a.group + kHeadRows - 1) / kHeadRows), a.B);
+#define SLA2_DECODE(D)                                                                                                          \
+  (a.quant == SLA2_QUANT_NONE  ? cache_attention_kernel<D, SLA2_QUANT_NONE><<<grid, kDecodeWaves * kWave, 0, stream>>>(a)       \
+   : a.quant == SLA2_QUANT_FP8 ? cache_attention_kernel<D, SLA2_QUANT_FP8><<<grid, kDecodeWaves * kWave, 0, stream>>>(a)        \
+                               : cache_attention_kernel<D, SLA2_QUANT_INT8><<<grid, kDecodeWaves * kWave, 0, stream>>>(a))
+  if (a.d == 128) SLA2_DECODE(128);
+  else SLA2_DECODE(64);
+#undef SLA2_DECODE
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.chunks == 1) return e;
+  const dim3 heads(a.H, a.B);
+  if (a.d == 128) cache_join_kernel<128><<<heads, kJoinWaves * kWave, 0, stream>>>(a);
+  else cache_join_kernel<64><<<heads, kJoinWaves * kWave, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace sla2

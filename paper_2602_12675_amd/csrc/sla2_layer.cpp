@@ -10,74 +10,8 @@
 
 namespace sla2 {
 
-static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// A strided tensor: `inner` neighbouring elements, `dims` times repeated.
-struct View {
-  const void* p;
-  int esz, dims;
-  long long inner, count[3], stride[3];
-  size_t bytes() const {
-    long long n = inner;
-    for (int i = 0; i < dims; i++) n += (count[i] - 1) * stride[i];
-    return (size_t)n * esz;
-  }
-  bool same_layout(const View& o) const {
-    if (esz != o.esz || inner != o.inner || dims != o.dims) return false;
-    for (int i = 0; i < dims; i++)
-      if (count[i] != o.count[i] || (count[i] > 1 && stride[i] != o.stride[i])) return false;
-    return true;
-  }
-};
-static View flat(const void* p, int esz, long long n) { return View{p, esz, 0, n, {}, {}}; }
-
-// Whether two tensors may share an element.  Slices of one buffer, of the same layout, interleave: they are apart if at one of the
-// strides they are, what that stride repeats being the smaller ones' extent.
-static bool may_meet(const View& a, const View& b) {
-  if (!a.p || !b.p || !overlaps(a.p, a.bytes(), b.p, b.bytes())) return false;
-  if (!a.same_layout(b)) return true;
-  for (int k = 0; k < a.dims; k++) {
-    if (a.count[k] == 1) continue;
-    long long extent = a.inner;
-    bool multiple = true;
-    for (int i = 0; i < a.dims; i++) {
-      if (i == k || a.count[i] == 1) continue;
-      if (a.stride[i] < a.stride[k]) extent += (a.count[i] - 1) * a.stride[i];
-      else multiple = multiple && a.stride[i] % a.stride[k] == 0;
-    }
-    if (multiple && stretches_disjoint(a.p, b.p, a.esz, a.stride[k], extent)) return false;
-  }
-  return true;
-}
-
-struct Output {
-  View v;
-  const void* in_place[2];                   // the inputs that it may be, where these have its layout
-};
-// No output on an input, unless it is that input as a whole and may be, and none on another output.  A workspace is an output.
-static bool aliased(const Output* out, int outs, const View* in, int ins) {
-  for (int i = 0; i < outs; i++) {
-    const Output& o = out[i];
-    for (int j = 0; j < ins; j++) {
-      if (!may_meet(o.v, in[j])) continue;
-      const bool whole = o.v.p == in[j].p && o.v.same_layout(in[j]) && (o.v.p == o.in_place[0] || o.v.p == o.in_place[1]);
-      if (!whole) return true;
-    }
-    for (int j = 0; j < i; j++)
-      if (may_meet(o.v, out[j].v)) return true;
-  }
-  return false;
-}
-
 static bool eps_ok(float eps) { return eps >= FLT_MIN && eps <= FLT_MAX; }      // not NaN, nothing that the root would take for 0
 static bool vector_ok(const float* p) { return !misaligned16(p); }        // null too
-
-// Sum of (count - 1) stride + inner as 128 bits: whether it can be an extent in memory.
-static bool extent_ok(int dims, const long long* count, const long long* stride, long long inner) {
-  __int128 n = inner;
-  for (int i = 0; i < dims; i++) n += (__int128)(count[i] - 1) * stride[i];
-  return n < ((__int128)1 << 60);
-}
 
 static int make_rope(const sla2_rope_params* p, bool backward, int tensors, RopeArgs* a) {
   if (!p) return SLA2_EINVAL;
@@ -198,10 +132,6 @@ static View mod_view(const NormArgs& a, const void* p) {
   return View{p, 4, 2, a.C, {a.B, a.mods == SLA2_MOD_TOKEN ? a.N : 1}, {a.mod_b, a.mod_n}};
 }
 static size_t norm_partial_bytes(const NormArgs& a) { return (size_t)3 * a.B * a.walkers * a.C * sizeof(float); }
-
-static int check_workspace(size_t need, const void* ws, size_t bytes) {
-  return !ws || ((uintptr_t)ws & 255) || bytes < need ? SLA2_EWORKSPACE : SLA2_OK;
-}
 
 }  // namespace sla2
 

@@ -1,0 +1,339 @@
+"""sla2_cache_write, sla2_cache_read (bit for bit) and sla2_cache_attention (bounds of stream_helpers) against the fp64 oracle."""
+import numpy as np
+import pytest
+
+import stream_oracle as S
+from paper_2602_12675_amd import workloads as W
+from stream_helpers import close, dev, f64, lse_bound, out_bound, rows_like, starts, weight_error
+
+pytestmark = pytest.mark.gpu
+QUANTS = ["none", "fp8", "int8"]
+
+
+def stored(quant):
+    import torch
+    return {"none": torch.bfloat16, "fp8": torch.float8_e4m3fn, "int8": torch.int8}[quant]
+
+
+class Cache:
+    """Pages with guards in front and behind, in one of three orders."""
+
+    def __init__(self, pages, Hkv, page, d, quant, order="heads"):
+        import torch
+        self.quant, self.pages, self.page, self.Hkv, self.d = quant, pages, page, Hkv, d
+        esz = 2 if quant == "none" else 1
+        shape = {"heads": (pages, Hkv, page, d), "tokens": (pages, page, Hkv, d), "joint": (pages, 2, Hkv, page, d)}[order]
+        self.raw = [torch.full((int(np.prod(shape)) * esz + 512,), 0x77, dtype=torch.uint8, device="cuda") for _ in range(1 if order == "joint" else 2)]
+        t = [r[256:-256].view(stored(quant)).view(shape) for r in self.raw]
+        if order == "joint":
+            self.kv = [t[0][:, 0], t[0][:, 1]]
+        else:
+            self.kv = t if order == "heads" else [x.transpose(1, 2) for x in t]
+        self.stride = {"heads": None, "tokens": (page * Hkv * d, d, Hkv * d), "joint": (2 * Hkv * page * d, page * d, d)}[order]
+        self.scale = [None, None] if quant == "none" else [torch.full((pages, Hkv, page), 7.0, device="cuda") for _ in range(2)]
+
+    def guards(self):
+        for r in self.raw:
+            assert bool((r[:256] == 0x77).all()) and bool((r[-256:] == 0x77).all())
+
+    def values(self, x):
+        """What is stored, fp64 [pages, Hkv, page, d]: codes, and scales"""
+        t = self.kv[x].float().cpu().numpy()
+        return t, None if self.quant == "none" else self.scale[x].cpu().numpy()
+
+    def fill(self, gen):
+        """Random codes and scales, without passing through the library."""
+        import torch
+        for x in range(2):
+            y = torch.randn((self.pages, self.Hkv, self.page, self.d), generator=gen, device="cuda")
+            if self.quant == "none":
+                self.kv[x].copy_(y.bfloat16())
+            else:
+                self.kv[x].copy_((30 * y).clamp(-127, 127).round().to(torch.int8) if self.quant == "int8" else (100 * y).clamp(-448, 448).to(stored("fp8")))
+                self.scale[x].copy_(torch.rand((self.pages, self.Hkv, self.page), generator=gen, device="cuda") * (0.02 if self.quant == "int8" else 0.006) + 0.005)
+
+
+def tables(rng, lengths, page, extra=2, wide=0):
+    """int32 [B, columns], pages in any order; unused columns hold what must not be looked at"""
+    need = [-(-n // page) for n in lengths]
+    ids, cols, at = rng.permutation(sum(need) + extra), max(max(need), 1) + wide, 0
+    t = np.full((len(lengths), cols), 2 ** 30, dtype=np.int32)
+    for b, n in enumerate(need):
+        t[b, :n] = ids[at:at + n]
+        at += n
+    return t, sum(need) + extra
+
+
+def params(c, B, H, cols, tokens=0, **kw):
+    from paper_2602_12675_amd import api
+    q = {"none": api.SLA2_QUANT_NONE, "fp8": api.SLA2_QUANT_FP8, "int8": api.SLA2_QUANT_INT8}[c.quant]
+    return api.make_cache_params(B, H, c.Hkv, c.d, c.pages, c.page, cols, tokens=tokens, quant_mode=q, cache_stride=c.stride, **kw)
+
+
+def move(quant, d, Hkv, page, lengths, new, order="heads", layout="plain", seed=0, lead=0, behind=0, edit=None, table_edit=None, given=True):
+    """New tokens into a cache and back, both checked bit for bit."""
+    import torch
+    from paper_2602_12675_amd import api
+    rng, gen = np.random.default_rng(seed), torch.Generator(device="cuda").manual_seed(seed)
+    table, pages = tables(rng, lengths, page)
+    if table_edit:
+        table_edit(table)
+    c = Cache(pages, Hkv, page, d, quant, order)
+    T = lead + sum(new) + behind if given else len(new)
+    k, st, _ = rows_like(T, Hkv, d, layout, gen)
+    v, _, _ = rows_like(T, Hkv, d, layout, gen, 30.0)
+    if edit:
+        edit(k, v)
+    start = starts(new, lead) if given else None
+    first = [n - m for n, m in zip(lengths, new)]
+    p = params(c, len(lengths), Hkv, table.shape[1], T, kv_stride=st)
+    tt, ts, tf = dev(table), dev(start) if given else None, dev(first)
+    api.sla2_cache_write(p, k, v, tt, *c.kv, k_scale=c.scale[0], v_scale=c.scale[1], start=ts, first=tf)
+    torch.cuda.synchronize()
+    want = []
+    for x, rows in enumerate((k, v)):
+        before = Cache(pages, Hkv, page, d, quant, order)
+        codes, scale = before.values(x)
+        new_rows = rows.float().cpu().numpy()
+        cc, ss = (new_rows, None) if quant == "none" else S.code_rows(new_rows, quant)
+        back = np.full(new_rows.shape, 7.0, dtype=np.float32)
+        for i, b, t in S.rows_of(start, first, T, len(lengths)):
+            at = S.place(b, t, table, page, pages)
+            back[i] = 0
+            if at is None:
+                continue
+            codes[at[0], :, at[1]] = cc[i]
+            if quant != "none":
+                scale[at[0], :, at[1]] = ss[i]
+                back[i] = W.bf16_bits_to_f32(W.f32_to_bf16_bits(np.nan_to_num(cc[i] * ss[i][:, None])))
+                back[i][np.isnan(ss[i])] = np.nan
+            else:
+                back[i] = cc[i]
+        got, gs = c.values(x)
+        np.testing.assert_array_equal(got, codes)
+        if quant != "none":
+            np.testing.assert_array_equal(gs, scale)
+        want.append(back)
+    c.guards()
+    k2, _, _ = rows_like(T, Hkv, d, layout)
+    v2, _, _ = rows_like(T, Hkv, d, layout)
+    api.sla2_cache_read(p, *c.kv, tt, k2, v2, k_scale=c.scale[0], v_scale=c.scale[1], start=ts, first=tf)
+    torch.cuda.synchronize()
+    for got, back in zip((k2, v2), want):
+        np.testing.assert_array_equal(got.float().cpu().numpy(), back)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 256])
+def test_write_and_read(quant, d, page):
+    move(quant, d, 2, page, [1, 40, 300, 17], [1, 40, 13, 0])
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("order,layout", [("tokens", "padded"), ("joint", "heads"), ("heads", "padded")])
+def test_orders_of_the_cache(quant, order, layout):
+    move(quant, 128, 3, 32, [70, 5], [33, 5], order, layout, lead=2, behind=3)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_one_token_each(quant):
+    lengths = [1 + 7 * i % 90 for i in range(150)]
+    move(quant, 128, 2, 16, lengths, [1] * 150)
+    move(quant, 64, 2, 16, lengths, [1] * 150, given=False)
+    move(quant, 64, 1, 64, [5], [1], given=False)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_many_sequences(quant):
+    lengths = [i % 7 for i in range(200)]
+    move(quant, 64, 1, 16, lengths, [n if i % 3 else n // 2 for i, n in enumerate(lengths)], lead=1, behind=70)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_pages_that_are_none_and_places_outside(quant):
+    def bad(t):
+        t[0, 1], t[1, 0], t[2, 0] = -1, 2 ** 31 - 1, -2 ** 31
+    move(quant, 128, 2, 16, [50, 20, 5], [50, 7, 5], table_edit=bad)
+    import torch
+    from paper_2602_12675_amd import api
+    c = Cache(4, 1, 16, 64, quant)
+    k, _, _ = rows_like(10, 1, 64, "plain", torch.Generator(device="cuda").manual_seed(1))
+    p = params(c, 2, 1, 2, 10)
+    t, s = dev([[0, 1], [2, 3]]), dev([0, 4, 10])
+    before = [x.clone() for x in c.kv]
+    for first in ([-4, 32], [2 ** 31 - 1, -2 ** 31], [100, 1 << 20]):
+        back = torch.ones_like(k)
+        api.sla2_cache_write(p, k, k, t, *c.kv, k_scale=c.scale[0], v_scale=c.scale[1], start=s, first=dev(first))
+        api.sla2_cache_read(p, *c.kv, t, back, back.clone(), k_scale=c.scale[0], v_scale=c.scale[1], start=s, first=dev(first))
+        assert not bool(back.any())
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(c.kv, before))
+    c.guards()
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_rows_of_zeros_tiny_numbers_and_what_is_not_finite(quant):
+    import torch
+
+    def edit(k, v):
+        k[0], k[1], k[2] = 0.0, 2.0 ** -101, 2.0 ** -99
+        k[3, :, 5], k[4, :, 0], k[5, :, -1] = float("nan"), float("inf"), -float("inf")
+        k[6], k[7] = 3.0e38, 0.0
+        k[7, :, 9] = -1.0
+        k[8] = torch.linspace(-127, 127, 64, device="cuda").bfloat16()
+    if quant == "none":
+        pytest.skip("copied as they are: test_write_and_read")
+    move(quant, 64, 2, 16, [12], [12], edit=edit)
+
+
+def attend(quant, d, H, Hkv, page, lengths, order="heads", seed=0, scale=0.0, wide=0, table_edit=None, cache_edit=None, q_layout="plain", lse=True,
+           table_room=0):
+    import torch
+    from paper_2602_12675_amd import api
+    rng, gen = np.random.default_rng(seed), torch.Generator(device="cuda").manual_seed(seed)
+    table, pages = tables(rng, [max(n, 0) for n in lengths], page, wide=wide)
+    if table_edit:
+        table_edit(table)
+    c = Cache(pages, Hkv, page, d, quant, order)
+    c.fill(gen)
+    B, cols = table.shape
+    if cache_edit:
+        cache_edit(c, table)
+    q, sq, _ = rows_like(B, H, d, q_layout, gen)
+    out, so, obuf = rows_like(B, H, d, q_layout)
+    p = params(c, B, H, cols, scale=scale, q_stride=sq, out_stride=so, table_stride=cols + table_room if table_room else 0)
+    tt = dev(np.pad(table, ((0, 0), (0, table_room)), constant_values=-9))
+    ws = torch.empty(api.sla2_cache_workspace_bytes(p), dtype=torch.uint8, device="cuda").fill_(255)
+    L = torch.full((B, H), 7.0, device="cuda") if lse else None
+    tl = dev(lengths)
+    args = (p, q, *c.kv, tt[:, :cols], tl, out)
+    kw = dict(k_scale=c.scale[0], v_scale=c.scale[1], lse=L, workspace=ws)
+    api.sla2_cache_attention(*args, **kw)
+    torch.cuda.synchronize()
+    real, vals = scale or d ** -0.5, []
+    for x in range(2):
+        codes, s = c.values(x)
+        vals.append(codes.astype(np.float64) * (1 if s is None else s.astype(np.float64)[..., None]))
+    ref, mag, rl, sm = np.zeros((B, H, d)), np.zeros((B, H, d)), np.zeros((B, H)), np.zeros((B, H))
+    qn = f64(q)
+    for b, n in enumerate(lengths):
+        at = [S.place(b, t, table, page, pages) for t in range(min(max(n, 0), cols * page))]
+        at = [x for x in at if x is not None]
+        pg, sl = [x[0] for x in at], [x[1] for x in at]
+        for h in range(H):
+            k, v = (vals[x][pg, h // (H // Hkv), sl].reshape(-1, d) for x in range(2))
+            o, l_, m_, s_ = S.attend(qn[b, h][None], k, v, np.ones((1, len(at)), dtype=bool), real)
+            ref[b, h], rl[b, h], mag[b, h], sm[b, h] = o[0], l_[0], m_[0], s_[0]
+    r = weight_error(d, max(max(lengths), 1), sm)
+    close(out, ref, out_bound(ref, mag, r[..., None]), "out")
+    if lse:
+        close(L, rl, lse_bound(rl, r), "lse")
+    first = out.clone()
+    ws.random_(0, 255)
+    api.sla2_cache_attention(*args, **kw)                          # the same bits, whatever the workspace holds
+    assert torch.equal(first, out)
+    return c
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 32, 256])
+def test_attention(quant, d, page):
+    attend(quant, d, 4, 2, page, [1, 15, 16, 17, 31, 33, 0, 64, 129, 300], seed=page)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("heads", [(1, 1), (16, 1), (7, 1), (17, 1), (40, 2), (6, 6)])
+def test_attention_of_groups(quant, heads):
+    attend(quant, 128 if heads[0] < 20 else 64, *heads, 64, [77, 3], order="tokens", seed=2)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("lengths", [[3001], [1023, 1024, 1025, 0, 2100], [255, 256, 257, 4500]])
+def test_attention_in_chunks(quant, lengths):
+    attend(quant, 128, 2, 1, 64, lengths, order="joint", seed=5, q_layout="padded")
+    attend(quant, 64, 3, 3, 16, lengths, seed=6, wide=40, lse=False, table_room=3)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_attention_over_pages_that_are_none(quant):
+    def bad(t):
+        t[0, 0], t[0, 2], t[1, 0], t[1, 1] = -1, 2 ** 31 - 1, -2 ** 31, 2 ** 30
+    attend(quant, 128, 4, 2, 16, [70, 20, 9], table_edit=bad)
+    attend(quant, 64, 4, 2, 64, [300, 100, 9], table_edit=bad)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_attention_does_not_see_what_lies_behind(quant):
+    def dirt(c, table):
+        for b, n in enumerate((70, 33, 1)):
+            last, slot = int(table[b, (n - 1) // 32]), n % 32
+            for x in range(2):
+                if slot:
+                    if quant == "none":
+                        c.kv[x][last, :, slot:] = float("nan")
+                    else:
+                        c.scale[x][last, :, slot:] = float("nan")
+                        if quant == "fp8":
+                            c.kv[x][last, :, slot:] = float("nan")
+    attend(quant, 128, 4, 2, 32, [70, 33, 1], cache_edit=dirt)
+
+
+def test_attention_lengths_that_do_not_fit():
+    """A negative length is 0, one past the page table ends with it."""
+    attend("fp8", 64, 2, 1, 16, [-5, 40, -2 ** 31])
+    import torch
+    from paper_2602_12675_amd import api
+    c = Cache(3, 1, 16, 64, "none")
+    c.fill(torch.Generator(device="cuda").manual_seed(3))
+    p = params(c, 1, 1, 3)
+    q = torch.randn(1, 1, 64, device="cuda").bfloat16()
+    ws = torch.empty(api.sla2_cache_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    got = []
+    for n in (48, 49, 2 ** 31 - 1):
+        out = torch.zeros_like(q)
+        api.sla2_cache_attention(p, q, *c.kv, dev([[2, 0, 1]]), dev([n]), out, workspace=ws)
+        got.append(out)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2]) and bool(got[0].any())
+
+
+def test_attention_scale_in_place_and_shared_pages():
+    import torch
+    from paper_2602_12675_amd import api
+    attend("int8", 128, 4, 1, 16, [200, 3], scale=0.9)
+    c = Cache(2, 1, 64, 64, "fp8")
+    c.fill(torch.Generator(device="cuda").manual_seed(4))
+    p = params(c, 3, 2, 1)
+    q = torch.randn(1, 2, 64, device="cuda").bfloat16().expand(3, 2, 64).contiguous()
+    out = torch.zeros_like(q)
+    ws = torch.empty(api.sla2_cache_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    args = (*c.kv, dev([[1], [1], [0]]), dev([50, 50, 50]))
+    kw = dict(k_scale=c.scale[0], v_scale=c.scale[1], workspace=ws)
+    api.sla2_cache_attention(p, q, *args, out, **kw)               # a page of two sequences is read by both
+    assert torch.equal(out[0], out[1]) and not torch.equal(out[0], out[2])
+    api.sla2_cache_attention(p, q, *args, q, **kw)                 # out may be q
+    assert torch.equal(q, out)
+
+
+def test_offsets_past_32_bits():
+    """A cache of 5 GB of keys: tokens in its last pages."""
+    import torch
+    from paper_2602_12675_amd import api
+    page, Hkv, d, pages = 256, 8, 128, 9000
+    c = Cache(pages, Hkv, page, d, "none")
+    assert c.kv[0].numel() > 2 ** 31
+    table = dev([[pages - 1, 0, pages - 2]])
+    k, _, _ = rows_like(600, Hkv, d, "plain", torch.Generator(device="cuda").manual_seed(5))
+    p = params(c, 1, Hkv, 3, 600)
+    s = dev([0, 600])
+    api.sla2_cache_write(p, k, k, table, *c.kv, start=s)
+    back = torch.zeros_like(k)
+    api.sla2_cache_read(p, *c.kv, table, back, torch.zeros_like(k), start=s)
+    assert torch.equal(back, k) and torch.equal(c.kv[0][pages - 1, 3, 7], k[7, 3]) and torch.equal(c.kv[1][pages - 2, 5, 80], k[592, 5])
+    q = torch.randn(1, Hkv, d, device="cuda").bfloat16()
+    out, ws = torch.zeros_like(q), torch.empty(api.sla2_cache_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    api.sla2_cache_attention(p, q, *c.kv, table, dev([600]), out, workspace=ws)
+    kn = f64(k)
+    for h in range(Hkv):
+        o, _, m, sm = S.attend(f64(q)[0, h][None], kn[:, h], kn[:, h], np.ones((1, 600), dtype=bool), d ** -0.5)
+        close(out[0, h][None], o, out_bound(o, m, weight_error(d, 600, sm)[:, None]))

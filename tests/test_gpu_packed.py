@@ -1,0 +1,200 @@
+"""sla2_packed_forward and sla2_packed_backward against the fp64 oracle, element by element, with the bounds of stream_helpers."""
+import numpy as np
+import pytest
+
+import stream_oracle as S
+from stream_helpers import HALF, UNIT, close, dev, f64, guards_ok, lse_bound, out_bound, rows_like, starts, tiny, weight_error
+
+pytestmark = pytest.mark.gpu
+
+
+def run(lens_q, lens_k, H, Hkv, d, causal, layout="plain", scale=0.0, seed=0, lead=0, behind=0, edit=None, by=1.0, backward=True):
+    """A forward and a backward call, checked.  lead, behind: rows in front of the first and behind the last sequence."""
+    import torch
+    from paper_2602_12675_amd import api
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    Tq, Tk = lead + sum(lens_q) + behind, lead + sum(lens_k) + behind
+    q, sq, _ = rows_like(Tq, H, d, layout, gen, by)
+    k, sk, _ = rows_like(Tk, Hkv, d, layout, gen)
+    v, _, _ = rows_like(Tk, Hkv, d, layout, gen)
+    out, so, obuf = rows_like(Tq, H, d, layout)
+    dout, _, _ = rows_like(Tq, H, d, layout, gen)
+    lse = torch.full((H, Tq), 7.0, device="cuda")
+    qs, ks = starts(lens_q, lead), starts(lens_k, lead)
+    if edit:
+        edit(q, k, v, dout, qs, ks)
+    p = api.make_packed_params(len(lens_q), Tq, Tk, H, Hkv, d, causal=causal, scale=scale, q_stride=sq, kv_stride=sk, out_stride=so)
+    tqs, tks = dev(qs), dev(ks)
+    ws = torch.empty(api.sla2_packed_workspace_bytes(p, True), dtype=torch.uint8, device="cuda").fill_(255)
+    api.sla2_packed_forward(p, q, k, v, tqs, tks, out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    real = scale or d ** -0.5
+    ref = S.packed_forward(f64(q), f64(k), f64(v), qs, ks, causal, real)
+    inside = ~np.isnan(ref["out"][:, 0, 0])
+    n = max(lens_k) if lens_k else 0
+    r = weight_error(d, n, ref["smag"])                            # [H, Tq]
+    close(out[dev(inside, torch.bool)], ref["out"][inside], out_bound(ref["out"], ref["mag"], r.T[..., None])[inside], "out")
+    close(lse[:, dev(inside, torch.bool)], ref["lse"][:, inside], lse_bound(ref["lse"], r)[:, inside], "lse")
+    assert bool((out[dev(~inside, torch.bool)] == 7).all()) and bool((lse[:, dev(~inside, torch.bool)] == 7).all())
+    guards_ok(layout, obuf, H, d)
+    if not backward:
+        return p, (q, k, v, tqs, tks, out, lse, dout), ref
+    dq, _, qbuf = rows_like(Tq, H, d, layout)
+    dk, _, kbuf = rows_like(Tk, Hkv, d, layout)
+    dv, _, vbuf = rows_like(Tk, Hkv, d, layout)
+    ws.fill_(255)
+    api.sla2_packed_backward(p, q, k, v, tqs, tks, out, lse, dout, dq, dk, dv, workspace=ws)
+    torch.cuda.synchronize()
+    b = S.packed_backward(f64(q), f64(k), f64(v), qs, ks, causal, real, f64(out), f64(lse), f64(dout))
+    rows = (H // Hkv) * max(lens_q + [0])
+    e = weight_error(d, max(rows, n), b["smag"])
+    for name, got, member in (("dq", dq, qs), ("dk", dk, ks), ("dv", dv, ks)):
+        sel = slice(member[0], member[-1])
+        small = b[name + "_small"][sel] if name != "dv" else 0.0
+        bound = HALF * np.abs(b[name][sel]) + (1 + HALF) * ((HALF + e) * b[name + "_mag"][sel] + UNIT * (d + 8) * small) + tiny(max(rows, n), f64(k if name == "dq" else q if name == "dk" else dout))
+        close(got[sel], b[name][sel], bound, name)
+        assert bool((got[:member[0]] == 7).all()) and bool((got[member[-1]:] == 7).all()), name
+    guards_ok(layout, qbuf, H, d)
+    guards_ok(layout, kbuf, Hkv, d)
+    guards_ok(layout, vbuf, Hkv, d)
+    return p, (q, k, v, tqs, tks, out, lse, dout, dq, dk, dv), ref
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 2, 31, 63, 64, 65, 127, 128, 129, 257, 300])
+def test_lengths(n, d, causal):
+    run([n], [n], 2, 1, d, causal, seed=n)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [([5, 1, 200, 33], [5, 1, 200, 33]), ([1, 3, 40], [300, 64, 129]), ([130, 70, 5], [3, 1, 64]),
+                                  ([7, 0, 9], [7, 12, 0]), ([0, 0, 3], [0, 4, 3]), ([64, 129], [0, 0])])
+def test_packed_sequences(lens, d, causal):
+    run(*lens, 3, 3, d, causal)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads", [(8, 1), (6, 2), (5, 5), (20, 1)])
+@pytest.mark.parametrize("layout", ["plain", "padded", "heads"])
+def test_groups_and_layouts(heads, layout, causal):
+    run([70, 2, 131], [90, 2, 131], *heads, 64 if heads[0] > 8 else 128, causal, layout, seed=4)
+
+
+def test_rows_outside_of_sequences_are_left():
+    run([9, 130], [70, 3], 2, 2, 128, False, lead=3, behind=5)
+    run([9, 130], [9, 130], 2, 1, 64, True, lead=130, behind=200)
+
+
+def test_many_short_sequences():
+    lens = [(7 * i) % 5 for i in range(150)]
+    run(lens, lens, 2, 1, 64, True)
+    run(lens, [(3 * i) % 4 for i in range(150)], 1, 1, 128, False)
+
+
+def test_scale_and_large_scores():
+    run([65], [130], 2, 2, 64, False, scale=0.7)
+    run([65], [130], 2, 1, 128, True, scale=1.5, by=4.0)           # rows of one weight; references that move by thousands
+
+
+def test_keys_rise_along_the_sequence():
+    """The running maximum moves at every step."""
+    def edit(q, k, v, dout, qs, ks):
+        import torch
+        q.fill_(1.0)
+        k.copy_((torch.arange(k.shape[0], device="cuda")[:, None, None] * 0.05).expand_as(k))
+    run([33], [400], 1, 1, 64, False, edit=edit)
+    run([400], [400], 1, 1, 128, True, edit=edit)
+
+
+def test_what_is_not_finite_stays_in_its_sequence():
+    def edit(q, k, v, dout, qs, ks):
+        k[ks[1]:ks[2], 0, 3] = float("nan")
+        v[ks[1]:ks[2], 0, 5] = float("inf")
+        q[qs[1]:qs[2]] = float("nan")
+        dout[qs[1]:qs[2]] = float("nan")
+    import torch
+    from paper_2602_12675_amd import api
+    for lens, causal in (([40, 30, 50], False), ([64, 64, 64], True), ([1, 1, 1], False)):
+        clean = run(lens, lens, 2, 1, 64, causal, seed=9)[1]
+        with_nan = [t.clone() for t in clean[:3]] + [clean[7].clone()]
+        q, k, v, dout = with_nan
+        qs = starts(lens)
+        edit(q, k, v, dout, qs, qs)
+        p = api.make_packed_params(3, sum(lens), sum(lens), 2, 1, 64, causal=causal)
+        ws = torch.empty(api.sla2_packed_workspace_bytes(p, True), dtype=torch.uint8, device="cuda")
+        out, lse = torch.zeros_like(clean[5]), torch.zeros_like(clean[6])
+        api.sla2_packed_forward(p, q, k, v, clean[3], clean[4], out, lse=lse, workspace=ws)
+        keep = torch.ones(sum(lens), dtype=torch.bool, device="cuda")
+        keep[qs[1]:qs[2]] = False
+        assert torch.equal(out[keep], clean[5][keep]) and torch.equal(lse[:, keep], clean[6][:, keep])
+        assert bool(torch.isnan(out[~keep]).any())
+        dq, dk, dv = (torch.zeros_like(t) for t in clean[8:11])
+        api.sla2_packed_backward(p, q, k, v, clean[3], clean[4], out, lse, dout, dq, dk, dv, workspace=ws)
+        for got, want in zip((dq, dk, dv), clean[8:11]):
+            assert torch.equal(got[keep], want[keep]) and bool(torch.isnan(got[~keep]).any())
+
+
+def test_offsets_that_do_not_fit_stay_inside():
+    """Descending, negative and too large offsets: each sequence is what is left of it inside the tensors."""
+    import torch
+    from paper_2602_12675_amd import api
+    q, k, v = (torch.randn(100, 1, 64, device="cuda").bfloat16() for _ in range(3))
+    buf = torch.full((140, 1, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[20:120]
+    p = api.make_packed_params(3, 100, 100, 1, 1, 64)
+    ws = torch.empty(api.sla2_packed_workspace_bytes(p, True), dtype=torch.uint8, device="cuda")
+    lse = torch.zeros(1, 100, device="cuda")
+    for qs in ([-5, 20, 10, 400], [90, 50, 2 ** 31 - 1, -2 ** 31], [0, 200, 300, 400]):
+        api.sla2_packed_forward(p, q, k, v, dev(qs), dev(qs), out, lse=lse, workspace=ws)
+        dq, dk, dv = (torch.zeros_like(q) for _ in range(3))
+        api.sla2_packed_backward(p, q, k, v, dev(qs), dev(qs), out, lse, q, dq, dk, dv, workspace=ws)
+        torch.cuda.synchronize()
+        assert bool((buf[:20] == 7).all()) and bool((buf[120:] == 7).all())
+
+
+def test_gradients_in_one_buffer_and_empty_sides():
+    """dq, dk and dv as slices of the gradient of one projection, with other numbers of heads; no queries, no keys."""
+    import torch
+    from paper_2602_12675_amd import api
+    T, H, Hkv, d = 77, 6, 2, 64
+    p, t, _ = run([T], [T], H, Hkv, d, True)
+    q, k, v, qs, ks, out, lse, dout, dq, dk, dv = t
+    row = (H + 2 * Hkv) * d
+    buf = torch.zeros((T, H + 2 * Hkv, d), dtype=torch.bfloat16, device="cuda")
+    qkv = torch.cat([q, k, v], 1)
+    p2 = api.make_packed_params(1, T, T, H, Hkv, d, causal=True, q_stride=(d, row), kv_stride=(d, row))
+    ws = torch.empty(api.sla2_packed_workspace_bytes(p2, True), dtype=torch.uint8, device="cuda")
+    api.sla2_packed_backward(p2, qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:], qs, ks, out, lse, dout, buf[:, :H], buf[:, H:H + Hkv],
+                             buf[:, H + Hkv:], workspace=ws)
+    assert torch.equal(buf, torch.cat([dq, dk, dv], 1))
+    none, zero = torch.empty((0, H, d), dtype=torch.bfloat16, device="cuda"), dev([0, 0])
+    p3 = api.make_packed_params(1, 0, T, H, Hkv, d)
+    e = torch.empty((H, 0), device="cuda")
+    dk.fill_(1), dv.fill_(1)
+    api.sla2_packed_forward(p3, None, k, v, zero, ks, None, workspace=ws)
+    api.sla2_packed_backward(p3, None, k, v, zero, ks, None, None, None, None, dk, dv, workspace=ws)
+    assert not bool(dk.any()) and not bool(dv.any()) and none.numel() == e.numel() == 0
+    p4 = api.make_packed_params(1, T, 0, H, Hkv, d)
+    ws = torch.empty(api.sla2_packed_workspace_bytes(p4, True), dtype=torch.uint8, device="cuda")
+    api.sla2_packed_forward(p4, q, None, None, qs, zero, out, lse=lse, workspace=ws)
+    assert not bool(out.any()) and bool((lse == -float("inf")).all())
+    api.sla2_packed_backward(p4, q, None, None, qs, zero, out, lse, dout, dq, None, None, workspace=ws)
+    assert not bool(dq.any())
+
+
+@pytest.mark.parametrize("case", [([700], [700], 4, 2, 128, True), ([300, 41], [1500, 900], 2, 2, 64, False), ([9], [5000], 2, 1, 128, False),
+                                  ([1], [3000], 4, 4, 64, True), ([2500], [70], 3, 3, 128, False), ([1200], [1200], 2, 1, 64, True),
+                                  ([5, 900, 1], [5, 2000, 700], 8, 2, 128, True)])
+def test_longer_sequences_and_the_same_bits_twice(case):
+    import torch
+    from paper_2602_12675_amd import api
+    p, t, _ = run(*case)
+    q, k, v, qs, ks, out, lse, dout, dq, dk, dv = t
+    again = [torch.zeros_like(x) for x in (out, lse, dq, dk, dv)]
+    ws = torch.empty(api.sla2_packed_workspace_bytes(p, True), dtype=torch.uint8, device="cuda")
+    api.sla2_packed_forward(p, q, k, v, qs, ks, again[0], lse=again[1], workspace=ws)
+    api.sla2_packed_backward(p, q, k, v, qs, ks, out, lse, dout, *again[2:], workspace=ws)
+    for x, y in zip(again, (out, lse, dq, dk, dv)):
+        assert torch.equal(x, y)
