@@ -389,9 +389,9 @@ int sla2_packed_backward(const sla2_packed_params* params, const void* q, const 
                          void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* The cache: `pages` pages of page_size tokens of every key head.  Token t of sequence b is in page page_table[b][t / page_size], at
- * t % page_size.  SLA2_QUANT_FP8 and SLA2_QUANT_INT8 keep codes with one scale for each token and head, of keys and of values: the rule
- * of sla2_quant with the d channels of a row in the place of its block (amax = max|x|, code = rne(x * (448 or 127 / amax)), scale =
- * amax / 448 or 127, both divisions in fp32).  A row whose amax is below 2^-100 has scale 1 and codes 0; one with a NaN or an infinity
+ * t % page_size.  SLA2_QUANT_FP8 and SLA2_QUANT_INT8 keep codes with one scale for each token and head, of keys and of values: amax =
+ * max|x| over the d channels, code = rne(x (top (1 / amax))), scale = amax (1 / top) with top = 448 or 127, every quotient and product
+ * rounded to fp32.  A row whose amax is below 2^-100 has scale 1 and codes 0; one with a NaN or an infinity
  * has a NaN for its scale and codes 0, and reads back as NaN. */
 typedef struct sla2_cache_params {
   int B;                     /* sequences, 1 .. 65535 */

@@ -92,10 +92,10 @@ def code_rows(x, quant):
     fine = np.isfinite(x).all(-1)
     amax = np.where(fine, np.abs(np.where(np.isfinite(x), x, 0)).max(-1), 0).astype(np.float32)
     some = amax >= np.float32(2.0 ** -100)
-    by = np.where(some, top / np.where(some, amax, 1), 0).astype(np.float32)
+    by = np.where(some, top * (np.float32(1) / np.where(some, amax, np.float32(1))), 0).astype(np.float32)
     y = (np.where(np.isfinite(x), x, 0).astype(np.float32) * by[..., None]).astype(np.float32)
     codes = O.e4m3_round(y.astype(np.float64)).astype(np.float32) if quant == "fp8" else np.rint(y)
-    scale = np.where(some, (np.where(some, amax, 1) / top).astype(np.float32), np.float32(1.0))
+    scale = np.where(some, (np.where(some, amax, np.float32(1)) * (np.float32(1) / top)).astype(np.float32), np.float32(1.0))
     return np.where(fine[..., None], codes, 0).astype(np.float32), np.where(fine, scale, np.float32(np.nan)).astype(np.float32)
 
 

@@ -59,8 +59,8 @@ template <int LANES> __device__ __forceinline__ float row_amax(const Raw<true>& 
 template <int QUANT> __device__ __forceinline__ u32x2 codes_of(const Raw<true>& r, float amax, float* scale) {
   constexpr float top = QUANT == SLA2_QUANT_FP8 ? kE4M3Max : kInt8Max;
   const bool some = amax >= 0x1p-100f && amax < INFINITY;
-  const float by = some ? top / amax : 0.f;
-  *scale = some ? amax / top : amax < INFINITY ? 1.f : NAN;
+  const float by = some ? top * (1.f / amax) : 0.f;
+  *scale = some ? amax * (1.f / top) : amax < INFINITY ? 1.f : NAN;
   float x[8];
   unpack8<true>(r, x);
   u32x2 c;
