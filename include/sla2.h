@@ -361,13 +361,14 @@ typedef struct sla2_packed_params {
                                 all of them; one before the first key none); 0: all of its sequence */
   float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */
   /* (head, token) element strides of q, dq; of k, v, dk, dv; of out, dout.  Both zero: contiguous [tokens, heads, d].  As in
-   * sla2_params; below 2^24 elements a token */
+   * sla2_params; below 2^24 elements a token; tokens_q H, tokens_k H below 2^31 - 1024 */
   long long q_stride[2];
   long long kv_stride[2];
   long long out_stride[2];
 } sla2_packed_params;
 
-/* Bytes of the workspace of sla2_packed_forward (backward = 0) or sla2_packed_backward (1); 0: params are invalid.  Pure host function. */
+/* Bytes of the workspace of sla2_packed_forward (backward = 0), or of sla2_packed_backward and sla2_packed_forward, one after the other
+ * (1); 0: params are invalid.  Pure host function. */
 size_t sla2_packed_workspace_bytes(const sla2_packed_params* params, int backward);
 
 /* out, lse of every query.  Sequence s has the queries q_start[s] .. q_start[s + 1] - 1 and the keys k_start[s] .. k_start[s + 1] - 1.

@@ -1,4 +1,7 @@
 // Attention over packed sequences: what its kernels (sla2_packed.hip, sla2_packed_bwd.hip) share.
+//
+// The queries of a sequence and of all heads of a key head's group are taken as the rows of one matrix, row r being query r / group of
+// head r % group: they read the same keys and values, and with few queries of many heads a tile has no empty rows.
 #pragma once
 #include "mfma_tiles.h"
 
@@ -15,40 +18,45 @@ struct PackedArgs {
   uint16_t *o, *dq, *dk, *dv;
   float* lse_out;
   RowStrides sq, skv, so;
-  int S, Tq, Tk, H, group, d;                // group: query heads of a key head
+  int S, Tq, Tk, H, Hkv, group, d;           // group: query heads of a key head
+  unsigned group_inv;                        // 2^32 / group, rounded up (group > 1)
   bool causal;
   float scale;                               // of the scores
-  // scratch
-  float* delta;                              // backward: [H][Tq], sum of dO . O of a row
+  // The steps of a tile's inner loop are dealt to this many workgroups, whose sums another kernel joins (1: none)
+  int q_parts, k_parts;
+  // scratch.  Rows of all key heads: [Hkv][Tq group]; sums of parts: O or dQ [q_parts][rows][d], (m, l) [q_parts][rows][2], dK and dV
+  // [2][k_parts][Tk][Hkv][d]
+  float *lse2, *delta;                       // backward: lse log2(e) and D of every row
+  float *part_o, *part_ml, *part_kv;
 };
 
+constexpr int kRowTile = 128, kKeyTile = 128;        // rows, and keys, of a workgroup: 32 a wave
+
+void plan_packed(PackedArgs* a, bool backward);
 hipError_t launch_packed_fwd(const PackedArgs& a, hipStream_t stream);
 hipError_t launch_packed_bwd(const PackedArgs& a, hipStream_t stream);
 
 // Tiles of `rows` rows that sequences of `tokens` rows in all have at most.
-inline long long most_tiles(int tokens, int sequences, int rows) {
-  return tokens / rows + (long long)(sequences < tokens ? sequences : tokens);
+inline long long most_tiles(long long tokens, int sequences, int rows) {
+  return tokens / rows + (sequences < tokens ? sequences : tokens);
 }
 
 #ifdef __HIPCC__
-// A sequence: where its queries and keys lie, whatever the offsets hold inside the tensors.
-struct Stretch {
-  int q0, nq, k0, nk;
-};
+// first row and number of rows of a sequence, whatever the offsets hold inside the tensor
 __device__ __forceinline__ int2 stretch_of(const int32_t* start, int s, int tokens) {
   const int a = min(max(start[s], 0), tokens), b = min(max(start[s + 1], a), tokens);
   return make_int2(a, b - a);
 }
 
-// The n-th tile, of `rows` rows, of the sequences one behind the other: its sequence, and its number in it.  A wave looks at 64
-// sequences at a time; all lanes return the same.  s < 0: there are fewer tiles.
+// The n-th tile, of `rows` rows, of the sequences one behind the other, each token being `group` rows: its sequence, its number in it and
+// how many that sequence has.  A wave looks at 64 sequences at a time; all lanes return the same.  s < 0: there are fewer tiles.
 struct TilePlace {
-  int s, tile;
+  int s, tile, tiles;
 };
-__device__ __forceinline__ TilePlace find_tile(const int32_t* start, int S, int tokens, int rows, int n, int lane) {
+__device__ __forceinline__ TilePlace find_tile(const int32_t* start, int S, int tokens, int group, int rows, int n, int lane) {
   for (int s0 = 0; s0 < S; s0 += kWave) {
     const int s = s0 + lane;
-    const int own = s < S ? (stretch_of(start, s, tokens).y + rows - 1) / rows : 0;
+    const int own = s < S ? (int)(((unsigned)stretch_of(start, s, tokens).y * (unsigned)group + rows - 1) / (unsigned)rows) : 0;
     int sum = own;                                     // of the lanes up to this one
 #pragma unroll
     for (int by = 1; by < kWave; by *= 2) {
@@ -58,11 +66,42 @@ __device__ __forceinline__ TilePlace find_tile(const int32_t* start, int S, int 
     const unsigned long long has = __builtin_amdgcn_ballot_w64(sum > n);
     if (has) {
       const int f = __builtin_ctzll(has);
-      return TilePlace{s0 + f, __builtin_amdgcn_readfirstlane(n - __shfl(sum - own, f))};
+      return TilePlace{s0 + f, n - __builtin_amdgcn_readlane(sum - own, f), __builtin_amdgcn_readlane(own, f)};
     }
     n -= __builtin_amdgcn_readlane(sum, kWave - 1);
   }
-  return TilePlace{-1, 0};
+  return TilePlace{-1, 0, 0};
+}
+
+// query and head (inside the group) of a row
+__device__ __forceinline__ int2 query_of(const PackedArgs& a, int row) {
+  if (a.group == 1) return make_int2(row, 0);
+  const int i = row / a.group;
+  return make_int2(i, row - i * a.group);
+}
+// the same for rows below 2^16 and groups up to 2^15: a multiplication
+__device__ __forceinline__ int2 near_query_of(const PackedArgs& a, unsigned row) {
+  const unsigned i = a.group == 1 ? row : __umulhi(row, a.group_inv);
+  return make_int2((int)i, (int)(row - i * (unsigned)a.group));
+}
+
+// Workgroup n of a launch over tiles x key heads: consecutive workgroups go to the XCDs in turn, so that where the heads are a multiple
+// of the XCDs each of these has heads, and their keys and values, of its own.
+struct TileHead {
+  int tile, head;
+};
+__device__ __forceinline__ TileHead tile_head(int n, int heads) { return TileHead{n / heads, n % heads}; }
+
+template <int D> using PackedTile = typename std::conditional<D == 128, SwizzledLayoutB<128>, SwizzledLayout<64>>::type;   // no bank conflicts
+
+// LDS byte offsets of a lane's operand reads inside a 64-row tile, both for the rows 32 h further by 64 h D bytes.
+// Row-wise: row l % 32, channel step ks at (offset of step 0) ^ 32 ks.  Transposing (cf. read_tr4): rows 4 g + (l % 16) / 4 (lo) and 8
+// further (hi), channel tile et at (offset of tile 0) ^ 64 et, 16-row step ks 32 D ks further.
+template <int D> __device__ __forceinline__ unsigned row_read_offset(int lane) {
+  return (unsigned)PackedTile<D>::offset(lane % 32, 8 * (lane / 32)) * 2;
+}
+template <int D> __device__ __forceinline__ unsigned tr_read_offset(int lane, int hi) {
+  return (unsigned)PackedTile<D>::offset(8 * hi + 4 * (lane / 32) + (lane % 16) / 4, 16 * ((lane / 16) % 2) + 4 * (lane % 4)) * 2;
 }
 #endif
 

@@ -1,95 +1,192 @@
 // Forward pass of attention over packed sequences: out = softmax(scale Q K^T) V, lse, with grouped heads and a causal mask.
 //
-// One workgroup = 4 waves = 128 query rows of one head and sequence; a wave has 32 of them, one on lanes l and l + 32.  One pass over
-// the keys, 64 at a time, with the running maximum and sum of the softmax: S^T = K Q^T (keys x rows), so that a lane holds scores of
-// one row, P^T goes back into O^T += V^T P^T as it lies in the registers, and a row's maximum and sum are its lane's own and one
-// exchange with the other half of the wave.
+// One workgroup = 4 waves = 128 rows of one key head and sequence (packed.h); a wave has 32 of them, one on lanes l and l + 32.  One
+// pass over the keys, 64 at a time, with the running maximum and sum of the softmax: S^T = K Q^T (keys x rows), so that a lane holds
+// scores of one row, P^T goes back into O^T += V^T P^T as it lies in the registers, and a row's maximum and sum are its lane's own and
+// one exchange with the other half of the wave.  K and V tiles go from memory into LDS past the registers, one tile ahead; two
+// workgroups share a CU, so that one's products run beside the other's exponentials.
 #include "packed.h"
 
 namespace sla2 {
 
-template <int D>
-__global__ __launch_bounds__(256) void packed_fwd_kernel(PackedArgs a, int heads_first) {
-  constexpr int BQ = 128, NT = 256, KS = D / 16, ET = D / 32;
-  typedef PaddedLayout<D> PL;
-  __shared__ __attribute__((aligned(16))) uint16_t ks_[kTileTokens * PL::kRowElems], vs_[kTileTokens * PL::kRowElems];
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, g = lane / 32;
-  const int h = blockIdx.x % a.H;
-  const TilePlace at = find_tile(a.q_start, a.S, a.Tq, BQ, blockIdx.x / a.H, lane);
+template <int D> struct PackedSmem {
+  static constexpr int kTile = PackedTile<D>::kTileBytes;
+  static constexpr int kLd = D + 8;
+  static constexpr int kBytes = 4 * kTile;                     // two buffers of (K, V); afterwards the output tile [128][D + 8]
+  static_assert(kRowTile * kLd * 2 <= kBytes, "");
+};
+
+template <int D, bool PARTS>
+__global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
+  constexpr int NW = 4, KS = D / 16, ET = D / 32, LD = D + 8;
+  typedef PackedSmem<D> SM;
+  typedef PackedTile<D> SL;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid % kWave, g = lane / 32;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const TileHead th = tile_head(blockIdx.x, a.Hkv);
+  const int hk = th.head;
+  TilePlace at = find_tile(a.q_start, a.S, a.Tq, a.group, kRowTile, th.tile, lane);
   if (at.s < 0) return;
+  if (a.causal) at.tile = at.tiles - 1 - at.tile;      // the longest first
   const int2 qs = stretch_of(a.q_start, at.s, a.Tq), kx = stretch_of(a.k_start, at.s, a.Tk);
-  const int nq = qs.y, nk = kx.y, row0 = at.tile * BQ, row = row0 + 32 * w + lane % 32;
-  const uint16_t* qh = a.q + (size_t)h * a.sq.h + (size_t)qs.x * a.sq.t;
-  const uint16_t* kh = a.k + (size_t)(h / a.group) * a.skv.h + (size_t)kx.x * a.skv.t;
-  const uint16_t* vh = a.v + (size_t)(h / a.group) * a.skv.h + (size_t)kx.x * a.skv.t;
-  const int past = a.causal ? nk - nq : nk;            // row i reads keys below i + past + 1 (causal), all otherwise
-  const int last = min(row0 + BQ, nq);                 // behind the tile's last row
-  const int keys = a.causal ? min(nk, max(0, last + past)) : nk;
-  const int mine = a.causal ? min(nk, row + past + 1) : nk;      // this lane's row: below this
-  bf16x8 qf[KS];
+  const int nr = qs.y * a.group, nk = kx.y, row0 = at.tile * kRowTile, row = row0 + 32 * w + lane % 32;
+  const uint16_t* kh = a.k + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
+  const uint16_t* vh = a.v + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
+  const int past = nk - qs.y;                          // query i reads the keys below i + past + 1 (causal), all otherwise
+  const int2 my = query_of(a, min(row, nr - 1));       // this lane's query and head
+  const int mine = a.causal ? min(nk, my.x + past + 1) : nk;
+  // the keys that the tile, and this wave, have to do with: below ..; and those that all rows of the wave read
+  const int keys = a.causal ? min(nk, max(0, query_of(a, min(row0 + kRowTile, nr) - 1).x + past + 1)) : nk;
+  const int w_row = row0 + 32 * w;
+  const int w_keys = w_row >= nr ? 0 : __builtin_amdgcn_readlane(mine, 31), w_full = __builtin_amdgcn_readfirstlane(mine);
+  int t_begin = 0, t_end = (keys + kTileTokens - 1) / kTileTokens;
+  if (PARTS) {
+    const int n = t_end;
+    t_begin = (int)((long long)n * blockIdx.y / a.q_parts);
+    t_end = (int)((long long)n * (blockIdx.y + 1) / a.q_parts);
+  }
+  auto kbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
+  auto dma = [&](int t) {                              // rows past the end repeat the last one: their scores are masked
+    const int t0 = t * kTileTokens, valid = min(kTileTokens, nk - t0), ln = (int)lane_again();
+    dma_tile<D, NW, SL>(kh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t), w, ln);
+    dma_tile<D, NW, SL>(vh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t) + SM::kTile, w, ln);
+  };
+  if (t_begin < t_end) dma(t_begin);
+  bf16x8 qf[KS];                                       // B operand: lane <- Q[row][16 ks + 8 g + 0..7]
   {
-    const uint16_t* src = qh + (size_t)min(row, nq - 1) * a.sq.t + 8 * g;
+    const uint16_t* src = a.q + (size_t)(hk * a.group + my.y) * a.sq.h + (size_t)(qs.x + my.x) * a.sq.t + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
   }
-  f32x16 oacc[ET];
+  f32x16 oacc[ET], sacc[2];
 #pragma unroll
   for (int et = 0; et < ET; et++)
 #pragma unroll
     for (int e = 0; e < 16; e++) oacc[et][e] = 0.f;
-  float m_run = -1e30f, l_run = 0.f;
+  float m_run = -1e30f, l_run = 0.f;                   // reference of the exponentials and running sum, log2 domain
   const float c1 = kLog2e * a.scale;
-  for (int t0 = 0; t0 < keys; t0 += kTileTokens) {
-    u32x4 r[TileCopy<D, NT>::kLoads], rv[TileCopy<D, NT>::kLoads];
-    TileCopy<D, NT>::load(r, kh + (size_t)t0 * a.skv.t, a.skv.t, min(kTileTokens, nk - t0), tid);
-    TileCopy<D, NT>::load(rv, vh + (size_t)t0 * a.skv.t, a.skv.t, min(kTileTokens, nk - t0), tid);
-    __syncthreads();
-    TileCopy<D, NT>::store(r, ks_, tid);
-    TileCopy<D, NT>::store(rv, vs_, tid);
-    __syncthreads();
-    f32x16 sacc[2];
+  const unsigned k_off = row_read_offset<D>(lane), v_lo = tr_read_offset<D>(lane, 0), v_hi = tr_read_offset<D>(lane, 1);
+  wait_vmcnt<0>();
 #pragma unroll
-    for (int mt = 0; mt < 2; mt++) {
+  for (int ks = 0; ks < KS; ks++) settle(qf[ks]);
+  phase_barrier();
+  for (int t = t_begin; t < t_end; t++) {
+    if (t + 1 < t_end) dma(t + 1);
+    const int t0 = t * kTileTokens;
+    if (t0 < w_keys) {
+      // S^T = K Q^T, two 32-key halves; reads run two steps ahead
+      {
+        const unsigned ka = kbuf(t) + k_off;
+        constexpr int KA = 2;
+        u32x4 kr[KA + 1][2];
 #pragma unroll
-      for (int e = 0; e < 16; e++) sacc[mt][e] = 0.f;
+        for (int ks = 0; ks < KA; ks++) {
+          kr[ks][0] = lds_read16_untracked<0>(ka ^ (32u * ks));
+          kr[ks][1] = lds_read16_untracked<32 * D * 2>(ka ^ (32u * ks));
+        }
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++)
-        sacc[mt] = mfma_bf16(row_fragment<PL>(ks_, 32 * mt + lane % 32, 16 * ks + 8 * g), qf[ks], sacc[mt]);
-    }
-    float mx = -INFINITY;
+        for (int mt = 0; mt < 2; mt++)
 #pragma unroll
-    for (int mt = 0; mt < 2; mt++)
+          for (int e = 0; e < 16; e++) sacc[mt][e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        if (t0 + 32 * mt + 8 * (e / 4) + 4 * g + e % 4 >= mine) sacc[mt][e] = -INFINITY;
-        mx = fmaxf(mx, sacc[mt][e]);
+        for (int ks = 0; ks < KS; ks++) {
+          if (ks + KA < KS) {
+            kr[(ks + KA) % (KA + 1)][0] = lds_read16_untracked<0>(ka ^ (32u * (ks + KA)));
+            kr[(ks + KA) % (KA + 1)][1] = lds_read16_untracked<32 * D * 2>(ka ^ (32u * (ks + KA)));
+          }
+          const int ahead = KS - 1 - ks < KA ? KS - 1 - ks : KA;
+#pragma unroll
+          for (int mt = 0; mt < 2; mt++) {
+            wait_lgkmcnt(2 * ahead + 1 - mt);
+            settle(kr[ks % (KA + 1)][mt]);
+            sacc[mt] = mfma_bf16(__builtin_bit_cast(bf16x8, kr[ks % (KA + 1)][mt]), qf[ks], sacc[mt]);
+          }
+        }
       }
-    mx = swap_halves_max(mx) * c1;
-    const float m_new = fmaxf(m_run, mx), corr = fast_exp2(m_run - m_new);
-    m_run = m_new;
-    float rs = 0.f;
-    bf16x8 pf[4];
+      if (t0 + kTileTokens > w_full) {
 #pragma unroll
-    for (int mt = 0; mt < 2; mt++)
+        for (int mt = 0; mt < 2; mt++)
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        const float p = fast_exp2(sacc[mt][e] * c1 - m_new);
-        rs += p;
-        pf[2 * mt + e / 8][e % 8] = (__bf16)p;
+          for (int e = 0; e < 16; e++)
+            if (t0 + 32 * mt + 8 * (e / 4) + 4 * g + e % 4 >= mine) sacc[mt][e] = -INFINITY;
       }
-    l_run = l_run * corr + swap_halves_sum(rs);
+      bf16x8 pf[4];
+      {
+        float mx = -INFINITY;
 #pragma unroll
-    for (int et = 0; et < ET; et++) {
+        for (int mt = 0; mt < 2; mt++)
 #pragma unroll
-      for (int e = 0; e < 16; e++) oacc[et][e] *= corr;
+          for (int e = 0; e < 16; e++) mx = fmaxf(mx, sacc[mt][e]);
+        mx = swap_halves_max(mx) * c1;
+        // the reference is kept while the row maximum stays within 2^8 of it (decided for the whole wave)
+        const bool rescale = __builtin_amdgcn_ballot_w64(mx > m_run + 8.f) != 0;
+        const float m_new = rescale ? fmaxf(m_run, mx) : m_run;
+        float rs = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < 4; ks++) oacc[et] = mfma_bf16(v_fragment<PL>(vs_, ks, 32 * et, lane), pf[ks], oacc[et]);
+        for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            const float p0 = fast_exp2(sacc[mt][e] * c1 - m_new), p1 = fast_exp2(sacc[mt][e + 1] * c1 - m_new);
+            rs += p0 + p1;
+            pf[2 * mt + e / 8][e % 8] = (__bf16)p0;
+            pf[2 * mt + e / 8][e % 8 + 1] = (__bf16)p1;
+          }
+        if (rescale) {
+          const float corr = fast_exp2(m_run - m_new);   // 0 on the first tile
+          l_run *= corr;
+          m_run = m_new;
+#pragma unroll
+          for (int et = 0; et < ET; et++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) oacc[et][e] *= corr;
+        }
+        l_run += swap_halves_sum(rs);
+      }
+      // O^T += V^T P^T: fragment (ks, et) = two transposing reads, kept three fragments ahead of the products
+      {
+        constexpr int kAhead = 3, kFrags = (kTileTokens / 16) * ET;
+        const unsigned va_lo = kbuf(t) + SM::kTile + v_lo, va_hi = kbuf(t) + SM::kTile + v_hi;
+        u32x2 vlo[kAhead + 1], vhi[kAhead + 1];
+        auto issue = [&](int f) {
+          vlo[f % (kAhead + 1)] = lds_read_tr_untracked_at<16 * D * 2>(va_lo ^ (64u * (f % ET)), f / ET);
+          vhi[f % (kAhead + 1)] = lds_read_tr_untracked_at<16 * D * 2>(va_hi ^ (64u * (f % ET)), f / ET);
+        };
+#pragma unroll
+        for (int f = 0; f < kAhead; f++) issue(f);
+#pragma unroll
+        for (int f = 0; f < kFrags; f++) {
+          if (f + kAhead < kFrags) issue(f + kAhead);
+          const int left = kFrags - 1 - f;
+          wait_lgkmcnt(2 * (left < kAhead ? left : kAhead));
+          u32x2 &lo = vlo[f % (kAhead + 1)], &hi = vhi[f % (kAhead + 1)];
+          settle(lo);
+          settle(hi);
+          const u32x4 v4 = {lo[0], lo[1], hi[0], hi[1]};
+          oacc[f % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, v4), pf[f / ET], oacc[f % ET]);
+        }
+      }
     }
+    wait_vmcnt<0>();                                   // the next tile has landed, for everyone behind the barrier
+    phase_barrier();
   }
-  if (row >= nq) return;
   const bool any = l_run != 0.f;                       // NaN is some
+  const size_t row_at = (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group + row;       // among the rows of all key heads
+  if (PARTS) {
+    if (row >= nr) return;
+    float* dst = a.part_o + ((size_t)blockIdx.y * a.Tq * a.H + row_at) * D;
+#pragma unroll
+    for (int et = 0; et < ET; et++)
+#pragma unroll
+      for (int v4 = 0; v4 < 4; v4++)
+        *reinterpret_cast<f32x4*>(dst + 32 * et + 8 * v4 + 4 * g) =
+            f32x4{oacc[et][4 * v4], oacc[et][4 * v4 + 1], oacc[et][4 * v4 + 2], oacc[et][4 * v4 + 3]};
+    if (g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)blockIdx.y * a.Tq * a.H + row_at)) = make_float2(m_run, l_run);
+    return;
+  }
+  // ---- normalise, transpose through LDS, whole rows out ----
+  uint16_t* os = reinterpret_cast<uint16_t*>(smem);
   const float inv = any ? 1.f / l_run : 0.f;
-  uint16_t* dst = a.o + (size_t)h * a.so.h + (size_t)(qs.x + row) * a.so.t;
 #pragma unroll
   for (int et = 0; et < ET; et++)
 #pragma unroll
@@ -97,17 +194,75 @@ __global__ __launch_bounds__(256) void packed_fwd_kernel(PackedArgs a, int heads
       bf16x4 pk;
 #pragma unroll
       for (int r = 0; r < 4; r++) pk[r] = (__bf16)(any ? inv * oacc[et][4 * v4 + r] : 0.f);
-      *reinterpret_cast<bf16x4*>(dst + 32 * et + 8 * v4 + 4 * g) = pk;
+      *reinterpret_cast<bf16x4*>(os + (32 * w + lane % 32) * LD + 32 * et + 8 * v4 + 4 * g) = pk;
     }
-  if (a.lse_out && g == 0) a.lse_out[(size_t)h * a.Tq + qs.x + row] = any ? (m_run + log2f(l_run)) * (1.f / kLog2e) : -INFINITY;
+  if (a.lse_out && g == 0 && row < nr)
+    a.lse_out[(size_t)(hk * a.group + my.y) * a.Tq + qs.x + my.x] = any ? (m_run + log2f(l_run)) * (1.f / kLog2e) : -INFINITY;
+  wave_lds_fence();                                    // a wave stores the rows that it wrote
+#pragma unroll
+  for (int i = 0; i < 32 * (D / 8) / kWave; i++) {
+    const int idx = lane + kWave * i, r = 32 * w + idx / (D / 8), ch = idx % (D / 8);
+    if (row0 + r >= nr) continue;
+    const int2 x = query_of(a, row0 + r);
+    *reinterpret_cast<u32x4*>(a.o + (size_t)(hk * a.group + x.y) * a.so.h + (size_t)(qs.x + x.x) * a.so.t + 8 * ch) =
+        *reinterpret_cast<const u32x4*>(os + r * LD + 8 * ch);
+  }
 }
 
-hipError_t launch_packed_fwd(const PackedArgs& a, hipStream_t stream) {
-  const long long grid = most_tiles(a.Tq, a.S, 128) * a.H;
+// The parts of one row: their O, weighted with 2^(m - the largest m), over their l, weighted alike.  A wave a row.
+template <int D>
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
+  constexpr int E = D / kWave;
+  const int lane = threadIdx.x % kWave;
+  const long long row = (long long)blockIdx.x * 4 + threadIdx.x / kWave, rows = (long long)a.Tq * a.H;
+  if (row >= rows) return;
+  const int hk = (int)(row / ((long long)a.Tq * a.group));
+  const int2 x = query_of(a, (int)(row - (long long)hk * a.Tq * a.group));       // x.x: token
+  if (x.x < a.q_start[0] || x.x >= a.q_start[a.S]) return;                       // of no sequence
+  const int h = hk * a.group + x.y;
+  float m = -INFINITY;
+  for (int i = 0; i < a.q_parts; i++) m = fmaxf(m, a.part_ml[2 * (i * rows + row)]);
+  float l = 0.f, o[E] = {};
+  for (int i = 0; i < a.q_parts; i++) {
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (i * rows + row));
+    const float by = fast_exp2(ml.x - m);
+    l += by * ml.y;
+#pragma unroll
+    for (int e = 0; e < E; e++) o[e] += by * a.part_o[(i * rows + row) * D + E * lane + e];
+  }
+  const bool any = l != 0.f;
+#pragma unroll
+  for (int e = 0; e < E; e++)
+    a.o[(size_t)h * a.so.h + (size_t)x.x * a.so.t + E * lane + e] = __builtin_bit_cast(uint16_t, (__bf16)(any ? o[e] / l : 0.f));
+  if (a.lse_out && lane == 0) a.lse_out[(size_t)h * a.Tq + x.x] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
+}
+
+// Parts: as many as fill two workgroups a CU where the tiles alone do not fill half of them, none shorter than 256 keys or rows.
+void plan_packed(PackedArgs* a, bool backward) {
+  a->q_parts = a->k_parts = 1;
+  const long long rows = (long long)a->Tq * a->group, places = 512;
+  const long long q_tiles = most_tiles(rows, a->S, kRowTile) * a->Hkv, k_tiles = most_tiles(a->Tk, a->S, kKeyTile) * a->Hkv;
+  auto parts = [&](long long tiles, long long length) {
+    if (!tiles || tiles * 2 > places) return 1;
+    const long long n = places / tiles, most = length / 256;
+    return (int)(n < most ? n : most < 1 ? 1 : most);
+  };
+  a->q_parts = parts(q_tiles, a->Tk);
+  if (backward) a->k_parts = parts(k_tiles, rows);
+}
+
+template <int D> static hipError_t launch_fwd(const PackedArgs& a, hipStream_t stream) {
+  const long long grid = most_tiles((long long)a.Tq * a.group, a.S, kRowTile) * a.Hkv;
   if (!grid) return hipSuccess;
-  if (a.d == 128) packed_fwd_kernel<128><<<(unsigned)grid, 256, 0, stream>>>(a, 0);
-  else packed_fwd_kernel<64><<<(unsigned)grid, 256, 0, stream>>>(a, 0);
+  if (a.q_parts == 1) {
+    packed_fwd_kernel<D, false><<<(unsigned)grid, 256, PackedSmem<D>::kBytes, stream>>>(a);
+    return hipGetLastError();
+  }
+  packed_fwd_kernel<D, true><<<dim3((unsigned)grid, a.q_parts), 256, PackedSmem<D>::kBytes, stream>>>(a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  packed_join_kernel<D><<<(unsigned)(((long long)a.Tq * a.H + 3) / 4), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
+hipError_t launch_packed_fwd(const PackedArgs& a, hipStream_t stream) { return a.d == 128 ? launch_fwd<128>(a, stream) : launch_fwd<64>(a, stream); }
 
 }  // namespace sla2

@@ -1,38 +1,125 @@
 // Backward pass of attention over packed sequences.  With P = exp(scale Q K^T - lse) and D = rowsum(dO . O):
 //   dV = P^T dO,   dS = P . (dO V^T - D),   dQ = scale dS K,   dK = scale dS^T Q.
 //
-// Two kernels, so that every sum has one owner and a fixed order: one for each tile of queries (D and dQ), one for each tile of keys (dK
-// and dV, over the queries of all heads of the group).  Both form P and dO V^T themselves: 7 products in all for 5 that are needed, where
+// Two kernels, so that every sum has one owner and a fixed order: one for each tile of rows (D and dQ), one for each tile of keys (dK
+// and dV, over the rows of all heads of the group).  Both form P and dO V^T themselves: 7 products in all for 5 that are needed, where
 // a sum of dQ over workgroups would take a d-wide row of fp32 written and read back for each tile of keys.
 #include "packed.h"
 
 namespace sla2 {
 
-// D and dQ of 128 rows: S^T = K Q^T and dP^T = V dO^T (keys x rows), dQ^T += K^T dS^T, as in the forward pass with K in the place of V.
+template <int D> struct PackedBwdSmem {
+  static constexpr int kTile = PackedTile<D>::kTileBytes;
+  static constexpr int kLd = D + 8;
+  static constexpr int kStatOff = 4 * kTile;                   // float [2][2][64]: lse log2(e) and D of a step's rows (key side)
+  static constexpr int kBytes = kStatOff + 4 * 64 * 4;
+  static_assert(4 * 32 * kLd * 2 <= kStatOff, "32 result rows of a wave in the place of the tiles");
+};
+
+// 32 rows of a wave from accumulators (channels x rows) through LDS to memory, times `by`; row_ptr(r): where row r goes, null: nowhere
+template <int D, class Row>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float by, uint16_t* os /* [32][D + 8], of this wave */, int lane, Row row_ptr) {
+  constexpr int LD = D + 8;
+#pragma unroll
+  for (int et = 0; et < D / 32; et++)
+#pragma unroll
+    for (int v4 = 0; v4 < 4; v4++) {
+      bf16x4 pk;
+#pragma unroll
+      for (int r = 0; r < 4; r++) pk[r] = (__bf16)(by * acc[et][4 * v4 + r]);
+      *reinterpret_cast<bf16x4*>(os + lane % 32 * LD + 32 * et + 8 * v4 + 4 * (lane / 32)) = pk;
+    }
+  wave_lds_fence();
+#pragma unroll
+  for (int i = 0; i < 32 * (D / 8) / kWave; i++) {
+    const int idx = lane + kWave * i, r = idx / (D / 8), ch = idx % (D / 8);
+    uint16_t* dst = row_ptr(r);
+    if (dst) *reinterpret_cast<u32x4*>(dst + 8 * ch) = *reinterpret_cast<const u32x4*>(os + r * LD + 8 * ch);
+  }
+  wave_lds_fence();
+}
 template <int D>
-__global__ __launch_bounds__(256) void packed_dq_kernel(PackedArgs a) {
-  constexpr int BQ = 128, NT = 256, KS = D / 16, ET = D / 32;
-  typedef PaddedLayout<D> PL;
-  __shared__ __attribute__((aligned(16))) uint16_t ks_[kTileTokens * PL::kRowElems], vs_[kTileTokens * PL::kRowElems];
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, g = lane / 32;
-  const int h = blockIdx.x % a.H;
-  const TilePlace at = find_tile(a.q_start, a.S, a.Tq, BQ, blockIdx.x / a.H, lane);
+__device__ __forceinline__ void store_part(const f32x16 (&acc)[D / 32], float* dst, int g) {
+#pragma unroll
+  for (int et = 0; et < D / 32; et++)
+#pragma unroll
+    for (int v4 = 0; v4 < 4; v4++)
+      *reinterpret_cast<f32x4*>(dst + 32 * et + 8 * v4 + 4 * g) =
+          f32x4{acc[et][4 * v4], acc[et][4 * v4 + 1], acc[et][4 * v4 + 2], acc[et][4 * v4 + 3]};
+}
+__device__ __forceinline__ void pin(bf16x8& f) {       // converted here: eight registers less than the fp32 values
+  u32x4 u = __builtin_bit_cast(u32x4, f);
+  settle(u);
+  f = __builtin_bit_cast(bf16x8, u);
+}
+
+// acc[et] += A^T f: the 32 rows of a tile at `lo` / `hi` (tr_read_offset) contracted, as two 16-row steps, into all channels
+template <int D>
+__device__ __forceinline__ void contract32(f32x16 (&acc)[D / 32], const bf16x8* f, unsigned lo_at, unsigned hi_at) {
+  constexpr int ET = D / 32, kFrags = 2 * ET, kAhead = 3, kSlots = kAhead + 1;
+  u32x2 lo[kSlots], hi[kSlots];
+  auto issue = [&](int n) {
+    lo[n % kSlots] = lds_read_tr_untracked_at<32 * D>(lo_at ^ (64u * (n % ET)), n / ET);
+    hi[n % kSlots] = lds_read_tr_untracked_at<32 * D>(hi_at ^ (64u * (n % ET)), n / ET);
+  };
+#pragma unroll
+  for (int n = 0; n < kAhead; n++) issue(n);
+#pragma unroll
+  for (int n = 0; n < kFrags; n++) {
+    if (n + kAhead < kFrags) issue(n + kAhead);
+    wait_lgkmcnt(2 * (n + kAhead < kFrags ? kAhead : kFrags - 1 - n));
+    settle(lo[n % kSlots]);
+    settle(hi[n % kSlots]);
+    const u32x4 v4 = {lo[n % kSlots][0], lo[n % kSlots][1], hi[n % kSlots][0], hi[n % kSlots][1]};
+    acc[n % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, v4), f[n / ET], acc[n % ET]);
+  }
+}
+
+// D and dQ of 128 rows: S^T = K Q^T and dP^T = V dO^T (keys x rows), dQ^T += K^T dS^T, as in the forward pass with K in the place of V.
+template <int D, bool PARTS>
+__global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
+  constexpr int NW = 4, KS = D / 16, ET = D / 32;
+  typedef PackedBwdSmem<D> SM;
+  typedef PackedTile<D> SL;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid % kWave, g = lane / 32;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const TileHead th = tile_head(blockIdx.x, a.Hkv);
+  const int hk = th.head;
+  TilePlace at = find_tile(a.q_start, a.S, a.Tq, a.group, kRowTile, th.tile, lane);
   if (at.s < 0) return;
+  if (a.causal) at.tile = at.tiles - 1 - at.tile;      // the longest first
   const int2 qs = stretch_of(a.q_start, at.s, a.Tq), kx = stretch_of(a.k_start, at.s, a.Tk);
-  const int nq = qs.y, nk = kx.y, row0 = at.tile * BQ, row = row0 + 32 * w + lane % 32;
-  const size_t first = (size_t)qs.x + min(row, nq - 1);          // this lane's row, in range
-  const uint16_t* kh = a.k + (size_t)(h / a.group) * a.skv.h + (size_t)kx.x * a.skv.t;
-  const uint16_t* vh = a.v + (size_t)(h / a.group) * a.skv.h + (size_t)kx.x * a.skv.t;
-  const int past = a.causal ? nk - nq : nk;
-  const int last = min(row0 + BQ, nq);
-  const int keys = a.causal ? min(nk, max(0, last + past)) : nk;
-  const int mine = a.causal ? min(nk, row + past + 1) : nk;
+  const int nr = qs.y * a.group, nk = kx.y, row0 = at.tile * kRowTile, row = row0 + 32 * w + lane % 32;
+  const uint16_t* kh = a.k + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
+  const uint16_t* vh = a.v + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
+  const int past = nk - qs.y;
+  const int2 my = query_of(a, min(row, nr - 1));
+  const int mine = a.causal ? min(nk, my.x + past + 1) : nk;
+  const int keys = a.causal ? min(nk, max(0, query_of(a, min(row0 + kRowTile, nr) - 1).x + past + 1)) : nk;
+  const int w_row = row0 + 32 * w;
+  const int w_keys = w_row >= nr ? 0 : __builtin_amdgcn_readlane(mine, 31), w_full = __builtin_amdgcn_readfirstlane(mine);
+  int t_begin = 0, t_end = (keys + kTileTokens - 1) / kTileTokens;
+  if (PARTS) {
+    const int n = t_end;
+    t_begin = (int)((long long)n * blockIdx.y / a.q_parts);
+    t_end = (int)((long long)n * (blockIdx.y + 1) / a.q_parts);
+  }
+  auto kbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
+  auto dma = [&](int t) {
+    const int t0 = t * kTileTokens, valid = min(kTileTokens, nk - t0), ln = (int)lane_again();
+    dma_tile<D, NW, SL>(kh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t), w, ln);
+    dma_tile<D, NW, SL>(vh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t) + SM::kTile, w, ln);
+  };
+  if (t_begin < t_end) dma(t_begin);
   bf16x8 qf[KS], gf[KS];
   float delta = 0.f;
+  const size_t row_at = (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group + row;       // among the rows of all key heads
+  const int h = hk * a.group + my.y, token = qs.x + my.x;
   {
-    const uint16_t* src = a.q + (size_t)h * a.sq.h + first * a.sq.t + 8 * g;
-    const uint16_t* gsrc = a.dout + (size_t)h * a.so.h + first * a.so.t + 8 * g;
-    const uint16_t* osrc = a.out + (size_t)h * a.so.h + first * a.so.t + 8 * g;
+    const uint16_t* src = a.q + (size_t)h * a.sq.h + (size_t)token * a.sq.t + 8 * g;
+    const uint16_t* gsrc = a.dout + (size_t)h * a.so.h + (size_t)token * a.so.t + 8 * g;
+    const uint16_t* osrc = a.out + (size_t)h * a.so.h + (size_t)token * a.so.t + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) {
       qf[ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
@@ -43,78 +130,153 @@ __global__ __launch_bounds__(256) void packed_dq_kernel(PackedArgs a) {
     }
   }
   delta = swap_halves_sum(delta);
-  if (row < nq && g == 0) a.delta[(size_t)h * a.Tq + first] = delta;
-  const float lse = a.lse[(size_t)h * a.Tq + first];
+  const float lse = a.lse[(size_t)h * a.Tq + token];
   const float l2 = lse == -INFINITY ? INFINITY : lse * kLog2e;   // a row that reads no key: P = 0
+  if (row < nr && g == 0 && (!PARTS || blockIdx.y == 0)) {
+    a.delta[row_at] = delta;
+    a.lse2[row_at] = l2;
+  }
   const float c1 = kLog2e * a.scale;
   f32x16 acc[ET];
 #pragma unroll
   for (int et = 0; et < ET; et++)
 #pragma unroll
     for (int e = 0; e < 16; e++) acc[et][e] = 0.f;
-  for (int t0 = 0; t0 < keys; t0 += kTileTokens) {
-    u32x4 r[TileCopy<D, NT>::kLoads], rv[TileCopy<D, NT>::kLoads];
-    TileCopy<D, NT>::load(r, kh + (size_t)t0 * a.skv.t, a.skv.t, min(kTileTokens, nk - t0), tid);
-    TileCopy<D, NT>::load(rv, vh + (size_t)t0 * a.skv.t, a.skv.t, min(kTileTokens, nk - t0), tid);
-    __syncthreads();
-    TileCopy<D, NT>::store(r, ks_, tid);
-    TileCopy<D, NT>::store(rv, vs_, tid);
-    __syncthreads();
-    bf16x8 df[4];
+  const unsigned k_off = row_read_offset<D>(lane), t_lo = tr_read_offset<D>(lane, 0), t_hi = tr_read_offset<D>(lane, 1);
+  wait_vmcnt<0>();
 #pragma unroll
-    for (int mt = 0; mt < 2; mt++) {
-      f32x16 s, dp;
+  for (int ks = 0; ks < KS; ks++) { settle(qf[ks]); settle(gf[ks]); }
+  phase_barrier();
+  for (int t = t_begin; t < t_end; t++) {
+    if (t + 1 < t_end) dma(t + 1);
+    const int t0 = t * kTileTokens;
+    if (t0 < w_keys) {
 #pragma unroll
-      for (int e = 0; e < 16; e++) s[e] = dp[e] = 0.f;
+      for (int mt = 0; mt < 2; mt++) {
+        const unsigned ka = kbuf(t) + 64 * D * mt;
+        f32x16 s, dp;
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) {
-        s = mfma_bf16(row_fragment<PL>(ks_, 32 * mt + lane % 32, 16 * ks + 8 * g), qf[ks], s);
-        dp = mfma_bf16(row_fragment<PL>(vs_, 32 * mt + lane % 32, 16 * ks + 8 * g), gf[ks], dp);
-      }
+        for (int e = 0; e < 16; e++) s[e] = dp[e] = 0.f;
+        bf16x8 df[2];
+        const bool edge = t0 + 32 * mt + 32 > w_full;
+        constexpr int kItems = 2 * KS, kAhead = 4, kSlots = kAhead + 1;
+        u32x4 ring[kSlots];
+        auto issue = [&](int n) {
+          ring[n % kSlots] = lds_read16_untracked<0>((ka + (n < KS ? 0 : SM::kTile) + k_off) ^ (32u * (n % KS)));
+        };
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        const float p = fast_exp2(s[e] * c1 - l2);
-        const float ds = t0 + 32 * mt + 8 * (e / 4) + 4 * g + e % 4 >= mine ? 0.f : p * (dp[e] - delta);
-        df[2 * mt + e / 8][e % 8] = (__bf16)ds;
+        for (int n = 0; n < kAhead; n++) issue(n);
+#pragma unroll
+        for (int n = 0; n < kItems; n++) {
+          if (n + kAhead < kItems) issue(n + kAhead);
+          wait_lgkmcnt(n + kAhead < kItems ? kAhead : kItems - 1 - n);
+          settle(ring[n % kSlots]);
+          const bf16x8 f = __builtin_bit_cast(bf16x8, ring[n % kSlots]);
+          if (n < KS) {
+            s = mfma_bf16(f, qf[n], s);
+          } else {
+            dp = mfma_bf16(f, gf[n - KS], dp);
+            constexpr int kStep = KS / 4;              // behind every quarter of the products of dP four exponentials
+            if ((n - KS) % kStep == kStep - 1) {
+              const int v4 = (n - KS) / kStep;
+#pragma unroll
+              for (int r = 0; r < 4; r++) {
+                float p = fast_exp2(s[4 * v4 + r] * c1 - l2);
+                settle(p);
+                s[4 * v4 + r] = p;
+              }
+            }
+          }
+        }
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 16; e++)
+            if (t0 + 32 * mt + 8 * (e / 4) + 4 * g + e % 4 >= mine) s[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e++) df[e / 8][e % 8] = (__bf16)(s[e] * (dp[e] - delta));
+        pin(df[0]);
+        pin(df[1]);
+        contract32<D>(acc, df, ka + t_lo, ka + t_hi);
       }
     }
-#pragma unroll
-    for (int et = 0; et < ET; et++)
-#pragma unroll
-      for (int ks = 0; ks < 4; ks++) acc[et] = mfma_bf16(v_fragment<PL>(ks_, ks, 32 * et, lane), df[ks], acc[et]);
+    wait_vmcnt<0>();
+    phase_barrier();
   }
-  if (row >= nq) return;
-  uint16_t* dst = a.dq + (size_t)h * a.sq.h + first * a.sq.t;
-#pragma unroll
-  for (int et = 0; et < ET; et++)
-#pragma unroll
-    for (int v4 = 0; v4 < 4; v4++) {
-      bf16x4 pk;
-#pragma unroll
-      for (int r = 0; r < 4; r++) pk[r] = (__bf16)(a.scale * acc[et][4 * v4 + r]);
-      *reinterpret_cast<bf16x4*>(dst + 32 * et + 8 * v4 + 4 * g) = pk;
-    }
+  if (PARTS) {
+    if (row < nr) store_part<D>(acc, a.part_o + ((size_t)blockIdx.y * a.Tq * a.H + row_at) * D, g);
+    return;
+  }
+  store_rows<D>(acc, a.scale, reinterpret_cast<uint16_t*>(smem) + w * 32 * SM::kLd, lane, [&](int r) -> uint16_t* {
+    if (w_row + r >= nr) return nullptr;
+    const int2 x = query_of(a, w_row + r);
+    return a.dq + (size_t)(hk * a.group + x.y) * a.sq.h + (size_t)(qs.x + x.x) * a.sq.t;
+  });
 }
 
 // dK and dV of 128 keys: S = Q K^T and dP = dO V^T (rows x keys), a key on lanes l and l + 32 with its row of K and V in registers;
-// dV^T += dO^T P and dK^T += Q^T dS over the rows, 64 at a time, of every head of the group.
-template <int D>
-__global__ __launch_bounds__(256) void packed_dkv_kernel(PackedArgs a) {
-  constexpr int BK = 128, NT = 256, KS = D / 16, ET = D / 32;
-  typedef PaddedLayout<D> PL;
-  __shared__ __attribute__((aligned(16))) uint16_t qs_[kTileTokens * PL::kRowElems], gs_[kTileTokens * PL::kRowElems];
-  __shared__ __attribute__((aligned(16))) float ls_[kTileTokens], ds_[kTileTokens];
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, g = lane / 32;
-  const int hkv = a.H / a.group, hk = blockIdx.x % hkv;
-  const TilePlace at = find_tile(a.k_start, a.S, a.Tk, BK, blockIdx.x / hkv, lane);
+// dV^T += dO^T P and dK^T += Q^T dS, 64 rows a step, which arrive in LDS one step ahead.
+template <int D, bool PARTS>
+__global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
+  constexpr int NW = 4, KS = D / 16, ET = D / 32;
+  typedef PackedBwdSmem<D> SM;
+  typedef PackedTile<D> SL;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  float* stat = reinterpret_cast<float*>(smem + SM::kStatOff);
+  const int tid = threadIdx.x, lane = tid % kWave, g = lane / 32;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const TileHead th = tile_head(blockIdx.x, a.Hkv);
+  const int hk = th.head;
+  const TilePlace at = find_tile(a.k_start, a.S, a.Tk, 1, kKeyTile, th.tile, lane);
   if (at.s < 0) return;
-  const int2 qx = stretch_of(a.q_start, at.s, a.Tq), kx = stretch_of(a.k_start, at.s, a.Tk);
-  const int nq = qx.y, nk = kx.y, key0 = at.tile * BK, key = key0 + 32 * w + lane % 32;
-  const size_t first = (size_t)kx.x + min(key, nk - 1);
+  const int2 qs = stretch_of(a.q_start, at.s, a.Tq), kx = stretch_of(a.k_start, at.s, a.Tk);
+  const int nr = qs.y * a.group, nk = kx.y, key0 = at.tile * kKeyTile, key = key0 + 32 * w + lane % 32;
+  const size_t token = (size_t)kx.x + min(key, nk - 1);
+  const int past = nk - qs.y;
+  const uint16_t* qh = a.q + (size_t)hk * a.group * a.sq.h + (size_t)qs.x * a.sq.t;
+  const uint16_t* gh = a.dout + (size_t)hk * a.group * a.so.h + (size_t)qs.x * a.so.t;
+  const float* lh = a.lse2 + (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group;
+  const float* dh = a.delta + (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group;
+  // the rows that read a key: from this one on (causal)
+  auto from_of = [&](int j) { return a.causal ? max(0, j - past) * a.group : 0; };
+  const int from = from_of(key), w_from = from_of(key0 + 32 * w), w_last = from_of(key0 + 32 * w + 31);
+  int t_begin = from_of(key0) / kTileTokens, t_end = max(t_begin, (nr + kTileTokens - 1) / kTileTokens);
+  if (PARTS) {
+    const int n = t_end - t_begin, b = t_begin;
+    t_begin = b + (int)((long long)n * blockIdx.y / a.k_parts);
+    t_end = b + (int)((long long)n * (blockIdx.y + 1) / a.k_parts);
+  }
+  auto qbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
+  // Step t: rows [64 t, + 64) of Q and dO and their lse log2(e) and D; rows past the end repeat the last one, see no_rows
+  auto request = [&](int t) {
+    constexpr int kRowsPerInstr = 1024 / (D * 2), kInstrs = kTileTokens / kRowsPerInstr / NW;
+    const int ln = (int)lane_again(), r0 = t * kTileTokens, valid = min(kTileTokens, nr - r0);
+    const int2 q0 = query_of(a, r0);
+    const int row_w = w * kRowsPerInstr + ln / SL::kChunks;
+    const unsigned col = 16u * (unsigned)((ln % SL::kChunks) ^ SL::swz(row_w));
+    const char *qb = (const char*)(qh + (size_t)q0.x * a.sq.t), *gb = (const char*)(gh + (size_t)q0.x * a.so.t);
+#pragma unroll
+    for (int i = 0; i < kInstrs; i++) {
+      const int2 x = near_query_of(a, (unsigned)(q0.y + min(row_w + i * NW * kRowsPerInstr, valid - 1)));
+      dma_lane16(qb, ((unsigned)x.x * (unsigned)a.sq.t + (unsigned)x.y * (unsigned)a.sq.h) * 2 + col, qbuf(t) + (i * NW + w) * 1024);
+      dma_lane16(gb, ((unsigned)x.x * (unsigned)a.so.t + (unsigned)x.y * (unsigned)a.so.h) * 2 + col, qbuf(t) + SM::kTile + (i * NW + w) * 1024);
+    }
+    const unsigned so = 4u * (unsigned)min(ln, valid - 1);
+    if (w == 0) dma_lane4(lh + r0, so, lds_address(stat + (t & 1) * 128));
+    if (w == 1) dma_lane4(dh + r0, so, lds_address(stat + (t & 1) * 128 + 64));
+  };
+  // behind the arrival of step t: lse = +inf for rows past the end, their P is 0
+  auto no_rows = [&](int t) {
+    if (w == 0 && (t + 1) * kTileTokens > nr) {
+      if (t * kTileTokens + lane >= nr) stat[(t & 1) * 128 + lane] = INFINITY;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  };
+  if (t_begin < t_end) request(t_begin);
   bf16x8 kf[KS], vf[KS];
   {
-    const uint16_t* src = a.k + (size_t)hk * a.skv.h + first * a.skv.t + 8 * g;
-    const uint16_t* vsrc = a.v + (size_t)hk * a.skv.h + first * a.skv.t + 8 * g;
+    const uint16_t* src = a.k + (size_t)hk * a.skv.h + token * a.skv.t + 8 * g;
+    const uint16_t* vsrc = a.v + (size_t)hk * a.skv.h + token * a.skv.t + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) {
       kf[ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
@@ -122,96 +284,161 @@ __global__ __launch_bounds__(256) void packed_dkv_kernel(PackedArgs a) {
     }
   }
   const float c1 = kLog2e * a.scale;
-  const int from = a.causal ? max(0, key - (nk - nq)) : 0;       // this lane's key is read by the rows from this one on
-  const int start = a.causal ? max(0, key0 - (nk - nq)) / kTileTokens * kTileTokens : 0;
   f32x16 dk[ET], dv[ET];
 #pragma unroll
   for (int et = 0; et < ET; et++)
 #pragma unroll
     for (int e = 0; e < 16; e++) dk[et][e] = dv[et][e] = 0.f;
-  for (int h = hk * a.group; h < (hk + 1) * a.group; h++) {
-    const uint16_t* qh = a.q + (size_t)h * a.sq.h + (size_t)qx.x * a.sq.t;
-    const uint16_t* gh = a.dout + (size_t)h * a.so.h + (size_t)qx.x * a.so.t;
-    const float* lh = a.lse + (size_t)h * a.Tq + qx.x;
-    const float* dh = a.delta + (size_t)h * a.Tq + qx.x;
-    for (int r0 = start; r0 < nq; r0 += kTileTokens) {
-      u32x4 r[TileCopy<D, NT>::kLoads], rg[TileCopy<D, NT>::kLoads];
-      TileCopy<D, NT>::load(r, qh + (size_t)r0 * a.sq.t, a.sq.t, min(kTileTokens, nq - r0), tid);
-      TileCopy<D, NT>::load(rg, gh + (size_t)r0 * a.so.t, a.so.t, min(kTileTokens, nq - r0), tid);
-      float l = 0.f, d = 0.f;
-      if (tid < kTileTokens) {
-        const int i = min(r0 + tid, nq - 1);
-        l = lh[i];
-        l = l == -INFINITY ? INFINITY : l * kLog2e;
-        d = dh[i];
-      }
-      __syncthreads();
-      TileCopy<D, NT>::store(r, qs_, tid);
-      TileCopy<D, NT>::store(rg, gs_, tid);
-      if (tid < kTileTokens) {
-        ls_[tid] = l;
-        ds_[tid] = d;
-      }
-      __syncthreads();
-      bf16x8 pf[4], df[4];
+  const unsigned r_off = row_read_offset<D>(lane), t_lo = tr_read_offset<D>(lane, 0), t_hi = tr_read_offset<D>(lane, 1);
+  wait_vmcnt<0>();
 #pragma unroll
-      for (int mt = 0; mt < 2; mt++) {
-        f32x16 s, dp;
+  for (int ks = 0; ks < KS; ks++) { settle(kf[ks]); settle(vf[ks]); }
+  if (t_begin < t_end) no_rows(t_begin);
+  phase_barrier();
+  for (int t = t_begin; t < t_end; t++) {
+    if (t + 1 < t_end) request(t + 1);
 #pragma unroll
-        for (int e = 0; e < 16; e++) s[e] = dp[e] = 0.f;
+    for (int rh = 0; rh < 2; rh++) {
+      const int r0 = t * kTileTokens + 32 * rh;
+      if (r0 + 32 <= w_from || r0 >= nr) continue;
+      const unsigned qa = qbuf(t) + 64 * D * rh, ga = qa + SM::kTile;
+      const unsigned st = lds_address(stat + (t & 1) * 128 + 32 * rh + 4 * g);
+      f32x16 s, dp;
+      bf16x8 pf[2], df[2];
 #pragma unroll
-        for (int ks = 0; ks < KS; ks++) {
-          s = mfma_bf16(row_fragment<PL>(qs_, 32 * mt + lane % 32, 16 * ks + 8 * g), kf[ks], s);
-          dp = mfma_bf16(row_fragment<PL>(gs_, 32 * mt + lane % 32, 16 * ks + 8 * g), vf[ks], dp);
+      for (int e = 0; e < 16; e++) s[e] = dp[e] = 0.f;
+      // One stream of LDS reads, kAhead of them in flight: the rows of Q for S; four groups of a quarter of the rows of dO for dP and lse
+      // of four rows, whose exponentials then run beside the products; D of the rows.
+      constexpr int kGroup = KS / 4 + 1, kItems = KS + 4 * kGroup + 4, kAhead = 4, kSlots = kAhead + 1;
+      u32x4 ring[kSlots];
+      auto issue = [&](int n) {
+        const int m = n - KS, v4 = m / kGroup;
+        if (n < KS) ring[n % kSlots] = lds_read16_untracked<0>((qa + r_off) ^ (32u * n));
+        else if (m >= 4 * kGroup) ring[n % kSlots] = lds_read16_untracked<0>(st + 256 + 32 * (m - 4 * kGroup));
+        else if (m % kGroup == kGroup - 1) ring[n % kSlots] = lds_read16_untracked<0>(st + 32 * v4);
+        else ring[n % kSlots] = lds_read16_untracked<0>((ga + r_off) ^ (32u * (v4 * (kGroup - 1) + m % kGroup)));
+      };
+      const bool edge = r0 < w_last;
+#pragma unroll
+      for (int n = 0; n < kAhead; n++) issue(n);
+#pragma unroll
+      for (int n = 0; n < kItems; n++) {
+        if (n + kAhead < kItems) issue(n + kAhead);
+        wait_lgkmcnt(n + kAhead < kItems ? kAhead : kItems - 1 - n);
+        settle(ring[n % kSlots]);
+        const int m = n - KS, v4 = m / kGroup;
+        if (n < KS) {
+          s = mfma_bf16(__builtin_bit_cast(bf16x8, ring[n % kSlots]), kf[n], s);
+        } else if (m >= 4 * kGroup) {
+          const int x = m - 4 * kGroup;
+          const f32x4 d4 = __builtin_bit_cast(f32x4, ring[n % kSlots]);
+#pragma unroll
+          for (int r = 0; r < 4; r++) {
+            const int e = 4 * x + r;
+            pf[x / 2][e % 8] = (__bf16)s[e];
+            df[x / 2][e % 8] = (__bf16)(s[e] * (dp[e] - d4[r]));
+          }
+          if (x % 2 == 1) {
+            pin(pf[x / 2]);
+            pin(df[x / 2]);
+          }
+        } else if (m % kGroup == kGroup - 1) {
+          const f32x4 l4 = __builtin_bit_cast(f32x4, ring[n % kSlots]);
+#pragma unroll
+          for (int r = 0; r < 4; r++) {
+            const int e = 4 * v4 + r;
+            float p = fast_exp2(s[e] * c1 - l4[r]);
+            if (edge) p = r0 + 8 * v4 + 4 * g + r >= from ? p : 0.f;
+            settle(p);                                 // here, not where the compiler would gather them
+            s[e] = p;
+          }
+        } else {
+          dp = mfma_bf16(__builtin_bit_cast(bf16x8, ring[n % kSlots]), vf[v4 * (kGroup - 1) + m % kGroup], dp);
         }
-#pragma unroll
-        for (int e = 0; e < 16; e++) {
-          const int i = 32 * mt + 8 * (e / 4) + 4 * g + e % 4;
-          const bool reads = r0 + i >= from && r0 + i < nq;
-          const float p = reads ? fast_exp2(s[e] * c1 - ls_[i]) : 0.f;
-          pf[2 * mt + e / 8][e % 8] = (__bf16)p;
-          df[2 * mt + e / 8][e % 8] = (__bf16)(reads ? p * (dp[e] - ds_[i]) : 0.f);
-        }
       }
-#pragma unroll
-      for (int et = 0; et < ET; et++)
-#pragma unroll
-        for (int ks = 0; ks < 4; ks++) {
-          dv[et] = mfma_bf16(v_fragment<PL>(gs_, ks, 32 * et, lane), pf[ks], dv[et]);
-          dk[et] = mfma_bf16(v_fragment<PL>(qs_, ks, 32 * et, lane), df[ks], dk[et]);
-        }
+      contract32<D>(dv, pf, ga + t_lo, ga + t_hi);
+      contract32<D>(dk, df, qa + t_lo, qa + t_hi);
     }
+    wait_vmcnt<0>();                                   // the next step's rows have landed ...
+    if (t + 1 < t_end) no_rows(t + 1);
+    phase_barrier();                                   // ... for everyone; this step's tiles are free
   }
-  if (key >= nk) return;
-  uint16_t* dst = a.dk + (size_t)hk * a.skv.h + first * a.skv.t;
-  uint16_t* vdst = a.dv + (size_t)hk * a.skv.h + first * a.skv.t;
-#pragma unroll
-  for (int et = 0; et < ET; et++)
-#pragma unroll
-    for (int v4 = 0; v4 < 4; v4++) {
-      bf16x4 pk, pv;
-#pragma unroll
-      for (int r = 0; r < 4; r++) {
-        pk[r] = (__bf16)(a.scale * dk[et][4 * v4 + r]);
-        pv[r] = (__bf16)dv[et][4 * v4 + r];
-      }
-      *reinterpret_cast<bf16x4*>(dst + 32 * et + 8 * v4 + 4 * g) = pk;
-      *reinterpret_cast<bf16x4*>(vdst + 32 * et + 8 * v4 + 4 * g) = pv;
-    }
+  if (PARTS) {
+    if (key >= nk) return;
+    const size_t part = ((size_t)blockIdx.y * a.Tk + token) * a.Hkv + hk;
+    store_part<D>(dk, a.part_kv + part * D, g);
+    store_part<D>(dv, a.part_kv + ((size_t)a.k_parts * a.Tk * a.Hkv + part) * D, g);
+    return;
+  }
+  uint16_t* os = reinterpret_cast<uint16_t*>(smem) + w * 32 * SM::kLd;
+  auto to = [&](uint16_t* p) {
+    return [=](int r) -> uint16_t* {
+      return key0 + 32 * w + r < nk ? p + (size_t)hk * a.skv.h + (size_t)(kx.x + key0 + 32 * w + r) * a.skv.t : nullptr;
+    };
+  };
+  store_rows<D>(dk, a.scale, os, lane, to(a.dk));
+  store_rows<D>(dv, 1.f, os, lane, to(a.dv));
 }
 
-hipError_t launch_packed_bwd(const PackedArgs& a, hipStream_t stream) {
-  const long long q_tiles = most_tiles(a.Tq, a.S, 128) * a.H, k_tiles = most_tiles(a.Tk, a.S, 128) * (a.H / a.group);
+// Sums of the parts, four channels a thread: dQ (rows of all key heads), dK and dV.
+template <int D>
+__global__ __launch_bounds__(256) void packed_sum_q_kernel(PackedArgs a) {
+  const long long idx = (long long)blockIdx.x * 256 + threadIdx.x, row = idx / (D / 4), rows = (long long)a.Tq * a.H;
+  const int c = (int)(idx % (D / 4)) * 4;
+  if (row >= rows) return;
+  const int hk = (int)(row / ((long long)a.Tq * a.group));
+  const int2 x = query_of(a, (int)(row - (long long)hk * a.Tq * a.group));
+  if (x.x < a.q_start[0] || x.x >= a.q_start[a.S]) return;       // of no sequence
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < a.q_parts; i++) sum += *reinterpret_cast<const f32x4*>(a.part_o + (i * rows + row) * D + c);
+  bf16x4 r;
+#pragma unroll
+  for (int e = 0; e < 4; e++) r[e] = (__bf16)(a.scale * sum[e]);
+  *reinterpret_cast<bf16x4*>(a.dq + (size_t)(hk * a.group + x.y) * a.sq.h + (size_t)x.x * a.sq.t + c) = r;
+}
+template <int D>
+__global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
+  const long long idx = (long long)blockIdx.x * 256 + threadIdx.x, row = idx / (D / 4), rows = (long long)a.Tk * a.Hkv;
+  const int c = (int)(idx % (D / 4)) * 4;
+  if (row >= rows) return;
+  const int token = (int)(row / a.Hkv), hk = (int)(row % a.Hkv);
+  if (token < a.k_start[0] || token >= a.k_start[a.S]) return;
+  const float* src = a.part_kv + (blockIdx.y ? a.k_parts * rows * D : 0);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < a.k_parts; i++) sum += *reinterpret_cast<const f32x4*>(src + (i * rows + row) * D + c);
+  const float by = blockIdx.y ? 1.f : a.scale;
+  bf16x4 r;
+#pragma unroll
+  for (int e = 0; e < 4; e++) r[e] = (__bf16)(by * sum[e]);
+  *reinterpret_cast<bf16x4*>((blockIdx.y ? a.dv : a.dk) + (size_t)hk * a.skv.h + (size_t)token * a.skv.t + c) = r;
+}
+
+template <int D> static hipError_t launch_bwd(const PackedArgs& a, hipStream_t stream) {
+  constexpr int smem = PackedBwdSmem<D>::kBytes;
+  static OncePerDevice once[4];
+  const void* kernels[4] = {(const void*)packed_dq_kernel<D, false>, (const void*)packed_dq_kernel<D, true>,
+                            (const void*)packed_dkv_kernel<D, false>, (const void*)packed_dkv_kernel<D, true>};
+  const long long q_tiles = most_tiles((long long)a.Tq * a.group, a.S, kRowTile) * a.Hkv, k_tiles = most_tiles(a.Tk, a.S, kKeyTile) * a.Hkv;
+  const int q = a.q_parts > 1, k = a.k_parts > 1;
+  if (hipError_t e = allow_dynamic_lds(once[q], kernels[q], smem); e != hipSuccess) return e;
+  if (hipError_t e = allow_dynamic_lds(once[2 + k], kernels[2 + k], smem); e != hipSuccess) return e;
   if (q_tiles) {
-    if (a.d == 128) packed_dq_kernel<128><<<(unsigned)q_tiles, 256, 0, stream>>>(a);
-    else packed_dq_kernel<64><<<(unsigned)q_tiles, 256, 0, stream>>>(a);
+    if (q) packed_dq_kernel<D, true><<<dim3((unsigned)q_tiles, a.q_parts), 256, smem, stream>>>(a);
+    else packed_dq_kernel<D, false><<<(unsigned)q_tiles, 256, smem, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (q) {
+      packed_sum_q_kernel<D><<<(unsigned)(((long long)a.Tq * a.H * (D / 4) + 255) / 256), 256, 0, stream>>>(a);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
   }
   if (k_tiles) {
-    if (a.d == 128) packed_dkv_kernel<128><<<(unsigned)k_tiles, 256, 0, stream>>>(a);
-    else packed_dkv_kernel<64><<<(unsigned)k_tiles, 256, 0, stream>>>(a);
+    if (k) packed_dkv_kernel<D, true><<<dim3((unsigned)k_tiles, a.k_parts), 256, smem, stream>>>(a);
+    else packed_dkv_kernel<D, false><<<(unsigned)k_tiles, 256, smem, stream>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (k) packed_sum_kv_kernel<D><<<dim3((unsigned)(((long long)a.Tk * a.Hkv * (D / 4) + 255) / 256), 2), 256, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
+hipError_t launch_packed_bwd(const PackedArgs& a, hipStream_t stream) { return a.d == 128 ? launch_bwd<128>(a, stream) : launch_bwd<64>(a, stream); }
 
 }  // namespace sla2

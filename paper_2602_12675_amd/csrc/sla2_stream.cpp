@@ -34,9 +34,26 @@ static View rows_view(const void* p, int rows, int heads, int d, long long h, lo
   return View{rows ? p : nullptr, 2, 2, d, {heads, rows}, {h, t}};
 }
 
-static size_t packed_bytes(const PackedArgs& a, bool backward) {
-  const size_t n = backward ? align256((size_t)a.H * a.Tq * sizeof(float)) : 0;
-  return n ? n : 256;
+// The workspace of a call, and where its parts lie
+static size_t packed_layout(PackedArgs* a, bool backward, void* ws) {
+  size_t off = 0;
+  auto take = [&](size_t floats) {
+    float* p = ws ? (float*)((char*)ws + off) : nullptr;
+    off = align256(off + floats * sizeof(float));
+    return p;
+  };
+  const size_t rows = (size_t)a->Tq * a->H;
+  plan_packed(a, backward);
+  if (backward) {
+    a->lse2 = take(rows);
+    a->delta = take(rows);
+    if (a->k_parts > 1) a->part_kv = take(2 * (size_t)a->k_parts * a->Tk * a->Hkv * a->d);
+  }
+  if (a->q_parts > 1) {
+    a->part_o = take(a->q_parts * rows * a->d);
+    if (!backward) a->part_ml = take(2 * a->q_parts * rows);
+  }
+  return off ? off : 256;
 }
 
 static int make_packed(const sla2_packed_params* p, PackedArgs* a) {
@@ -57,16 +74,20 @@ static int make_packed(const sla2_packed_params* p, PackedArgs* a) {
   a->Tq = p->tokens_q;
   a->Tk = p->tokens_k;
   a->H = p->H;
+  a->Hkv = p->H_kv;
   a->group = p->H / p->H_kv;
+  a->group_inv = a->group > 1 ? (unsigned)(((1ull << 32) + a->group - 1) / a->group) : 0;
   a->d = p->d;
   a->causal = p->causal != 0;
   a->scale = rate_or_default(p->scale, p->d);
-  // one workgroup for each tile and head, in one dimension of a launch
-  if (most_tiles(a->Tq, a->S, 32) * a->H > INT_MAX || most_tiles(a->Tk, a->S, 32) * a->H > INT_MAX) return SLA2_EUNSUPPORTED;
+  // rows (queries of all heads) and workgroups are counted in 31 bits, a step's rows lie within 4 GB
+  if ((long long)a->Tq * a->H > INT_MAX - 1024 || (long long)a->Tk * a->H > INT_MAX - 1024 || a->group > 1 << 15) return SLA2_EUNSUPPORTED;
+  for (const RowStrides* s : {&a->sq, &a->so})
+    if (a->group > 1 && (a->group - 1) * (__int128)s->h + 64ll * s->t >= 1ll << 31) return SLA2_EUNSUPPORTED;
   return SLA2_OK;
 }
 static View q_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tq, a.H, a.d, a.sq.h, a.sq.t); }
-static View kv_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tk, a.H / a.group, a.d, a.skv.h, a.skv.t); }
+static View kv_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tk, a.Hkv, a.d, a.skv.h, a.skv.t); }
 static View out_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tq, a.H, a.d, a.so.h, a.so.t); }
 static View starts_view(const PackedArgs& a, const int32_t* p) { return flat(p, 4, (long long)a.S + 1); }
 static View lse_view(const PackedArgs& a, const float* p) { return flat(a.Tq ? p : nullptr, 4, (long long)a.H * a.Tq); }
@@ -172,7 +193,9 @@ extern "C" {
 
 size_t sla2_packed_workspace_bytes(const sla2_packed_params* params, int backward) {
   PackedArgs a;
-  return (backward != 0 && backward != 1) || make_packed(params, &a) != SLA2_OK ? 0 : packed_bytes(a, backward != 0);
+  if ((backward != 0 && backward != 1) || make_packed(params, &a) != SLA2_OK) return 0;
+  const size_t fwd = packed_layout(&a, false, nullptr), bwd = backward ? packed_layout(&a, true, nullptr) : 0;
+  return fwd > bwd ? fwd : bwd;
 }
 
 int sla2_packed_forward(const sla2_packed_params* params, const void* q, const void* k, const void* v, const int32_t* q_start,
@@ -183,7 +206,7 @@ int sla2_packed_forward(const sla2_packed_params* params, const void* q, const v
   if ((a.Tq && (!q || !out)) || (a.Tk && (!k || !v)) || !q_start || !k_start) return SLA2_EINVAL;
   if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out)) return SLA2_EINVAL;
   if (misaligned4(q_start) || misaligned4(k_start) || misaligned4(lse_or_null)) return SLA2_EINVAL;
-  const size_t need = packed_bytes(a, false);
+  const size_t need = packed_layout(&a, false, workspace);
   const View in[5] = {q_view(a, q), kv_view(a, k), kv_view(a, v), starts_view(a, q_start), starts_view(a, k_start)};
   const Output outs[3] = {{out_view(a, out), {}}, {lse_view(a, lse_or_null), {}}, {flat(workspace, 1, (long long)need), {}}};
   if (aliased(outs, 3, in, 5)) return SLA2_EALIAS;
@@ -208,7 +231,7 @@ int sla2_packed_backward(const sla2_packed_params* params, const void* q, const 
   for (const void* p : {q, k, v, out, dout, (const void*)dq, (const void*)dk, (const void*)dv})
     if (misaligned16(p)) return SLA2_EINVAL;
   if (misaligned4(q_start) || misaligned4(k_start) || misaligned4(lse)) return SLA2_EINVAL;
-  const size_t need = packed_bytes(a, true);
+  const size_t need = packed_layout(&a, true, workspace);
   const View in[8] = {q_view(a, q), kv_view(a, k), kv_view(a, v), out_view(a, out), out_view(a, dout), lse_view(a, lse),
                       starts_view(a, q_start), starts_view(a, k_start)};
   const Output outs[4] = {{q_view(a, dq), {}}, {kv_view(a, dk), {}}, {kv_view(a, dv), {}}, {flat(workspace, 1, (long long)need), {}}};
@@ -225,7 +248,6 @@ int sla2_packed_backward(const sla2_packed_params* params, const void* q, const 
   a.dq = (uint16_t*)dq;
   a.dk = (uint16_t*)dk;
   a.dv = (uint16_t*)dv;
-  a.delta = (float*)workspace;
   return launch_packed_bwd(a, (hipStream_t)hip_stream) == hipSuccess ? SLA2_OK : SLA2_EHIP;
 }
 
