@@ -18,14 +18,14 @@ struct CacheArgs {
   long long kv_h, kv_t, q_h, q_b, out_h, out_b;
   int B, H, Hkv, group, d, pages, page_shift, max_pages, tokens, quant;
   float scale;
-  // attention: every workgroup takes `chunk` tokens of a sequence, there are `chunks` of them at most; with more than one the parts
-  // are in scratch: O [B, H, chunks, d] fp32 and (m, l) [B, H, chunks, 2]
-  int chunk, chunks;
+  // attention: the workgroups of a key head that share the tokens of all sequences (0: one for each sequence); with more than one, parts
+  // of sequences are in scratch: O [parts][2][H][d] fp32 and (m, l) [parts][2][H][2]
+  int parts;
   float *part_o, *part_ml;
 };
 
 void plan_cache_attention(CacheArgs* a);
-inline size_t cache_part_floats(const CacheArgs& a) { return a.chunks > 1 ? (size_t)a.B * a.H * a.chunks * (a.d + 2) : 0; }
+inline size_t cache_part_floats(const CacheArgs& a) { return a.parts > 1 ? (size_t)a.parts * 2 * a.H * (a.d + 2) : 0; }
 hipError_t launch_cache_write(const CacheArgs& a, hipStream_t stream);
 hipError_t launch_cache_read(const CacheArgs& a, hipStream_t stream);
 hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t stream);

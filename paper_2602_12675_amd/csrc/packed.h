@@ -22,8 +22,9 @@ struct PackedArgs {
   unsigned group_inv;                        // 2^32 / group, rounded up (group > 1)
   bool causal;
   float scale;                               // of the scores
-  // The steps of a tile's inner loop are dealt to this many workgroups, whose sums another kernel joins (1: none)
-  int q_parts, k_parts;
+  // The steps of a tile's inner loop are dealt to several workgroups, whose sums another kernel joins.  Of a tile of rows evenly to
+  // q_parts; of a tile of keys k_chunk steps to each, k_parts at most.  1: none
+  int q_parts, k_parts, k_chunk;
   // scratch.  Rows of all key heads: [Hkv][Tq group]; sums of parts: O or dQ [q_parts][rows][d], (m, l) [q_parts][rows][2], dK and dV
   // [2][k_parts][Tk][Hkv][d]
   float *lse2, *delta;                       // backward: lse log2(e) and D of every row
@@ -42,35 +43,41 @@ inline long long most_tiles(long long tokens, int sequences, int rows) {
 }
 
 #ifdef __HIPCC__
-// first row and number of rows of a sequence, whatever the offsets hold inside the tensor
-__device__ __forceinline__ int2 stretch_of(const int32_t* start, int s, int tokens) {
-  const int a = min(max(start[s], 0), tokens), b = min(max(start[s + 1], a), tokens);
-  return make_int2(a, b - a);
-}
-
-// The n-th tile, of `rows` rows, of the sequences one behind the other, each token being `group` rows: its sequence, its number in it and
-// how many that sequence has.  A wave looks at 64 sequences at a time; all lanes return the same.  s < 0: there are fewer tiles.
+// The n-th tile, of `rows` rows (of `rows` keys), of the sequences one behind the other: its number in its sequence, how many that one
+// has, and where its queries and keys lie, whatever the offsets hold inside the tensors.  A wave looks at 64 sequences at a time; all
+// lanes return the same.  tile < 0: there are fewer tiles.
 struct TilePlace {
-  int s, tile, tiles;
+  int tile, tiles, q0, nq, k0, nk;
 };
-__device__ __forceinline__ TilePlace find_tile(const int32_t* start, int S, int tokens, int group, int rows, int n, int lane) {
-  for (int s0 = 0; s0 < S; s0 += kWave) {
+template <bool KEYS> __device__ __forceinline__ TilePlace find_tile(const PackedArgs& a, int rows, int n, int lane) {
+  for (int s0 = 0; s0 < a.S; s0 += kWave) {
     const int s = s0 + lane;
-    const int own = s < S ? (int)(((unsigned)stretch_of(start, s, tokens).y * (unsigned)group + rows - 1) / (unsigned)rows) : 0;
+    int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
+    if (s < a.S) {
+      q0 = a.q_start[s], q1 = a.q_start[s + 1], k0 = a.k_start[s], k1 = a.k_start[s + 1];
+      q0 = min(max(q0, 0), a.Tq);
+      q1 = min(max(q1, q0), a.Tq);
+      k0 = min(max(k0, 0), a.Tk);
+      k1 = min(max(k1, k0), a.Tk);
+    }
+    const int own = (int)(((unsigned)(KEYS ? k1 - k0 : (q1 - q0) * a.group) + rows - 1) / (unsigned)rows);
     int sum = own;                                     // of the lanes up to this one
+    if (a.S > 1) {
 #pragma unroll
-    for (int by = 1; by < kWave; by *= 2) {
-      const int x = __shfl_up(sum, by);
-      sum += lane >= by ? x : 0;
+      for (int by = 1; by < kWave; by *= 2) {
+        const int x = __shfl_up(sum, by);
+        sum += lane >= by ? x : 0;
+      }
     }
     const unsigned long long has = __builtin_amdgcn_ballot_w64(sum > n);
     if (has) {
       const int f = __builtin_ctzll(has);
-      return TilePlace{s0 + f, n - __builtin_amdgcn_readlane(sum - own, f), __builtin_amdgcn_readlane(own, f)};
+      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, f); };
+      return TilePlace{n - of(sum - own), of(own), of(q0), of(q1 - q0), of(k0), of(k1 - k0)};
     }
     n -= __builtin_amdgcn_readlane(sum, kWave - 1);
   }
-  return TilePlace{-1, 0, 0};
+  return TilePlace{-1, 0, 0, 0, 0, 0};
 }
 
 // query and head (inside the group) of a row

@@ -1,21 +1,74 @@
 // Attention of one new token of each sequence over a paged cache of keys and values.
 //
-// Bound by the bytes of the cache, which are read once: a workgroup has a chunk of a sequence's tokens and a key head, with up to 16
-// query heads of its group as the 16 rows of the matrix products, and each of its waves works on blocks of 32 tokens by itself, from
-// registers alone: no operand passes through LDS, no barrier stands in the loop.
+// Bound by the bytes of the cache, which are read once: a workgroup has tokens of a sequence and a key head, with up to 16 query heads of
+// its group as the 16 rows of the matrix products, and each of its waves works on blocks of 32 tokens by itself, from registers alone:
+// no operand passes through LDS, no barrier stands in the loop.
 //   S^T = K Q^T (v_mfma_f32_16x16x32_bf16, 16 tokens a product): lane l feeds the token of row l % 16.  Row m of product t is token
 //   8 (m / 4) + 4 t + m % 4 of the block, so that lane l ends with head l % 16 and the scores of the 8 tokens 8 (l / 16) + 0..7: what it
 //   has to feed as P in O = P V.
 //   V: a lane reads D / 16 neighbouring channels of each of the same 8 tokens, whole rows a quarter wave, and turns its 8 x (D / 16)
 //   block in registers (v_perm_b32, two channels of two tokens at a time) into the operands of D / 16 products, the i-th of which has
 //   the channels D / 16 (l % 16) + i.
-// Codes become bf16 exactly; a token's scales multiply its scores and its probability.  Chunks of a sequence are joined by a second kernel.
+// Codes become bf16 exactly; a token's scales multiply its scores and its probability.  Parts of a sequence are joined by a second kernel.
+#include <limits.h>
+
 #include "cache.h"
 #include "mfma_tiles.h"
 
 namespace sla2 {
 
-constexpr int kDecodeWaves = 4, kDecodeBlock = 32, kMaxChunk = 1024, kHeadRows = 16;
+constexpr int kDecodeWaves = 4, kDecodeBlock = 32, kHeadRows = 16;
+constexpr int kIdBlocks = 32;                // blocks whose pages a wave holds, one for 16 tokens a lane
+
+// What is worked on: the blocks of all sequences one behind the other, each sequence with kOverhead blocks' worth of time in front of its
+// own (first reads, the joining of the waves).  Of this line every one of a.parts workgroups (of a key head) has an equal stretch, whatever
+// the lengths: whole sequences, and at its two ends parts of one, which go into slot 0 (a sequence that began before the stretch) or
+// slot 1 (one that goes on behind it) of the workgroup.
+constexpr int kOverhead = 6;
+__device__ __forceinline__ int tokens_of(const CacheArgs& a, int b) {
+  return (int)min((long long)max(a.length[b], 0), (long long)a.max_pages << a.page_shift);
+}
+__device__ __forceinline__ int blocks_of(int tokens) { return (int)(((unsigned)tokens + kDecodeBlock - 1) / kDecodeBlock); }
+__device__ __forceinline__ long long wave_total(long long x) {
+#pragma unroll
+  for (int by = 1; by < kWave; by *= 2) x += __shfl_xor(x, by);
+  return x;
+}
+__device__ __forceinline__ long long uniform64(long long x) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x), hi = __builtin_amdgcn_readfirstlane((unsigned)((unsigned long long)x >> 32));
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
+// the length of the line; all lanes of the wave take part
+__device__ __forceinline__ long long line_length(const CacheArgs& a, int lane) {
+  long long n = 0;
+  for (int b = lane; b < a.B; b += kWave) n += kOverhead + blocks_of(tokens_of(a, b));
+  return wave_total(n);
+}
+// The sequence that place x of the line is in, and where on the line it begins; with `of` >= 0 where sequence `of` begins.
+struct OnLine {
+  int b;
+  long long at;
+};
+__device__ __forceinline__ OnLine on_line(const CacheArgs& a, long long x, int of, int lane) {
+  long long at = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    const int b = b0 + lane;
+    const int own = b < a.B ? kOverhead + blocks_of(tokens_of(a, b)) : 0;
+    long long sum = own;
+#pragma unroll
+    for (int by = 1; by < kWave; by *= 2) {
+      const long long y = __shfl_up(sum, by);
+      sum += lane >= by ? y : 0;
+    }
+    const unsigned long long has = of >= 0 ? (of < b0 + kWave ? 1ull << (of - b0) : 0) : __builtin_amdgcn_ballot_w64(at + sum > x);
+    if (has) {
+      const int f = __builtin_ctzll(has);
+      return OnLine{b0 + f, at + __shfl(sum - own, f)};
+    }
+    at += __shfl(sum, kWave - 1);
+  }
+  return OnLine{a.B, at};
+}
 
 __device__ __forceinline__ float over_quarters_max(float x) {       // lanes l, l ^ 16, l ^ 32, l ^ 48
   const unsigned u = __builtin_bit_cast(unsigned, x);
@@ -58,51 +111,37 @@ template <int BYTES> __device__ __forceinline__ void load_words(const void* p, u
   }
 }
 
+// What a wave keeps of 16 query heads: O (rows 4 (l / 16) + 0..3 of the i-th product's channels), the reference m of the exponentials and the
+// sum l of this lane's tokens, of head l % 16.
+template <int D> struct HeadSums {
+  f32x4 o[D / 16];
+  float m, l;
+};
+
+// The blocks lo + w, lo + w + 4, .. below hi of sequence b, of which it reads the tokens below `end`
 template <int D, int QUANT>
-__global__ __launch_bounds__(kDecodeWaves * kWave) void cache_attention_kernel(CacheArgs a) {
+__device__ __forceinline__ void attend_blocks(const CacheArgs& a, int b, int hk, int lo, int hi, int end, const bf16x8 (&qf)[D / 32], HeadSums<D>& sums,
+                                              int w, int lane) {
   constexpr int ESZ = QUANT == SLA2_QUANT_NONE ? 2 : 1;
   constexpr int KE = QUANT == SLA2_QUANT_NONE ? 8 : 16;            // channels of a 16-byte read of a key
-  constexpr int KL = D / (4 * KE), KS = D / 32;                    // reads and products of a key row
+  constexpr int KL = D / (4 * KE);                                 // reads of a key row
   constexpr int C = D / 16;                                        // channels of a lane's read of a value row
-  __shared__ float part[kDecodeWaves][kHeadRows][D + 4];           // a wave's O, m and l
-  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave), g = lane / 16, n = lane % 16;
-  const int tiles = (a.group + kHeadRows - 1) / kHeadRows;         // of query heads
-  const int hk = blockIdx.y / tiles, row0 = blockIdx.y % tiles * kHeadRows, rows = min(kHeadRows, a.group - row0);
-  const int b = blockIdx.z;
-  const long long most = (long long)a.max_pages << a.page_shift;
-  const int len = (int)min((long long)max(a.length[b], 0), most);
-  const int begin = blockIdx.x * a.chunk, end = min(len, begin + a.chunk);
-  if (begin >= end && blockIdx.x) return;
-  const int h0 = hk * a.group + row0;                              // first query head
-  // Q as B operand: lane <- head l % 16, the channels that its reads of a key have
-  bf16x8 qf[KS];
-  {
-    const uint16_t* src = a.q + (size_t)b * a.q_b + (size_t)(h0 + min(n, rows - 1)) * a.q_h;
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++) {
-      const int c = KE == 8 ? 32 * ks + 8 * g : 64 * (ks / 2) + 16 * g + 8 * (ks % 2);
-      qf[ks] = *reinterpret_cast<const bf16x8*>(src + c);
-    }
-  }
-  // the pages of the chunk, 16 tokens a lane
-  int id = -1;
-  {
-    const long long column = ((long long)begin + 16 * lane) >> a.page_shift;
-    if (begin + 16 * lane < end) id = a.table[b * a.table_stride + column];
-  }
-  f32x4 oacc[C];
-#pragma unroll
-  for (int i = 0; i < C; i++) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = -1e30f, l_run = 0.f;                               // of head l % 16; l: of this lane's tokens
+  const int g = lane / 16, n = lane % 16, slot_mask = (1 << a.page_shift) - 1;
   const float c1 = kLog2e * a.scale;
   const char* kc = (const char*)a.kc + hk * a.head_stride * ESZ;
   const char* vc = (const char*)a.vc + hk * a.head_stride * ESZ;
-  const int slot_mask = (1 << a.page_shift) - 1;
-  for (int t0 = begin + w * kDecodeBlock; t0 < end; t0 += kDecodeWaves * kDecodeBlock) {
-    const int i0 = (t0 - begin) / 16;
+  f32x4(&oacc)[C] = sums.o;
+  int id = -1;                                                     // the pages of the next 32 blocks, 16 tokens a lane
+  for (int block = lo + w, c0 = lo - kIdBlocks; block < hi; block += kDecodeWaves) {
+    if (block >= c0 + kIdBlocks) {
+      c0 += kIdBlocks;
+      const unsigned t = (unsigned)c0 * kDecodeBlock + 16 * lane;
+      id = t < (unsigned)end ? a.table[b * a.table_stride + (t >> a.page_shift)] : -1;
+    }
+    const int t0 = block * kDecodeBlock, i0 = 2 * (block - c0);
     int p0 = __builtin_amdgcn_readlane(id, i0), p1 = __builtin_amdgcn_readlane(id, i0 + 1);
     const bool ok0 = p0 >= 0 && p0 < a.pages, ok1 = p1 >= 0 && p1 < a.pages;
-    const bool whole = ok0 && ok1 && t0 + kDecodeBlock <= end;
+    const bool whole = ok0 && ok1 && end - t0 >= kDecodeBlock;
     p0 = ok0 ? p0 : 0;
     p1 = ok1 ? p1 : p0;
     const int s0 = t0 & slot_mask, s1 = (t0 + 16) & slot_mask;
@@ -172,10 +211,10 @@ __global__ __launch_bounds__(kDecodeWaves * kWave) void cache_attention_kernel(C
 #pragma unroll
     for (int j = 1; j < 8; j++) mx = fmaxf(mx, sc[j]);
     mx = over_quarters_max(mx) * c1;
-    if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {           // the reference is kept while the maximum stays within 2^8 of it
-      const float m_new = fmaxf(m_run, mx), corr = fast_exp2(m_run - m_new);
-      m_run = m_new;
-      l_run *= corr;
+    if (__builtin_amdgcn_ballot_w64(mx > sums.m + 8.f)) {           // the reference is kept while the maximum stays within 2^8 of it
+      const float m_new = fmaxf(sums.m, mx), corr = fast_exp2(sums.m - m_new);
+      sums.m = m_new;
+      sums.l *= corr;
 #pragma unroll
       for (int r = 0; r < 4; r++) {
         const float cr = __shfl(corr, 4 * g + r);                  // of the head of this accumulator row
@@ -186,8 +225,8 @@ __global__ __launch_bounds__(kDecodeWaves * kWave) void cache_attention_kernel(C
     bf16x8 pf;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-      const float p = fast_exp2(sc[j] * c1 - m_run);
-      l_run += p;
+      const float p = fast_exp2(sc[j] * c1 - sums.m);
+      sums.l += p;
       if constexpr (QUANT == SLA2_QUANT_NONE) pf[j] = (__bf16)p;
       else pf[j] = (__bf16)(p * vs[j]);
     }
@@ -211,67 +250,116 @@ __global__ __launch_bounds__(kDecodeWaves * kWave) void cache_attention_kernel(C
       oacc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf, __builtin_bit_cast(bf16x8, v4), oacc[i], 0, 0, 0);
     }
   }
-  // ---- the waves' parts ----
-  l_run = over_quarters_sum(l_run);
-  if (g == 0) {
-    part[w][n][D] = m_run;
-    part[w][n][D + 1] = l_run;
+}
+
+template <int D, int QUANT>
+__global__ __launch_bounds__(kDecodeWaves * kWave, 2) void cache_attention_kernel(CacheArgs a) {
+  constexpr int KE = QUANT == SLA2_QUANT_NONE ? 8 : 16;            // channels of a 16-byte read of a key
+  constexpr int KS = D / 32;                                       // products of a key row
+  constexpr int C = D / 16;                                        // channels of a lane's read of a value row
+  __shared__ float part[kDecodeWaves][kHeadRows][D + 4];           // a wave's O, m and l
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave), g = lane / 16, n = lane % 16;
+  const int tiles = (a.group + kHeadRows - 1) / kHeadRows;         // of query heads
+  const int hk = blockIdx.y / tiles, row0 = blockIdx.y % tiles * kHeadRows, rows = min(kHeadRows, a.group - row0);
+  const int h0 = hk * a.group + row0;                              // first query head
+  // this workgroup's stretch [x, y) of the line; without parts: one sequence
+  long long x = 0, y = LLONG_MAX, at = 0;
+  int b = blockIdx.x;
+  if (a.parts) {
+    const long long all = uniform64(line_length(a, lane));
+    x = all * blockIdx.x / a.parts;
+    y = all * (blockIdx.x + 1) / a.parts;
+    if (x == y) return;
+    const OnLine o = on_line(a, x, -1, lane);
+    b = __builtin_amdgcn_readfirstlane(o.b);
+    at = uniform64(o.at);
   }
+  const int b_end = a.parts ? a.B : b + 1;
+  for (; b < b_end && at < y; b++) {
+    const int len = __builtin_amdgcn_readfirstlane(tokens_of(a, b)), nb = blocks_of(len);
+    const long long first = at + kOverhead;                        // the place of its first block
+    const bool begins = at >= x;
+    at = first + nb;
+    const int lo = (int)min((long long)nb, max(0ll, x - first)), hi = (int)min((long long)nb, max(0ll, y - first));
+    if (lo >= hi && !(nb == 0 && begins)) continue;
+    // Q as B operand: lane <- head l % 16, the channels that its reads of a key have
+    bf16x8 qf[KS];
+    const uint16_t* src = a.q + (size_t)b * a.q_b + (size_t)(h0 + min(n, rows - 1)) * a.q_h;
 #pragma unroll
-  for (int r = 0; r < 4; r++)
-    if (4 * g + r < rows) {
+    for (int ks = 0; ks < KS; ks++)
+      qf[ks] = *reinterpret_cast<const bf16x8*>(src + (KE == 8 ? 32 * ks + 8 * g : 64 * (ks / 2) + 16 * g + 8 * (ks % 2)));
+    HeadSums<D> sums;
 #pragma unroll
-      for (int i = 0; i < C; i++) part[w][4 * g + r][C * n + i] = oacc[i][r];
+    for (int i = 0; i < C; i++) sums.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    sums.m = -1e30f;
+    sums.l = 0.f;
+    attend_blocks<D, QUANT>(a, b, hk, lo, hi, (int)min((unsigned)len, (unsigned)hi * kDecodeBlock), qf, sums, w, lane);
+    // ---- the waves' parts ----
+    sums.l = over_quarters_sum(sums.l);
+    if (g == 0) {
+      part[w][n][D] = sums.m;
+      part[w][n][D + 1] = sums.l;
     }
-  __syncthreads();
-  for (int idx = tid; idx < rows * (D / 2); idx += kDecodeWaves * kWave) {
-    const int row = idx / (D / 2), c = idx % (D / 2) * 2, h = h0 + row;
-    float m = part[0][row][D];
 #pragma unroll
-    for (int x = 1; x < kDecodeWaves; x++) m = fmaxf(m, part[x][row][D]);
-    float l = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int r = 0; r < 4; r++)
+      if (4 * g + r < rows) {
 #pragma unroll
-    for (int x = 0; x < kDecodeWaves; x++) {
-      const float by = fast_exp2(part[x][row][D] - m);
-      l += by * part[x][row][D + 1];
-      o0 += by * part[x][row][c];
-      o1 += by * part[x][row][c + 1];
+        for (int i = 0; i < C; i++) part[w][4 * g + r][C * n + i] = sums.o[i][r];
+      }
+    __syncthreads();
+    for (int idx = tid; idx < rows * (D / 2); idx += kDecodeWaves * kWave) {
+      const int row = idx / (D / 2), c = idx % (D / 2) * 2, h = h0 + row;
+      float m = part[0][row][D];
+#pragma unroll
+      for (int x = 1; x < kDecodeWaves; x++) m = fmaxf(m, part[x][row][D]);
+      float l = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+      for (int x = 0; x < kDecodeWaves; x++) {
+        const float by = fast_exp2(part[x][row][D] - m);
+        l += by * part[x][row][D + 1];
+        o0 += by * part[x][row][c];
+        o1 += by * part[x][row][c + 1];
+      }
+      if (lo > 0 || hi < nb) {
+        const size_t slot = ((size_t)blockIdx.x * 2 + (lo > 0 ? 0 : 1)) * a.H + h;
+        *(float2*)(a.part_o + slot * D + c) = make_float2(o0, o1);
+        if (c == 0) *(float2*)(a.part_ml + 2 * slot) = make_float2(m, l);
+      } else {
+        const bool any = l != 0.f;
+        const float inv = any ? 1.f / l : 0.f;
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+        *(bf16x2*)(a.out + (size_t)b * a.out_b + (size_t)h * a.out_h + c) = bf16x2{(__bf16)(any ? o0 * inv : 0.f), (__bf16)(any ? o1 * inv : 0.f)};
+        if (a.lse && c == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
+      }
     }
-    if (a.chunks > 1) {
-      const size_t at = ((size_t)b * a.H + h) * a.chunks + blockIdx.x;
-      *(float2*)(a.part_o + at * D + c) = make_float2(o0, o1);
-      if (c == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
-    } else {
-      const bool any = l != 0.f;
-      const float inv = any ? 1.f / l : 0.f;
-      typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-      *(bf16x2*)(a.out + (size_t)b * a.out_b + (size_t)h * a.out_h + c) = bf16x2{(__bf16)(any ? o0 * inv : 0.f), (__bf16)(any ? o1 * inv : 0.f)};
-      if (a.lse && c == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
-    }
+    __syncthreads();
   }
 }
 
-// The chunks of one sequence and head: their O, weighted with e^(m - the largest m), over their l, weighted alike.
+// A sequence and head whose blocks several workgroups had: their O, weighted with 2^(m - the largest m), over their l, weighted alike.
 constexpr int kJoinWaves = 8;
 template <int D>
 __global__ __launch_bounds__(kJoinWaves * kWave) void cache_join_kernel(CacheArgs a) {
   constexpr int E = D / kWave;                                     // channels of a lane
   __shared__ float part[kJoinWaves][D + 1];
   const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, h = blockIdx.x, b = blockIdx.y;
-  const long long most = (long long)a.max_pages << a.page_shift;
-  const int len = (int)min((long long)max(a.length[b], 0), most);
-  const int n = max(1, (len + a.chunk - 1) / a.chunk);             // the first chunk's part is there in any case
-  const size_t at = ((size_t)b * a.H + h) * a.chunks;
+  const int nb = blocks_of(tokens_of(a, b));
+  if (!nb) return;
+  const long long all = line_length(a, lane), first = on_line(a, 0, b, lane).at + kOverhead;
+  // workgroup p has place f of the line if all p / parts, rounded down, is the last of these up to f
+  const int p0 = (int)(((first + 1) * a.parts - 1) / all), p1 = (int)(((first + nb) * a.parts - 1) / all);
+  if (p0 == p1) return;                                            // written by the one that had it
+  auto slot = [&](int p) { return ((size_t)p * 2 + (p == p0 ? 1 : 0)) * a.H + h; };
   float m = -INFINITY;
-  for (int i = lane; i < n; i += kWave) m = fmaxf(m, a.part_ml[2 * (at + i)]);
+  for (int p = p0 + lane; p <= p1; p += kWave) m = fmaxf(m, a.part_ml[2 * slot(p)]);
   m = wave_max(m);
   float l = 0.f, o[E] = {};
-  for (int i = w; i < n; i += kJoinWaves) {
-    const float2 ml = *(const float2*)(a.part_ml + 2 * (at + i));
+  for (int p = p0 + w; p <= p1; p += kJoinWaves) {
+    const float2 ml = *(const float2*)(a.part_ml + 2 * slot(p));
     const float by = fast_exp2(ml.x - m);
     l += by * ml.y;
 #pragma unroll
-    for (int e = 0; e < E; e++) o[e] += by * a.part_o[(at + i) * D + E * lane + e];
+    for (int e = 0; e < E; e++) o[e] += by * a.part_o[slot(p) * D + E * lane + e];
   }
 #pragma unroll
   for (int e = 0; e < E; e++) part[w][E * lane + e] = o[e];
@@ -290,18 +378,19 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void cache_join_kernel(CacheArg
   if (a.lse && tid == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(total)) * (1.f / kLog2e) : -INFINITY;
 }
 
-// Chunks: as long as two workgroups a CU allow, in steps of 128 tokens.
+// Sequences of at most 1,024 tokens: a workgroup each.  Longer ones: as many workgroups as two to a CU are, which share the line.
 void plan_cache_attention(CacheArgs* a) {
-  const long long most = (long long)a->max_pages << a->page_shift;
-  const long long heads = (long long)a->B * a->Hkv * ((a->group + kHeadRows - 1) / kHeadRows);
-  long long chunk = kMaxChunk;
-  while (chunk > 256 && heads * ((most + chunk - 1) / chunk) < 512) chunk /= 2;
-  a->chunk = (int)chunk;
-  a->chunks = (int)((most + chunk - 1) / chunk);
+  const long long most = (long long)a->max_pages << a->page_shift, heads = (long long)a->Hkv * ((a->group + kHeadRows - 1) / kHeadRows);
+  a->parts = 0;
+  if (most <= 1024) return;
+  const long long blocks = a->B * ((most + kDecodeBlock - 1) / kDecodeBlock);
+  long long parts = 512 / heads;
+  if (parts > blocks / 16) parts = blocks / 16;                    // 4 blocks a wave at least
+  a->parts = parts < 1 ? 1 : (int)parts;
 }
 
 hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t stream) {
-  const dim3 grid(a.chunks, a.Hkv * ((a.group + kHeadRows - 1) / kHeadRows), a.B);
+  const dim3 grid(a.parts ? a.parts : a.B, a.Hkv * ((a.group + kHeadRows - 1) / kHeadRows));
 #define SLA2_DECODE(D)                                                                                                          \
   (a.quant == SLA2_QUANT_NONE  ? cache_attention_kernel<D, SLA2_QUANT_NONE><<<grid, kDecodeWaves * kWave, 0, stream>>>(a)       \
    : a.quant == SLA2_QUANT_FP8 ? cache_attention_kernel<D, SLA2_QUANT_FP8><<<grid, kDecodeWaves * kWave, 0, stream>>>(a)        \
@@ -309,7 +398,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t stream) {
   if (a.d == 128) SLA2_DECODE(128);
   else SLA2_DECODE(64);
 #undef SLA2_DECODE
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.chunks == 1) return e;
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.parts <= 1) return e;
   const dim3 heads(a.H, a.B);
   if (a.d == 128) cache_join_kernel<128><<<heads, kJoinWaves * kWave, 0, stream>>>(a);
   else cache_join_kernel<64><<<heads, kJoinWaves * kWave, 0, stream>>>(a);

@@ -3,8 +3,9 @@
 // One workgroup = 4 waves = 128 rows of one key head and sequence (packed.h); a wave has 32 of them, one on lanes l and l + 32.  One
 // pass over the keys, 64 at a time, with the running maximum and sum of the softmax: S^T = K Q^T (keys x rows), so that a lane holds
 // scores of one row, P^T goes back into O^T += V^T P^T as it lies in the registers, and a row's maximum and sum are its lane's own and
-// one exchange with the other half of the wave.  K and V tiles go from memory into LDS past the registers, one tile ahead; two
-// workgroups share a CU, so that one's products run beside the other's exponentials.
+// one exchange with the other half of the wave.  K and V tiles go from memory into LDS past the registers: V into one of two buffers,
+// a tile ahead, K into its one buffer behind the scores.  So two workgroups (d = 64: four) fit a CU, and one's products run beside
+// another's exponentials, first reads and results.
 #include "packed.h"
 
 namespace sla2 {
@@ -12,12 +13,12 @@ namespace sla2 {
 template <int D> struct PackedSmem {
   static constexpr int kTile = PackedTile<D>::kTileBytes;
   static constexpr int kLd = D + 8;
-  static constexpr int kBytes = 4 * kTile;                     // two buffers of (K, V); afterwards the output tile [128][D + 8]
+  static constexpr int kBytes = 3 * kTile;                     // K, two of V; afterwards the output tile [128][D + 8]
   static_assert(kRowTile * kLd * 2 <= kBytes, "");
 };
 
 template <int D, bool PARTS>
-__global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedArgs a) {
   constexpr int NW = 4, KS = D / 16, ET = D / 32, LD = D + 8;
   typedef PackedSmem<D> SM;
   typedef PackedTile<D> SL;
@@ -26,14 +27,13 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const TileHead th = tile_head(blockIdx.x, a.Hkv);
   const int hk = th.head;
-  TilePlace at = find_tile(a.q_start, a.S, a.Tq, a.group, kRowTile, th.tile, lane);
-  if (at.s < 0) return;
+  TilePlace at = find_tile<false>(a, kRowTile, th.tile, lane);
+  if (at.tile < 0) return;
   if (a.causal) at.tile = at.tiles - 1 - at.tile;      // the longest first
-  const int2 qs = stretch_of(a.q_start, at.s, a.Tq), kx = stretch_of(a.k_start, at.s, a.Tk);
-  const int nr = qs.y * a.group, nk = kx.y, row0 = at.tile * kRowTile, row = row0 + 32 * w + lane % 32;
-  const uint16_t* kh = a.k + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
-  const uint16_t* vh = a.v + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
-  const int past = nk - qs.y;                          // query i reads the keys below i + past + 1 (causal), all otherwise
+  const int nr = at.nq * a.group, nk = at.nk, row0 = at.tile * kRowTile, row = row0 + 32 * w + lane % 32;
+  const uint16_t* kh = a.k + (size_t)hk * a.skv.h + (size_t)at.k0 * a.skv.t;
+  const uint16_t* vh = a.v + (size_t)hk * a.skv.h + (size_t)at.k0 * a.skv.t;
+  const int past = nk - at.nq;                          // query i reads the keys below i + past + 1 (causal), all otherwise
   const int2 my = query_of(a, min(row, nr - 1));       // this lane's query and head
   const int mine = a.causal ? min(nk, my.x + past + 1) : nk;
   // the keys that the tile, and this wave, have to do with: below ..; and those that all rows of the wave read
@@ -46,16 +46,19 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
     t_begin = (int)((long long)n * blockIdx.y / a.q_parts);
     t_end = (int)((long long)n * (blockIdx.y + 1) / a.q_parts);
   }
-  auto kbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
-  auto dma = [&](int t) {                              // rows past the end repeat the last one: their scores are masked
-    const int t0 = t * kTileTokens, valid = min(kTileTokens, nk - t0), ln = (int)lane_again();
-    dma_tile<D, NW, SL>(kh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t), w, ln);
-    dma_tile<D, NW, SL>(vh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t) + SM::kTile, w, ln);
+  const unsigned kbuf = lds_address(smem);
+  auto vbuf = [&](int t) { return kbuf + (1 + (t & 1)) * SM::kTile; };
+  auto dma = [&](const uint16_t* src, int t, unsigned to) {     // rows past the end repeat the last one: their scores are masked
+    const int t0 = t * kTileTokens;
+    dma_tile<D, NW, SL>(src + (size_t)t0 * a.skv.t, a.skv.t, min(kTileTokens, nk - t0), to, w, (int)lane_again());
   };
-  if (t_begin < t_end) dma(t_begin);
+  if (t_begin < t_end) {
+    dma(kh, t_begin, kbuf);
+    dma(vh, t_begin, vbuf(t_begin));
+  }
   bf16x8 qf[KS];                                       // B operand: lane <- Q[row][16 ks + 8 g + 0..7]
   {
-    const uint16_t* src = a.q + (size_t)(hk * a.group + my.y) * a.sq.h + (size_t)(qs.x + my.x) * a.sq.t + 8 * g;
+    const uint16_t* src = a.q + (size_t)(hk * a.group + my.y) * a.sq.h + (size_t)(at.q0 + my.x) * a.sq.t + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
   }
@@ -72,12 +75,13 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
   for (int ks = 0; ks < KS; ks++) settle(qf[ks]);
   phase_barrier();
   for (int t = t_begin; t < t_end; t++) {
-    if (t + 1 < t_end) dma(t + 1);
+    if (t + 1 < t_end) dma(vh, t + 1, vbuf(t + 1));
     const int t0 = t * kTileTokens;
-    if (t0 < w_keys) {
+    const bool work = t0 < w_keys;
+    if (work) {
       // S^T = K Q^T, two 32-key halves; reads run two steps ahead
       {
-        const unsigned ka = kbuf(t) + k_off;
+        const unsigned ka = kbuf + k_off;
         constexpr int KA = 2;
         u32x4 kr[KA + 1][2];
 #pragma unroll
@@ -104,6 +108,10 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
           }
         }
       }
+    }
+    phase_barrier();                                   // K has been read
+    if (t + 1 < t_end) dma(kh, t + 1, kbuf);
+    if (work) {
       if (t0 + kTileTokens > w_full) {
 #pragma unroll
         for (int mt = 0; mt < 2; mt++)
@@ -146,7 +154,7 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
       // O^T += V^T P^T: fragment (ks, et) = two transposing reads, kept three fragments ahead of the products
       {
         constexpr int kAhead = 3, kFrags = (kTileTokens / 16) * ET;
-        const unsigned va_lo = kbuf(t) + SM::kTile + v_lo, va_hi = kbuf(t) + SM::kTile + v_hi;
+        const unsigned va_lo = vbuf(t) + v_lo, va_hi = vbuf(t) + v_hi;
         u32x2 vlo[kAhead + 1], vhi[kAhead + 1];
         auto issue = [&](int f) {
           vlo[f % (kAhead + 1)] = lds_read_tr_untracked_at<16 * D * 2>(va_lo ^ (64u * (f % ET)), f / ET);
@@ -171,17 +179,19 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
     phase_barrier();
   }
   const bool any = l_run != 0.f;                       // NaN is some
-  const size_t row_at = (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group + row;       // among the rows of all key heads
+  // from here on the lane's place is made again: it is not kept through the loop
+  const int ln = (int)lane_again(), ge = ln / 32, rowe = row0 + 32 * w + ln % 32;
   if (PARTS) {
-    if (row >= nr) return;
-    float* dst = a.part_o + ((size_t)blockIdx.y * a.Tq * a.H + row_at) * D;
+    if (rowe >= nr) return;
+    const size_t row_at = (size_t)blockIdx.y * a.Tq * a.H + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + rowe;   // among the rows of all key heads
+    float* dst = a.part_o + row_at * D;
 #pragma unroll
     for (int et = 0; et < ET; et++)
 #pragma unroll
       for (int v4 = 0; v4 < 4; v4++)
-        *reinterpret_cast<f32x4*>(dst + 32 * et + 8 * v4 + 4 * g) =
+        *reinterpret_cast<f32x4*>(dst + 32 * et + 8 * v4 + 4 * ge) =
             f32x4{oacc[et][4 * v4], oacc[et][4 * v4 + 1], oacc[et][4 * v4 + 2], oacc[et][4 * v4 + 3]};
-    if (g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)blockIdx.y * a.Tq * a.H + row_at)) = make_float2(m_run, l_run);
+    if (ge == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * row_at) = make_float2(m_run, l_run);
     return;
   }
   // ---- normalise, transpose through LDS, whole rows out ----
@@ -194,17 +204,19 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedArgs a) {
       bf16x4 pk;
 #pragma unroll
       for (int r = 0; r < 4; r++) pk[r] = (__bf16)(any ? inv * oacc[et][4 * v4 + r] : 0.f);
-      *reinterpret_cast<bf16x4*>(os + (32 * w + lane % 32) * LD + 32 * et + 8 * v4 + 4 * g) = pk;
+      *reinterpret_cast<bf16x4*>(os + (32 * w + ln % 32) * LD + 32 * et + 8 * v4 + 4 * ge) = pk;
     }
-  if (a.lse_out && g == 0 && row < nr)
-    a.lse_out[(size_t)(hk * a.group + my.y) * a.Tq + qs.x + my.x] = any ? (m_run + log2f(l_run)) * (1.f / kLog2e) : -INFINITY;
+  if (a.lse_out && ge == 0 && rowe < nr) {
+    const int2 x = query_of(a, rowe);
+    a.lse_out[(size_t)(hk * a.group + x.y) * a.Tq + at.q0 + x.x] = any ? (m_run + log2f(l_run)) * (1.f / kLog2e) : -INFINITY;
+  }
   wave_lds_fence();                                    // a wave stores the rows that it wrote
 #pragma unroll
   for (int i = 0; i < 32 * (D / 8) / kWave; i++) {
-    const int idx = lane + kWave * i, r = 32 * w + idx / (D / 8), ch = idx % (D / 8);
+    const int idx = ln + kWave * i, r = 32 * w + idx / (D / 8), ch = idx % (D / 8);
     if (row0 + r >= nr) continue;
     const int2 x = query_of(a, row0 + r);
-    *reinterpret_cast<u32x4*>(a.o + (size_t)(hk * a.group + x.y) * a.so.h + (size_t)(qs.x + x.x) * a.so.t + 8 * ch) =
+    *reinterpret_cast<u32x4*>(a.o + (size_t)(hk * a.group + x.y) * a.so.h + (size_t)(at.q0 + x.x) * a.so.t + 8 * ch) =
         *reinterpret_cast<const u32x4*>(os + r * LD + 8 * ch);
   }
 }
@@ -237,18 +249,26 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   if (a.lse_out && lane == 0) a.lse_out[(size_t)h * a.Tq + x.x] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
 }
 
-// Parts: as many as fill two workgroups a CU where the tiles alone do not fill half of them, none shorter than 256 keys or rows.
+// Parts of a tile of rows: as many as fill two workgroups a CU where the tiles alone do not fill half of them, none shorter than 256 keys.
+// Parts of a tile of keys: so that no workgroup has much more than its share of all steps, which with a causal mask or sequences of
+// different lengths the first tiles have.
 void plan_packed(PackedArgs* a, bool backward) {
   a->q_parts = a->k_parts = 1;
   const long long rows = (long long)a->Tq * a->group, places = 512;
   const long long q_tiles = most_tiles(rows, a->S, kRowTile) * a->Hkv, k_tiles = most_tiles(a->Tk, a->S, kKeyTile) * a->Hkv;
-  auto parts = [&](long long tiles, long long length) {
-    if (!tiles || tiles * 2 > places) return 1;
-    const long long n = places / tiles, most = length / 256;
-    return (int)(n < most ? n : most < 1 ? 1 : most);
-  };
-  a->q_parts = parts(q_tiles, a->Tk);
-  if (backward) a->k_parts = parts(k_tiles, rows);
+  if (q_tiles && q_tiles * 2 <= places) {
+    const long long n = places / q_tiles, most = a->Tk / 256;
+    a->q_parts = (int)(n < most ? n : most < 1 ? 1 : most);
+  }
+  if (!backward || !k_tiles || !rows) return;
+  // Steps of 64 rows of all tiles of keys, were the sequences alike, over the places, and a little more, so that the last round is not
+  // a few workgroups; at most 16 parts of the longest sequence that there can be.
+  const long long steps = (rows + 63) / 64, all = (a->Tk + kKeyTile - 1) / kKeyTile * a->Hkv * ((steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
+  long long chunk = all / places + all / (places * 12) + 1;
+  if (chunk < 16) chunk = 16;
+  if (chunk < (steps + 15) / 16) chunk = (steps + 15) / 16;
+  a->k_chunk = (int)chunk;
+  a->k_parts = (int)((steps + chunk - 1) / chunk);
 }
 
 template <int D> static hipError_t launch_fwd(const PackedArgs& a, hipStream_t stream) {

@@ -86,14 +86,13 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const TileHead th = tile_head(blockIdx.x, a.Hkv);
   const int hk = th.head;
-  TilePlace at = find_tile(a.q_start, a.S, a.Tq, a.group, kRowTile, th.tile, lane);
-  if (at.s < 0) return;
+  TilePlace at = find_tile<false>(a, kRowTile, th.tile, lane);
+  if (at.tile < 0) return;
   if (a.causal) at.tile = at.tiles - 1 - at.tile;      // the longest first
-  const int2 qs = stretch_of(a.q_start, at.s, a.Tq), kx = stretch_of(a.k_start, at.s, a.Tk);
-  const int nr = qs.y * a.group, nk = kx.y, row0 = at.tile * kRowTile, row = row0 + 32 * w + lane % 32;
-  const uint16_t* kh = a.k + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
-  const uint16_t* vh = a.v + (size_t)hk * a.skv.h + (size_t)kx.x * a.skv.t;
-  const int past = nk - qs.y;
+  const int nr = at.nq * a.group, nk = at.nk, row0 = at.tile * kRowTile, row = row0 + 32 * w + lane % 32;
+  const uint16_t* kh = a.k + (size_t)hk * a.skv.h + (size_t)at.k0 * a.skv.t;
+  const uint16_t* vh = a.v + (size_t)hk * a.skv.h + (size_t)at.k0 * a.skv.t;
+  const int past = nk - at.nq;
   const int2 my = query_of(a, min(row, nr - 1));
   const int mine = a.causal ? min(nk, my.x + past + 1) : nk;
   const int keys = a.causal ? min(nk, max(0, query_of(a, min(row0 + kRowTile, nr) - 1).x + past + 1)) : nk;
@@ -114,8 +113,8 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
   if (t_begin < t_end) dma(t_begin);
   bf16x8 qf[KS], gf[KS];
   float delta = 0.f;
-  const size_t row_at = (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group + row;       // among the rows of all key heads
-  const int h = hk * a.group + my.y, token = qs.x + my.x;
+  const size_t row_at = (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + row;       // among the rows of all key heads
+  const int h = hk * a.group + my.y, token = at.q0 + my.x;
   {
     const uint16_t* src = a.q + (size_t)h * a.sq.h + (size_t)token * a.sq.t + 8 * g;
     const uint16_t* gsrc = a.dout + (size_t)h * a.so.h + (size_t)token * a.so.t + 8 * g;
@@ -210,7 +209,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
   store_rows<D>(acc, a.scale, reinterpret_cast<uint16_t*>(smem) + w * 32 * SM::kLd, lane, [&](int r) -> uint16_t* {
     if (w_row + r >= nr) return nullptr;
     const int2 x = query_of(a, w_row + r);
-    return a.dq + (size_t)(hk * a.group + x.y) * a.sq.h + (size_t)(qs.x + x.x) * a.sq.t;
+    return a.dq + (size_t)(hk * a.group + x.y) * a.sq.h + (size_t)(at.q0 + x.x) * a.sq.t;
   });
 }
 
@@ -227,24 +226,24 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const TileHead th = tile_head(blockIdx.x, a.Hkv);
   const int hk = th.head;
-  const TilePlace at = find_tile(a.k_start, a.S, a.Tk, 1, kKeyTile, th.tile, lane);
-  if (at.s < 0) return;
-  const int2 qs = stretch_of(a.q_start, at.s, a.Tq), kx = stretch_of(a.k_start, at.s, a.Tk);
-  const int nr = qs.y * a.group, nk = kx.y, key0 = at.tile * kKeyTile, key = key0 + 32 * w + lane % 32;
-  const size_t token = (size_t)kx.x + min(key, nk - 1);
-  const int past = nk - qs.y;
-  const uint16_t* qh = a.q + (size_t)hk * a.group * a.sq.h + (size_t)qs.x * a.sq.t;
-  const uint16_t* gh = a.dout + (size_t)hk * a.group * a.so.h + (size_t)qs.x * a.so.t;
-  const float* lh = a.lse2 + (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group;
-  const float* dh = a.delta + (size_t)hk * a.Tq * a.group + (size_t)qs.x * a.group;
+  const TilePlace at = find_tile<true>(a, kKeyTile, th.tile, lane);
+  if (at.tile < 0) return;
+  const int nr = at.nq * a.group, nk = at.nk, key0 = at.tile * kKeyTile, key = key0 + 32 * w + lane % 32;
+  const size_t token = (size_t)at.k0 + min(key, nk - 1);
+  const int past = nk - at.nq;
+  const uint16_t* qh = a.q + (size_t)hk * a.group * a.sq.h + (size_t)at.q0 * a.sq.t;
+  const uint16_t* gh = a.dout + (size_t)hk * a.group * a.so.h + (size_t)at.q0 * a.so.t;
+  const float* lh = a.lse2 + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group;
+  const float* dh = a.delta + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group;
   // the rows that read a key: from this one on (causal)
   auto from_of = [&](int j) { return a.causal ? max(0, j - past) * a.group : 0; };
   const int from = from_of(key), w_from = from_of(key0 + 32 * w), w_last = from_of(key0 + 32 * w + 31);
   int t_begin = from_of(key0) / kTileTokens, t_end = max(t_begin, (nr + kTileTokens - 1) / kTileTokens);
+  const bool parts = PARTS && t_end - t_begin > a.k_chunk;
   if (PARTS) {
-    const int n = t_end - t_begin, b = t_begin;
-    t_begin = b + (int)((long long)n * blockIdx.y / a.k_parts);
-    t_end = b + (int)((long long)n * (blockIdx.y + 1) / a.k_parts);
+    t_begin += (int)blockIdx.y * a.k_chunk;
+    if (t_begin >= t_end && blockIdx.y) return;
+    t_end = min(t_end, t_begin + a.k_chunk);
   }
   auto qbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
   // Step t: rows [64 t, + 64) of Q and dO and their lse log2(e) and D; rows past the end repeat the last one, see no_rows
@@ -363,7 +362,7 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
     if (t + 1 < t_end) no_rows(t + 1);
     phase_barrier();                                   // ... for everyone; this step's tiles are free
   }
-  if (PARTS) {
+  if (parts) {
     if (key >= nk) return;
     const size_t part = ((size_t)blockIdx.y * a.Tk + token) * a.Hkv + hk;
     store_part<D>(dk, a.part_kv + part * D, g);
@@ -373,7 +372,7 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   uint16_t* os = reinterpret_cast<uint16_t*>(smem) + w * 32 * SM::kLd;
   auto to = [&](uint16_t* p) {
     return [=](int r) -> uint16_t* {
-      return key0 + 32 * w + r < nk ? p + (size_t)hk * a.skv.h + (size_t)(kx.x + key0 + 32 * w + r) * a.skv.t : nullptr;
+      return key0 + 32 * w + r < nk ? p + (size_t)hk * a.skv.h + (size_t)(at.k0 + key0 + 32 * w + r) * a.skv.t : nullptr;
     };
   };
   store_rows<D>(dk, a.scale, os, lane, to(a.dk));
@@ -398,19 +397,28 @@ __global__ __launch_bounds__(256) void packed_sum_q_kernel(PackedArgs a) {
 }
 template <int D>
 __global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
-  const long long idx = (long long)blockIdx.x * 256 + threadIdx.x, row = idx / (D / 4), rows = (long long)a.Tk * a.Hkv;
-  const int c = (int)(idx % (D / 4)) * 4;
-  if (row >= rows) return;
-  const int token = (int)(row / a.Hkv), hk = (int)(row % a.Hkv);
-  if (token < a.k_start[0] || token >= a.k_start[a.S]) return;
+  const TileHead th = tile_head(blockIdx.x, a.Hkv);
+  const TilePlace at = find_tile<true>(a, kKeyTile, th.tile, threadIdx.x % kWave);
+  if (at.tile < 0) return;
+  // as packed_dkv_kernel has it
+  const int key0 = at.tile * kKeyTile, from = a.causal ? max(0, key0 - (at.nk - at.nq)) * a.group : 0, t_begin = from / kTileTokens;
+  const int steps = (at.nq * a.group + kTileTokens - 1) / kTileTokens - t_begin;
+  if (steps <= a.k_chunk) return;
+  const int n = (steps + a.k_chunk - 1) / a.k_chunk;
+  const size_t rows = (size_t)a.Tk * a.Hkv;
   const float* src = a.part_kv + (blockIdx.y ? a.k_parts * rows * D : 0);
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < a.k_parts; i++) sum += *reinterpret_cast<const f32x4*>(src + (i * rows + row) * D + c);
   const float by = blockIdx.y ? 1.f : a.scale;
-  bf16x4 r;
+  uint16_t* dst = (blockIdx.y ? a.dv : a.dk) + (size_t)th.head * a.skv.h;
+  for (int idx = threadIdx.x + 256 * blockIdx.z; idx < min(kKeyTile, at.nk - key0) * (D / 4); idx += 256 * gridDim.z) {
+    const int token = at.k0 + key0 + idx / (D / 4), c = idx % (D / 4) * 4;
+    const float* p = src + ((size_t)token * a.Hkv + th.head) * D + c;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; i++) sum += *reinterpret_cast<const f32x4*>(p + i * rows * D);
+    bf16x4 r;
 #pragma unroll
-  for (int e = 0; e < 4; e++) r[e] = (__bf16)(by * sum[e]);
-  *reinterpret_cast<bf16x4*>((blockIdx.y ? a.dv : a.dk) + (size_t)hk * a.skv.h + (size_t)token * a.skv.t + c) = r;
+    for (int e = 0; e < 4; e++) r[e] = (__bf16)(by * sum[e]);
+    *reinterpret_cast<bf16x4*>(dst + (size_t)token * a.skv.t + c) = r;
+  }
 }
 
 template <int D> static hipError_t launch_bwd(const PackedArgs& a, hipStream_t stream) {
@@ -435,7 +443,7 @@ template <int D> static hipError_t launch_bwd(const PackedArgs& a, hipStream_t s
     if (k) packed_dkv_kernel<D, true><<<dim3((unsigned)k_tiles, a.k_parts), 256, smem, stream>>>(a);
     else packed_dkv_kernel<D, false><<<(unsigned)k_tiles, 256, smem, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (k) packed_sum_kv_kernel<D><<<dim3((unsigned)(((long long)a.Tk * a.Hkv * (D / 4) + 255) / 256), 2), 256, 0, stream>>>(a);
+    if (k) packed_sum_kv_kernel<D><<<dim3((unsigned)k_tiles, 2, 4), 256, 0, stream>>>(a);
   }
   return hipGetLastError();
 }

@@ -293,7 +293,7 @@ int sla2_cache_attention(const sla2_cache_params* params, const void* q, const v
   a.out = (uint16_t*)out;
   a.lse = lse_or_null;
   a.part_o = (float*)workspace;
-  a.part_ml = a.part_o + (size_t)a.B * a.H * a.chunks * a.d;
+  a.part_ml = a.part_o + (size_t)a.parts * 2 * a.H * a.d;
   return launch_cache_attention(a, (hipStream_t)hip_stream) == hipSuccess ? SLA2_OK : SLA2_EHIP;
 }
 

@@ -256,6 +256,15 @@ def test_attention_in_chunks(quant, lengths):
 
 
 @pytest.mark.parametrize("quant", QUANTS)
+def test_attention_of_many_lengths(quant):
+    """Long and short sequences and none, shared among workgroups; more of them than a wave looks at at once."""
+    lengths = [(37 * i * i) % 700 * (i % 3) for i in range(70)]
+    attend(quant, 64, 2, 1, 16, lengths + [2600], seed=7)
+    attend(quant, 64, 1, 1, 64, [0] * 66 + [1500, 0, 1, 3200] + [0] * 3, seed=8)
+    attend(quant, 128, 4, 4, 256, [0, 0, 0], seed=9, wide=12)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
 def test_attention_over_pages_that_are_none(quant):
     def bad(t):
         t[0, 0], t[0, 2], t[1, 0], t[1, 1] = -1, 2 ** 31 - 1, -2 ** 31, 2 ** 30
