@@ -361,7 +361,7 @@ typedef struct sla2_packed_params {
                                 all of them; one before the first key none); 0: all of its sequence */
   float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */
   /* (head, token) element strides of q, dq; of k, v, dk, dv; of out, dout.  Both zero: contiguous [tokens, heads, d].  As in
-   * sla2_params; below 2^24 elements a token; tokens_q H, tokens_k H below 2^31 - 1024 */
+   * sla2_params; below 2^24 elements a token; (tokens_q + 16 sequences) H and tokens_k H below 2^31 - 1024 */
   long long q_stride[2];
   long long kv_stride[2];
   long long out_stride[2];

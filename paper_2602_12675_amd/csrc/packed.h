@@ -19,15 +19,14 @@ struct PackedArgs {
   float* lse_out;
   RowStrides sq, skv, so;
   int S, Tq, Tk, H, Hkv, group, d;           // group: query heads of a key head
-  unsigned group_inv;                        // 2^32 / group, rounded up (group > 1)
   bool causal;
   float scale;                               // of the scores
   // The steps of a tile's inner loop are dealt to several workgroups, whose sums another kernel joins.  Of a tile of rows evenly to
   // q_parts; of a tile of keys k_chunk steps to each, k_parts at most.  1: none
   int q_parts, k_parts, k_chunk;
-  // scratch.  Rows of all key heads: [Hkv][Tq group]; sums of parts: O or dQ [q_parts][rows][d], (m, l) [q_parts][rows][2], dK and dV
-  // [2][k_parts][Tk][Hkv][d]
-  float *lse2, *delta;                       // backward: lse log2(e) and D of every row
+  // scratch.  Sums of parts: O or dQ [q_parts][rows][d], (m, l) [q_parts][rows][2], the rows of all key heads being [Hkv][Tq group]; dK and
+  // dV [2][k_parts][Tk][Hkv][d]
+  float *lse2, *delta;                       // backward: lse log2(e) and D of every row, see stat_at
   float *part_o, *part_ml, *part_kv;
 };
 
@@ -47,7 +46,7 @@ inline long long most_tiles(long long tokens, int sequences, int rows) {
 // has, and where its queries and keys lie, whatever the offsets hold inside the tensors.  A wave looks at 64 sequences at a time; all
 // lanes return the same.  tile < 0: there are fewer tiles.
 struct TilePlace {
-  int tile, tiles, q0, nq, k0, nk;
+  int tile, tiles, s, q0, nq, k0, nk;
 };
 template <bool KEYS> __device__ __forceinline__ TilePlace find_tile(const PackedArgs& a, int rows, int n, int lane) {
   for (int s0 = 0; s0 < a.S; s0 += kWave) {
@@ -73,11 +72,11 @@ template <bool KEYS> __device__ __forceinline__ TilePlace find_tile(const Packed
     if (has) {
       const int f = __builtin_ctzll(has);
       auto of = [&](int x) { return __builtin_amdgcn_readlane(x, f); };
-      return TilePlace{n - of(sum - own), of(own), of(q0), of(q1 - q0), of(k0), of(k1 - k0)};
+      return TilePlace{n - of(sum - own), of(own), s0 + f, of(q0), of(q1 - q0), of(k0), of(k1 - k0)};
     }
     n -= __builtin_amdgcn_readlane(sum, kWave - 1);
   }
-  return TilePlace{-1, 0, 0, 0, 0, 0};
+  return TilePlace{-1, 0, 0, 0, 0, 0, 0};
 }
 
 // query and head (inside the group) of a row
@@ -86,10 +85,15 @@ __device__ __forceinline__ int2 query_of(const PackedArgs& a, int row) {
   const int i = row / a.group;
   return make_int2(i, row - i * a.group);
 }
-// the same for rows below 2^16 and groups up to 2^15: a multiplication
-__device__ __forceinline__ int2 near_query_of(const PackedArgs& a, unsigned row) {
-  const unsigned i = a.group == 1 ? row : __umulhi(row, a.group_inv);
-  return make_int2((int)i, (int)(row - i * (unsigned)a.group));
+// Where the backward pass keeps what belongs to a row: for each key head the blocks of its sequences, 16 queries of one head each, the
+// heads of the group one after the other.  Sequence s has room for 16 queries more than it has, from query q0 + 16 s of the key head on.
+constexpr int kQueryBlock = 16;
+__host__ __device__ __forceinline__ size_t stat_rows(const PackedArgs& a) { return ((size_t)a.Tq + (size_t)kQueryBlock * a.S) * a.group; }
+__device__ __forceinline__ size_t stat_first(const PackedArgs& a, int hk, int s, int q0) {
+  return (size_t)hk * stat_rows(a) + ((size_t)q0 + (size_t)kQueryBlock * s) * a.group;
+}
+__device__ __forceinline__ size_t stat_at(const PackedArgs& a, int query, int head) {
+  return ((size_t)(query / kQueryBlock) * a.group + head) * kQueryBlock + query % kQueryBlock;
 }
 
 // Workgroup n of a launch over tiles x key heads: consecutive workgroups go to the XCDs in turn, so that where the heads are a multiple

@@ -8,10 +8,11 @@
 
 namespace sla2 {
 
-constexpr int kCacheThreads = 256;
+constexpr int kCacheThreads = 256, kCacheRows = 64;      // rows of a workgroup: one for each lane of a wave while their places are looked up
 
-// Where row i of k and v is in the cache: page and slot; page -1: nowhere, -2: the row is of no sequence.  All lanes of the wave take part: the sequence is the
-// number of sequences that end at or in front of the row, counted 64 at a time.
+// Where row i of k and v is in the cache: page and slot; page -1: nowhere, -2: the row is of no sequence.  A row a lane, the rows of a
+// wave being neighbours.  Its sequence is the number of sequences that end at or in front of it, counted 64 at a time: for all rows at
+// once where no sequence ends between them.
 struct Place {
   int page, slot;
 };
@@ -19,15 +20,15 @@ __device__ __forceinline__ Place place_of(const CacheArgs& a, int i, int lane) {
   int b = i;
   long long at = 0;
   if (a.start) {
+    const int i0 = __builtin_amdgcn_readfirstlane(i), i1 = __builtin_amdgcn_readlane(i, kWave - 1);
     b = 0;
     for (int s0 = 0; s0 < a.B; s0 += kWave) {
       const int end = s0 + lane < a.B ? a.start[s0 + lane + 1] : INT32_MAX;
-#pragma unroll
-      for (int r = 0; r < kWave / 8; r++) {              // the rows of the wave's teams (8 or 16 lanes each)
-        const int row = __builtin_amdgcn_readlane(i, 8 * r);
-        const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= row));
-        b += lane / 8 == r ? n : 0;
-      }
+      const unsigned long long before = __builtin_amdgcn_ballot_w64(end <= i0);
+      const unsigned long long between = __builtin_amdgcn_ballot_w64(end <= i1) & ~before;
+      b += __builtin_popcountll(before);
+      for (unsigned long long rest = between; rest; rest &= rest - 1)
+        b += __builtin_amdgcn_readlane(end, __builtin_ctzll(rest)) <= i ? 1 : 0;
     }
   }
   if (i >= a.tokens || b >= a.B) return Place{-2, 0};
@@ -97,48 +98,81 @@ template <int QUANT> __device__ __forceinline__ Raw<true> values_of(u32x2 c, flo
   return pack8<true>(x);
 }
 
+// Keys and values of 64 neighbouring rows of a head, U of each on their way to a thread.
 template <int D, int QUANT, bool WRITE>
 __global__ __launch_bounds__(kCacheThreads) void cache_rows_kernel(CacheArgs a) {
-  constexpr int LANES = D / 8, ROWS = kCacheThreads / LANES, ESZ = QUANT == SLA2_QUANT_NONE ? 2 : 1;
-  const int tid = threadIdx.x, lane = tid % kWave, col = 8 * (tid % LANES), h = blockIdx.y;
-  const bool values = blockIdx.z != 0;
-  const int i = blockIdx.x * ROWS + tid / LANES;
-  uint16_t* rows = values ? a.v : a.k;
-  uint16_t* mine = rows + (size_t)h * a.kv_h + (size_t)min(i, a.tokens - 1) * a.kv_t + col;
-  Raw<true> r;
-  if (WRITE) r = load8<true>(mine, 0u);
-  const Place p = place_of(a, i, lane);
-  if (p.page < -1) return;
-  const long long slot = p.page * a.page_stride + h * a.head_stride + p.slot * a.token_stride + col;
-  char* cache = (char*)(values ? a.vc : a.kc) + slot * ESZ;
-  float* scale = nullptr;
-  if constexpr (QUANT != SLA2_QUANT_NONE)
-    scale = (values ? a.vs : a.ks) + (((long long)p.page * a.Hkv + h) << a.page_shift) + p.slot;
+  constexpr int LANES = D / 8, ROWS = kCacheThreads / LANES, U = kCacheRows / ROWS, ESZ = QUANT == SLA2_QUANT_NONE ? 2 : 1;
+  const int tid = threadIdx.x, lane = tid % kWave, col = 8 * (tid % LANES), h = blockIdx.y, i0 = blockIdx.x * kCacheRows;
+  Raw<true> r[2][U];
+  const long long own = (long long)h * a.kv_h + col;
+  if (WRITE) {
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const long long at = own + (long long)min(i0 + u * ROWS + tid / LANES, a.tokens - 1) * a.kv_t;
+      r[0][u] = load8<true>(a.k, at);
+      r[1][u] = load8<true>(a.v, at);
+    }
+  }
+  const Place mine = place_of(a, i0 + lane, lane);
+  Place p[U];
+  long long slot[U];
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const int x = u * ROWS + tid / LANES;
+    p[u] = Place{__shfl(mine.page, x), __shfl(mine.slot, x)};
+    slot[u] = p[u].page * a.page_stride + h * a.head_stride + p[u].slot * a.token_stride + col;
+  }
+  auto scale_at = [&](int u) { return (((long long)p[u].page * a.Hkv + h) << a.page_shift) + p[u].slot; };
   if constexpr (WRITE) {
-    if constexpr (QUANT == SLA2_QUANT_NONE) {
-      if (p.page >= 0) *(u32x4*)cache = r.a[0];
-    } else {
-      float s;
-      const u32x2 c = codes_of<QUANT>(r, row_amax<LANES>(r), &s);
-      if (p.page >= 0) {
-        *(u32x2*)cache = c;
-        if (col == 0) *scale = s;
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        char* cache = (char*)(x ? a.vc : a.kc) + slot[u] * ESZ;
+        if constexpr (QUANT == SLA2_QUANT_NONE) {
+          if (p[u].page >= 0) *(u32x4*)cache = r[x][u].a[0];
+        } else {
+          float s;
+          const u32x2 c = codes_of<QUANT>(r[x][u], row_amax<LANES>(r[x][u]), &s);
+          if (p[u].page >= 0) {
+            *(u32x2*)cache = c;
+            if (col == 0) (x ? a.vs : a.ks)[scale_at(u)] = s;
+          }
+        }
       }
-    }
   } else {
-    r = zero8<true>();
-    if (p.page >= 0) {
-      if constexpr (QUANT == SLA2_QUANT_NONE) r.a[0] = *(const u32x4*)cache;
-      else r = values_of<QUANT>(*(const u32x2*)cache, *scale);
-    }
-    store8<true>(mine, 0u, r);
+    u32x2 c[2][U];
+    float s[2][U];
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const char* cache = (const char*)(x ? a.vc : a.kc) + slot[u] * ESZ;
+        r[x][u] = zero8<true>();
+        c[x][u] = u32x2{0, 0};
+        s[x][u] = 0.f;
+        if (p[u].page < 0) continue;
+        if constexpr (QUANT == SLA2_QUANT_NONE) {
+          r[x][u].a[0] = *(const u32x4*)cache;
+        } else {
+          c[x][u] = *(const u32x2*)cache;
+          s[x][u] = (x ? a.vs : a.ks)[scale_at(u)];
+        }
+      }
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        if (p[u].page < -1) continue;
+        if constexpr (QUANT != SLA2_QUANT_NONE) r[x][u] = values_of<QUANT>(c[x][u], s[x][u]);
+        store8<true>(x ? a.v : a.k, own + (long long)(i0 + u * ROWS + tid / LANES) * a.kv_t, r[x][u]);
+      }
   }
 }
 
 template <bool WRITE> static hipError_t launch_rows(const CacheArgs& a, hipStream_t stream) {
   if (!a.tokens) return hipSuccess;
-  const int rows = kCacheThreads / (a.d / 8);
-  const dim3 grid((a.tokens + rows - 1) / rows, a.Hkv, 2);
+  const dim3 grid((a.tokens + kCacheRows - 1) / kCacheRows, a.Hkv);
 #define SLA2_ROWS(D)                                                                                                          \
   (a.quant == SLA2_QUANT_NONE  ? cache_rows_kernel<D, SLA2_QUANT_NONE, WRITE><<<grid, kCacheThreads, 0, stream>>>(a)          \
    : a.quant == SLA2_QUANT_FP8 ? cache_rows_kernel<D, SLA2_QUANT_FP8, WRITE><<<grid, kCacheThreads, 0, stream>>>(a)           \

@@ -263,7 +263,7 @@ void plan_packed(PackedArgs* a, bool backward) {
   if (!backward || !k_tiles || !rows) return;
   // Steps of 64 rows of all tiles of keys, were the sequences alike, over the places, and a little more, so that the last round is not
   // a few workgroups; at most 16 parts of the longest sequence that there can be.
-  const long long steps = (rows + 63) / 64, all = (a->Tk + kKeyTile - 1) / kKeyTile * a->Hkv * ((steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
+  const long long steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + kKeyTile - 1) / kKeyTile * a->Hkv * ((steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
   long long chunk = all / places + all / (places * 12) + 1;
   if (chunk < 16) chunk = 16;
   if (chunk < (steps + 15) / 16) chunk = (steps + 15) / 16;

@@ -53,14 +53,29 @@ __device__ __forceinline__ void pin(bf16x8& f) {       // converted here: eight 
   f = __builtin_bit_cast(bf16x8, u);
 }
 
-// acc[et] += A^T f: the 32 rows of a tile at `lo` / `hi` (tr_read_offset) contracted, as two 16-row steps, into all channels
-template <int D>
+// 16 bytes of a step's row quantities, 32 bytes apart: lse at n = 0 .. 3 and D, 256 bytes on, at 4 .. 7
+__device__ __forceinline__ u32x4 stat_read(unsigned base, int n) {
+  switch (n) {
+    case 0: return lds_read16_untracked<0>(base);
+    case 1: return lds_read16_untracked<32>(base);
+    case 2: return lds_read16_untracked<64>(base);
+    case 3: return lds_read16_untracked<96>(base);
+    case 4: return lds_read16_untracked<256>(base);
+    case 5: return lds_read16_untracked<288>(base);
+    case 6: return lds_read16_untracked<320>(base);
+    default: return lds_read16_untracked<352>(base);
+  }
+}
+
+// acc[et] += A^T f: the 32 rows of a tile at `lo` / `hi` (tr_read_offset), OFF bytes on, contracted, as two 16-row steps, into all channels
+template <int D, int OFF>
 __device__ __forceinline__ void contract32(f32x16 (&acc)[D / 32], const bf16x8* f, unsigned lo_at, unsigned hi_at) {
   constexpr int ET = D / 32, kFrags = 2 * ET, kAhead = 3, kSlots = kAhead + 1;
   u32x2 lo[kSlots], hi[kSlots];
   auto issue = [&](int n) {
-    lo[n % kSlots] = lds_read_tr_untracked_at<32 * D>(lo_at ^ (64u * (n % ET)), n / ET);
-    hi[n % kSlots] = lds_read_tr_untracked_at<32 * D>(hi_at ^ (64u * (n % ET)), n / ET);
+    const unsigned at_lo = lo_at ^ (64u * (n % ET)), at_hi = hi_at ^ (64u * (n % ET));
+    lo[n % kSlots] = n < ET ? lds_read_tr_untracked<OFF>(at_lo) : lds_read_tr_untracked<OFF + 32 * D>(at_lo);
+    hi[n % kSlots] = n < ET ? lds_read_tr_untracked<OFF>(at_hi) : lds_read_tr_untracked<OFF + 32 * D>(at_hi);
   };
 #pragma unroll
   for (int n = 0; n < kAhead; n++) issue(n);
@@ -132,8 +147,9 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
   const float lse = a.lse[(size_t)h * a.Tq + token];
   const float l2 = lse == -INFINITY ? INFINITY : lse * kLog2e;   // a row that reads no key: P = 0
   if (row < nr && g == 0 && (!PARTS || blockIdx.y == 0)) {
-    a.delta[row_at] = delta;
-    a.lse2[row_at] = l2;
+    const size_t st = stat_first(a, hk, at.s, at.q0) + stat_at(a, my.x, my.y);
+    a.delta[st] = delta;
+    a.lse2[st] = l2;
   }
   const float c1 = kLog2e * a.scale;
   f32x16 acc[ET];
@@ -161,7 +177,8 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
         constexpr int kItems = 2 * KS, kAhead = 4, kSlots = kAhead + 1;
         u32x4 ring[kSlots];
         auto issue = [&](int n) {
-          ring[n % kSlots] = lds_read16_untracked<0>((ka + (n < KS ? 0 : SM::kTile) + k_off) ^ (32u * (n % KS)));
+          const unsigned x = (ka + k_off) ^ (32u * (n % KS));
+          ring[n % kSlots] = n < KS ? lds_read16_untracked<0>(x) : lds_read16_untracked<SM::kTile>(x);
         };
 #pragma unroll
         for (int n = 0; n < kAhead; n++) issue(n);
@@ -196,7 +213,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
         for (int e = 0; e < 16; e++) df[e / 8][e % 8] = (__bf16)(s[e] * (dp[e] - delta));
         pin(df[0]);
         pin(df[1]);
-        contract32<D>(acc, df, ka + t_lo, ka + t_hi);
+        contract32<D, 0>(acc, df, ka + t_lo, ka + t_hi);
       }
     }
     wait_vmcnt<0>();
@@ -222,60 +239,76 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   typedef PackedTile<D> SL;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   float* stat = reinterpret_cast<float*>(smem + SM::kStatOff);
-  const int tid = threadIdx.x, lane = tid % kWave, g = lane / 32;
-  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lane = threadIdx.x % kWave;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const TileHead th = tile_head(blockIdx.x, a.Hkv);
   const int hk = th.head;
   const TilePlace at = find_tile<true>(a, kKeyTile, th.tile, lane);
   if (at.tile < 0) return;
-  const int nr = at.nq * a.group, nk = at.nk, key0 = at.tile * kKeyTile, key = key0 + 32 * w + lane % 32;
-  const size_t token = (size_t)at.k0 + min(key, nk - 1);
-  const int past = nk - at.nq;
-  const uint16_t* qh = a.q + (size_t)hk * a.group * a.sq.h + (size_t)at.q0 * a.sq.t;
-  const uint16_t* gh = a.dout + (size_t)hk * a.group * a.so.h + (size_t)at.q0 * a.so.t;
-  const float* lh = a.lse2 + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group;
-  const float* dh = a.delta + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group;
-  // the rows that read a key: from this one on (causal)
-  auto from_of = [&](int j) { return a.causal ? max(0, j - past) * a.group : 0; };
-  const int from = from_of(key), w_from = from_of(key0 + 32 * w), w_last = from_of(key0 + 32 * w + 31);
-  int t_begin = from_of(key0) / kTileTokens, t_end = max(t_begin, (nr + kTileTokens - 1) / kTileTokens);
+  const int nk = at.nk, nq = at.nq, past = nk - nq, key0 = at.tile * kKeyTile, w_key = key0 + 32 * w;
+  // The rows in blocks of 16 queries of one head (packed.h), four blocks a step: within a block a transfer's addresses are a lane's place
+  // beside a scalar.  A key is read by the queries from this one on (causal):
+  auto from_of = [&](int j) { return a.causal ? max(0, j - past) : 0; };
+  const int w_from = from_of(w_key), w_last = from_of(w_key + 31), q_blocks = (nq + kQueryBlock - 1) / kQueryBlock;
+  int t_begin = from_of(key0) / kQueryBlock * a.group / 4, t_end = max(t_begin, (q_blocks * a.group + 3) / 4);
   const bool parts = PARTS && t_end - t_begin > a.k_chunk;
   if (PARTS) {
     t_begin += (int)blockIdx.y * a.k_chunk;
     if (t_begin >= t_end && blockIdx.y) return;
     t_end = min(t_end, t_begin + a.k_chunk);
   }
+  const uint16_t* qh = a.q + (size_t)hk * a.group * a.sq.h + (size_t)at.q0 * a.sq.t;
+  const uint16_t* gh = a.dout + (size_t)hk * a.group * a.so.h + (size_t)at.q0 * a.so.t;
+  const size_t st0 = stat_first(a, hk, at.s, at.q0);
+  // block 4 t, counted along: query block and head
+  struct Block {
+    int q, h;
+  };
+  const int four_q = 4 / a.group, four_h = 4 % a.group;
+  auto next = [&](Block b) { return b.h + 1 == a.group ? Block{b.q + 1, 0} : Block{b.q, b.h + 1}; };
+  auto after4 = [&](Block b) { return b.h + four_h >= a.group ? Block{b.q + four_q + 1, b.h + four_h - a.group} : Block{b.q + four_q, b.h + four_h}; };
   auto qbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
-  // Step t: rows [64 t, + 64) of Q and dO and their lse log2(e) and D; rows past the end repeat the last one, see no_rows
-  auto request = [&](int t) {
-    constexpr int kRowsPerInstr = 1024 / (D * 2), kInstrs = kTileTokens / kRowsPerInstr / NW;
-    const int ln = (int)lane_again(), r0 = t * kTileTokens, valid = min(kTileTokens, nr - r0);
-    const int2 q0 = query_of(a, r0);
-    const int row_w = w * kRowsPerInstr + ln / SL::kChunks;
-    const unsigned col = 16u * (unsigned)((ln % SL::kChunks) ^ SL::swz(row_w));
-    const char *qb = (const char*)(qh + (size_t)q0.x * a.sq.t), *gb = (const char*)(gh + (size_t)q0.x * a.so.t);
+  // Step t, whose first block is b: the rows of four blocks of Q and dO and their lse log2(e) and D.  Queries past the end repeat the
+  // last one, see no_rows.
+  auto request = [&](int t, Block b) {
+    constexpr int kRows = 1024 / (D * 2), kInstrs = kTileTokens / kRows / NW;          // of a transfer; a wave's transfers
+    const int ln = (int)lane_again(), row = w * kRows % kQueryBlock + ln / SL::kChunks;
+    const unsigned col = 16u * (unsigned)((ln % SL::kChunks) ^ SL::swz(w * kRows + ln / SL::kChunks));
+    const unsigned q_off = (unsigned)row * (unsigned)a.sq.t * 2 + col, g_off = (unsigned)row * (unsigned)a.so.t * 2 + col;
+    if (kRows * NW > kQueryBlock && w * kRows >= kQueryBlock) b = next(b);             // two blocks a transfer of all waves
 #pragma unroll
     for (int i = 0; i < kInstrs; i++) {
-      const int2 x = near_query_of(a, (unsigned)(q0.y + min(row_w + i * NW * kRowsPerInstr, valid - 1)));
-      dma_lane16(qb, ((unsigned)x.x * (unsigned)a.sq.t + (unsigned)x.y * (unsigned)a.sq.h) * 2 + col, qbuf(t) + (i * NW + w) * 1024);
-      dma_lane16(gb, ((unsigned)x.x * (unsigned)a.so.t + (unsigned)x.y * (unsigned)a.so.h) * 2 + col, qbuf(t) + SM::kTile + (i * NW + w) * 1024);
+      const Block x = b.q < q_blocks ? b : Block{q_blocks - 1, 0};
+      const int valid = nq - x.q * kQueryBlock;
+      unsigned qo = q_off, go = g_off;
+      if (valid < kQueryBlock) {
+        const unsigned back = (unsigned)max(0, row - (valid - 1));
+        qo -= back * (unsigned)a.sq.t * 2;
+        go -= back * (unsigned)a.so.t * 2;
+      }
+      dma_lane16(qh + (size_t)x.h * a.sq.h + (size_t)x.q * kQueryBlock * a.sq.t, qo, qbuf(t) + (i * NW + w) * 1024);
+      dma_lane16(gh + (size_t)x.h * a.so.h + (size_t)x.q * kQueryBlock * a.so.t, go, qbuf(t) + SM::kTile + (i * NW + w) * 1024);
+      b = next(b);
+      if (kRows * NW > kQueryBlock) b = next(b);
     }
-    const unsigned so = 4u * (unsigned)min(ln, valid - 1);
-    if (w == 0) dma_lane4(lh + r0, so, lds_address(stat + (t & 1) * 128));
-    if (w == 1) dma_lane4(dh + r0, so, lds_address(stat + (t & 1) * 128 + 64));
+    if (w < 2) dma_lane4((w == 0 ? a.lse2 : a.delta) + st0 + (size_t)t * kTileTokens, 4u * (unsigned)ln, lds_address(stat + (t & 1) * 128 + 64 * w));
   };
-  // behind the arrival of step t: lse = +inf for rows past the end, their P is 0
-  auto no_rows = [&](int t) {
-    if (w == 0 && (t + 1) * kTileTokens > nr) {
-      if (t * kTileTokens + lane >= nr) stat[(t & 1) * 128 + lane] = INFINITY;
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
+  // Behind the arrival of step t, by the waves that asked for them: what was read for queries past the end has no meaning.  With
+  // lse = +inf and D = 0 their P and dS are 0.
+  auto no_rows = [&](int t, Block b) {
+    const Block b1 = next(b), b2 = next(b1), b3 = next(b2);
+    if (w > 1 || b3.q * kQueryBlock + kQueryBlock <= nq) return;
+    const int ln = (int)lane_again(), q = ln < 32 ? ln < 16 ? b.q : b1.q : ln < 48 ? b2.q : b3.q;
+    if (q * kQueryBlock + ln % kQueryBlock >= nq) stat[(t & 1) * 128 + 64 * w + ln] = w == 0 ? INFINITY : 0.f;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
-  if (t_begin < t_end) request(t_begin);
+  Block cur{t_begin * 4 / a.group, t_begin * 4 % a.group};
+  if (t_begin < t_end) request(t_begin, cur);
   bf16x8 kf[KS], vf[KS];
   {
-    const uint16_t* src = a.k + (size_t)hk * a.skv.h + token * a.skv.t + 8 * g;
-    const uint16_t* vsrc = a.v + (size_t)hk * a.skv.h + token * a.skv.t + 8 * g;
+    const size_t token = (size_t)at.k0 + min(w_key + lane % 32, nk - 1);
+    const uint16_t* src = a.k + (size_t)hk * a.skv.h + token * a.skv.t + 8 * (lane / 32);
+    const uint16_t* vsrc = a.v + (size_t)hk * a.skv.h + token * a.skv.t + 8 * (lane / 32);
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) {
       kf[ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
@@ -292,44 +325,49 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   wait_vmcnt<0>();
 #pragma unroll
   for (int ks = 0; ks < KS; ks++) { settle(kf[ks]); settle(vf[ks]); }
-  if (t_begin < t_end) no_rows(t_begin);
+  if (t_begin < t_end) no_rows(t_begin, cur);
   phase_barrier();
   for (int t = t_begin; t < t_end; t++) {
-    if (t + 1 < t_end) request(t + 1);
+    const Block following = after4(cur);
+    if (t + 1 < t_end) request(t + 1, following);
 #pragma unroll
     for (int rh = 0; rh < 2; rh++) {
-      const int r0 = t * kTileTokens + 32 * rh;
-      if (r0 + 32 <= w_from || r0 >= nr) continue;
-      const unsigned qa = qbuf(t) + 64 * D * rh, ga = qa + SM::kTile;
-      const unsigned st = lds_address(stat + (t & 1) * 128 + 32 * rh + 4 * g);
+      const Block b0 = rh ? next(next(cur)) : cur, b1 = next(b0);
+      if (b0.q >= q_blocks || b1.q * kQueryBlock + kQueryBlock <= w_from) continue;
+      const unsigned qa = qbuf(t) + 64 * D * rh, ra = qa + r_off;
+      const unsigned st = lds_address(stat + (t & 1) * 128 + 32 * rh) + lane_again() / 32 * 16;
       f32x16 s, dp;
       bf16x8 pf[2], df[2];
 #pragma unroll
       for (int e = 0; e < 16; e++) s[e] = dp[e] = 0.f;
       // One stream of LDS reads, kAhead of them in flight: the rows of Q for S; four groups of a quarter of the rows of dO for dP and lse
       // of four rows, whose exponentials then run beside the products; D of the rows.
-      constexpr int kGroup = KS / 4 + 1, kItems = KS + 4 * kGroup + 4, kAhead = 4, kSlots = kAhead + 1;
+      constexpr int kGroup = KS / 4 + 1, kItems = KS + 4 * kGroup + 4, kAhead = D == 64 ? 4 : 2 /* the registers */, kSlots = kAhead + 1;
       u32x4 ring[kSlots];
       auto issue = [&](int n) {
         const int m = n - KS, v4 = m / kGroup;
-        if (n < KS) ring[n % kSlots] = lds_read16_untracked<0>((qa + r_off) ^ (32u * n));
-        else if (m >= 4 * kGroup) ring[n % kSlots] = lds_read16_untracked<0>(st + 256 + 32 * (m - 4 * kGroup));
-        else if (m % kGroup == kGroup - 1) ring[n % kSlots] = lds_read16_untracked<0>(st + 32 * v4);
-        else ring[n % kSlots] = lds_read16_untracked<0>((ga + r_off) ^ (32u * (v4 * (kGroup - 1) + m % kGroup)));
+        if (n < KS) ring[n % kSlots] = lds_read16_untracked<0>(ra ^ (32u * n));
+        else if (m >= 4 * kGroup) ring[n % kSlots] = stat_read(st, 4 + m - 4 * kGroup);
+        else if (m % kGroup == kGroup - 1) ring[n % kSlots] = stat_read(st, v4);
+        else ring[n % kSlots] = lds_read16_untracked<SM::kTile>(ra ^ (32u * (v4 * (kGroup - 1) + m % kGroup)));
       };
-      const bool edge = r0 < w_last;
 #pragma unroll
       for (int n = 0; n < kAhead; n++) issue(n);
-#pragma unroll
-      for (int n = 0; n < kItems; n++) {
+      unrolled<kItems>([&](auto at_n) {
+        constexpr int n = decltype(at_n)::value, m = n - KS, v4 = m / kGroup;
         if (n + kAhead < kItems) issue(n + kAhead);
         wait_lgkmcnt(n + kAhead < kItems ? kAhead : kItems - 1 - n);
         settle(ring[n % kSlots]);
-        const int m = n - KS, v4 = m / kGroup;
-        if (n < KS) {
+        if constexpr (n < KS) {
           s = mfma_bf16(__builtin_bit_cast(bf16x8, ring[n % kSlots]), kf[n], s);
-        } else if (m >= 4 * kGroup) {
-          const int x = m - 4 * kGroup;
+          if (n == KS - 1 && b0.q * kQueryBlock < w_last) {            // some rows do not read some of the keys
+            const int ln = (int)lane_again(), from = from_of(w_key + ln % 32) - 4 * (ln / 32);
+#pragma unroll
+            for (int e = 0; e < 16; e++)
+              if ((e < 8 ? b0.q : b1.q) * kQueryBlock + e % 8 / 4 * 8 + e % 4 < from) s[e] = -INFINITY;
+          }
+        } else if constexpr (m >= 4 * kGroup) {
+          constexpr int x = m - 4 * kGroup;
           const f32x4 d4 = __builtin_bit_cast(f32x4, ring[n % kSlots]);
 #pragma unroll
           for (int r = 0; r < 4; r++) {
@@ -341,42 +379,43 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
             pin(pf[x / 2]);
             pin(df[x / 2]);
           }
-        } else if (m % kGroup == kGroup - 1) {
+        } else if constexpr (m % kGroup == kGroup - 1) {
           const f32x4 l4 = __builtin_bit_cast(f32x4, ring[n % kSlots]);
 #pragma unroll
           for (int r = 0; r < 4; r++) {
-            const int e = 4 * v4 + r;
-            float p = fast_exp2(s[e] * c1 - l4[r]);
-            if (edge) p = r0 + 8 * v4 + 4 * g + r >= from ? p : 0.f;
+            float p = fast_exp2(s[4 * v4 + r] * c1 - l4[r]);
             settle(p);                                 // here, not where the compiler would gather them
-            s[e] = p;
+            s[4 * v4 + r] = p;
           }
         } else {
           dp = mfma_bf16(__builtin_bit_cast(bf16x8, ring[n % kSlots]), vf[v4 * (kGroup - 1) + m % kGroup], dp);
         }
-      }
-      contract32<D>(dv, pf, ga + t_lo, ga + t_hi);
-      contract32<D>(dk, df, qa + t_lo, qa + t_hi);
+      });
+      contract32<D, SM::kTile>(dv, pf, qa + t_lo, qa + t_hi);
+      contract32<D, 0>(dk, df, qa + t_lo, qa + t_hi);
     }
     wait_vmcnt<0>();                                   // the next step's rows have landed ...
-    if (t + 1 < t_end) no_rows(t + 1);
+    if (t + 1 < t_end) no_rows(t + 1, following);
     phase_barrier();                                   // ... for everyone; this step's tiles are free
+    cur = following;
   }
+  const int ln = (int)lane_again();                    // what is made of the lane's place is not kept through the loop
   if (parts) {
+    const int key = w_key + ln % 32;
     if (key >= nk) return;
-    const size_t part = ((size_t)blockIdx.y * a.Tk + token) * a.Hkv + hk;
-    store_part<D>(dk, a.part_kv + part * D, g);
-    store_part<D>(dv, a.part_kv + ((size_t)a.k_parts * a.Tk * a.Hkv + part) * D, g);
+    const size_t part = ((size_t)blockIdx.y * a.Tk + at.k0 + key) * a.Hkv + hk;
+    store_part<D>(dk, a.part_kv + part * D, ln / 32);
+    store_part<D>(dv, a.part_kv + ((size_t)a.k_parts * a.Tk * a.Hkv + part) * D, ln / 32);
     return;
   }
   uint16_t* os = reinterpret_cast<uint16_t*>(smem) + w * 32 * SM::kLd;
   auto to = [&](uint16_t* p) {
     return [=](int r) -> uint16_t* {
-      return key0 + 32 * w + r < nk ? p + (size_t)hk * a.skv.h + (size_t)(at.k0 + key0 + 32 * w + r) * a.skv.t : nullptr;
+      return w_key + r < nk ? p + (size_t)hk * a.skv.h + (size_t)(at.k0 + w_key + r) * a.skv.t : nullptr;
     };
   };
-  store_rows<D>(dk, a.scale, os, lane, to(a.dk));
-  store_rows<D>(dv, 1.f, os, lane, to(a.dv));
+  store_rows<D>(dk, a.scale, os, ln, to(a.dk));
+  store_rows<D>(dv, 1.f, os, ln, to(a.dv));
 }
 
 // Sums of the parts, four channels a thread: dQ (rows of all key heads), dK and dV.
@@ -401,8 +440,8 @@ __global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
   const TilePlace at = find_tile<true>(a, kKeyTile, th.tile, threadIdx.x % kWave);
   if (at.tile < 0) return;
   // as packed_dkv_kernel has it
-  const int key0 = at.tile * kKeyTile, from = a.causal ? max(0, key0 - (at.nk - at.nq)) * a.group : 0, t_begin = from / kTileTokens;
-  const int steps = (at.nq * a.group + kTileTokens - 1) / kTileTokens - t_begin;
+  const int key0 = at.tile * kKeyTile, from = a.causal ? max(0, key0 - (at.nk - at.nq)) : 0, t_begin = from / kQueryBlock * a.group / 4;
+  const int steps = ((at.nq + kQueryBlock - 1) / kQueryBlock * a.group + 3) / 4 - t_begin;
   if (steps <= a.k_chunk) return;
   const int n = (steps + a.k_chunk - 1) / a.k_chunk;
   const size_t rows = (size_t)a.Tk * a.Hkv;

@@ -45,8 +45,8 @@ static size_t packed_layout(PackedArgs* a, bool backward, void* ws) {
   const size_t rows = (size_t)a->Tq * a->H;
   plan_packed(a, backward);
   if (backward) {
-    a->lse2 = take(rows);
-    a->delta = take(rows);
+    a->lse2 = take(stat_rows(*a) * a->Hkv + 64);       // a step's 64 are read whole
+    a->delta = take(stat_rows(*a) * a->Hkv + 64);
     if (a->k_parts > 1) a->part_kv = take(2 * (size_t)a->k_parts * a->Tk * a->Hkv * a->d);
   }
   if (a->q_parts > 1) {
@@ -76,14 +76,11 @@ static int make_packed(const sla2_packed_params* p, PackedArgs* a) {
   a->H = p->H;
   a->Hkv = p->H_kv;
   a->group = p->H / p->H_kv;
-  a->group_inv = a->group > 1 ? (unsigned)(((1ull << 32) + a->group - 1) / a->group) : 0;
   a->d = p->d;
   a->causal = p->causal != 0;
   a->scale = rate_or_default(p->scale, p->d);
-  // rows (queries of all heads) and workgroups are counted in 31 bits, a step's rows lie within 4 GB
-  if ((long long)a->Tq * a->H > INT_MAX - 1024 || (long long)a->Tk * a->H > INT_MAX - 1024 || a->group > 1 << 15) return SLA2_EUNSUPPORTED;
-  for (const RowStrides* s : {&a->sq, &a->so})
-    if (a->group > 1 && (a->group - 1) * (__int128)s->h + 64ll * s->t >= 1ll << 31) return SLA2_EUNSUPPORTED;
+  // rows (queries of all heads, the backward pass's blocks of 16 filled up) and workgroups are counted in 31 bits
+  if (((long long)a->Tq + 16ll * a->S) * a->H > INT_MAX - 1024 || (long long)a->Tk * a->H > INT_MAX - 1024) return SLA2_EUNSUPPORTED;
   return SLA2_OK;
 }
 static View q_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tq, a.H, a.d, a.sq.h, a.sq.t); }
