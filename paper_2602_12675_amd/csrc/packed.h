@@ -105,6 +105,14 @@ __device__ __forceinline__ TileHead tile_head(int n, int heads) { return TileHea
 
 template <int D> using PackedTile = typename std::conditional<D == 128, SwizzledLayoutB<128>, SwizzledLayout<64>>::type;   // no bank conflicts
 
+// Rows t0 .. t0 + 63 of n into a tile; rows past the end repeat the last one.  lane_off: tile_lane_off.
+template <int D, int NW>
+__device__ __forceinline__ void packed_dma(const uint16_t* src, int stride, int t0, int n, unsigned to, int w, unsigned lane_off) {
+  const uint16_t* first = src + (size_t)t0 * stride;
+  if (t0 + kTileTokens <= n) dma_tile_full<D, NW, PackedTile<D>>(first, stride, to, w, lane_off);
+  else dma_tile<D, NW, PackedTile<D>>(first, stride, n - t0, to, w, (int)lane_again());
+}
+
 // LDS byte offsets of a lane's operand reads inside a 64-row tile, both for the rows 32 h further by 64 h D bytes.
 // Row-wise: row l % 32, channel step ks at (offset of step 0) ^ 32 ks.  Transposing (cf. read_tr4): rows 4 g + (l % 16) / 4 (lo) and 8
 // further (hi), channel tile et at (offset of tile 0) ^ 64 et, 16-row step ks 32 D ks further.

@@ -48,9 +48,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
   }
   const unsigned kbuf = lds_address(smem);
   auto vbuf = [&](int t) { return kbuf + (1 + (t & 1)) * SM::kTile; };
-  auto dma = [&](const uint16_t* src, int t, unsigned to) {     // rows past the end repeat the last one: their scores are masked
-    const int t0 = t * kTileTokens;
-    dma_tile<D, NW, SL>(src + (size_t)t0 * a.skv.t, a.skv.t, min(kTileTokens, nk - t0), to, w, (int)lane_again());
+  const unsigned lane_off = tile_lane_off<D, NW, SL>(a.skv.t, w, lane);
+  auto dma = [&](const uint16_t* src, int t, unsigned to) {
+    packed_dma<D, NW>(src, a.skv.t, t * kTileTokens, nk, to, w, lane_off);
   };
   if (t_begin < t_end) {
     dma(kh, t_begin, kbuf);

@@ -120,10 +120,10 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
     t_end = (int)((long long)n * (blockIdx.y + 1) / a.q_parts);
   }
   auto kbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
+  const unsigned lane_off = tile_lane_off<D, NW, SL>(a.skv.t, w, lane);
   auto dma = [&](int t) {
-    const int t0 = t * kTileTokens, valid = min(kTileTokens, nk - t0), ln = (int)lane_again();
-    dma_tile<D, NW, SL>(kh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t), w, ln);
-    dma_tile<D, NW, SL>(vh + (size_t)t0 * a.skv.t, a.skv.t, valid, kbuf(t) + SM::kTile, w, ln);
+    packed_dma<D, NW>(kh, a.skv.t, t * kTileTokens, nk, kbuf(t), w, lane_off);
+    packed_dma<D, NW>(vh, a.skv.t, t * kTileTokens, nk, kbuf(t) + SM::kTile, w, lane_off);
   };
   if (t_begin < t_end) dma(t_begin);
   bf16x8 qf[KS], gf[KS];
