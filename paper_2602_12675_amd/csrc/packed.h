@@ -105,6 +105,43 @@ __device__ __forceinline__ TileHead tile_head(int n, int heads) { return TileHea
 
 template <int D> using PackedTile = typename std::conditional<D == 128, SwizzledLayoutB<128>, SwizzledLayout<64>>::type;   // no bank conflicts
 
+// A lane's row of accumulators (channels x rows) to memory: as fp32 ..
+template <int D>
+__device__ __forceinline__ void store_part(const f32x16 (&acc)[D / 32], float* dst, int g) {
+#pragma unroll
+  for (int et = 0; et < D / 32; et++)
+#pragma unroll
+    for (int v4 = 0; v4 < 4; v4++)
+      *reinterpret_cast<f32x4*>(dst + 32 * et + 8 * v4 + 4 * g) =
+          f32x4{acc[et][4 * v4], acc[et][4 * v4 + 1], acc[et][4 * v4 + 2], acc[et][4 * v4 + 3]};
+}
+// .. and times `by` as bf16: lanes l and l + 32 have four channels each of every eight, and exchange them for all eight of every other
+// eight, 16 bytes a store.
+template <int D>
+__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], float by, uint16_t* dst, int g, bool there) {
+#pragma unroll
+  for (int et = 0; et < D / 32; et++)
+#pragma unroll
+    for (int v = 0; v < 2; v++) {
+      u32x2 c[2];                                      // channels 16 v + 8 i + 4 g + 0..3
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        bf16x4 pk;
+#pragma unroll
+        for (int r = 0; r < 4; r++) pk[r] = (__bf16)(by * acc[et][8 * v + 4 * i + r]);
+        c[i] = __builtin_bit_cast(u32x2, pk);
+      }
+      u32x4 out;                                       // channels 16 v + 8 g + 0..7
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        const auto r = __builtin_amdgcn_permlane32_swap(c[0][i], c[1][i], false, false);
+        out[i] = r[0];
+        out[2 + i] = r[1];
+      }
+      if (there) *reinterpret_cast<u32x4*>(dst + 32 * et + 16 * v + 8 * g) = out;
+    }
+}
+
 // Rows t0 .. t0 + 63 of n into a tile; rows past the end repeat the last one.  lane_off: tile_lane_off.
 template <int D, int NW>
 __device__ __forceinline__ void packed_dma(const uint16_t* src, int stride, int t0, int n, unsigned to, int w, unsigned lane_off) {

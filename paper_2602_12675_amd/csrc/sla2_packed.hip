@@ -10,35 +10,152 @@
 
 namespace sla2 {
 
-template <int D> struct PackedSmem {
-  static constexpr int kTile = PackedTile<D>::kTileBytes;
-  static constexpr int kLd = D + 8;
-  static constexpr int kBytes = 3 * kTile;                     // K, two of V; afterwards the output tile [128][D + 8]
-  static_assert(kRowTile * kLd * 2 <= kBytes, "");
+// S^T = K Q^T of 64 keys at `ka` (with row_read_offset) and a wave's 32 rows, two 32-key halves; reads run two steps ahead
+template <int D>
+__device__ __forceinline__ void packed_scores(unsigned ka, const bf16x8 (&qf)[D / 16], f32x16 (&sacc)[2]) {
+  constexpr int KS = D / 16, KA = 2;
+  u32x4 kr[KA + 1][2];
+#pragma unroll
+  for (int ks = 0; ks < KA; ks++) {
+    kr[ks][0] = lds_read16_untracked<0>(ka ^ (32u * ks));
+    kr[ks][1] = lds_read16_untracked<32 * D * 2>(ka ^ (32u * ks));
+  }
+#pragma unroll
+  for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) sacc[mt][e] = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) {
+    if (ks + KA < KS) {
+      kr[(ks + KA) % (KA + 1)][0] = lds_read16_untracked<0>(ka ^ (32u * (ks + KA)));
+      kr[(ks + KA) % (KA + 1)][1] = lds_read16_untracked<32 * D * 2>(ka ^ (32u * (ks + KA)));
+    }
+    const int ahead = KS - 1 - ks < KA ? KS - 1 - ks : KA;
+#pragma unroll
+    for (int mt = 0; mt < 2; mt++) {
+      wait_lgkmcnt(2 * ahead + 1 - mt);
+      settle(kr[ks % (KA + 1)][mt]);
+      sacc[mt] = mfma_bf16(__builtin_bit_cast(bf16x8, kr[ks % (KA + 1)][mt]), qf[ks], sacc[mt]);
+    }
+  }
+}
+
+// What a wave keeps of its rows: O^T, the reference m of the exponentials (log2) and their sum l
+template <int D> struct RowSums {
+  f32x16 o[D / 32];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int et = 0; et < D / 32; et++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) o[et][e] = 0.f;
+    m = -1e30f;
+    l = 0.f;
+  }
 };
+// .. and what 64 more keys with scores sacc bring to it; V at va (with tr_read_offset)
+template <int D>
+__device__ __forceinline__ void packed_absorb(f32x16 (&sacc)[2], float c1, RowSums<D>& r, unsigned va_lo, unsigned va_hi) {
+  constexpr int ET = D / 32;
+  bf16x8 pf[4];
+  float mx = -INFINITY;
+#pragma unroll
+  for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) mx = fmaxf(mx, sacc[mt][e]);
+  mx = swap_halves_max(mx) * c1;
+  // the reference is kept while the row maximum stays within 2^8 of it (decided for the whole wave)
+  const bool rescale = __builtin_amdgcn_ballot_w64(mx > r.m + 8.f) != 0;
+  const float m_new = rescale ? fmaxf(r.m, mx) : r.m;
+  float rs = 0.f;
+#pragma unroll
+  for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const float p0 = fast_exp2(sacc[mt][e] * c1 - m_new), p1 = fast_exp2(sacc[mt][e + 1] * c1 - m_new);
+      rs += p0 + p1;
+      pf[2 * mt + e / 8][e % 8] = (__bf16)p0;
+      pf[2 * mt + e / 8][e % 8 + 1] = (__bf16)p1;
+    }
+  if (rescale) {
+    const float corr = fast_exp2(r.m - m_new);         // 0 on the first step
+    r.l *= corr;
+    r.m = m_new;
+#pragma unroll
+    for (int et = 0; et < ET; et++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) r.o[et][e] *= corr;
+  }
+  r.l += swap_halves_sum(rs);
+  // O^T += V^T P^T: fragment (ks, et) = two transposing reads, kept three fragments ahead of the products
+  constexpr int kAhead = 3, kFrags = (kTileTokens / 16) * ET;
+  u32x2 vlo[kAhead + 1], vhi[kAhead + 1];
+  auto issue = [&](int f) {
+    vlo[f % (kAhead + 1)] = lds_read_tr_untracked_at<16 * D * 2>(va_lo ^ (64u * (f % ET)), f / ET);
+    vhi[f % (kAhead + 1)] = lds_read_tr_untracked_at<16 * D * 2>(va_hi ^ (64u * (f % ET)), f / ET);
+  };
+#pragma unroll
+  for (int f = 0; f < kAhead; f++) issue(f);
+#pragma unroll
+  for (int f = 0; f < kFrags; f++) {
+    if (f + kAhead < kFrags) issue(f + kAhead);
+    const int left = kFrags - 1 - f;
+    wait_lgkmcnt(2 * (left < kAhead ? left : kAhead));
+    u32x2 &lo = vlo[f % (kAhead + 1)], &hi = vhi[f % (kAhead + 1)];
+    settle(lo);
+    settle(hi);
+    const u32x4 v4 = {lo[0], lo[1], hi[0], hi[1]};
+    r.o[f % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, v4), pf[f / ET], r.o[f % ET]);
+  }
+}
+// scores of the keys from `mine` on (counted from the first of the 64) out of the softmax
+__device__ __forceinline__ void packed_mask(f32x16 (&sacc)[2], int mine, int g) {
+#pragma unroll
+  for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+    for (int e = 0; e < 16; e++)
+      if (32 * mt + 8 * (e / 4) + e % 4 >= mine - 4 * g) sacc[mt][e] = -INFINITY;
+}
+// Q as B operand: lane <- Q[row][16 ks + 8 g + 0..7]; a row past the end repeats the last one
+template <int D>
+__device__ __forceinline__ void packed_load_q(const PackedArgs& a, const TilePlace& at, int hk, int row, int lane, bf16x8 (&qf)[D / 16]) {
+  const int2 x = query_of(a, min(row, at.nq * a.group - 1));
+  const uint16_t* src = a.q + (size_t)(hk * a.group + x.y) * a.sq.h + (size_t)(at.q0 + x.x) * a.sq.t + 8 * (lane / 32);
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
+}
+// a lane's row of the result, and its lse
+template <int D>
+__device__ __forceinline__ void packed_result(const PackedArgs& a, const TilePlace& at, int hk, int row, int lane, RowSums<D>& r) {
+  const bool any = r.l != 0.f, there = row < at.nq * a.group;      // NaN is some
+  if (!any) r.clear();
+  const int2 x = query_of(a, min(row, at.nq * a.group - 1));
+  const int h = hk * a.group + x.y, token = at.q0 + x.x;
+  store_row<D>(r.o, any ? 1.f / r.l : 0.f, a.o + (size_t)h * a.so.h + (size_t)token * a.so.t, lane / 32, there);
+  if (a.lse_out && lane < 32 && there) a.lse_out[(size_t)h * a.Tq + token] = any ? (r.m + log2f(r.l)) * (1.f / kLog2e) : -INFINITY;
+}
+
+// LDS: K, two of V.
+template <int D> constexpr int kPackedSmem = 3 * PackedTile<D>::kTileBytes;
 
 template <int D, bool PARTS>
-__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedArgs a) {
-  constexpr int NW = 4, KS = D / 16, ET = D / 32, LD = D + 8;
-  typedef PackedSmem<D> SM;
-  typedef PackedTile<D> SL;
+__global__ __launch_bounds__(256, D == 128 ? 2 : PARTS ? 3 : 4) void packed_fwd_kernel(PackedArgs a) {
+  constexpr int NW = 4, KS = D / 16, kTile = PackedTile<D>::kTileBytes;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid % kWave, g = lane / 32;
-  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lane = threadIdx.x % kWave;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const TileHead th = tile_head(blockIdx.x, a.Hkv);
   const int hk = th.head;
   TilePlace at = find_tile<false>(a, kRowTile, th.tile, lane);
   if (at.tile < 0) return;
   if (a.causal) at.tile = at.tiles - 1 - at.tile;      // the longest first
-  const int nr = at.nq * a.group, nk = at.nk, row0 = at.tile * kRowTile, row = row0 + 32 * w + lane % 32;
+  const int nr = at.nq * a.group, nk = at.nk, row0 = at.tile * kRowTile, w_row = row0 + 32 * w;
   const uint16_t* kh = a.k + (size_t)hk * a.skv.h + (size_t)at.k0 * a.skv.t;
   const uint16_t* vh = a.v + (size_t)hk * a.skv.h + (size_t)at.k0 * a.skv.t;
-  const int past = nk - at.nq;                          // query i reads the keys below i + past + 1 (causal), all otherwise
-  const int2 my = query_of(a, min(row, nr - 1));       // this lane's query and head
-  const int mine = a.causal ? min(nk, my.x + past + 1) : nk;
+  const int past = nk - at.nq;                         // query i reads the keys below i + past + 1 (causal), all otherwise
+  const int mine = a.causal ? min(nk, query_of(a, min(w_row + lane % 32, nr - 1)).x + past + 1) : nk;
   // the keys that the tile, and this wave, have to do with: below ..; and those that all rows of the wave read
   const int keys = a.causal ? min(nk, max(0, query_of(a, min(row0 + kRowTile, nr) - 1).x + past + 1)) : nk;
-  const int w_row = row0 + 32 * w;
   const int w_keys = w_row >= nr ? 0 : __builtin_amdgcn_readlane(mine, 31), w_full = __builtin_amdgcn_readfirstlane(mine);
   int t_begin = 0, t_end = (keys + kTileTokens - 1) / kTileTokens;
   if (PARTS) {
@@ -47,27 +164,17 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
     t_end = (int)((long long)n * (blockIdx.y + 1) / a.q_parts);
   }
   const unsigned kbuf = lds_address(smem);
-  auto vbuf = [&](int t) { return kbuf + (1 + (t & 1)) * SM::kTile; };
-  const unsigned lane_off = tile_lane_off<D, NW, SL>(a.skv.t, w, lane);
-  auto dma = [&](const uint16_t* src, int t, unsigned to) {
-    packed_dma<D, NW>(src, a.skv.t, t * kTileTokens, nk, to, w, lane_off);
-  };
+  auto vbuf = [&](int t) { return kbuf + (1 + (t & 1)) * kTile; };
+  const unsigned lane_off = tile_lane_off<D, NW, PackedTile<D>>(a.skv.t, w, lane);
+  auto dma = [&](const uint16_t* src, int t, unsigned to) { packed_dma<D, NW>(src, a.skv.t, t * kTileTokens, nk, to, w, lane_off); };
   if (t_begin < t_end) {
     dma(kh, t_begin, kbuf);
     dma(vh, t_begin, vbuf(t_begin));
   }
-  bf16x8 qf[KS];                                       // B operand: lane <- Q[row][16 ks + 8 g + 0..7]
-  {
-    const uint16_t* src = a.q + (size_t)(hk * a.group + my.y) * a.sq.h + (size_t)(at.q0 + my.x) * a.sq.t + 8 * g;
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
-  }
-  f32x16 oacc[ET], sacc[2];
-#pragma unroll
-  for (int et = 0; et < ET; et++)
-#pragma unroll
-    for (int e = 0; e < 16; e++) oacc[et][e] = 0.f;
-  float m_run = -1e30f, l_run = 0.f;                   // reference of the exponentials and running sum, log2 domain
+  bf16x8 qf[KS];
+  packed_load_q<D>(a, at, hk, w_row + lane % 32, lane, qf);
+  RowSums<D> sums;
+  sums.clear();
   const float c1 = kLog2e * a.scale;
   const unsigned k_off = row_read_offset<D>(lane), v_lo = tr_read_offset<D>(lane, 0), v_hi = tr_read_offset<D>(lane, 1);
   wait_vmcnt<0>();
@@ -78,147 +185,27 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
     if (t + 1 < t_end) dma(vh, t + 1, vbuf(t + 1));
     const int t0 = t * kTileTokens;
     const bool work = t0 < w_keys;
-    if (work) {
-      // S^T = K Q^T, two 32-key halves; reads run two steps ahead
-      {
-        const unsigned ka = kbuf + k_off;
-        constexpr int KA = 2;
-        u32x4 kr[KA + 1][2];
-#pragma unroll
-        for (int ks = 0; ks < KA; ks++) {
-          kr[ks][0] = lds_read16_untracked<0>(ka ^ (32u * ks));
-          kr[ks][1] = lds_read16_untracked<32 * D * 2>(ka ^ (32u * ks));
-        }
-#pragma unroll
-        for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-          for (int e = 0; e < 16; e++) sacc[mt][e] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++) {
-          if (ks + KA < KS) {
-            kr[(ks + KA) % (KA + 1)][0] = lds_read16_untracked<0>(ka ^ (32u * (ks + KA)));
-            kr[(ks + KA) % (KA + 1)][1] = lds_read16_untracked<32 * D * 2>(ka ^ (32u * (ks + KA)));
-          }
-          const int ahead = KS - 1 - ks < KA ? KS - 1 - ks : KA;
-#pragma unroll
-          for (int mt = 0; mt < 2; mt++) {
-            wait_lgkmcnt(2 * ahead + 1 - mt);
-            settle(kr[ks % (KA + 1)][mt]);
-            sacc[mt] = mfma_bf16(__builtin_bit_cast(bf16x8, kr[ks % (KA + 1)][mt]), qf[ks], sacc[mt]);
-          }
-        }
-      }
-    }
+    f32x16 sacc[2];
+    if (work) packed_scores<D>(kbuf + k_off, qf, sacc);
     phase_barrier();                                   // K has been read
     if (t + 1 < t_end) dma(kh, t + 1, kbuf);
     if (work) {
-      if (t0 + kTileTokens > w_full) {
-#pragma unroll
-        for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-          for (int e = 0; e < 16; e++)
-            if (t0 + 32 * mt + 8 * (e / 4) + 4 * g + e % 4 >= mine) sacc[mt][e] = -INFINITY;
-      }
-      bf16x8 pf[4];
-      {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-          for (int e = 0; e < 16; e++) mx = fmaxf(mx, sacc[mt][e]);
-        mx = swap_halves_max(mx) * c1;
-        // the reference is kept while the row maximum stays within 2^8 of it (decided for the whole wave)
-        const bool rescale = __builtin_amdgcn_ballot_w64(mx > m_run + 8.f) != 0;
-        const float m_new = rescale ? fmaxf(m_run, mx) : m_run;
-        float rs = 0.f;
-#pragma unroll
-        for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            const float p0 = fast_exp2(sacc[mt][e] * c1 - m_new), p1 = fast_exp2(sacc[mt][e + 1] * c1 - m_new);
-            rs += p0 + p1;
-            pf[2 * mt + e / 8][e % 8] = (__bf16)p0;
-            pf[2 * mt + e / 8][e % 8 + 1] = (__bf16)p1;
-          }
-        if (rescale) {
-          const float corr = fast_exp2(m_run - m_new);   // 0 on the first tile
-          l_run *= corr;
-          m_run = m_new;
-#pragma unroll
-          for (int et = 0; et < ET; et++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) oacc[et][e] *= corr;
-        }
-        l_run += swap_halves_sum(rs);
-      }
-      // O^T += V^T P^T: fragment (ks, et) = two transposing reads, kept three fragments ahead of the products
-      {
-        constexpr int kAhead = 3, kFrags = (kTileTokens / 16) * ET;
-        const unsigned va_lo = vbuf(t) + v_lo, va_hi = vbuf(t) + v_hi;
-        u32x2 vlo[kAhead + 1], vhi[kAhead + 1];
-        auto issue = [&](int f) {
-          vlo[f % (kAhead + 1)] = lds_read_tr_untracked_at<16 * D * 2>(va_lo ^ (64u * (f % ET)), f / ET);
-          vhi[f % (kAhead + 1)] = lds_read_tr_untracked_at<16 * D * 2>(va_hi ^ (64u * (f % ET)), f / ET);
-        };
-#pragma unroll
-        for (int f = 0; f < kAhead; f++) issue(f);
-#pragma unroll
-        for (int f = 0; f < kFrags; f++) {
-          if (f + kAhead < kFrags) issue(f + kAhead);
-          const int left = kFrags - 1 - f;
-          wait_lgkmcnt(2 * (left < kAhead ? left : kAhead));
-          u32x2 &lo = vlo[f % (kAhead + 1)], &hi = vhi[f % (kAhead + 1)];
-          settle(lo);
-          settle(hi);
-          const u32x4 v4 = {lo[0], lo[1], hi[0], hi[1]};
-          oacc[f % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, v4), pf[f / ET], oacc[f % ET]);
-        }
-      }
+      if (t0 + kTileTokens > w_full) packed_mask(sacc, mine - t0, lane / 32);
+      packed_absorb<D>(sacc, c1, sums, vbuf(t) + v_lo, vbuf(t) + v_hi);
     }
-    wait_vmcnt<0>();                                   // the next tile has landed, for everyone behind the barrier
+    wait_vmcnt<0>();                                   // the next step's K and V have landed, for everyone behind the barrier
     phase_barrier();
   }
-  const bool any = l_run != 0.f;                       // NaN is some
   // from here on the lane's place is made again: it is not kept through the loop
-  const int ln = (int)lane_again(), ge = ln / 32, rowe = row0 + 32 * w + ln % 32;
+  const int ln = (int)lane_again(), row = w_row + ln % 32;
   if (PARTS) {
-    if (rowe >= nr) return;
-    const size_t row_at = (size_t)blockIdx.y * a.Tq * a.H + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + rowe;   // among the rows of all key heads
-    float* dst = a.part_o + row_at * D;
-#pragma unroll
-    for (int et = 0; et < ET; et++)
-#pragma unroll
-      for (int v4 = 0; v4 < 4; v4++)
-        *reinterpret_cast<f32x4*>(dst + 32 * et + 8 * v4 + 4 * ge) =
-            f32x4{oacc[et][4 * v4], oacc[et][4 * v4 + 1], oacc[et][4 * v4 + 2], oacc[et][4 * v4 + 3]};
-    if (ge == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * row_at) = make_float2(m_run, l_run);
+    if (row >= nr) return;
+    const size_t row_at = (size_t)blockIdx.y * a.Tq * a.H + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + row;   // among the rows of all key heads
+    store_part<D>(sums.o, a.part_o + row_at * D, ln / 32);
+    if (ln < 32) *reinterpret_cast<float2*>(a.part_ml + 2 * row_at) = make_float2(sums.m, sums.l);
     return;
   }
-  // ---- normalise, transpose through LDS, whole rows out ----
-  uint16_t* os = reinterpret_cast<uint16_t*>(smem);
-  const float inv = any ? 1.f / l_run : 0.f;
-#pragma unroll
-  for (int et = 0; et < ET; et++)
-#pragma unroll
-    for (int v4 = 0; v4 < 4; v4++) {
-      bf16x4 pk;
-#pragma unroll
-      for (int r = 0; r < 4; r++) pk[r] = (__bf16)(any ? inv * oacc[et][4 * v4 + r] : 0.f);
-      *reinterpret_cast<bf16x4*>(os + (32 * w + ln % 32) * LD + 32 * et + 8 * v4 + 4 * ge) = pk;
-    }
-  if (a.lse_out && ge == 0 && rowe < nr) {
-    const int2 x = query_of(a, rowe);
-    a.lse_out[(size_t)(hk * a.group + x.y) * a.Tq + at.q0 + x.x] = any ? (m_run + log2f(l_run)) * (1.f / kLog2e) : -INFINITY;
-  }
-  wave_lds_fence();                                    // a wave stores the rows that it wrote
-#pragma unroll
-  for (int i = 0; i < 32 * (D / 8) / kWave; i++) {
-    const int idx = ln + kWave * i, r = 32 * w + idx / (D / 8), ch = idx % (D / 8);
-    if (row0 + r >= nr) continue;
-    const int2 x = query_of(a, row0 + r);
-    *reinterpret_cast<u32x4*>(a.o + (size_t)(hk * a.group + x.y) * a.so.h + (size_t)(at.q0 + x.x) * a.so.t + 8 * ch) =
-        *reinterpret_cast<const u32x4*>(os + r * LD + 8 * ch);
-  }
+  packed_result<D>(a, at, hk, row, ln, sums);
 }
 
 // The parts of one row: their O, weighted with 2^(m - the largest m), over their l, weighted alike.  A wave a row.
@@ -275,10 +262,10 @@ template <int D> static hipError_t launch_fwd(const PackedArgs& a, hipStream_t s
   const long long grid = most_tiles((long long)a.Tq * a.group, a.S, kRowTile) * a.Hkv;
   if (!grid) return hipSuccess;
   if (a.q_parts == 1) {
-    packed_fwd_kernel<D, false><<<(unsigned)grid, 256, PackedSmem<D>::kBytes, stream>>>(a);
+    packed_fwd_kernel<D, false><<<(unsigned)grid, 256, kPackedSmem<D>, stream>>>(a);
     return hipGetLastError();
   }
-  packed_fwd_kernel<D, true><<<dim3((unsigned)grid, a.q_parts), 256, PackedSmem<D>::kBytes, stream>>>(a);
+  packed_fwd_kernel<D, true><<<dim3((unsigned)grid, a.q_parts), 256, kPackedSmem<D>, stream>>>(a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   packed_join_kernel<D><<<(unsigned)(((long long)a.Tq * a.H + 3) / 4), 256, 0, stream>>>(a);
   return hipGetLastError();

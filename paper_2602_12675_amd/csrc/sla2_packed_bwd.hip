@@ -10,43 +10,10 @@ namespace sla2 {
 
 template <int D> struct PackedBwdSmem {
   static constexpr int kTile = PackedTile<D>::kTileBytes;
-  static constexpr int kLd = D + 8;
   static constexpr int kStatOff = 4 * kTile;                   // float [2][2][64]: lse log2(e) and D of a step's rows (key side)
   static constexpr int kBytes = kStatOff + 4 * 64 * 4;
-  static_assert(4 * 32 * kLd * 2 <= kStatOff, "32 result rows of a wave in the place of the tiles");
 };
 
-// 32 rows of a wave from accumulators (channels x rows) through LDS to memory, times `by`; row_ptr(r): where row r goes, null: nowhere
-template <int D, class Row>
-__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float by, uint16_t* os /* [32][D + 8], of this wave */, int lane, Row row_ptr) {
-  constexpr int LD = D + 8;
-#pragma unroll
-  for (int et = 0; et < D / 32; et++)
-#pragma unroll
-    for (int v4 = 0; v4 < 4; v4++) {
-      bf16x4 pk;
-#pragma unroll
-      for (int r = 0; r < 4; r++) pk[r] = (__bf16)(by * acc[et][4 * v4 + r]);
-      *reinterpret_cast<bf16x4*>(os + lane % 32 * LD + 32 * et + 8 * v4 + 4 * (lane / 32)) = pk;
-    }
-  wave_lds_fence();
-#pragma unroll
-  for (int i = 0; i < 32 * (D / 8) / kWave; i++) {
-    const int idx = lane + kWave * i, r = idx / (D / 8), ch = idx % (D / 8);
-    uint16_t* dst = row_ptr(r);
-    if (dst) *reinterpret_cast<u32x4*>(dst + 8 * ch) = *reinterpret_cast<const u32x4*>(os + r * LD + 8 * ch);
-  }
-  wave_lds_fence();
-}
-template <int D>
-__device__ __forceinline__ void store_part(const f32x16 (&acc)[D / 32], float* dst, int g) {
-#pragma unroll
-  for (int et = 0; et < D / 32; et++)
-#pragma unroll
-    for (int v4 = 0; v4 < 4; v4++)
-      *reinterpret_cast<f32x4*>(dst + 32 * et + 8 * v4 + 4 * g) =
-          f32x4{acc[et][4 * v4], acc[et][4 * v4 + 1], acc[et][4 * v4 + 2], acc[et][4 * v4 + 3]};
-}
 __device__ __forceinline__ void pin(bf16x8& f) {       // converted here: eight registers less than the fp32 values
   u32x4 u = __builtin_bit_cast(u32x4, f);
   settle(u);
@@ -128,7 +95,6 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
   if (t_begin < t_end) dma(t_begin);
   bf16x8 qf[KS], gf[KS];
   float delta = 0.f;
-  const size_t row_at = (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + row;       // among the rows of all key heads
   const int h = hk * a.group + my.y, token = at.q0 + my.x;
   {
     const uint16_t* src = a.q + (size_t)h * a.sq.h + (size_t)token * a.sq.t + 8 * g;
@@ -219,15 +185,14 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
     wait_vmcnt<0>();
     phase_barrier();
   }
+  const int ln = (int)lane_again(), last_row = w_row + ln % 32;    // what is made of the lane's place is not kept through the loop
   if (PARTS) {
-    if (row < nr) store_part<D>(acc, a.part_o + ((size_t)blockIdx.y * a.Tq * a.H + row_at) * D, g);
+    const size_t part = (size_t)blockIdx.y * a.Tq * a.H + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + last_row;   // among the rows of all key heads
+    if (last_row < nr) store_part<D>(acc, a.part_o + part * D, ln / 32);
     return;
   }
-  store_rows<D>(acc, a.scale, reinterpret_cast<uint16_t*>(smem) + w * 32 * SM::kLd, lane, [&](int r) -> uint16_t* {
-    if (w_row + r >= nr) return nullptr;
-    const int2 x = query_of(a, w_row + r);
-    return a.dq + (size_t)(hk * a.group + x.y) * a.sq.h + (size_t)(at.q0 + x.x) * a.sq.t;
-  });
+  const int2 x = query_of(a, min(last_row, nr - 1));
+  store_row<D>(acc, a.scale, a.dq + (size_t)(hk * a.group + x.y) * a.sq.h + (size_t)(at.q0 + x.x) * a.sq.t, ln / 32, last_row < nr);
 }
 
 // dK and dV of 128 keys: S = Q K^T and dP = dO V^T (rows x keys), a key on lanes l and l + 32 with its row of K and V in registers;
@@ -399,23 +364,17 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
     phase_barrier();                                   // ... for everyone; this step's tiles are free
     cur = following;
   }
-  const int ln = (int)lane_again();                    // what is made of the lane's place is not kept through the loop
+  const int ln = (int)lane_again(), key = w_key + ln % 32, g = ln / 32;      // what is made of the lane's place is not kept through the loop
   if (parts) {
-    const int key = w_key + ln % 32;
     if (key >= nk) return;
     const size_t part = ((size_t)blockIdx.y * a.Tk + at.k0 + key) * a.Hkv + hk;
-    store_part<D>(dk, a.part_kv + part * D, ln / 32);
-    store_part<D>(dv, a.part_kv + ((size_t)a.k_parts * a.Tk * a.Hkv + part) * D, ln / 32);
+    store_part<D>(dk, a.part_kv + part * D, g);
+    store_part<D>(dv, a.part_kv + ((size_t)a.k_parts * a.Tk * a.Hkv + part) * D, g);
     return;
   }
-  uint16_t* os = reinterpret_cast<uint16_t*>(smem) + w * 32 * SM::kLd;
-  auto to = [&](uint16_t* p) {
-    return [=](int r) -> uint16_t* {
-      return w_key + r < nk ? p + (size_t)hk * a.skv.h + (size_t)(at.k0 + w_key + r) * a.skv.t : nullptr;
-    };
-  };
-  store_rows<D>(dk, a.scale, os, ln, to(a.dk));
-  store_rows<D>(dv, 1.f, os, ln, to(a.dv));
+  const size_t to = (size_t)hk * a.skv.h + (size_t)(at.k0 + key) * a.skv.t;
+  store_row<D>(dk, a.scale, a.dk + to, g, key < nk);
+  store_row<D>(dv, 1.f, a.dv + to, g, key < nk);
 }
 
 // Sums of the parts, four channels a thread: dQ (rows of all key heads), dK and dV.
