@@ -8,6 +8,7 @@ import of this module fails: there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -439,57 +440,72 @@ def sla2_packed_workspace_bytes(params: PackedParams, backward=False) -> int:
     return _lib.sla2_packed_workspace_bytes(ctypes.byref(params), int(backward))
 
 
-def _packed_sizes(p):
-    """(elements of q, of k; element type; elements of q_start; whether q, k and out are contiguous)"""
-    return (p.tokens_q * p.H * p.d, p.tokens_k * p.H_kv * p.d, _TYPES.get(p.dtype), p.sequences + 1, p.q_stride[1] == 0,
-            p.kv_stride[1] == 0, p.out_stride[1] == 0)
+# What the binding checks tensors against follows from the parameters' content alone; worked out once for each content (reading the fields
+# of a structure takes a quarter of a small call's time).
+@functools.lru_cache(maxsize=256)
+def _packed_sizes(content):
+    """(elements of q, of k; element type; elements of q_start, of lse; whether q, k and out are contiguous)"""
+    p = PackedParams.from_buffer_copy(content)
+    return (p.tokens_q * p.H * p.d, p.tokens_k * p.H_kv * p.d, _TYPES.get(p.dtype), p.sequences + 1, p.H * p.tokens_q,
+            p.q_stride[1] == 0, p.kv_stride[1] == 0, p.out_stride[1] == 0)
 
 
 def sla2_packed_forward(params, q, k, v, q_start, k_start, out, lse=None, workspace=None, stream=None, check=True, ws_bytes=None) -> int:
-    nq, nk, dt, ns, cq, ck, co = _packed_sizes(params)
+    nq, nk, dt, ns, nl, cq, ck, co = _packed_sizes(bytes(params))
     return _call(_lib.sla2_packed_forward, params, (
         (q, dt, nq, cq), (k, dt, nk, ck), (v, dt, nk, ck), (q_start, torch.int32, ns, True), (k_start, torch.int32, ns, True),
-        (out, dt, nq, co), (lse, torch.float32, params.H * params.tokens_q, True), _scratch(workspace)), stream, check,
+        (out, dt, nq, co), (lse, torch.float32, nl, True), _scratch(workspace)), stream, check,
         _bytes(workspace, ws_bytes))
 
 
 def sla2_packed_backward(params, q, k, v, q_start, k_start, out, lse, dout, dq, dk, dv, workspace=None, stream=None, check=True,
                          ws_bytes=None) -> int:
-    nq, nk, dt, ns, cq, ck, co = _packed_sizes(params)
+    nq, nk, dt, ns, nl, cq, ck, co = _packed_sizes(bytes(params))
     return _call(_lib.sla2_packed_backward, params, (
         (q, dt, nq, cq), (k, dt, nk, ck), (v, dt, nk, ck), (q_start, torch.int32, ns, True), (k_start, torch.int32, ns, True),
-        (out, dt, nq, co), (lse, torch.float32, params.H * params.tokens_q, True), (dout, dt, nq, co), (dq, dt, nq, cq), (dk, dt, nk, ck),
+        (out, dt, nq, co), (lse, torch.float32, nl, True), (dout, dt, nq, co), (dq, dt, nq, cq), (dk, dt, nk, ck),
         (dv, dt, nk, ck), _scratch(workspace)), stream, check, _bytes(workspace, ws_bytes))
 
 
 _CODES = {SLA2_QUANT_NONE: (torch.bfloat16,), SLA2_QUANT_FP8: (torch.float8_e4m3fn, torch.uint8), SLA2_QUANT_INT8: (torch.int8,)}
 
 
-def _cache_tensors(p, k_cache, v_cache, k_scale, v_scale, page_table):
+@functools.lru_cache(maxsize=256)
+def _cache_sizes(content):
+    """(sequences; element type; elements of k, q and lse; whether k, q and out are contiguous; types, elements of a cache, of its scales,
+    of the page table; whether cache and table are contiguous)"""
+    p = CacheParams.from_buffer_copy(content)
+    rows = p.pages * p.H_kv * p.page_size
+    return (p.B, _TYPES.get(p.dtype), p.tokens * p.H_kv * p.d, p.B * p.H * p.d, p.B * p.H, p.kv_stride[1] == 0, p.q_stride[1] == 0,
+            p.out_stride[1] == 0, _CODES.get(p.quant_mode, (None,)), rows * p.d, rows, 0 if p.table_stride else p.B * p.max_pages,
+            p.cache_stride[2] == 0, p.table_stride == 0)
+
+
+def _cache_tensors(sizes, k_cache, v_cache, k_scale, v_scale, page_table):
     """The arguments of the cache as _call takes them.  Codes of FP8 may be held as uint8."""
-    types = _CODES.get(p.quant_mode, (None,))
-    rows, dense = p.pages * p.H_kv * p.page_size, p.cache_stride[2] == 0
-    table = (p.B - 1) * p.table_stride + p.max_pages if p.table_stride else p.B * p.max_pages
-    kinds = [getattr(t, "dtype", None) if getattr(t, "dtype", None) in types else types[0] for t in (k_cache, v_cache)]
-    return ((k_cache, kinds[0], rows * p.d, dense), (v_cache, kinds[1], rows * p.d, dense), (k_scale, torch.float32, rows, True),
-            (v_scale, torch.float32, rows, True), (page_table, torch.int32, 0 if p.table_stride else table, p.table_stride == 0))
+    types, n, rows, columns, dense, table = sizes[8:]
+    kt, vt = getattr(k_cache, "dtype", None), getattr(v_cache, "dtype", None)
+    return ((k_cache, kt if kt in types else types[0], n, dense), (v_cache, vt if vt in types else types[0], n, dense),
+            (k_scale, torch.float32, rows, True), (v_scale, torch.float32, rows, True), (page_table, torch.int32, columns, table))
 
 
 def sla2_cache_write(params, k, v, page_table, k_cache, v_cache, k_scale=None, v_scale=None, start=None, first=None, stream=None,
                      check=True) -> int:
-    n, dense, dt = params.tokens * params.H_kv * params.d, params.kv_stride[1] == 0, _TYPES.get(params.dtype)
-    kc, vc, ks, vs, table = _cache_tensors(params, k_cache, v_cache, k_scale, v_scale, page_table)
+    sizes = _cache_sizes(bytes(params))
+    b, dt, n, dense = sizes[0], sizes[1], sizes[2], sizes[5]
+    kc, vc, ks, vs, table = _cache_tensors(sizes, k_cache, v_cache, k_scale, v_scale, page_table)
     return _call(_lib.sla2_cache_write, params, (
-        (k, dt, n, dense), (v, dt, n, dense), (start, torch.int32, params.B + 1, True), (first, torch.int32, params.B, True), table, kc, vc,
+        (k, dt, n, dense), (v, dt, n, dense), (start, torch.int32, b + 1, True), (first, torch.int32, b, True), table, kc, vc,
         ks, vs), stream, check)
 
 
 def sla2_cache_read(params, k_cache, v_cache, page_table, k, v, k_scale=None, v_scale=None, start=None, first=None, stream=None,
                     check=True) -> int:
-    n, dense, dt = params.tokens * params.H_kv * params.d, params.kv_stride[1] == 0, _TYPES.get(params.dtype)
-    kc, vc, ks, vs, table = _cache_tensors(params, k_cache, v_cache, k_scale, v_scale, page_table)
+    sizes = _cache_sizes(bytes(params))
+    b, dt, n, dense = sizes[0], sizes[1], sizes[2], sizes[5]
+    kc, vc, ks, vs, table = _cache_tensors(sizes, k_cache, v_cache, k_scale, v_scale, page_table)
     return _call(_lib.sla2_cache_read, params, (
-        kc, vc, ks, vs, (start, torch.int32, params.B + 1, True), (first, torch.int32, params.B, True), table, (k, dt, n, dense),
+        kc, vc, ks, vs, (start, torch.int32, b + 1, True), (first, torch.int32, b, True), table, (k, dt, n, dense),
         (v, dt, n, dense)), stream, check)
 
 
@@ -499,11 +515,12 @@ def sla2_cache_workspace_bytes(params: CacheParams) -> int:
 
 def sla2_cache_attention(params, q, k_cache, v_cache, page_table, length, out, k_scale=None, v_scale=None, lse=None, workspace=None,
                          stream=None, check=True, ws_bytes=None) -> int:
-    n, dt, f32 = params.B * params.H * params.d, _TYPES.get(params.dtype), torch.float32
-    kc, vc, ks, vs, table = _cache_tensors(params, k_cache, v_cache, k_scale, v_scale, page_table)
+    sizes = _cache_sizes(bytes(params))
+    b, dt, n, rows = sizes[0], sizes[1], sizes[3], sizes[4]
+    kc, vc, ks, vs, table = _cache_tensors(sizes, k_cache, v_cache, k_scale, v_scale, page_table)
     return _call(_lib.sla2_cache_attention, params, (
-        (q, dt, n, params.q_stride[1] == 0), kc, vc, ks, vs, (length, torch.int32, params.B, True), table,
-        (out, dt, n, params.out_stride[1] == 0), (lse, f32, params.B * params.H, True), _scratch(workspace)), stream, check,
+        (q, dt, n, sizes[6]), kc, vc, ks, vs, (length, torch.int32, b, True), table,
+        (out, dt, n, sizes[7]), (lse, torch.float32, rows, True), _scratch(workspace)), stream, check,
         _bytes(workspace, ws_bytes))
 
 

@@ -12,7 +12,7 @@ constexpr int kCacheThreads = 256, kCacheRows = 64;      // rows of a workgroup:
 
 // Where row i of k and v is in the cache: page and slot; page -1: nowhere, -2: the row is of no sequence.  A row a lane, the rows of a
 // wave being neighbours.  Its sequence is the number of sequences that end at or in front of it, counted 64 at a time: for all rows at
-// once where no sequence ends between them.
+// once where no sequence ends between them.  (Offsets that do not ascend give some sequence, whose pages bound the place.)
 struct Place {
   int page, slot;
 };
@@ -25,10 +25,14 @@ __device__ __forceinline__ Place place_of(const CacheArgs& a, int i, int lane) {
     for (int s0 = 0; s0 < a.B; s0 += kWave) {
       const int end = s0 + lane < a.B ? a.start[s0 + lane + 1] : INT32_MAX;
       const unsigned long long before = __builtin_amdgcn_ballot_w64(end <= i0);
-      const unsigned long long between = __builtin_amdgcn_ballot_w64(end <= i1) & ~before;
-      b += __builtin_popcountll(before);
-      for (unsigned long long rest = between; rest; rest &= rest - 1)
-        b += __builtin_amdgcn_readlane(end, __builtin_ctzll(rest)) <= i ? 1 : 0;
+      if (__builtin_amdgcn_ballot_w64(end <= i1) == before) {
+        b += __builtin_popcountll(before);
+        continue;
+      }
+      int n = 0;                                         // halving: the ends ascend
+#pragma unroll
+      for (int step = kWave / 2; step; step /= 2) n += __shfl(end, n + step - 1) <= i ? step : 0;
+      b += n + (__shfl(end, n) <= i ? 1 : 0);
     }
   }
   if (i >= a.tokens || b >= a.B) return Place{-2, 0};

@@ -40,6 +40,7 @@ __device__ __forceinline__ long long uniform64(long long x) {
 }
 // the length of the line; all lanes of the wave take part
 __device__ __forceinline__ long long line_length(const CacheArgs& a, int lane) {
+  if (a.B == 1) return kOverhead + blocks_of(tokens_of(a, 0));
   long long n = 0;
   for (int b = lane; b < a.B; b += kWave) n += kOverhead + blocks_of(tokens_of(a, b));
   return wave_total(n);
@@ -51,6 +52,7 @@ struct OnLine {
 };
 __device__ __forceinline__ OnLine on_line(const CacheArgs& a, long long x, int of, int lane) {
   long long at = 0;
+  if (a.B == 1) return OnLine{0, 0};
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const int b = b0 + lane;
     const int own = b < a.B ? kOverhead + blocks_of(tokens_of(a, b)) : 0;
@@ -337,12 +339,14 @@ __global__ __launch_bounds__(kDecodeWaves * kWave, 2) void cache_attention_kerne
 }
 
 // A sequence and head whose blocks several workgroups had: their O, weighted with 2^(m - the largest m), over their l, weighted alike.
+// W of a workgroup's 8 waves for each head.
 constexpr int kJoinWaves = 8;
-template <int D>
+template <int D, int W>
 __global__ __launch_bounds__(kJoinWaves * kWave) void cache_join_kernel(CacheArgs a) {
   constexpr int E = D / kWave;                                     // channels of a lane
   __shared__ float part[kJoinWaves][D + 1];
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, h = blockIdx.x, b = blockIdx.y;
+  const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), b = blockIdx.y;
+  const int h = blockIdx.x * (kJoinWaves / W) + w / W;
   const int nb = blocks_of(tokens_of(a, b));
   if (!nb) return;
   const long long all = line_length(a, lane), first = on_line(a, 0, b, lane).at + kOverhead;
@@ -350,32 +354,38 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void cache_join_kernel(CacheArg
   const int p0 = (int)(((first + 1) * a.parts - 1) / all), p1 = (int)(((first + nb) * a.parts - 1) / all);
   if (p0 == p1) return;                                            // written by the one that had it
   auto slot = [&](int p) { return ((size_t)p * 2 + (p == p0 ? 1 : 0)) * a.H + h; };
-  float m = -INFINITY;
-  for (int p = p0 + lane; p <= p1; p += kWave) m = fmaxf(m, a.part_ml[2 * slot(p)]);
-  m = wave_max(m);
-  float l = 0.f, o[E] = {};
-  for (int p = p0 + w; p <= p1; p += kJoinWaves) {
-    const float2 ml = *(const float2*)(a.part_ml + 2 * slot(p));
-    const float by = fast_exp2(ml.x - m);
-    l += by * ml.y;
+  float m = -INFINITY, l = 0.f, o[E] = {};
+  if (h < a.H) {
+    for (int p = p0 + lane; p <= p1; p += kWave) m = fmaxf(m, a.part_ml[2 * slot(p)]);
+    m = wave_max(m);
+#pragma unroll 4
+    for (int p = p0 + w % W; p <= p1; p += W) {
+      const float2 ml = *(const float2*)(a.part_ml + 2 * slot(p));
+      const float by = fast_exp2(ml.x - m);
+      l += by * ml.y;
 #pragma unroll
-    for (int e = 0; e < E; e++) o[e] += by * a.part_o[slot(p) * D + E * lane + e];
+      for (int e = 0; e < E; e++) o[e] += by * a.part_o[slot(p) * D + E * lane + e];
+    }
   }
+  if (W > 1) {
 #pragma unroll
-  for (int e = 0; e < E; e++) part[w][E * lane + e] = o[e];
-  if (lane == 0) part[w][D] = l;
-  __syncthreads();
-  if (tid >= D) return;
-  float sum = 0.f, total = 0.f;
+    for (int e = 0; e < E; e++) part[w][E * lane + e] = o[e];
+    if (lane == 0) part[w][D] = l;
+    __syncthreads();
+    if (w) return;
 #pragma unroll
-  for (int x = 0; x < kJoinWaves; x++) {
-    sum += part[x][tid];
-    total += part[x][D];
+    for (int x = 1; x < W; x++) {
+      l += part[x][D];
+#pragma unroll
+      for (int e = 0; e < E; e++) o[e] += part[x][E * lane + e];
+    }
   }
-  const bool any = total != 0.f;
-  const __bf16 r = (__bf16)(any ? sum / total : 0.f);
-  a.out[(size_t)b * a.out_b + (size_t)h * a.out_h + tid] = __builtin_bit_cast(uint16_t, r);
-  if (a.lse && tid == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(total)) * (1.f / kLog2e) : -INFINITY;
+  if (h >= a.H) return;
+  const bool any = l != 0.f;
+  uint16_t* dst = a.out + (size_t)b * a.out_b + (size_t)h * a.out_h + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; e++) dst[e] = __builtin_bit_cast(uint16_t, (__bf16)(any ? o[e] / l : 0.f));
+  if (a.lse && lane == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
 }
 
 // Sequences of at most 1,024 tokens: a workgroup each.  Longer ones: as many workgroups as two to a CU are, which share the line.
@@ -399,9 +409,15 @@ hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t stream) {
   else SLA2_DECODE(64);
 #undef SLA2_DECODE
   if (hipError_t e = hipGetLastError(); e != hipSuccess || a.parts <= 1) return e;
-  const dim3 heads(a.H, a.B);
-  if (a.d == 128) cache_join_kernel<128><<<heads, kJoinWaves * kWave, 0, stream>>>(a);
-  else cache_join_kernel<64><<<heads, kJoinWaves * kWave, 0, stream>>>(a);
+  // few sequences and heads: all waves of a workgroup for one, so that its parts are read at once
+  const bool few = (long long)a.B * a.H < 256;
+  const dim3 join(few ? a.H : (a.H + kJoinWaves - 1) / kJoinWaves, a.B);
+#define SLA2_JOIN(D)                                                                                    \
+  (few ? cache_join_kernel<D, kJoinWaves><<<join, kJoinWaves * kWave, 0, stream>>>(a)                   \
+       : cache_join_kernel<D, 1><<<join, kJoinWaves * kWave, 0, stream>>>(a))
+  if (a.d == 128) SLA2_JOIN(128);
+  else SLA2_JOIN(64);
+#undef SLA2_JOIN
   return hipGetLastError();
 }
 
