@@ -410,7 +410,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t stream) {
 #undef SLA2_DECODE
   if (hipError_t e = hipGetLastError(); e != hipSuccess || a.parts <= 1) return e;
   // few sequences and heads: all waves of a workgroup for one, so that its parts are read at once
-  const bool few = (long long)a.B * a.H < 256;
+  const bool few = (long long)a.B * a.H < 1024;
   const dim3 join(few ? a.H : (a.H + kJoinWaves - 1) / kJoinWaves, a.B);
 #define SLA2_JOIN(D)                                                                                    \
   (few ? cache_join_kernel<D, kJoinWaves><<<join, kJoinWaves * kWave, 0, stream>>>(a)                   \

@@ -236,26 +236,37 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   if (a.lse_out && lane == 0) a.lse_out[(size_t)h * a.Tq + x.x] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
 }
 
-// Parts of a tile of rows: as many as fill two workgroups a CU where the tiles alone do not fill half of them, none shorter than 256 keys.
+// Parts of a tile of rows, where the tiles leave places for them (two workgroups a CU): as many as take the least time, by what was measured
+// of each: a step 1.1 us (backward 1.5) for a workgroup on its own, the joining 6 us and 4 TB/s of parts written and read.  Not known here
+// are the lengths; the longest sequence is taken to have twice its share of the keys.
 // Parts of a tile of keys: so that no workgroup has much more than its share of all steps, which with a causal mask or sequences of
 // different lengths the first tiles have.
 void plan_packed(PackedArgs* a, bool backward) {
   a->q_parts = a->k_parts = 1;
   const long long rows = (long long)a->Tq * a->group, places = 512;
   const long long q_tiles = most_tiles(rows, a->S, kRowTile) * a->Hkv, k_tiles = most_tiles(a->Tk, a->S, kKeyTile) * a->Hkv;
-  if (q_tiles && q_tiles * 2 <= places) {
-    const long long n = places / q_tiles, most = a->Tk / 256;
-    a->q_parts = (int)(n < most ? n : most < 1 ? 1 : most);
+  const long long longest = a->S == 1 ? a->Tk : a->S == 2 ? a->Tk * 3 / 4 : 2ll * a->Tk / a->S, steps = (longest + kTileTokens - 1) / kTileTokens;
+  if (q_tiles && q_tiles <= places && steps) {
+    const double step = backward ? 1.5 : 1.1, bytes = (double)a->Tq * a->H * a->d * 8;
+    double best = steps * step;
+    for (int n = 2; n <= 64 && (n - 1) * q_tiles < 2 * places && n * 4 <= steps; n++) {
+      const long long rounds = (n * q_tiles + places - 1) / places;      // a causal mask halves what they have on average
+      const double time = (double)((steps + n - 1) / n) * (a->causal ? (rounds + 1) / 2.0 : (double)rounds) * step + 6 + n * bytes / 4e6;
+      if (time < best) {
+        best = time;
+        a->q_parts = n;
+      }
+    }
   }
   if (!backward || !k_tiles || !rows) return;
   // Steps of 64 rows of all tiles of keys, were the sequences alike, over the places, and a little more, so that the last round is not
   // a few workgroups; at most 16 parts of the longest sequence that there can be.
-  const long long steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + kKeyTile - 1) / kKeyTile * a->Hkv * ((steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
+  const long long row_steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + kKeyTile - 1) / kKeyTile * a->Hkv * ((row_steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
   long long chunk = all / places + all / (places * 12) + 1;
   if (chunk < 16) chunk = 16;
-  if (chunk < (steps + 15) / 16) chunk = (steps + 15) / 16;
+  if (chunk < (row_steps + 15) / 16) chunk = (row_steps + 15) / 16;
   a->k_chunk = (int)chunk;
-  a->k_parts = (int)((steps + chunk - 1) / chunk);
+  a->k_parts = (int)((row_steps + chunk - 1) / chunk);
 }
 
 template <int D> static hipError_t launch_fwd(const PackedArgs& a, hipStream_t stream) {
