@@ -222,39 +222,52 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
     if (t_begin >= t_end && blockIdx.y) return;
     t_end = min(t_end, t_begin + a.k_chunk);
   }
-  const uint16_t* qh = a.q + (size_t)hk * a.group * a.sq.h + (size_t)at.q0 * a.sq.t;
-  const uint16_t* gh = a.dout + (size_t)hk * a.group * a.so.h + (size_t)at.q0 * a.so.t;
   const size_t st0 = stat_first(a, hk, at.s, at.q0);
-  // block 4 t, counted along: query block and head
+  // A block: its query block and head, and where it begins in Q and dO.  Counted along, not worked out: the scalar unit's multiplications
+  // and divisions, 320 instructions a step, took a quarter of the kernel's time.
   struct Block {
     int q, h;
+    const uint16_t *qp, *gp;
+  };
+  const long long q_row = (long long)kQueryBlock * a.sq.t, g_row = (long long)kQueryBlock * a.so.t;
+  auto next = [&](Block b) {
+    const bool wrap = b.h + 1 == a.group;              // on to the next queries
+    return Block{b.q + wrap, wrap ? 0 : b.h + 1, b.qp + (wrap ? q_row - (a.group - 1) * a.sq.h : a.sq.h),
+                 b.gp + (wrap ? g_row - (a.group - 1) * a.so.h : a.so.h)};
   };
   const int four_q = 4 / a.group, four_h = 4 % a.group;
-  auto next = [&](Block b) { return b.h + 1 == a.group ? Block{b.q + 1, 0} : Block{b.q, b.h + 1}; };
-  auto after4 = [&](Block b) { return b.h + four_h >= a.group ? Block{b.q + four_q + 1, b.h + four_h - a.group} : Block{b.q + four_q, b.h + four_h}; };
+  const long long q_four = four_q * q_row + four_h * a.sq.h, g_four = four_q * g_row + four_h * a.so.h;
+  auto after4 = [&](Block b) {
+    const bool wrap = b.h + four_h >= a.group;
+    return Block{b.q + four_q + wrap, b.h + four_h - (wrap ? a.group : 0), b.qp + q_four + (wrap ? q_row - a.group * a.sq.h : 0),
+                 b.gp + g_four + (wrap ? g_row - a.group * a.so.h : 0)};
+  };
   auto qbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
   // Step t, whose first block is b: the rows of four blocks of Q and dO and their lse log2(e) and D.  Queries past the end repeat the
-  // last one, see no_rows.
+  // last one, blocks past the end the one in front of them, see no_rows.
   auto request = [&](int t, Block b) {
     constexpr int kRows = 1024 / (D * 2), kInstrs = kTileTokens / kRows / NW;          // of a transfer; a wave's transfers
     const int ln = (int)lane_again(), row = w * kRows % kQueryBlock + ln / SL::kChunks;
     const unsigned col = 16u * (unsigned)((ln % SL::kChunks) ^ SL::swz(w * kRows + ln / SL::kChunks));
     const unsigned q_off = (unsigned)row * (unsigned)a.sq.t * 2 + col, g_off = (unsigned)row * (unsigned)a.so.t * 2 + col;
-    if (kRows * NW > kQueryBlock && w * kRows >= kQueryBlock) b = next(b);             // two blocks a transfer of all waves
+    auto on = [&]() {
+      const Block x = next(b);
+      if (x.q < q_blocks) b = x;
+    };
+    if (kRows * NW > kQueryBlock && w * kRows >= kQueryBlock) on();                    // two blocks a transfer of all waves
 #pragma unroll
     for (int i = 0; i < kInstrs; i++) {
-      const Block x = b.q < q_blocks ? b : Block{q_blocks - 1, 0};
-      const int valid = nq - x.q * kQueryBlock;
+      const int valid = nq - b.q * kQueryBlock;
       unsigned qo = q_off, go = g_off;
       if (valid < kQueryBlock) {
         const unsigned back = (unsigned)max(0, row - (valid - 1));
         qo -= back * (unsigned)a.sq.t * 2;
         go -= back * (unsigned)a.so.t * 2;
       }
-      dma_lane16(qh + (size_t)x.h * a.sq.h + (size_t)x.q * kQueryBlock * a.sq.t, qo, qbuf(t) + (i * NW + w) * 1024);
-      dma_lane16(gh + (size_t)x.h * a.so.h + (size_t)x.q * kQueryBlock * a.so.t, go, qbuf(t) + SM::kTile + (i * NW + w) * 1024);
-      b = next(b);
-      if (kRows * NW > kQueryBlock) b = next(b);
+      dma_lane16(b.qp, qo, qbuf(t) + (i * NW + w) * 1024);
+      dma_lane16(b.gp, go, qbuf(t) + SM::kTile + (i * NW + w) * 1024);
+      on();
+      if (kRows * NW > kQueryBlock) on();
     }
     if (w < 2) dma_lane4((w == 0 ? a.lse2 : a.delta) + st0 + (size_t)t * kTileTokens, 4u * (unsigned)ln, lds_address(stat + (t & 1) * 128 + 64 * w));
   };
@@ -267,7 +280,9 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
     if (q * kQueryBlock + ln % kQueryBlock >= nq) stat[(t & 1) * 128 + 64 * w + ln] = w == 0 ? INFINITY : 0.f;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
-  Block cur{t_begin * 4 / a.group, t_begin * 4 % a.group};
+  Block cur{t_begin * 4 / a.group, t_begin * 4 % a.group, nullptr, nullptr};
+  cur.qp = a.q + (size_t)(hk * a.group + cur.h) * a.sq.h + ((size_t)at.q0 + cur.q * kQueryBlock) * a.sq.t;
+  cur.gp = a.dout + (size_t)(hk * a.group + cur.h) * a.so.h + ((size_t)at.q0 + cur.q * kQueryBlock) * a.so.t;
   if (t_begin < t_end) request(t_begin, cur);
   bf16x8 kf[KS], vf[KS];
   {
