@@ -216,11 +216,14 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   auto from_of = [&](int j) { return a.causal ? max(0, j - past) : 0; };
   const int w_from = from_of(w_key), w_last = from_of(w_key + 31), q_blocks = (nq + kQueryBlock - 1) / kQueryBlock;
   int t_begin = from_of(key0) / kQueryBlock * a.group / 4, t_end = max(t_begin, (q_blocks * a.group + 3) / 4);
-  const bool parts = PARTS && t_end - t_begin > a.k_chunk;
+  bool parts = false;
   if (PARTS) {
-    t_begin += (int)blockIdx.y * a.k_chunk;
-    if (t_begin >= t_end && blockIdx.y) return;
-    t_end = min(t_end, t_begin + a.k_chunk);
+    // chunks from the sequence's first row on, the same for all of its tiles: those at work at a time read the same rows
+    const int first = t_begin / a.k_chunk, last = max(first, (t_end - 1) / a.k_chunk), part = (int)blockIdx.y;
+    if (part < first || part > last) return;
+    parts = first < last;
+    t_begin = max(t_begin, part * a.k_chunk);
+    t_end = min(t_end, (part + 1) * a.k_chunk);
   }
   const size_t st0 = stat_first(a, hk, at.s, at.q0);
   // A block: its query block and head, and where it begins in Q and dO.  Counted along, not worked out: the scalar unit's multiplications
@@ -415,9 +418,9 @@ __global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
   if (at.tile < 0) return;
   // as packed_dkv_kernel has it
   const int key0 = at.tile * kKeyTile, from = a.causal ? max(0, key0 - (at.nk - at.nq)) : 0, t_begin = from / kQueryBlock * a.group / 4;
-  const int steps = ((at.nq + kQueryBlock - 1) / kQueryBlock * a.group + 3) / 4 - t_begin;
-  if (steps <= a.k_chunk) return;
-  const int n = (steps + a.k_chunk - 1) / a.k_chunk;
+  const int t_end = max(t_begin, ((at.nq + kQueryBlock - 1) / kQueryBlock * a.group + 3) / 4);
+  const int p0 = t_begin / a.k_chunk, p1 = max(p0, (t_end - 1) / a.k_chunk);
+  if (p0 == p1) return;
   const size_t rows = (size_t)a.Tk * a.Hkv;
   const float* src = a.part_kv + (blockIdx.y ? a.k_parts * rows * D : 0);
   const float by = blockIdx.y ? 1.f : a.scale;
@@ -426,7 +429,7 @@ __global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
     const int token = at.k0 + key0 + idx / (D / 4), c = idx % (D / 4) * 4;
     const float* p = src + ((size_t)token * a.Hkv + th.head) * D + c;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < n; i++) sum += *reinterpret_cast<const f32x4*>(p + i * rows * D);
+    for (int i = p0; i <= p1; i++) sum += *reinterpret_cast<const f32x4*>(p + i * rows * D);
     bf16x4 r;
 #pragma unroll
     for (int e = 0; e < 4; e++) r[e] = (__bf16)(by * sum[e]);
