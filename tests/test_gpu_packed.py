@@ -198,3 +198,45 @@ def test_longer_sequences_and_the_same_bits_twice(case):
     api.sla2_packed_backward(p, q, k, v, qs, ks, out, lse, dout, *again[2:], workspace=ws)
     for x, y in zip(again, (out, lse, dq, dk, dv)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_random_shapes(seed):
+    """A sample of the parameter space: lengths around the tiles, groups, strides, masks, both head dimensions."""
+    rng = np.random.default_rng(1000 + seed)
+    S = int(rng.choice([1, 2, 3, 7]))
+    Hkv, group = [(1, 1), (2, 3), (1, 8), (3, 2), (2, 16), (1, 5)][int(rng.integers(6))]
+    edge = [0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 320, 513]
+    lens_k = [int(rng.choice(edge)) for _ in range(S)]
+    lens_q = [int(rng.choice(edge[:12])) for _ in range(S)] if rng.random() < 0.6 else list(lens_k)
+    lens_q[0], lens_k[0] = max(1, lens_q[0]), max(1, lens_k[0])
+    run(lens_q, lens_k, Hkv * group, Hkv, int(rng.choice([64, 128])), bool(rng.integers(2)), str(rng.choice(["plain", "padded", "heads"])), seed=seed,
+        lead=int(rng.integers(3)), behind=int(rng.integers(4)))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_dealt_to_several_workgroups_with_a_mask(d):
+    """Long rows over few tiles of keys and few rows over many keys: parts of both, some of them empty, and sequences without parts."""
+    run([1500, 3, 0], [200, 900, 5], 8, 1, d, True)
+    run([40, 1], [2600, 4], 4, 1, d, True)
+    run([1, 1, 700], [1, 2200, 0], 6, 2, d, False)
+
+
+def test_offsets_past_32_bits():
+    """5 GB of queries: rows at their end read the right keys and are written where they belong."""
+    import torch
+    from paper_2602_12675_amd import api
+    T, H, d, n = 600_000, 32, 128, 70
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    q = torch.zeros((T, H, d), dtype=torch.bfloat16, device="cuda")
+    assert q.numel() > 2 ** 31
+    q[-200:] = torch.randn((200, H, d), generator=gen, device="cuda").bfloat16()
+    k, v = (torch.randn((2 * n, 4, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    out = torch.full_like(q, 7.0)
+    p = api.make_packed_params(2, T, 2 * n, H, 4, d)
+    ws = torch.empty(api.sla2_packed_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    api.sla2_packed_forward(p, q, k, v, dev([0, T - 100, T]), dev([0, n, 2 * n]), out, workspace=ws)
+    r = S.packed_forward(f64(q[-200:]), f64(k), f64(v), [0, 100, 200], [0, n, 2 * n], False, d ** -0.5)
+    e = weight_error(d, n, r["smag"])
+    close(out[-200:], r["out"], out_bound(r["out"], r["mag"], e.T[..., None]))
+    close(out[:1].float(), np.repeat(f64(v[:n]).mean(0), 8, 0)[None], np.full((1, H, d), 2.0 ** -6))     # equal scores: the mean
