@@ -361,7 +361,7 @@ typedef struct sla2_packed_params {
                                 all of them; one before the first key none); 0: all of its sequence */
   float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */
   /* (head, token) element strides of q, dq; of k, v, dk, dv; of out, dout.  Both zero: contiguous [tokens, heads, d].  As in
-   * sla2_params; below 2^24 elements a token; (tokens_q + 16 sequences) H and tokens_k H below 2^31 - 1024 */
+   * sla2_params; below 2^24 elements a token; (tokens_q + 128 sequences) H and (tokens_k + 128 sequences) H below 2^31 - 1024 */
   long long q_stride[2];
   long long kv_stride[2];
   long long out_stride[2];
@@ -384,7 +384,8 @@ int sla2_packed_forward(const sla2_packed_params* params, const void* q, const v
 /* Gradients of q, k and v from that of out.
  *   out, lse     of the forward call
  *   dq, dk, dv   written; they may be slices of one buffer, with other numbers of heads too, that share no element, and share none with
- *                an input.  A key that no query reads has dk = dv = 0 */
+ *                an input.  A key that no query reads has dk = dv = 0
+ * What is NaN or infinite in dout, out or lse stays in its sequence too, and may reach any of its gradients. */
 int sla2_packed_backward(const sla2_packed_params* params, const void* q, const void* k, const void* v, const int32_t* q_start,
                          const int32_t* k_start, const void* out, const float* lse, const void* dout, void* dq, void* dk, void* dv,
                          void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -399,7 +400,7 @@ typedef struct sla2_cache_params {
   int H, H_kv, d;            /* as in sla2_packed_params (H: sla2_cache_attention alone) */
   int pages, page_size;      /* page_size: 16, 32, 64, 128 or 256 */
   int max_pages;             /* columns of page_table: a sequence has max_pages page_size tokens (< 2^31) at most */
-  int tokens;                /* sla2_cache_write, _read: rows of k and v; >= 0 */
+  int tokens;                /* sla2_cache_write, _read: rows of k and v; >= 0, below 2^30 */
   int dtype;                 /* SLA2_BF16: of q, k, v, out */
   int quant_mode;            /* SLA2_QUANT_NONE (the cache is bf16), _FP8 or _INT8 */
   float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */
@@ -430,7 +431,7 @@ size_t sla2_cache_workspace_bytes(const sla2_cache_params* params);
 /* Attention of one new token of each sequence over the first length[b] tokens of the cache, its own among them if it was written.
  *   q, out        [B, H, d];  lse_or_null   DEVICE float [B, H]
  *   length        DEVICE int32 [B]; what is over max_pages page_size is not read.  0 (or less): out = 0, lse = -inf
- * Tokens in a page that is not one of 0 .. pages - 1 are left out.  What lies behind a sequence's last token is not read.  Codes are
+ * Tokens in a page that is not one of 0 .. pages - 1 are left out.  What lies behind a sequence's last token has no part in the result.  Codes are
  * exact in bf16; a token's scales meet its scores and its probability in fp32. */
 int sla2_cache_attention(const sla2_cache_params* params, const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                          const float* v_scale, const int32_t* length, const int32_t* page_table, void* out, float* lse_or_null,

@@ -15,6 +15,7 @@
 
 namespace sla2 {
 
+constexpr float kNoScore = -3e38f;                 // below all scores: where a running maximum begins that is subtracted from -inf too
 constexpr int kTileTokens = 64;                    // b_kv
 constexpr int kVmcnt0 = 0x0F70;                    // s_waitcnt vmcnt(0), other counters untouched
 

@@ -293,7 +293,7 @@ __global__ __launch_bounds__(kDecodeWaves * kWave, 2) void cache_attention_kerne
     HeadSums<D> sums;
 #pragma unroll
     for (int i = 0; i < C; i++) sums.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    sums.m = -1e30f;
+    sums.m = kNoScore;
     sums.l = 0.f;
     attend_blocks<D, QUANT>(a, b, hk, lo, hi, (int)min((unsigned)len, (unsigned)hi * kDecodeBlock), qf, sums, w, lane);
     // ---- the waves' parts ----

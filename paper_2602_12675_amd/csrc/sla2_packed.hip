@@ -49,7 +49,7 @@ template <int D> struct RowSums {
     for (int et = 0; et < D / 32; et++)
 #pragma unroll
       for (int e = 0; e < 16; e++) o[et][e] = 0.f;
-    m = -1e30f;
+    m = kNoScore;
     l = 0.f;
   }
 };
@@ -241,11 +241,12 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
 // are the lengths; the longest sequence is taken to have twice its share of the keys.
 // Parts of a tile of keys: so that no workgroup has much more than its share of all steps, which with a causal mask or sequences of
 // different lengths the first tiles have.
+constexpr long long kPartBytes = 4ll << 30;
 void plan_packed(PackedArgs* a, bool backward) {
   a->q_parts = a->k_parts = 1;
   const long long rows = (long long)a->Tq * a->group, places = 512;
   const long long q_tiles = most_tiles(rows, a->S, kRowTile) * a->Hkv, k_tiles = most_tiles(a->Tk, a->S, kKeyTile) * a->Hkv;
-  const long long longest = a->S == 1 ? a->Tk : a->S == 2 ? a->Tk * 3 / 4 : 2ll * a->Tk / a->S, steps = (longest + kTileTokens - 1) / kTileTokens;
+  const long long longest = a->S == 1 ? a->Tk : a->S == 2 ? a->Tk * 3ll / 4 : 2ll * a->Tk / a->S, steps = (longest + kTileTokens - 1) / kTileTokens;
   if (q_tiles && q_tiles <= places && steps) {
     const double step = backward ? 1.5 : 1.1, bytes = (double)a->Tq * a->H * a->d * 8;
     double best = steps * step;
@@ -260,11 +261,13 @@ void plan_packed(PackedArgs* a, bool backward) {
   }
   if (!backward || !k_tiles || !rows) return;
   // Steps of 64 rows of all tiles of keys, were the sequences alike, over the places, and a little more, so that the last round is not
-  // a few workgroups; at most 16 parts of the longest sequence that there can be.
+  // a few workgroups; at most 16 parts of the longest sequence that there can be, and kPartBytes of them.
   const long long row_steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + kKeyTile - 1) / kKeyTile * a->Hkv * ((row_steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
   long long chunk = all / places + all / (places * 12) + 1;
   if (chunk < 16) chunk = 16;
   if (chunk < (row_steps + 15) / 16) chunk = (row_steps + 15) / 16;
+  const long long part = 2ll * a->Tk * a->Hkv * a->d * 4, most = part > kPartBytes ? 1 : kPartBytes / part;    // bytes of one; as many as may be
+  if (chunk < (row_steps + most - 1) / most) chunk = (row_steps + most - 1) / most;
   a->k_chunk = (int)chunk;
   a->k_parts = (int)((row_steps + chunk - 1) / chunk);
 }

@@ -79,8 +79,10 @@ static int make_packed(const sla2_packed_params* p, PackedArgs* a) {
   a->d = p->d;
   a->causal = p->causal != 0;
   a->scale = rate_or_default(p->scale, p->d);
-  // rows (queries of all heads, the backward pass's blocks of 16 filled up) and workgroups are counted in 31 bits
-  if (((long long)a->Tq + 16ll * a->S) * a->H > INT_MAX - 1024 || (long long)a->Tk * a->H > INT_MAX - 1024) return SLA2_EUNSUPPORTED;
+  // Rows (queries of all heads, the backward pass's blocks of 16 filled up) are counted in 31 bits, and a launch has less than 2^24
+  // workgroups of 256: tiles of 128 rows or keys, and for each sequence one that is not full.
+  const long long last = 128ll * a->S;
+  if ((a->Tq + last) * a->H > INT_MAX - 1024 || (a->Tk + last) * a->H > INT_MAX - 1024) return SLA2_EUNSUPPORTED;
   return SLA2_OK;
 }
 static View q_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tq, a.H, a.d, a.sq.h, a.sq.t); }
@@ -98,7 +100,7 @@ static int make_cache(const sla2_cache_params* p, CacheArgs* a) {
   int shift = 0;
   while (shift < 9 && 1 << shift != p->page_size) shift++;
   if (shift < 4 || shift > 8) return SLA2_EUNSUPPORTED;
-  if (p->quant_mode == SLA2_QUANT_FP8_V || p->B > 65535 || (long long)p->max_pages << shift > INT_MAX) return SLA2_EUNSUPPORTED;
+  if (p->tokens >= 1 << 30 || p->quant_mode == SLA2_QUANT_FP8_V || p->B > 65535 || (long long)p->max_pages << shift > INT_MAX) return SLA2_EUNSUPPORTED;
   *a = CacheArgs{};
   a->table_stride = p->table_stride ? p->table_stride : p->max_pages;
   if (a->table_stride < p->max_pages) return SLA2_EINVAL;

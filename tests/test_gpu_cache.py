@@ -324,6 +324,24 @@ def test_attention_scale_in_place_and_shared_pages():
     assert torch.equal(q, out)
 
 
+def test_scores_far_below_zero():
+    """Scores around -1e34, powers of two all alike: no product rounds, and the result is the mean of the values."""
+    import torch
+    from paper_2602_12675_amd import api
+    c = Cache(40, 1, 64, 64, "none")
+    c.fill(torch.Generator(device="cuda").manual_seed(5))
+    c.kv[0].fill_(-2.0 ** 50)
+    p = params(c, 2, 3, 20)
+    q = torch.full((2, 3, 64), 2.0 ** 59, dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(q)
+    ws = torch.empty(api.sla2_cache_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    api.sla2_cache_attention(p, q, *c.kv, dev(np.arange(40).reshape(2, 20).tolist()), dev([1, 1203]), out, workspace=ws)
+    v = f64(c.kv[1])[:, 0].reshape(2, 1280, 64)
+    for b, n in enumerate((1, 1203)):
+        mean = np.repeat(v[b, :n].mean(0)[None], 3, 0)
+        close(out[b], mean, 2.0 ** -8 * np.abs(mean) + (n + 100) * 2.0 ** -24 * np.abs(v).max())     # P = 1 exactly; sums of n values in fp32
+
+
 def test_offsets_past_32_bits():
     """A cache of 5 GB of keys: tokens in its last pages."""
     import torch

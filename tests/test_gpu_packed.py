@@ -222,6 +222,19 @@ def test_rows_dealt_to_several_workgroups_with_a_mask(d):
     run([1, 1, 700], [1, 2200, 0], 6, 2, d, False)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_far_below_zero(d):
+    """Scores around -1e34, powers of two all alike: no product rounds, and the result is the mean of the values."""
+    def edit(q, k, v, dout, qs, ks):
+        q.fill_(2.0 ** 59)
+        k.fill_(-2.0 ** 50)
+    p, (q, k, v, _, _, out, lse, _), ref = run([3, 70], [1, 200], 4, 2, d, False, edit=edit, backward=False)
+    assert float(ref["lse"].max()) < -2e33
+    mean = np.concatenate([np.repeat(f64(v[:1]), 3, 0), np.repeat(f64(v[1:]).mean(0, keepdims=True), 70, 0)]).repeat(2, 1)
+    close(out, mean, HALF * np.abs(mean) + 300 * UNIT * float(v.float().abs().max()))   # P = 1 exactly; sums of 200 values in fp32
+    close(lse, ref["lse"], 4 * UNIT * np.abs(ref["lse"]))
+
+
 def test_offsets_past_32_bits():
     """5 GB of queries: rows at their end read the right keys and are written where they belong."""
     import torch

@@ -58,11 +58,22 @@ def backward(p, **kw):
     (dict(q_stride=(68, 256)), EUNSUPPORTED), (dict(kv_stride=(64, 56)), EUNSUPPORTED), (dict(q_stride=(64, 1 << 24)), EUNSUPPORTED),
     (dict(q_stride=(1 << 60, 256)), EUNSUPPORTED), (dict(H=65536, H_kv=65536), EUNSUPPORTED),
     (dict(H=65535, H_kv=65535, tokens_q=2 ** 31 - 1), EUNSUPPORTED),
+    (dict(sequences=65535, tokens_q=65535, tokens_k=65535, H=512, H_kv=512), EUNSUPPORTED),      # more workgroups than a launch may have
+    (dict(tokens_k=2 ** 31 - 1, H=1, H_kv=1), EUNSUPPORTED),
 ])
 def test_bad_packed_parameters(kw, status):
     p = packed(**kw)
     assert api.sla2_packed_workspace_bytes(p) == 0 and api.sla2_packed_workspace_bytes(p, True) == 0
     assert forward(p) == status and backward(p) == status
+
+
+def test_parts_of_keys_have_a_bound():
+    """Of many short sequences none has to be dealt to several workgroups, but one might be long: room for its parts, up to 4 GiB."""
+    p = api.make_packed_params(1000, 200_000, 200_000, 64, 8, 128)
+    n = 2 * (200_000 + 16 * 1000) * 64 * 4
+    assert n <= api.sla2_packed_workspace_bytes(p, True) <= n + (4 << 30) + 2048
+    p = api.make_packed_params(1, 1 << 25, 128, 1, 1, 64)                     # one tile of keys: 16 parts of it
+    assert api.sla2_packed_workspace_bytes(p, True) > 2 * 16 * 128 * 64 * 4
 
 
 def test_bad_packed_pointers():
@@ -143,6 +154,7 @@ def attention(p, **kw):
     (dict(cache_stride=(2048, 1024, 0)), EINVAL), (dict(cache_stride=(2048, 1024, 48)), EUNSUPPORTED), (dict(cache_stride=(2056, 1024, 64)), EUNSUPPORTED),
     (dict(cache_stride=(1 << 40, 1024, 64)), EUNSUPPORTED), (dict(cache_stride=(2048, 1024, 1 << 24)), EUNSUPPORTED),
     (dict(kv_stride=(64, 0)), EINVAL), (dict(q_stride=(60, 256)), EUNSUPPORTED), (dict(out_stride=(64, 32)), EUNSUPPORTED),
+    (dict(tokens=1 << 30), EUNSUPPORTED),
 ])
 def test_bad_cache_parameters(kw, status):
     p = cache(**kw)
