@@ -34,29 +34,6 @@ __device__ __forceinline__ u32x4 stat_read(unsigned base, int n) {
   }
 }
 
-// acc[et] += A^T f: the 32 rows of a tile at `lo` / `hi` (tr_read_offset), OFF bytes on, contracted, as two 16-row steps, into all channels
-template <int D, int OFF>
-__device__ __forceinline__ void contract32(f32x16 (&acc)[D / 32], const bf16x8* f, unsigned lo_at, unsigned hi_at) {
-  constexpr int ET = D / 32, kFrags = 2 * ET, kAhead = 3, kSlots = kAhead + 1;
-  u32x2 lo[kSlots], hi[kSlots];
-  auto issue = [&](int n) {
-    const unsigned at_lo = lo_at ^ (64u * (n % ET)), at_hi = hi_at ^ (64u * (n % ET));
-    lo[n % kSlots] = n < ET ? lds_read_tr_untracked<OFF>(at_lo) : lds_read_tr_untracked<OFF + 32 * D>(at_lo);
-    hi[n % kSlots] = n < ET ? lds_read_tr_untracked<OFF>(at_hi) : lds_read_tr_untracked<OFF + 32 * D>(at_hi);
-  };
-#pragma unroll
-  for (int n = 0; n < kAhead; n++) issue(n);
-#pragma unroll
-  for (int n = 0; n < kFrags; n++) {
-    if (n + kAhead < kFrags) issue(n + kAhead);
-    wait_lgkmcnt(2 * (n + kAhead < kFrags ? kAhead : kFrags - 1 - n));
-    settle(lo[n % kSlots]);
-    settle(hi[n % kSlots]);
-    const u32x4 v4 = {lo[n % kSlots][0], lo[n % kSlots][1], hi[n % kSlots][0], hi[n % kSlots][1]};
-    acc[n % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, v4), f[n / ET], acc[n % ET]);
-  }
-}
-
 // D and dQ of 128 rows: S^T = K Q^T and dP^T = V dO^T (keys x rows), dQ^T += K^T dS^T, as in the forward pass with K in the place of V.
 template <int D, bool PARTS>
 __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
@@ -140,46 +117,66 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
         for (int e = 0; e < 16; e++) s[e] = dp[e] = 0.f;
         bf16x8 df[2];
         const bool edge = t0 + 32 * mt + 32 > w_full;
-        constexpr int kItems = 2 * KS, kAhead = 4, kSlots = kAhead + 1;
+        // one stream of LDS reads, kAhead items of it in flight: K for S, V for dP, K again, transposed, for dQ
+        constexpr int kItems = 2 * KS + 2 * ET, kAhead = 6, kSlots = kAhead + 1;
         u32x4 ring[kSlots];
+        u32x2 lo[kSlots], hi[kSlots];
         auto issue = [&](int n) {
           const unsigned x = (ka + k_off) ^ (32u * (n % KS));
-          ring[n % kSlots] = n < KS ? lds_read16_untracked<0>(x) : lds_read16_untracked<SM::kTile>(x);
+          if (n < KS) ring[n % kSlots] = lds_read16_untracked<0>(x);
+          else if (n < 2 * KS) ring[n % kSlots] = lds_read16_untracked<SM::kTile>(x);
+          else {
+            const int f = n - 2 * KS;
+            const unsigned at_lo = (ka + t_lo) ^ (64u * (f % ET)), at_hi = (ka + t_hi) ^ (64u * (f % ET));
+            lo[n % kSlots] = f < ET ? lds_read_tr_untracked<0>(at_lo) : lds_read_tr_untracked<32 * D>(at_lo);
+            hi[n % kSlots] = f < ET ? lds_read_tr_untracked<0>(at_hi) : lds_read_tr_untracked<32 * D>(at_hi);
+          }
         };
 #pragma unroll
         for (int n = 0; n < kAhead; n++) issue(n);
-#pragma unroll
-        for (int n = 0; n < kItems; n++) {
+        unrolled<kItems>([&](auto at_n) {
+          constexpr int n = decltype(at_n)::value, f = n - 2 * KS;
           if (n + kAhead < kItems) issue(n + kAhead);
-          wait_lgkmcnt(n + kAhead < kItems ? kAhead : kItems - 1 - n);
-          settle(ring[n % kSlots]);
-          const bf16x8 f = __builtin_bit_cast(bf16x8, ring[n % kSlots]);
-          if (n < KS) {
-            s = mfma_bf16(f, qf[n], s);
-          } else {
-            dp = mfma_bf16(f, gf[n - KS], dp);
-            constexpr int kStep = KS / 4;              // behind every quarter of the products of dP four exponentials
-            if ((n - KS) % kStep == kStep - 1) {
-              const int v4 = (n - KS) / kStep;
+          int behind = 0;                              // reads asked for behind this item's
 #pragma unroll
-              for (int r = 0; r < 4; r++) {
-                float p = fast_exp2(s[4 * v4 + r] * c1 - l2);
-                settle(p);
-                s[4 * v4 + r] = p;
+          for (int y = 1; y <= kAhead; y++) behind += n + y < kItems ? (n + y < 2 * KS ? 1 : 2) : 0;
+          wait_lgkmcnt(behind);
+          if constexpr (n < 2 * KS) {
+            settle(ring[n % kSlots]);
+            const bf16x8 x = __builtin_bit_cast(bf16x8, ring[n % kSlots]);
+            if constexpr (n < KS) {
+              s = mfma_bf16(x, qf[n], s);
+            } else {
+              dp = mfma_bf16(x, gf[n - KS], dp);
+              constexpr int kStep = KS / 4;            // behind every quarter of the products of dP four exponentials
+              if constexpr ((n - KS) % kStep == kStep - 1) {
+                constexpr int v4 = (n - KS) / kStep;
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                  float p = fast_exp2(s[4 * v4 + r] * c1 - l2);
+                  settle(p);
+                  s[4 * v4 + r] = p;
+                }
               }
             }
+            if constexpr (n == 2 * KS - 1) {
+              if (edge) {
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                  if (t0 + 32 * mt + 8 * (e / 4) + 4 * g + e % 4 >= mine) s[e] = 0.f;
+              }
+#pragma unroll
+              for (int e = 0; e < 16; e++) df[e / 8][e % 8] = (__bf16)(s[e] * (dp[e] - delta));
+              pin(df[0]);
+              pin(df[1]);
+            }
+          } else {
+            settle(lo[n % kSlots]);
+            settle(hi[n % kSlots]);
+            const u32x4 u = {lo[n % kSlots][0], lo[n % kSlots][1], hi[n % kSlots][0], hi[n % kSlots][1]};
+            acc[f % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, u), df[f / ET], acc[f % ET]);
           }
-        }
-        if (edge) {
-#pragma unroll
-          for (int e = 0; e < 16; e++)
-            if (t0 + 32 * mt + 8 * (e / 4) + 4 * g + e % 4 >= mine) s[e] = 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < 16; e++) df[e / 8][e % 8] = (__bf16)(s[e] * (dp[e] - delta));
-        pin(df[0]);
-        pin(df[1]);
-        contract32<D, 0>(acc, df, ka + t_lo, ka + t_hi);
+        });
       }
     }
     wait_vmcnt<0>();
@@ -323,14 +320,29 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
       bf16x8 pf[2], df[2];
 #pragma unroll
       for (int e = 0; e < 16; e++) s[e] = dp[e] = 0.f;
-      // One stream of LDS reads, kAhead of them in flight: the rows of Q for S; four groups of a quarter of the rows of dO for dP and lse
-      // of four rows, whose exponentials then run beside the products; D of the rows.
-      constexpr int kGroup = KS / 4 + 1, kItems = KS + 4 * kGroup + 4, kAhead = D == 64 ? 4 : 2 /* the registers */, kSlots = kAhead + 1;
+      // One stream of LDS reads, kAhead items of it in flight: the rows of Q for S; four groups of a quarter of the rows of dO for dP and
+      // lse of four rows, whose exponentials then run beside the products; dO for dV, behind the first of which D of the rows; Q for dK.
+      constexpr int kGroup = KS / 4 + 1, kV = KS + 4 * kGroup, kK = kV + 4 + 2 * ET, kItems = kK + 2 * ET;
+      constexpr int kAhead = D == 64 ? 6 : 2 /* the registers: with 3 they spill */, kSlots = kAhead + 1;
       u32x4 ring[kSlots];
+      u32x2 lo[kSlots], hi[kSlots];
+      auto is_d = [](int n) { return n > kV && n <= kV + 4; };
+      auto fragment = [](int n) { return n >= kK ? n - kK : n == kV ? 0 : n - kV - 4; };           // of dO or Q, transposed
+      auto reads = [&](int n) { return n < kV || is_d(n) ? 1 : 2; };
       auto issue = [&](int n) {
-        const int m = n - KS, v4 = m / kGroup;
+        const int m = n - KS, v4 = m / kGroup, f = fragment(n);
         if (n < KS) ring[n % kSlots] = lds_read16_untracked<0>(ra ^ (32u * n));
-        else if (m >= 4 * kGroup) ring[n % kSlots] = stat_read(st, 4 + m - 4 * kGroup);
+        else if (is_d(n)) ring[n % kSlots] = stat_read(st, 4 + n - kV - 1);
+        else if (n >= kV) {
+          const unsigned at_lo = (qa + t_lo) ^ (64u * (f % ET)), at_hi = (qa + t_hi) ^ (64u * (f % ET));
+          if (n < kK) {
+            lo[n % kSlots] = f < ET ? lds_read_tr_untracked<SM::kTile>(at_lo) : lds_read_tr_untracked<SM::kTile + 32 * D>(at_lo);
+            hi[n % kSlots] = f < ET ? lds_read_tr_untracked<SM::kTile>(at_hi) : lds_read_tr_untracked<SM::kTile + 32 * D>(at_hi);
+          } else {
+            lo[n % kSlots] = f < ET ? lds_read_tr_untracked<0>(at_lo) : lds_read_tr_untracked<32 * D>(at_lo);
+            hi[n % kSlots] = f < ET ? lds_read_tr_untracked<0>(at_hi) : lds_read_tr_untracked<32 * D>(at_hi);
+          }
+        }
         else if (m % kGroup == kGroup - 1) ring[n % kSlots] = stat_read(st, v4);
         else ring[n % kSlots] = lds_read16_untracked<SM::kTile>(ra ^ (32u * (v4 * (kGroup - 1) + m % kGroup)));
       };
@@ -338,9 +350,18 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
       for (int n = 0; n < kAhead; n++) issue(n);
       unrolled<kItems>([&](auto at_n) {
         constexpr int n = decltype(at_n)::value, m = n - KS, v4 = m / kGroup;
+        constexpr bool d_item = n > kV && n <= kV + 4;
         if (n + kAhead < kItems) issue(n + kAhead);
-        wait_lgkmcnt(n + kAhead < kItems ? kAhead : kItems - 1 - n);
-        settle(ring[n % kSlots]);
+        int behind = 0;                                // reads asked for behind this item's
+#pragma unroll
+        for (int y = 1; y <= kAhead; y++) behind += n + y < kItems ? reads(n + y) : 0;
+        wait_lgkmcnt(behind);
+        if constexpr (n < kV || d_item) {
+          settle(ring[n % kSlots]);
+        } else {
+          settle(lo[n % kSlots]);
+          settle(hi[n % kSlots]);
+        }
         if constexpr (n < KS) {
           s = mfma_bf16(__builtin_bit_cast(bf16x8, ring[n % kSlots]), kf[n], s);
           if (n == KS - 1 && b0.q * kQueryBlock < w_last) {            // some rows do not read some of the keys
@@ -349,19 +370,17 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
             for (int e = 0; e < 16; e++)
               if ((e < 8 ? b0.q : b1.q) * kQueryBlock + e % 8 / 4 * 8 + e % 4 < from) s[e] = -INFINITY;
           }
-        } else if constexpr (m >= 4 * kGroup) {
-          constexpr int x = m - 4 * kGroup;
+        } else if constexpr (d_item) {
+          constexpr int x = n - kV - 1;
           const f32x4 d4 = __builtin_bit_cast(f32x4, ring[n % kSlots]);
 #pragma unroll
-          for (int r = 0; r < 4; r++) {
-            const int e = 4 * x + r;
-            pf[x / 2][e % 8] = (__bf16)s[e];
-            df[x / 2][e % 8] = (__bf16)(s[e] * (dp[e] - d4[r]));
-          }
-          if (x % 2 == 1) {
-            pin(pf[x / 2]);
-            pin(df[x / 2]);
-          }
+          for (int r = 0; r < 4; r++) df[x / 2][(4 * x + r) % 8] = (__bf16)(s[4 * x + r] * (dp[4 * x + r] - d4[r]));
+          if (x % 2 == 1) pin(df[x / 2]);
+        } else if constexpr (n >= kV) {
+          constexpr int f = n >= kK ? n - kK : n == kV ? 0 : n - kV - 4;
+          const u32x4 u = {lo[n % kSlots][0], lo[n % kSlots][1], hi[n % kSlots][0], hi[n % kSlots][1]};
+          if constexpr (n < kK) dv[f % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, u), pf[f / ET], dv[f % ET]);
+          else dk[f % ET] = mfma_bf16(__builtin_bit_cast(bf16x8, u), df[f / ET], dk[f % ET]);
         } else if constexpr (m % kGroup == kGroup - 1) {
           const f32x4 l4 = __builtin_bit_cast(f32x4, ring[n % kSlots]);
 #pragma unroll
@@ -369,13 +388,13 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
             float p = fast_exp2(s[4 * v4 + r] * c1 - l4[r]);
             settle(p);                                 // here, not where the compiler would gather them
             s[4 * v4 + r] = p;
+            pf[v4 / 2][(4 * v4 + r) % 8] = (__bf16)p;
           }
+          if (v4 % 2 == 1) pin(pf[v4 / 2]);
         } else {
           dp = mfma_bf16(__builtin_bit_cast(bf16x8, ring[n % kSlots]), vf[v4 * (kGroup - 1) + m % kGroup], dp);
         }
       });
-      contract32<D, SM::kTile>(dv, pf, qa + t_lo, qa + t_hi);
-      contract32<D, 0>(dk, df, qa + t_lo, qa + t_hi);
     }
     wait_vmcnt<0>();                                   // the next step's rows have landed ...
     if (t + 1 < t_end) no_rows(t + 1, following);
