@@ -20,6 +20,11 @@ __device__ __forceinline__ void pin(bf16x8& f) {       // converted here: eight 
   f = __builtin_bit_cast(bf16x8, u);
 }
 
+__device__ __forceinline__ long long kept(long long x) {   // a scalar that is held in registers and not worked out where it is used
+  asm("" : "+s"(x));
+  return x;
+}
+
 // 16 bytes of a step's row quantities, 32 bytes apart: lse at n = 0 .. 3 and D, 256 bytes on, at 4 .. 7
 __device__ __forceinline__ u32x4 stat_read(unsigned base, int n) {
   switch (n) {
@@ -229,19 +234,23 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
     int q, h;
     const uint16_t *qp, *gp;
   };
+  // How far a step of one block, and of four, goes on in the same queries and to later ones (elements; kept, not made again)
   const long long q_row = (long long)kQueryBlock * a.sq.t, g_row = (long long)kQueryBlock * a.so.t;
-  auto next = [&](Block b) {
-    const bool wrap = b.h + 1 == a.group;              // on to the next queries
-    return Block{b.q + wrap, wrap ? 0 : b.h + 1, b.qp + (wrap ? q_row - (a.group - 1) * a.sq.h : a.sq.h),
-                 b.gp + (wrap ? g_row - (a.group - 1) * a.so.h : a.so.h)};
-  };
   const int four_q = 4 / a.group, four_h = 4 % a.group;
-  const long long q_four = four_q * q_row + four_h * a.sq.h, g_four = four_q * g_row + four_h * a.so.h;
+  const long long q_one = a.sq.h, g_one = a.so.h, q_wrap = kept(q_row - (a.group - 1) * a.sq.h), g_wrap = kept(g_row - (a.group - 1) * a.so.h);
+  const long long q_four = kept(four_q * q_row + four_h * a.sq.h), g_four = kept(four_q * g_row + four_h * a.so.h);
+  const long long q_four_wrap = kept(q_four + q_row - a.group * a.sq.h), g_four_wrap = kept(g_four + g_row - a.group * a.so.h);
+  auto next = [&](Block b) {
+    const bool wrap = b.h + 1 == a.group;
+    return Block{b.q + wrap, wrap ? 0 : b.h + 1, b.qp + (wrap ? q_wrap : q_one), b.gp + (wrap ? g_wrap : g_one)};
+  };
   auto after4 = [&](Block b) {
     const bool wrap = b.h + four_h >= a.group;
-    return Block{b.q + four_q + wrap, b.h + four_h - (wrap ? a.group : 0), b.qp + q_four + (wrap ? q_row - a.group * a.sq.h : 0),
-                 b.gp + g_four + (wrap ? g_row - a.group * a.so.h : 0)};
+    return Block{b.q + four_q + wrap, b.h + four_h - (wrap ? a.group : 0), b.qp + (wrap ? q_four_wrap : q_four), b.gp + (wrap ? g_four_wrap : g_four)};
   };
+  // whether all queries of the four blocks from b on exist, told from the first one's: the fourth's are at most so many blocks further
+  const int further = 1 + 2 / a.group, whole_below = nq / kQueryBlock - further;
+  auto whole = [&](Block b) { return b.q < whole_below; };
   auto qbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
   // Step t, whose first block is b: the rows of four blocks of Q and dO and their lse log2(e) and D.  Queries past the end repeat the
   // last one, blocks past the end the one in front of them, see no_rows.
@@ -250,6 +259,17 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
     const int ln = (int)lane_again(), row = w * kRows % kQueryBlock + ln / SL::kChunks;
     const unsigned col = 16u * (unsigned)((ln % SL::kChunks) ^ SL::swz(w * kRows + ln / SL::kChunks));
     const unsigned q_off = (unsigned)row * (unsigned)a.sq.t * 2 + col, g_off = (unsigned)row * (unsigned)a.so.t * 2 + col;
+    if (w < 2) dma_lane4((w == 0 ? a.lse2 : a.delta) + st0 + (size_t)t * kTileTokens, 4u * (unsigned)ln, lds_address(stat + (t & 1) * 128 + 64 * w));
+    if (whole(b)) {
+      if (kRows * NW > kQueryBlock && w * kRows >= kQueryBlock) b = next(b);
+#pragma unroll
+      for (int i = 0; i < kInstrs; i++) {
+        dma_lane16(b.qp, q_off, qbuf(t) + (i * NW + w) * 1024);
+        dma_lane16(b.gp, g_off, qbuf(t) + SM::kTile + (i * NW + w) * 1024);
+        if (i + 1 < kInstrs) b = kRows * NW > kQueryBlock ? next(next(b)) : next(b);
+      }
+      return;
+    }
     auto on = [&]() {
       const Block x = next(b);
       if (x.q < q_blocks) b = x;
@@ -269,13 +289,12 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
       on();
       if (kRows * NW > kQueryBlock) on();
     }
-    if (w < 2) dma_lane4((w == 0 ? a.lse2 : a.delta) + st0 + (size_t)t * kTileTokens, 4u * (unsigned)ln, lds_address(stat + (t & 1) * 128 + 64 * w));
   };
   // Behind the arrival of step t, by the waves that asked for them: what was read for queries past the end has no meaning.  With
   // lse = +inf and D = 0 their P and dS are 0.
   auto no_rows = [&](int t, Block b) {
+    if (w > 1 || whole(b)) return;
     const Block b1 = next(b), b2 = next(b1), b3 = next(b2);
-    if (w > 1 || b3.q * kQueryBlock + kQueryBlock <= nq) return;
     const int ln = (int)lane_again(), q = ln < 32 ? ln < 16 ? b.q : b1.q : ln < 48 ? b2.q : b3.q;
     if (q * kQueryBlock + ln % kQueryBlock >= nq) stat[(t & 1) * 128 + 64 * w + ln] = w == 0 ? INFINITY : 0.f;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
