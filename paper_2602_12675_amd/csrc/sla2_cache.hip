@@ -3,6 +3,10 @@
 // A row (the d channels of a token and head) is 8 channels on each of d / 8 neighbouring lanes, read once and written once; its largest
 // magnitude is a maximum over those lanes, taken on the bits of |x|, which order finite numbers, infinities and NaNs alike.  A
 // workgroup has neighbouring tokens of one head, whose codes and scales are neighbours in a page.
+//
+// Bound by memory: 74,655 tokens of 40 heads from INT8 461 us = 5.0 TB/s, a copy's rate; 32,760 tokens of 12 heads into FP8 57 us in the
+// kernel, 5.3 TB/s (68 a call with the tensors out of the caches).  A row a thread, keys and values apart, took
+// 822 and 92 us: every workgroup looks up its rows' places before it moves anything.
 #include "cache.h"
 #include "rows.h"
 

@@ -6,6 +6,12 @@
 // one exchange with the other half of the wave.  K and V tiles go from memory into LDS past the registers: V into one of two buffers,
 // a tile ahead, K into its one buffer behind the scores.  So two workgroups (d = 64: four) fit a CU, and one's products run beside
 // another's exponentials, first reads and results.
+//
+// Bound by the vector unit beside the matrix cores: 32 keys x 32 rows take 512 cycles of products (d = 128) and some 350 of maximum,
+// exponential, sum and rounding, which only overlap as far as two waves of a SIMD happen to be in different phases (busy 60 % and 50 %).
+// Causal, 40 heads on 8, sequences of 4,096, 2,777, 1,021, 1 and 297: 280 us for 262 GFLOP = 0.94 PFLOP/s; 12 heads of 2 x 32,760
+// queries on 512 and 131 keys: 205 us for 129 GFLOP and 410 MB, 11 steps a tile between first reads and results that nothing of the
+// same tile covers.  K and V in two buffers each, one workgroup less a CU: 295 for 280.
 #include "packed.h"
 
 namespace sla2 {
@@ -241,7 +247,9 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
 // are the lengths; the longest sequence is taken to have twice its share of the keys.
 // Parts of a tile of keys: so that no workgroup has much more than its share of all steps, which with a causal mask or sequences of
 // different lengths the first tiles have.
-constexpr long long kPartBytes = 4ll << 30;
+// Backward with parts and without: 27,724 queries of 8 heads on 585 keys of one 270 us, 6.8 ms; 12 heads of 32,760 on 512 388, 1,157; causal, 40
+// heads on 8, 8,192 tokens 826, 1,009; d = 64, 17 and 26 queries on 4,789 and 145 keys 32, 83.
+constexpr long long kPartBytes = 1ll << 30;
 void plan_packed(PackedArgs* a, bool backward) {
   a->q_parts = a->k_parts = 1;
   const long long rows = (long long)a->Tq * a->group, places = 512;
@@ -260,12 +268,13 @@ void plan_packed(PackedArgs* a, bool backward) {
     }
   }
   if (!backward || !k_tiles || !rows) return;
-  // Steps of 64 rows of all tiles of keys, were the sequences alike, over the places, and a little more, so that the last round is not
-  // a few workgroups; at most 16 parts of the longest sequence that there can be, and kPartBytes of them.
-  const long long row_steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + kKeyTile - 1) / kKeyTile * a->Hkv * ((row_steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
+  // Steps of 64 rows of all tiles of keys, were the sequences alike and their last tiles half full, over the places, and a little more,
+  // so that the last round is not a few workgroups; at most 128 parts of the longest sequence that there can be, and kPartBytes of them
+  // (where two parts take more, there are tiles for several rounds).
+  const long long row_steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + (a->S - 1) * (kKeyTile / 2ll) + kKeyTile - 1) / kKeyTile * a->Hkv * ((row_steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
   long long chunk = all / places + all / (places * 12) + 1;
   if (chunk < 16) chunk = 16;
-  if (chunk < (row_steps + 15) / 16) chunk = (row_steps + 15) / 16;
+  if (chunk < (row_steps + 127) / 128) chunk = (row_steps + 127) / 128;
   const long long part = 2ll * a->Tk * a->Hkv * a->d * 4, most = part > kPartBytes ? 1 : kPartBytes / part;    // bytes of one; as many as may be
   if (chunk < (row_steps + most - 1) / most) chunk = (row_steps + most - 1) / most;
   a->k_chunk = (int)chunk;

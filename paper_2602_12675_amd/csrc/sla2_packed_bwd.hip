@@ -4,6 +4,14 @@
 // Two kernels, so that every sum has one owner and a fixed order: one for each tile of rows (D and dQ), one for each tile of keys (dK
 // and dV, over the rows of all heads of the group).  Both form P and dO V^T themselves: 7 products in all for 5 that are needed, where
 // a sum of dQ over workgroups would take a d-wide row of fp32 written and read back for each tile of keys.
+//
+// In both a wave asks LDS for the operands of all products of 32 rows (keys) in one stream, some reads ahead of the products, and the
+// exponentials run beside the products of dP.  Causal, 40 heads on 8, 8,192 tokens in sequences of 4,096, 2,048, 1,026, 1,021 and 1
+// (118 GFLOP a product): rows 350 us = 1.0 PFLOP/s, keys 505 us = 0.94, sums of parts 35.  Bound by the matrix cores' and the vector
+// unit's work one behind the other (44 to 54 and 30 % busy; two waves a SIMD, their registers full) and, on the key side, by moving Q and
+// dO for every tile of keys (10 % of the two together without it).  d = 64, causal, 48 heads on 3, 1,767 tokens: 130 us, 142 with a
+// stream for each product.  Not faster: one wave a SIMD with 64 keys, half the reads of LDS (results of products in the second half of the
+// register file, copied out for every exponential: 1,001 us for 880), transfers spread between the products (904 for 834: spills).
 #include "packed.h"
 
 namespace sla2 {
@@ -467,6 +475,7 @@ __global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
     const int token = at.k0 + key0 + idx / (D / 4), c = idx % (D / 4) * 4;
     const float* p = src + ((size_t)token * a.Hkv + th.head) * D + c;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int i = p0; i <= p1; i++) sum += *reinterpret_cast<const f32x4*>(p + i * rows * D);
     bf16x4 r;
 #pragma unroll
@@ -497,7 +506,7 @@ template <int D> static hipError_t launch_bwd(const PackedArgs& a, hipStream_t s
     if (k) packed_dkv_kernel<D, true><<<dim3((unsigned)k_tiles, a.k_parts), 256, smem, stream>>>(a);
     else packed_dkv_kernel<D, false><<<(unsigned)k_tiles, 256, smem, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (k) packed_sum_kv_kernel<D><<<dim3((unsigned)k_tiles, 2, 4), 256, 0, stream>>>(a);
+    if (k) packed_sum_kv_kernel<D><<<dim3((unsigned)k_tiles, 2, k_tiles < 256 ? D / 8 : 4), 256, 0, stream>>>(a);   // few tiles: one sum a thread
   }
   return hipGetLastError();
 }
