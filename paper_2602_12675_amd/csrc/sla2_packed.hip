@@ -8,9 +8,9 @@
 // another's exponentials, first reads and results.
 //
 // Bound by the vector unit beside the matrix cores: 32 keys x 32 rows take 512 cycles of products (d = 128) and some 350 of maximum,
-// exponential, sum and rounding, which only overlap as far as two waves of a SIMD happen to be in different phases (busy 60 % and 50 %).
+// exponential, sum and rounding, which only overlap as far as two waves of a SIMD happen to be in different phases (busy 45 % and 48 % of the cycles).
 // Causal, 40 heads on 8, sequences of 4,096, 2,777, 1,021, 1 and 297: 280 us for 262 GFLOP = 0.94 PFLOP/s; 12 heads of 2 x 32,760
-// queries on 512 and 131 keys: 205 us for 129 GFLOP and 410 MB, 11 steps a tile between first reads and results that nothing of the
+// queries on 512 and 131 keys: 200 us for 129 GFLOP and 410 MB, 11 steps a tile between first reads and results that nothing of the
 // same tile covers.  K and V in two buffers each, one workgroup less a CU: 295 for 280.
 #include "packed.h"
 
@@ -273,7 +273,10 @@ void plan_packed(PackedArgs* a, bool backward) {
   // (where two parts take more, there are tiles for several rounds).
   const long long row_steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + (a->S - 1) * (kKeyTile / 2ll) + kKeyTile - 1) / kKeyTile * a->Hkv * ((row_steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
   long long chunk = all / places + all / (places * 12) + 1;
-  if (chunk < 16) chunk = 16;
+  // A part has some 5 us of its own and is written and read: 8 steps at least for one sequence (16 heads of 6,410 queries on 339 keys 119 us,
+  // with 16 127), 16 where the longest is not known (five of 171 to 2,991: 146, with 8 148 and with 5 163).
+  const long long least = a->S == 1 ? 8 : 16;
+  if (chunk < least) chunk = least;
   if (chunk < (row_steps + 127) / 128) chunk = (row_steps + 127) / 128;
   const long long part = 2ll * a->Tk * a->Hkv * a->d * 4, most = part > kPartBytes ? 1 : kPartBytes / part;    // bytes of one; as many as may be
   if (chunk < (row_steps + most - 1) / most) chunk = (row_steps + most - 1) / most;

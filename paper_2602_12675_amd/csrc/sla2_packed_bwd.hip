@@ -7,8 +7,8 @@
 //
 // In both a wave asks LDS for the operands of all products of 32 rows (keys) in one stream, some reads ahead of the products, and the
 // exponentials run beside the products of dP.  Causal, 40 heads on 8, 8,192 tokens in sequences of 4,096, 2,048, 1,026, 1,021 and 1
-// (118 GFLOP a product): rows 350 us = 1.0 PFLOP/s, keys 505 us = 0.94, sums of parts 35.  Bound by the matrix cores' and the vector
-// unit's work one behind the other (44 to 54 and 30 % busy; two waves a SIMD, their registers full) and, on the key side, by moving Q and
+// (118 GFLOP a product): rows 345 us = 1.0 PFLOP/s, keys 475 us = 1.0, sums of parts 37.  Bound by the matrix cores' and the vector
+// unit's work one behind the other (49 to 53 and 32 to 41 % busy; two waves a SIMD, their registers full) and, on the key side, by moving Q and
 // dO for every tile of keys (10 % of the two together without it).  d = 64, causal, 48 heads on 3, 1,767 tokens: 130 us, 142 with a
 // stream for each product.  Not faster: one wave a SIMD with 64 keys, half the reads of LDS (results of products in the second half of the
 // register file, copied out for every exponential: 1,001 us for 880), transfers spread between the products (904 for 834: spills).
