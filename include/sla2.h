@@ -432,7 +432,7 @@ size_t sla2_cache_workspace_bytes(const sla2_cache_params* params);
  *   q, out        [B, H, d];  lse_or_null   DEVICE float [B, H]
  *   length        DEVICE int32 [B]; what is over max_pages page_size is not read.  0 (or less): out = 0, lse = -inf
  * Tokens in a page that is not one of 0 .. pages - 1 are left out.  What lies behind a sequence's last token has no part in the result.  Codes are
- * exact in bf16; a token's scales meet its scores and its probability in fp32. */
+ * exact in bf16; a token's scales meet its scores and its probability in fp32, and a probability is two bf16 numbers in the product with V. */
 int sla2_cache_attention(const sla2_cache_params* params, const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                          const float* v_scale, const int32_t* length, const int32_t* page_table, void* out, float* lse_or_null,
                          void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -227,13 +227,16 @@ __device__ __forceinline__ void attend_blocks(const CacheArgs& a, int b, int hk,
         for (int i = 0; i < C; i++) oacc[i][r] *= cr;
       }
     }
-    bf16x8 pf;
+    // P (times the value's scale) as two bf16 numbers, the second what the first leaves: rounded to one, P would add half as much again to the
+    // error of rounding the result, and the second product is free beside the reads.
+    bf16x8 pf, pr;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-      const float p = fast_exp2(sc[j] * c1 - sums.m);
+      float p = fast_exp2(sc[j] * c1 - sums.m);
       sums.l += p;
-      if constexpr (QUANT == SLA2_QUANT_NONE) pf[j] = (__bf16)p;
-      else pf[j] = (__bf16)(p * vs[j]);
+      if constexpr (QUANT != SLA2_QUANT_NONE) p *= vs[j];
+      pf[j] = (__bf16)p;
+      pr[j] = (__bf16)(p - (float)pf[j]);
     }
     // ---- O += P V ----
     unsigned vb[8][C / 2];
@@ -253,6 +256,7 @@ __device__ __forceinline__ void attend_blocks(const CacheArgs& a, int b, int hk,
       for (int x = 0; x < 4; x++)
         v4[x] = __builtin_amdgcn_perm(vb[2 * x + 1][i / 2], vb[2 * x][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
       oacc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf, __builtin_bit_cast(bf16x8, v4), oacc[i], 0, 0, 0);
+      oacc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pr, __builtin_bit_cast(bf16x8, v4), oacc[i], 0, 0, 0);
     }
   }
 }
