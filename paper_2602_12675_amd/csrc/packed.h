@@ -24,6 +24,7 @@ struct PackedArgs {
   // The steps of a tile's inner loop are dealt to several workgroups, whose sums another kernel joins.  Of a tile of rows evenly to
   // q_parts; of a tile of keys k_chunk steps to each, k_parts at most.  1: none
   int q_parts, k_parts, k_chunk;
+  bool rows_first;                           // backward, in one launch: the workgroups of the rows before those of the keys
   // scratch.  Sums of parts: O or dQ [q_parts][rows][d], (m, l) [q_parts][rows][2], the rows of all key heads being [Hkv][Tq group]; dK and
   // dV [2][k_parts][Tk][Hkv][d]
   float *lse2, *delta;                       // backward: lse log2(e) and D of every row, see stat_at
@@ -31,6 +32,7 @@ struct PackedArgs {
 };
 
 constexpr int kRowTile = 128, kKeyTile = 128;        // rows, and keys, of a workgroup: 32 a wave
+constexpr int kPlaces = 512;                         // workgroups that are at work at a time: two a CU
 
 void plan_packed(PackedArgs* a, bool backward);
 hipError_t launch_packed_fwd(const PackedArgs& a, hipStream_t stream);

@@ -48,15 +48,15 @@ __device__ __forceinline__ u32x4 stat_read(unsigned base, int n) {
 }
 
 // D and dQ of 128 rows: S^T = K Q^T and dP^T = V dO^T (keys x rows), dQ^T += K^T dS^T, as in the forward pass with K in the place of V.
-template <int D, bool PARTS>
-__global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
+template <int D, bool PARTS, bool STATS>
+__device__ __forceinline__ void packed_dq(const PackedArgs& a, int bx, int by) {
   constexpr int NW = 4, KS = D / 16, ET = D / 32;
   typedef PackedBwdSmem<D> SM;
   typedef PackedTile<D> SL;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid % kWave, g = lane / 32;
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const TileHead th = tile_head(blockIdx.x, a.Hkv);
+  const TileHead th = tile_head(bx, a.Hkv);
   const int hk = th.head;
   TilePlace at = find_tile<false>(a, kRowTile, th.tile, lane);
   if (at.tile < 0) return;
@@ -73,8 +73,8 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
   int t_begin = 0, t_end = (keys + kTileTokens - 1) / kTileTokens;
   if (PARTS) {
     const int n = t_end;
-    t_begin = (int)((long long)n * blockIdx.y / a.q_parts);
-    t_end = (int)((long long)n * (blockIdx.y + 1) / a.q_parts);
+    t_begin = (int)((long long)n * by / a.q_parts);
+    t_end = (int)((long long)n * (by + 1) / a.q_parts);
   }
   auto kbuf = [&](int t) { return lds_address(smem) + (t & 1) * 2 * SM::kTile; };
   const unsigned lane_off = tile_lane_off<D, NW, SL>(a.skv.t, w, lane);
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
   delta = swap_halves_sum(delta);
   const float lse = a.lse[(size_t)h * a.Tq + token];
   const float l2 = lse == -INFINITY ? INFINITY : lse * kLog2e;   // a row that reads no key: P = 0
-  if (row < nr && g == 0 && (!PARTS || blockIdx.y == 0)) {
+  if (STATS && row < nr && g == 0 && (!PARTS || by == 0)) {
     const size_t st = stat_first(a, hk, at.s, at.q0) + stat_at(a, my.x, my.y);
     a.delta[st] = delta;
     a.lse2[st] = l2;
@@ -196,8 +196,8 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
     phase_barrier();
   }
   const int ln = (int)lane_again(), last_row = w_row + ln % 32;    // what is made of the lane's place is not kept through the loop
-  if (PARTS) {
-    const size_t part = (size_t)blockIdx.y * a.Tq * a.H + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + last_row;   // among the rows of all key heads
+  if (PARTS && a.q_parts > 1) {
+    const size_t part = (size_t)by * a.Tq * a.H + (size_t)hk * a.Tq * a.group + (size_t)at.q0 * a.group + last_row;   // among the rows of all key heads
     if (last_row < nr) store_part<D>(acc, a.part_o + part * D, ln / 32);
     return;
   }
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
 // dK and dV of 128 keys: S = Q K^T and dP = dO V^T (rows x keys), a key on lanes l and l + 32 with its row of K and V in registers;
 // dV^T += dO^T P and dK^T += Q^T dS, 64 rows a step, which arrive in LDS one step ahead.
 template <int D, bool PARTS>
-__global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
+__device__ __forceinline__ void packed_dkv(const PackedArgs& a, int bx, int by) {
   constexpr int NW = 4, KS = D / 16, ET = D / 32;
   typedef PackedBwdSmem<D> SM;
   typedef PackedTile<D> SL;
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   float* stat = reinterpret_cast<float*>(smem + SM::kStatOff);
   const int lane = threadIdx.x % kWave;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const TileHead th = tile_head(blockIdx.x, a.Hkv);
+  const TileHead th = tile_head(bx, a.Hkv);
   const int hk = th.head;
   const TilePlace at = find_tile<true>(a, kKeyTile, th.tile, lane);
   if (at.tile < 0) return;
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   bool parts = false;
   if (PARTS) {
     // chunks from the sequence's first row on, the same for all of its tiles: those at work at a time read the same rows
-    const int first = t_begin / a.k_chunk, last = max(first, (t_end - 1) / a.k_chunk), part = (int)blockIdx.y;
+    const int first = t_begin / a.k_chunk, last = max(first, (t_end - 1) / a.k_chunk), part = by;
     if (part < first || part > last) return;
     parts = first < last;
     t_begin = max(t_begin, part * a.k_chunk);
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   const int ln = (int)lane_again(), key = w_key + ln % 32, g = ln / 32;      // what is made of the lane's place is not kept through the loop
   if (parts) {
     if (key >= nk) return;
-    const size_t part = ((size_t)blockIdx.y * a.Tk + at.k0 + key) * a.Hkv + hk;
+    const size_t part = ((size_t)by * a.Tk + at.k0 + key) * a.Hkv + hk;
     store_part<D>(dk, a.part_kv + part * D, g);
     store_part<D>(dv, a.part_kv + ((size_t)a.k_parts * a.Tk * a.Hkv + part) * D, g);
     return;
@@ -439,6 +439,53 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
   const size_t to = (size_t)hk * a.skv.h + (size_t)(at.k0 + key) * a.skv.t;
   store_row<D>(dk, a.scale, a.dk + to, g, key < nk);
   store_row<D>(dv, 1.f, a.dv + to, g, key < nk);
+}
+
+template <int D, bool PARTS>
+__global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
+  packed_dq<D, PARTS, true>(a, blockIdx.x, blockIdx.y);
+}
+template <int D, bool PARTS>
+__global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
+  packed_dkv<D, PARTS>(a, blockIdx.x, blockIdx.y);
+}
+// Both in one launch, where the tiles of rows do not fill the GPU: those whose workgroups take longer first (plan_packed).  Five heads of sequences
+// of 171 to 2,991 tokens 128 us, one launch after the other 146; 5,966 and 4,062 296, 324; tens of queries of 16 heads on 12,832 keys 40, 48.  (Where
+// the rows fill it, reading out and dout once more would cost what it saves.)
+template <int D>
+__global__ __launch_bounds__(256, 2) void packed_both_kernel(PackedArgs a, int k_tiles, int q_tiles) {
+  const int keys = k_tiles * a.k_parts, rows = q_tiles * a.q_parts, n = blockIdx.x, rows_first = a.rows_first ? rows : 0;
+  const int r = rows_first ? n : n - keys;               // the number among the rows' workgroups
+  if (r >= 0 && r < rows) packed_dq<D, true, false>(a, r % q_tiles, r / q_tiles);
+  else packed_dkv<D, true>(a, (n - rows_first) % k_tiles, (n - rows_first) / k_tiles);
+}
+// .. what the keys' side needs of every row before: D and lse log2(e), D / 8 lanes a row.
+template <int D>
+__global__ __launch_bounds__(256) void packed_stats_kernel(PackedArgs a) {
+  constexpr int LANES = D / 8;
+  const TileHead th = tile_head(blockIdx.x, a.Hkv);
+  const TilePlace at = find_tile<false>(a, kRowTile, th.tile, threadIdx.x % kWave);
+  if (at.tile < 0) return;
+  const int row0 = at.tile * kRowTile + threadIdx.x / LANES, col = threadIdx.x % LANES * 8, nr = at.nq * a.group;
+#pragma unroll
+  for (int i = 0; i < kRowTile * LANES / 256; i++) {
+    const int row = row0 + i * (256 / LANES);
+    const int2 x = query_of(a, min(row, nr - 1));
+    const int h = th.head * a.group + x.y, token = at.q0 + x.x;
+    const size_t from = (size_t)h * a.so.h + (size_t)token * a.so.t + col;
+    const bf16x8 o = *reinterpret_cast<const bf16x8*>(a.out + from), g = *reinterpret_cast<const bf16x8*>(a.dout + from);
+    float d = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; e++) d += (float)o[e] * (float)g[e];
+#pragma unroll
+    for (int by = 1; by < LANES; by *= 2) d += __shfl_xor(d, by);
+    if (row < nr && col == 0) {
+      const float lse = a.lse[(size_t)h * a.Tq + token];
+      const size_t st = stat_first(a, th.head, at.s, at.q0) + stat_at(a, x.x, x.y);
+      a.delta[st] = d;
+      a.lse2[st] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    }
+  }
 }
 
 // Sums of the parts, four channels a thread: dQ (rows of all key heads), dK and dV.
@@ -486,28 +533,37 @@ __global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
 
 template <int D> static hipError_t launch_bwd(const PackedArgs& a, hipStream_t stream) {
   constexpr int smem = PackedBwdSmem<D>::kBytes;
-  static OncePerDevice once[4];
-  const void* kernels[4] = {(const void*)packed_dq_kernel<D, false>, (const void*)packed_dq_kernel<D, true>,
-                            (const void*)packed_dkv_kernel<D, false>, (const void*)packed_dkv_kernel<D, true>};
+  static OncePerDevice once[5];
+  const void* kernels[5] = {(const void*)packed_dq_kernel<D, false>, (const void*)packed_dq_kernel<D, true>, (const void*)packed_dkv_kernel<D, false>,
+                            (const void*)packed_dkv_kernel<D, true>, (const void*)packed_both_kernel<D>};
   const long long q_tiles = most_tiles((long long)a.Tq * a.group, a.S, kRowTile) * a.Hkv, k_tiles = most_tiles(a.Tk, a.S, kKeyTile) * a.Hkv;
   const int q = a.q_parts > 1, k = a.k_parts > 1;
-  if (hipError_t e = allow_dynamic_lds(once[q], kernels[q], smem); e != hipSuccess) return e;
-  if (hipError_t e = allow_dynamic_lds(once[2 + k], kernels[2 + k], smem); e != hipSuccess) return e;
-  if (q_tiles) {
-    if (q) packed_dq_kernel<D, true><<<dim3((unsigned)q_tiles, a.q_parts), 256, smem, stream>>>(a);
-    else packed_dq_kernel<D, false><<<(unsigned)q_tiles, 256, smem, stream>>>(a);
+  const long long all = q_tiles * a.q_parts + k_tiles * a.k_parts;
+  if (q_tiles && k_tiles && q_tiles <= kPlaces && all < 1 << 22) {
+    if (hipError_t e = allow_dynamic_lds(once[4], kernels[4], smem); e != hipSuccess) return e;
+    packed_stats_kernel<D><<<(unsigned)q_tiles, 256, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (q) {
-      packed_sum_q_kernel<D><<<(unsigned)(((long long)a.Tq * a.H * (D / 4) + 255) / 256), 256, 0, stream>>>(a);
+    packed_both_kernel<D><<<(unsigned)all, 256, smem, stream>>>(a, (int)k_tiles, (int)q_tiles);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  } else {
+    if (hipError_t e = allow_dynamic_lds(once[q], kernels[q], smem); e != hipSuccess) return e;
+    if (hipError_t e = allow_dynamic_lds(once[2 + k], kernels[2 + k], smem); e != hipSuccess) return e;
+    if (q_tiles) {
+      if (q) packed_dq_kernel<D, true><<<dim3((unsigned)q_tiles, a.q_parts), 256, smem, stream>>>(a);
+      else packed_dq_kernel<D, false><<<(unsigned)q_tiles, 256, smem, stream>>>(a);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (k_tiles) {
+      if (k) packed_dkv_kernel<D, true><<<dim3((unsigned)k_tiles, a.k_parts), 256, smem, stream>>>(a);
+      else packed_dkv_kernel<D, false><<<(unsigned)k_tiles, 256, smem, stream>>>(a);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
   }
-  if (k_tiles) {
-    if (k) packed_dkv_kernel<D, true><<<dim3((unsigned)k_tiles, a.k_parts), 256, smem, stream>>>(a);
-    else packed_dkv_kernel<D, false><<<(unsigned)k_tiles, 256, smem, stream>>>(a);
+  if (q_tiles && q) {
+    packed_sum_q_kernel<D><<<(unsigned)(((long long)a.Tq * a.H * (D / 4) + 255) / 256), 256, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (k) packed_sum_kv_kernel<D><<<dim3((unsigned)k_tiles, 2, k_tiles < 256 ? D / 8 : 4), 256, 0, stream>>>(a);   // few tiles: one sum a thread
   }
+  if (k_tiles && k) packed_sum_kv_kernel<D><<<dim3((unsigned)k_tiles, 2, k_tiles < 256 ? D / 8 : 4), 256, 0, stream>>>(a);   // few tiles: one sum a thread
   return hipGetLastError();
 }
 hipError_t launch_packed_bwd(const PackedArgs& a, hipStream_t stream) { return a.d == 128 ? launch_bwd<128>(a, stream) : launch_bwd<64>(a, stream); }
