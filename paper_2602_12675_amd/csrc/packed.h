@@ -33,6 +33,7 @@ struct PackedArgs {
 
 constexpr int kRowTile = 128, kKeyTile = 128;        // rows, and keys, of a workgroup: 32 a wave
 constexpr int kPlaces = 512;                         // workgroups that are at work at a time: two a CU
+constexpr int kMostOfKeys = 1 << 22;                 // workgroups of the keys, where those of the rows are in the same launch
 
 void plan_packed(PackedArgs* a, bool backward);
 hipError_t launch_packed_fwd(const PackedArgs& a, hipStream_t stream);

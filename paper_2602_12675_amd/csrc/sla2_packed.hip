@@ -255,7 +255,7 @@ void plan_packed(PackedArgs* a, bool backward) {
   const long long rows = (long long)a->Tq * a->group, places = kPlaces;
   const long long q_tiles = most_tiles(rows, a->S, kRowTile) * a->Hkv, k_tiles = most_tiles(a->Tk, a->S, kKeyTile) * a->Hkv;
   const long long longest = a->S == 1 ? a->Tk : a->S == 2 ? a->Tk * 3ll / 4 : 2ll * a->Tk / a->S, steps = (longest + kTileTokens - 1) / kTileTokens;
-  if (q_tiles && q_tiles <= places && steps) {
+  if (q_tiles && q_tiles <= places && steps && (!backward || k_tiles < kMostOfKeys)) {
     const double step = backward ? 1.5 : 1.1, bytes = (double)a->Tq * a->H * a->d * 8;
     double best = steps * step;
     for (int n = 2; n <= 64 && (n - 1) * q_tiles < 2 * places && n * 4 <= steps; n++) {
@@ -271,7 +271,8 @@ void plan_packed(PackedArgs* a, bool backward) {
   // Steps of 64 rows of all tiles of keys, were the sequences alike and their last tiles half full, over the places, and a little more,
   // so that the last round is not a few workgroups; at most 128 parts of the longest sequence that there can be, and kPartBytes of them
   // (where two parts take more, there are tiles for several rounds).
-  const long long row_steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, all = (a->Tk + (a->S - 1) * (kKeyTile / 2ll) + kKeyTile - 1) / kKeyTile * a->Hkv * ((row_steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
+  const long long row_steps = ((a->Tq + 15ll) / 16 * a->group + 3) / 4, tiles = (a->Tk + (a->S - 1) * (kKeyTile / 2ll) + kKeyTile - 1) / kKeyTile;
+  const long long all = tiles * a->Hkv * ((row_steps + a->S - 1) / a->S) / (a->causal ? 2 : 1);
   long long chunk = all / places + all / (places * 12) + 1;
   // A part has some 5 us of its own and is written and read: 8 steps at least for one sequence (16 heads of 6,410 queries on 339 keys 119 us,
   // with 16 127), 16 where the longest is not known (five of 171 to 2,991: 146, with 8 148 and with 5 163).
@@ -280,6 +281,8 @@ void plan_packed(PackedArgs* a, bool backward) {
   if (chunk < (row_steps + 127) / 128) chunk = (row_steps + 127) / 128;
   const long long part = 2ll * a->Tk * a->Hkv * a->d * 4, most = part > kPartBytes ? 1 : kPartBytes / part;    // bytes of one; as many as may be
   if (chunk < (row_steps + most - 1) / most) chunk = (row_steps + most - 1) / most;
+  const long long places_for = k_tiles < kMostOfKeys ? kMostOfKeys / k_tiles : 1;
+  if (chunk < (row_steps + places_for - 1) / places_for) chunk = (row_steps + places_for - 1) / places_for;
   a->k_chunk = (int)chunk;
   a->k_parts = (int)((row_steps + chunk - 1) / chunk);
   // rows dealt to several workgroups with more steps each than those of the keys have: 40 us for 54 (tens of queries on 12,832 keys), otherwise 67 for 76

@@ -48,7 +48,7 @@ __device__ __forceinline__ u32x4 stat_read(unsigned base, int n) {
 }
 
 // D and dQ of 128 rows: S^T = K Q^T and dP^T = V dO^T (keys x rows), dQ^T += K^T dS^T, as in the forward pass with K in the place of V.
-template <int D, bool PARTS, bool STATS>
+template <int D, bool PARTS>
 __device__ __forceinline__ void packed_dq(const PackedArgs& a, int bx, int by) {
   constexpr int NW = 4, KS = D / 16, ET = D / 32;
   typedef PackedBwdSmem<D> SM;
@@ -102,7 +102,7 @@ __device__ __forceinline__ void packed_dq(const PackedArgs& a, int bx, int by) {
   delta = swap_halves_sum(delta);
   const float lse = a.lse[(size_t)h * a.Tq + token];
   const float l2 = lse == -INFINITY ? INFINITY : lse * kLog2e;   // a row that reads no key: P = 0
-  if (STATS && row < nr && g == 0 && (!PARTS || by == 0)) {
+  if (!PARTS && row < nr && g == 0) {                  // PARTS: packed_stats_kernel has them
     const size_t st = stat_first(a, hk, at.s, at.q0) + stat_at(a, my.x, my.y);
     a.delta[st] = delta;
     a.lse2[st] = l2;
@@ -441,9 +441,9 @@ __device__ __forceinline__ void packed_dkv(const PackedArgs& a, int bx, int by) 
   store_row<D>(dv, 1.f, a.dv + to, g, key < nk);
 }
 
-template <int D, bool PARTS>
+template <int D>
 __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a) {
-  packed_dq<D, PARTS, true>(a, blockIdx.x, blockIdx.y);
+  packed_dq<D, false>(a, blockIdx.x, 0);
 }
 template <int D, bool PARTS>
 __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a) {
@@ -456,7 +456,7 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void packed_both_kernel(PackedArgs a, int k_tiles, int q_tiles) {
   const int keys = k_tiles * a.k_parts, rows = q_tiles * a.q_parts, n = blockIdx.x, rows_first = a.rows_first ? rows : 0;
   const int r = rows_first ? n : n - keys;               // the number among the rows' workgroups
-  if (r >= 0 && r < rows) packed_dq<D, true, false>(a, r % q_tiles, r / q_tiles);
+  if (r >= 0 && r < rows) packed_dq<D, true>(a, r % q_tiles, r / q_tiles);
   else packed_dkv<D, true>(a, (n - rows_first) % k_tiles, (n - rows_first) / k_tiles);
 }
 // .. what the keys' side needs of every row before: D and lse log2(e), D / 8 lanes a row.
@@ -533,24 +533,22 @@ __global__ __launch_bounds__(256) void packed_sum_kv_kernel(PackedArgs a) {
 
 template <int D> static hipError_t launch_bwd(const PackedArgs& a, hipStream_t stream) {
   constexpr int smem = PackedBwdSmem<D>::kBytes;
-  static OncePerDevice once[5];
-  const void* kernels[5] = {(const void*)packed_dq_kernel<D, false>, (const void*)packed_dq_kernel<D, true>, (const void*)packed_dkv_kernel<D, false>,
-                            (const void*)packed_dkv_kernel<D, true>, (const void*)packed_both_kernel<D>};
+  static OncePerDevice once[4];
+  const void* kernels[4] = {(const void*)packed_dkv_kernel<D, false>, (const void*)packed_dkv_kernel<D, true>, (const void*)packed_dq_kernel<D>,
+                            (const void*)packed_both_kernel<D>};
   const long long q_tiles = most_tiles((long long)a.Tq * a.group, a.S, kRowTile) * a.Hkv, k_tiles = most_tiles(a.Tk, a.S, kKeyTile) * a.Hkv;
   const int q = a.q_parts > 1, k = a.k_parts > 1;
-  const long long all = q_tiles * a.q_parts + k_tiles * a.k_parts;
-  if (q_tiles && k_tiles && q_tiles <= kPlaces && all < 1 << 22) {
-    if (hipError_t e = allow_dynamic_lds(once[4], kernels[4], smem); e != hipSuccess) return e;
+  if (q_tiles && k_tiles && q_tiles <= kPlaces && k_tiles < kMostOfKeys) {       // so it is wherever rows have parts
+    if (hipError_t e = allow_dynamic_lds(once[3], kernels[3], smem); e != hipSuccess) return e;
     packed_stats_kernel<D><<<(unsigned)q_tiles, 256, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    packed_both_kernel<D><<<(unsigned)all, 256, smem, stream>>>(a, (int)k_tiles, (int)q_tiles);
+    packed_both_kernel<D><<<(unsigned)(q_tiles * a.q_parts + k_tiles * a.k_parts), 256, smem, stream>>>(a, (int)k_tiles, (int)q_tiles);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   } else {
-    if (hipError_t e = allow_dynamic_lds(once[q], kernels[q], smem); e != hipSuccess) return e;
-    if (hipError_t e = allow_dynamic_lds(once[2 + k], kernels[2 + k], smem); e != hipSuccess) return e;
+    if (hipError_t e = allow_dynamic_lds(once[2], kernels[2], smem); e != hipSuccess) return e;
+    if (hipError_t e = allow_dynamic_lds(once[k], kernels[k], smem); e != hipSuccess) return e;
     if (q_tiles) {
-      if (q) packed_dq_kernel<D, true><<<dim3((unsigned)q_tiles, a.q_parts), 256, smem, stream>>>(a);
-      else packed_dq_kernel<D, false><<<(unsigned)q_tiles, 256, smem, stream>>>(a);
+      packed_dq_kernel<D><<<(unsigned)q_tiles, 256, smem, stream>>>(a);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (k_tiles) {
