@@ -215,6 +215,15 @@ def test_random_shapes(seed):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_rows_that_fill_the_gpu(d, causal):
+    """More tiles of rows than are at work at a time: rows and keys in launches of their own, keys whole, in parts, and of short sequences."""
+    run([1 + i % 2 for i in range(40)], [1 + i % 3 for i in range(40)], 16, 16, d, causal)
+    run([4300, 3], [200, 9], 16, 1, d, causal, layout="heads" if causal else "padded")
+    run([(5 * i) % 7 for i in range(300)], [(3 * i) % 5 for i in range(300)], 4, 2, d, causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_rows_dealt_to_several_workgroups_with_a_mask(d):
     """Long rows over few tiles of keys and few rows over many keys: parts of both, some of them empty, and sequences without parts."""
     run([1500, 3, 0], [200, 900, 5], 8, 1, d, True)
