@@ -274,6 +274,13 @@ def test_attention_of_many_lengths(quant):
 
 
 @pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_many_sequences_and_heads(quant, d):
+    """1,080 of them: their parts are joined a wave each."""
+    attend(quant, d, 36, 4, 32, [1900, 0, 3, 1100] + [29 * i % 90 for i in range(25)] + [1300], seed=10)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
 def test_attention_over_pages_that_are_none(quant):
     def bad(t):
         t[0, 0], t[0, 2], t[1, 0], t[1, 1] = -1, 2 ** 31 - 1, -2 ** 31, 2 ** 30
