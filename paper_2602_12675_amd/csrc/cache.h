@@ -18,8 +18,8 @@ struct CacheArgs {
   long long kv_h, kv_t, q_h, q_b, out_h, out_b;
   int B, H, Hkv, group, d, pages, page_shift, max_pages, tokens, quant;
   float scale;
-  // attention: the workgroups of a key head that share the tokens of all sequences (0: one for each sequence); with more than one, parts
-  // of sequences are in scratch: O [parts][2][H][d] fp32 and (m, l) [parts][2][H][2]
+  // attention: the workgroups of a key head that share the tokens of all sequences, at most (0: one for each sequence; cache_line.h); with
+  // more than one, parts of sequences are in scratch: O [parts][2][H][d] fp32 and (m, l) [parts][2][H][2]
   int parts;
   float *part_o, *part_ml;
 };

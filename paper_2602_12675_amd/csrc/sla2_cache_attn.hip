@@ -16,18 +16,14 @@
 #include <limits.h>
 
 #include "cache.h"
+#include "cache_line.h"
 #include "mfma_tiles.h"
 
 namespace sla2 {
 
-constexpr int kDecodeWaves = 4, kDecodeBlock = 32, kHeadRows = 16;
+constexpr int kDecodeWaves = 4;
 constexpr int kIdBlocks = 32;                // blocks whose pages a wave holds, one for 16 tokens a lane
 
-// What is worked on: the blocks of all sequences one behind the other, each sequence with kOverhead blocks' worth of time in front of its
-// own (first reads, the joining of the waves).  Of this line every one of a.parts workgroups (of a key head) has an equal stretch, whatever
-// the lengths: whole sequences, and at its two ends parts of one, which go into slot 0 (a sequence that began before the stretch) or
-// slot 1 (one that goes on behind it) of the workgroup.  (3, 12 and 24 blocks were slower.)
-constexpr int kOverhead = 6;
 __device__ __forceinline__ int tokens_of(const CacheArgs& a, int b) {
   return (int)min((long long)max(a.length[b], 0), (long long)a.max_pages << a.page_shift);
 }
@@ -276,9 +272,10 @@ __global__ __launch_bounds__(kDecodeWaves * kWave, 2) void cache_attention_kerne
   int b = blockIdx.x;
   if (a.parts) {
     const long long all = uniform64(line_length(a, lane));
-    x = all * blockIdx.x / a.parts;
-    y = all * (blockIdx.x + 1) / a.parts;
-    if (x == y) return;
+    const int parts = parts_of(a.parts, all), p = blockIdx.x;
+    if (p >= parts) return;
+    x = stretch_begin(all, parts, p);
+    y = stretch_begin(all, parts, p + 1);
     const OnLine o = on_line(a, x, -1, lane);
     b = __builtin_amdgcn_readfirstlane(o.b);
     at = uniform64(o.at);
@@ -289,7 +286,8 @@ __global__ __launch_bounds__(kDecodeWaves * kWave, 2) void cache_attention_kerne
     const long long first = at + kOverhead;                        // the place of its first block
     const bool begins = at >= x;
     at = first + nb;
-    const int lo = (int)min((long long)nb, max(0ll, x - first)), hi = (int)min((long long)nb, max(0ll, y - first));
+    const BlockRange r = blocks_in(x, y, first, nb);
+    const int lo = r.lo, hi = r.hi;
     if (lo >= hi && !(nb == 0 && begins)) continue;
     // Q as B operand: lane <- head l % 16, the channels that its reads of a key have
     bf16x8 qf[KS];
@@ -330,7 +328,7 @@ __global__ __launch_bounds__(kDecodeWaves * kWave, 2) void cache_attention_kerne
         o1 += by * part[x][row][c + 1];
       }
       if (lo > 0 || hi < nb) {
-        const size_t slot = ((size_t)blockIdx.x * 2 + (lo > 0 ? 0 : 1)) * a.H + h;
+        const size_t slot = part_slot(blockIdx.x, lo == 0) * a.H + h;
         *(float2*)(a.part_o + slot * D + c) = make_float2(o0, o1);
         if (c == 0) *(float2*)(a.part_ml + 2 * slot) = make_float2(m, l);
       } else {
@@ -357,10 +355,9 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void cache_join_kernel(CacheArg
   const int nb = blocks_of(tokens_of(a, b));
   if (!nb) return;
   const long long all = line_length(a, lane), first = on_line(a, 0, b, lane).at + kOverhead;
-  // workgroup p has place f of the line if all p / parts, rounded down, is the last of these up to f
-  const int p0 = (int)(((first + 1) * a.parts - 1) / all), p1 = (int)(((first + nb) * a.parts - 1) / all);
+  const int parts = parts_of(a.parts, all), p0 = part_at(all, parts, first), p1 = part_at(all, parts, first + nb - 1);
   if (p0 == p1) return;                                            // written by the one that had it
-  auto slot = [&](int p) { return ((size_t)p * 2 + (p == p0 ? 1 : 0)) * a.H + h; };
+  auto slot = [&](int p) { return part_slot(p, p == p0) * a.H + h; };
   float m = -INFINITY, l = 0.f, o[E] = {};
   if (h < a.H) {
     for (int p = p0 + lane; p <= p1; p += kWave) m = fmaxf(m, a.part_ml[2 * slot(p)]);
@@ -395,16 +392,8 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void cache_join_kernel(CacheArg
   if (a.lse && lane == 0) a.lse[(size_t)b * a.H + h] = any ? (m + log2f(l)) * (1.f / kLog2e) : -INFINITY;
 }
 
-// Sequences of at most 1,024 tokens: a workgroup each.  Longer ones: as many workgroups as two to a CU are, which share the line.  (The
-// line from 256 tokens on: four sequences of up to 300 15 us for 11; from 4,096: 17 of up to 2,284 39 us for 21.)
 void plan_cache_attention(CacheArgs* a) {
-  const long long most = (long long)a->max_pages << a->page_shift, heads = (long long)a->Hkv * ((a->group + kHeadRows - 1) / kHeadRows);
-  a->parts = 0;
-  if (most <= 1024) return;
-  const long long blocks = a->B * ((most + kDecodeBlock - 1) / kDecodeBlock);
-  long long parts = 512 / heads;
-  if (parts > blocks / 16) parts = blocks / 16;                    // 4 blocks a wave at least
-  a->parts = parts < 1 ? 1 : (int)parts;
+  a->parts = most_parts(a->B, (long long)a->max_pages << a->page_shift, (long long)a->Hkv * ((a->group + kHeadRows - 1) / kHeadRows));
 }
 
 hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t stream) {

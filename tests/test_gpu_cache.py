@@ -281,6 +281,22 @@ def test_attention_of_many_sequences_and_heads(quant, d):
 
 
 @pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lengths", [[33], [500], [1792], [33, 100], [33, 40, 17, 65], [0, 1, 1500, 0, 3, 200, 64, 129]])
+def test_attention_of_short_sequences_in_long_tables(quant, d, lengths):
+    """Tables reserved for 32,768 tokens: the lengths' line is shorter than the table gives workgroups, and all that is joined was written."""
+    attend(quant, d, 16, 8, 64, lengths, seed=11, wide=512 - -(-max(lengths) // 64))
+    attend(quant, d, 2, 1, 16, lengths, seed=12, wide=2048 - -(-max(lengths) // 16), q_layout="padded")
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_attention_of_many_short_sequences_in_long_tables(quant):
+    """1,200 sequences and heads, whose parts are joined a wave each."""
+    attend(quant, 64, 40, 8, 64, [1 + 41 * i % 170 for i in range(30)], seed=13, wide=125)
+    attend(quant, 128, 40, 2, 64, [1 + 41 * i % 170 for i in range(29)] + [2100], seed=14, wide=2000)
+
+
+@pytest.mark.parametrize("quant", QUANTS)
 def test_attention_over_pages_that_are_none(quant):
     def bad(t):
         t[0, 0], t[0, 2], t[1, 0], t[1, 1] = -1, 2 ** 31 - 1, -2 ** 31, 2 ** 30

@@ -247,3 +247,51 @@ def test_decoding_steps_in_a_graph(quant):
         write(), attend(want, ws)
         torch.cuda.synchronize()
         assert torch.equal(out, want), rep
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_a_stream_grows_in_a_table_reserved_for_it(quant):
+    """One captured step, replayed from the first token on, in a table of 131,072 tokens; the workspace is never clean."""
+    import torch
+    from paper_2602_12675_amd import api
+    B, H, Hkv, d, page, cols, own = 2, 8, 1, 128, 256, 512, 8                  # `own` pages of each sequence exist
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    ids = np.full((B, cols), -1, dtype=np.int32)
+    ids[:, :own] = np.random.default_rng(2).permutation(B * own).reshape(B, own)
+    table = dev(ids.tolist())
+    kv, scale = new_cache(torch, B * own, Hkv, page, d, quant)
+    kw = dict(k_scale=scale[0], v_scale=scale[1])
+    n = own * page
+    k, v = (torch.randn((B * n, Hkv, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    fill = api.make_cache_params(B, H, Hkv, d, B * own, page, cols, tokens=B * n, quant_mode=codes(api, quant))
+    api.sla2_cache_write(fill, k, v, table, *kv, start=dev([0, n, 2 * n]), **kw)
+    p = api.make_cache_params(B, H, Hkv, d, B * own, page, cols, quant_mode=codes(api, quant))
+    q = torch.randn((B, H, d), generator=gen, device="cuda").bfloat16()
+    out, lse, length = torch.zeros_like(q), torch.zeros((B, H), device="cuda"), dev([1, 1])
+    ws = torch.empty(api.sla2_cache_workspace_bytes(p), dtype=torch.uint8, device="cuda").fill_(255)
+
+    def attend(o, w):
+        api.sla2_cache_attention(p, q, *kv, table, length, o, lse=lse, workspace=w, **kw)
+
+    attend(out, ws)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        attend(out, ws)
+    held = [[stored(f64(x[b * n:(b + 1) * n]), quant)[0] for x in (k, v)] for b in range(B)]
+    for lengths in ([1, 1], [33, 2], [40, 100], [700, 33], [2000, 1500], [64, 2048], [2, 0]):
+        length.copy_(dev(lengths))
+        ws.fill_(255)
+        out.fill_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.zeros_like(out)
+        attend(want, torch.randint(0, 255, ws.shape, dtype=torch.uint8, device="cuda"))
+        assert torch.equal(out, want), lengths
+        for b, m in enumerate(lengths):
+            for h in range(H):
+                o, l_, mag, sm = S.attend(f64(q)[b, h][None], held[b][0][:m, 0], held[b][1][:m, 0], np.ones((1, m), dtype=bool), d ** -0.5)
+                e = weight_error(d, max(m, 1), sm)
+                close(out[b, h][None], o, out_bound(o, mag, e[:, None]))
+                close(lse[b, h][None], l_, lse_bound(l_, e))
