@@ -360,11 +360,12 @@ typedef struct sla2_packed_params {
   int causal;                /* 1: query i of a sequence of n_q queries and n_k keys reads the keys 0 .. i + n_k - n_q (the last query
                                 all of them; one before the first key none); 0: all of its sequence */
   float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */
-  /* (head, token) element strides of q, dq; of k, v, dk, dv; of out, dout.  Both zero: contiguous [tokens, heads, d].  As in
-   * sla2_params; below 2^24 elements a token; (tokens_q + 128 sequences) H and (tokens_k + 128 sequences) H below 2^31 - 1024 */
+  /* (head, token) element strides of q, dq; of k, v, dk, dv; of out; of dout.  Both zero: contiguous [tokens, heads, d], dout_stride: those
+   * of out.  As in sla2_params; below 2^24 elements a token; (tokens_q + 128 sequences) H and (tokens_k + 128 sequences) H below 2^31 - 1024 */
   long long q_stride[2];
   long long kv_stride[2];
   long long out_stride[2];
+  long long dout_stride[2];
 } sla2_packed_params;
 
 /* Bytes of the workspace of sla2_packed_forward (backward = 0), or of sla2_packed_backward and sla2_packed_forward, one after the other

@@ -78,7 +78,8 @@ class PackedParams(ctypes.Structure):
     """struct sla2_packed_params"""
     _fields_ = [("sequences", ctypes.c_int), ("tokens_q", ctypes.c_int), ("tokens_k", ctypes.c_int), ("H", ctypes.c_int),
                 ("H_kv", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float),
-                ("q_stride", ctypes.c_longlong * 2), ("kv_stride", ctypes.c_longlong * 2), ("out_stride", ctypes.c_longlong * 2)]
+                ("q_stride", ctypes.c_longlong * 2), ("kv_stride", ctypes.c_longlong * 2), ("out_stride", ctypes.c_longlong * 2),
+                ("dout_stride", ctypes.c_longlong * 2)]
 
 
 class CacheParams(ctypes.Structure):
@@ -414,11 +415,11 @@ def sla2_norm_backward(params, x, dh, dx_out, dx, y=None, gate=None, out_weight=
 
 # ---- attention over packed sequences, and a paged cache of keys and values ---------------------------------------------
 def make_packed_params(sequences, tokens_q, tokens_k, H, H_kv, d, causal=False, scale=0.0, dtype=SLA2_BF16, q_stride=None, kv_stride=None,
-                       out_stride=None) -> PackedParams:
-    """scale of the scores: 0 = 1 / sqrt(d).  q_stride, kv_stride, out_stride: (head, token) element strides of q and dq, of k, v, dk and
-    dv, of out and dout; None = contiguous [tokens, heads, d]."""
+                       out_stride=None, dout_stride=None) -> PackedParams:
+    """scale of the scores: 0 = 1 / sqrt(d).  q_stride, kv_stride, out_stride, dout_stride: (head, token) element strides of q and dq, of k,
+    v, dk and dv, of out, of dout; None = contiguous [tokens, heads, d], dout_stride: those of out."""
     p = PackedParams(sequences, tokens_q, tokens_k, H, H_kv, d, dtype, int(causal), scale)
-    for dst, src in ((p.q_stride, q_stride), (p.kv_stride, kv_stride), (p.out_stride, out_stride)):
+    for dst, src in ((p.q_stride, q_stride), (p.kv_stride, kv_stride), (p.out_stride, out_stride), (p.dout_stride, dout_stride)):
         if src is not None:
             dst[:] = [int(x) for x in src]
     return p
@@ -444,26 +445,49 @@ def sla2_packed_workspace_bytes(params: PackedParams, backward=False) -> int:
 # of a structure takes a quarter of a small call's time).
 @functools.lru_cache(maxsize=256)
 def _packed_sizes(content):
-    """(elements of q, of k; element type; elements of q_start, of lse; whether q, k and out are contiguous)"""
+    """(elements of q, of k; element type; elements of q_start, of lse; whether q, k, out and dout are contiguous)"""
     p = PackedParams.from_buffer_copy(content)
     return (p.tokens_q * p.H * p.d, p.tokens_k * p.H_kv * p.d, _TYPES.get(p.dtype), p.sequences + 1, p.H * p.tokens_q,
-            p.q_stride[1] == 0, p.kv_stride[1] == 0, p.out_stride[1] == 0)
+            p.q_stride[1] == 0, p.kv_stride[1] == 0, p.out_stride[1] == 0, p.out_stride[1] == 0 and p.dout_stride[1] == 0)
 
 
 def sla2_packed_forward(params, q, k, v, q_start, k_start, out, lse=None, workspace=None, stream=None, check=True, ws_bytes=None) -> int:
-    nq, nk, dt, ns, nl, cq, ck, co = _packed_sizes(bytes(params))
+    nq, nk, dt, ns, nl, cq, ck, co, _ = _packed_sizes(bytes(params))
     return _call(_lib.sla2_packed_forward, params, (
         (q, dt, nq, cq), (k, dt, nk, ck), (v, dt, nk, ck), (q_start, torch.int32, ns, True), (k_start, torch.int32, ns, True),
         (out, dt, nq, co), (lse, torch.float32, nl, True), _scratch(workspace)), stream, check,
         _bytes(workspace, ws_bytes))
 
 
+def _is_view(t):
+    return isinstance(t, torch.Tensor) and not t.is_contiguous()
+
+
+def _with_strides_of(params, out, dout):
+    """params with the strides of out and dout, where it states neither's and one of them is a view [tokens_q, H, d] of another order: what
+    the forward pass kept and what a loss hands back come in orders of their own.  A view without such strides (one value or row for
+    all) is left to be refused as not contiguous."""
+    p = PackedParams.from_buffer_copy(params)
+    for dst, t in ((p.out_stride, out), (p.dout_stride, dout)):
+        if _is_view(t):
+            if t.dim() != 3 or t.shape != (p.tokens_q, p.H, p.d) or t.stride(2) != 1 or min(t.stride()) < 1:
+                return params
+            dst[:] = t.stride(1), t.stride(0)
+        else:
+            dst[:] = p.d, p.H * p.d
+    return p
+
+
 def sla2_packed_backward(params, q, k, v, q_start, k_start, out, lse, dout, dq, dk, dv, workspace=None, stream=None, check=True,
                          ws_bytes=None) -> int:
-    nq, nk, dt, ns, nl, cq, ck, co = _packed_sizes(bytes(params))
+    """Where params states strides neither of out nor of dout, each of the two may be a view [tokens_q, H, d] of any order of tokens and heads."""
+    nq, nk, dt, ns, nl, cq, ck, co, cg = _packed_sizes(bytes(params))
+    if co and cg and (_is_view(out) or _is_view(dout)):
+        params = _with_strides_of(params, out, dout)
+        co, cg = _packed_sizes(bytes(params))[7:]
     return _call(_lib.sla2_packed_backward, params, (
         (q, dt, nq, cq), (k, dt, nk, ck), (v, dt, nk, ck), (q_start, torch.int32, ns, True), (k_start, torch.int32, ns, True),
-        (out, dt, nq, co), (lse, torch.float32, nl, True), (dout, dt, nq, co), (dq, dt, nq, cq), (dk, dt, nk, ck),
+        (out, dt, nq, co), (lse, torch.float32, nl, True), (dout, dt, nq, cg), (dq, dt, nq, cq), (dk, dt, nk, ck),
         (dv, dt, nk, ck), _scratch(workspace)), stream, check, _bytes(workspace, ws_bytes))
 
 

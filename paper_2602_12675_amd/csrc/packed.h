@@ -17,7 +17,7 @@ struct PackedArgs {
   const float* lse;
   uint16_t *o, *dq, *dk, *dv;
   float* lse_out;
-  RowStrides sq, skv, so;
+  RowStrides sq, skv, so, sg;                // of q and dq; k, v, dk and dv; out; dout
   int S, Tq, Tk, H, Hkv, group, d;           // group: query heads of a key head
   bool causal;
   float scale;                               // of the scores

@@ -88,7 +88,7 @@ __device__ __forceinline__ void packed_dq(const PackedArgs& a, int bx, int by) {
   const int h = hk * a.group + my.y, token = at.q0 + my.x;
   {
     const uint16_t* src = a.q + (size_t)h * a.sq.h + (size_t)token * a.sq.t + 8 * g;
-    const uint16_t* gsrc = a.dout + (size_t)h * a.so.h + (size_t)token * a.so.t + 8 * g;
+    const uint16_t* gsrc = a.dout + (size_t)h * a.sg.h + (size_t)token * a.sg.t + 8 * g;
     const uint16_t* osrc = a.out + (size_t)h * a.so.h + (size_t)token * a.so.t + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) {
@@ -243,11 +243,11 @@ __device__ __forceinline__ void packed_dkv(const PackedArgs& a, int bx, int by) 
     const uint16_t *qp, *gp;
   };
   // How far a step of one block, and of four, goes on in the same queries and to later ones (elements; kept, not made again)
-  const long long q_row = (long long)kQueryBlock * a.sq.t, g_row = (long long)kQueryBlock * a.so.t;
+  const long long q_row = (long long)kQueryBlock * a.sq.t, g_row = (long long)kQueryBlock * a.sg.t;
   const int four_q = 4 / a.group, four_h = 4 % a.group;
-  const long long q_one = a.sq.h, g_one = a.so.h, q_wrap = kept(q_row - (a.group - 1) * a.sq.h), g_wrap = kept(g_row - (a.group - 1) * a.so.h);
-  const long long q_four = kept(four_q * q_row + four_h * a.sq.h), g_four = kept(four_q * g_row + four_h * a.so.h);
-  const long long q_four_wrap = kept(q_four + q_row - a.group * a.sq.h), g_four_wrap = kept(g_four + g_row - a.group * a.so.h);
+  const long long q_one = a.sq.h, g_one = a.sg.h, q_wrap = kept(q_row - (a.group - 1) * a.sq.h), g_wrap = kept(g_row - (a.group - 1) * a.sg.h);
+  const long long q_four = kept(four_q * q_row + four_h * a.sq.h), g_four = kept(four_q * g_row + four_h * a.sg.h);
+  const long long q_four_wrap = kept(q_four + q_row - a.group * a.sq.h), g_four_wrap = kept(g_four + g_row - a.group * a.sg.h);
   auto next = [&](Block b) {
     const bool wrap = b.h + 1 == a.group;
     return Block{b.q + wrap, wrap ? 0 : b.h + 1, b.qp + (wrap ? q_wrap : q_one), b.gp + (wrap ? g_wrap : g_one)};
@@ -266,7 +266,7 @@ __device__ __forceinline__ void packed_dkv(const PackedArgs& a, int bx, int by) 
     constexpr int kRows = 1024 / (D * 2), kInstrs = kTileTokens / kRows / NW;          // of a transfer; a wave's transfers
     const int ln = (int)lane_again(), row = w * kRows % kQueryBlock + ln / SL::kChunks;
     const unsigned col = 16u * (unsigned)((ln % SL::kChunks) ^ SL::swz(w * kRows + ln / SL::kChunks));
-    const unsigned q_off = (unsigned)row * (unsigned)a.sq.t * 2 + col, g_off = (unsigned)row * (unsigned)a.so.t * 2 + col;
+    const unsigned q_off = (unsigned)row * (unsigned)a.sq.t * 2 + col, g_off = (unsigned)row * (unsigned)a.sg.t * 2 + col;
     if (w < 2) dma_lane4((w == 0 ? a.lse2 : a.delta) + st0 + (size_t)t * kTileTokens, 4u * (unsigned)ln, lds_address(stat + (t & 1) * 128 + 64 * w));
     if (whole(b)) {
       if (kRows * NW > kQueryBlock && w * kRows >= kQueryBlock) b = next(b);
@@ -290,7 +290,7 @@ __device__ __forceinline__ void packed_dkv(const PackedArgs& a, int bx, int by) 
       if (valid < kQueryBlock) {
         const unsigned back = (unsigned)max(0, row - (valid - 1));
         qo -= back * (unsigned)a.sq.t * 2;
-        go -= back * (unsigned)a.so.t * 2;
+        go -= back * (unsigned)a.sg.t * 2;
       }
       dma_lane16(b.qp, qo, qbuf(t) + (i * NW + w) * 1024);
       dma_lane16(b.gp, go, qbuf(t) + SM::kTile + (i * NW + w) * 1024);
@@ -309,7 +309,7 @@ __device__ __forceinline__ void packed_dkv(const PackedArgs& a, int bx, int by) 
   };
   Block cur{t_begin * 4 / a.group, t_begin * 4 % a.group, nullptr, nullptr};
   cur.qp = a.q + (size_t)(hk * a.group + cur.h) * a.sq.h + ((size_t)at.q0 + cur.q * kQueryBlock) * a.sq.t;
-  cur.gp = a.dout + (size_t)(hk * a.group + cur.h) * a.so.h + ((size_t)at.q0 + cur.q * kQueryBlock) * a.so.t;
+  cur.gp = a.dout + (size_t)(hk * a.group + cur.h) * a.sg.h + ((size_t)at.q0 + cur.q * kQueryBlock) * a.sg.t;
   if (t_begin < t_end) request(t_begin, cur);
   bf16x8 kf[KS], vf[KS];
   {
@@ -472,8 +472,8 @@ __global__ __launch_bounds__(256) void packed_stats_kernel(PackedArgs a) {
     const int row = row0 + i * (256 / LANES);
     const int2 x = query_of(a, min(row, nr - 1));
     const int h = th.head * a.group + x.y, token = at.q0 + x.x;
-    const size_t from = (size_t)h * a.so.h + (size_t)token * a.so.t + col;
-    const bf16x8 o = *reinterpret_cast<const bf16x8*>(a.out + from), g = *reinterpret_cast<const bf16x8*>(a.dout + from);
+    const bf16x8 o = *reinterpret_cast<const bf16x8*>(a.out + (size_t)h * a.so.h + (size_t)token * a.so.t + col);
+    const bf16x8 g = *reinterpret_cast<const bf16x8*>(a.dout + (size_t)h * a.sg.h + (size_t)token * a.sg.t + col);
     float d = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; e++) d += (float)o[e] * (float)g[e];

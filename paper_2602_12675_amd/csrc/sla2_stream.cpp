@@ -63,13 +63,18 @@ static int make_packed(const sla2_packed_params* p, PackedArgs* a) {
   if (rc != SLA2_OK) return rc;
   if (p->sequences > 65535) return SLA2_EUNSUPPORTED;
   *a = PackedArgs{};
-  long long t[3];
+  long long t[4];
   if ((rc = row_strides(p->q_stride, p->tokens_q, p->H, p->d, &a->sq.h, &t[0])) != SLA2_OK) return rc;
   if ((rc = row_strides(p->kv_stride, p->tokens_k, p->H_kv, p->d, &a->skv.h, &t[1])) != SLA2_OK) return rc;
   if ((rc = row_strides(p->out_stride, p->tokens_q, p->H, p->d, &a->so.h, &t[2])) != SLA2_OK) return rc;
   a->sq.t = (int)t[0];
   a->skv.t = (int)t[1];
   a->so.t = (int)t[2];
+  a->sg = a->so;
+  if (p->dout_stride[0] || p->dout_stride[1]) {
+    if ((rc = row_strides(p->dout_stride, p->tokens_q, p->H, p->d, &a->sg.h, &t[3])) != SLA2_OK) return rc;
+    a->sg.t = (int)t[3];
+  }
   a->S = p->sequences;
   a->Tq = p->tokens_q;
   a->Tk = p->tokens_k;
@@ -88,6 +93,7 @@ static int make_packed(const sla2_packed_params* p, PackedArgs* a) {
 static View q_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tq, a.H, a.d, a.sq.h, a.sq.t); }
 static View kv_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tk, a.Hkv, a.d, a.skv.h, a.skv.t); }
 static View out_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tq, a.H, a.d, a.so.h, a.so.t); }
+static View dout_view(const PackedArgs& a, const void* p) { return rows_view(p, a.Tq, a.H, a.d, a.sg.h, a.sg.t); }
 static View starts_view(const PackedArgs& a, const int32_t* p) { return flat(p, 4, (long long)a.S + 1); }
 static View lse_view(const PackedArgs& a, const float* p) { return flat(a.Tq ? p : nullptr, 4, (long long)a.H * a.Tq); }
 
@@ -231,7 +237,7 @@ int sla2_packed_backward(const sla2_packed_params* params, const void* q, const 
     if (misaligned16(p)) return SLA2_EINVAL;
   if (misaligned4(q_start) || misaligned4(k_start) || misaligned4(lse)) return SLA2_EINVAL;
   const size_t need = packed_layout(&a, true, workspace);
-  const View in[8] = {q_view(a, q), kv_view(a, k), kv_view(a, v), out_view(a, out), out_view(a, dout), lse_view(a, lse),
+  const View in[8] = {q_view(a, q), kv_view(a, k), kv_view(a, v), out_view(a, out), dout_view(a, dout), lse_view(a, lse),
                       starts_view(a, q_start), starts_view(a, k_start)};
   const Output outs[4] = {{q_view(a, dq), {}}, {kv_view(a, dk), {}}, {kv_view(a, dv), {}}, {flat(workspace, 1, (long long)need), {}}};
   if (aliased(outs, 4, in, 8)) return SLA2_EALIAS;

@@ -184,6 +184,35 @@ def test_gradients_in_one_buffer_and_empty_sides():
     assert not bool(dq.any())
 
 
+@pytest.mark.parametrize("case", [([70, 2, 131], [90, 2, 131], 6, 2, 64, True), ([300, 41], [1500, 900], 2, 2, 128, False), ([40, 1], [2600, 4], 4, 1, 64, True),
+                                  ([4300, 3], [200, 9], 16, 1, 128, False), ([2300], [150], 32, 32, 64, False)])
+def test_out_and_dout_in_orders_of_their_own(case):
+    """What the forward pass kept is head-major, what the loss hands back token-major, or the other way around: the same bits as of contiguous
+    copies, by strides that are stated and by those of the views.  All launches of the backward pass are reached."""
+    import torch
+    from paper_2602_12675_amd import api
+    p, t, _ = run(*case)
+    q, k, v, qs, ks, out, lse, dout, dq, dk, dv = t
+    T, H, d = q.shape
+    ws = torch.empty(api.sla2_packed_workspace_bytes(p, True), dtype=torch.uint8, device="cuda")
+
+    def of(layout, x):
+        y, st, _ = rows_like(T, H, d, layout)
+        y.copy_(x)
+        return y, st or (d, H * d)
+    for a, b in (("heads", "plain"), ("plain", "heads"), ("padded", "heads"), ("heads", "padded")):
+        (o, so), (g, sg) = of(a, out), of(b, dout)
+        stated = api.make_packed_params(p.sequences, T, k.shape[0], H, k.shape[1], d, causal=bool(p.causal), out_stride=so, dout_stride=sg)
+        for params in (p, stated):
+            got = [torch.full_like(x, 5) for x in (dq, dk, dv)]
+            ws.fill_(255)
+            api.sla2_packed_backward(params, q, k, v, qs, ks, o, lse, g, *got, workspace=ws)
+            for x, y in zip(got, (dq, dk, dv)):
+                assert torch.equal(x, y), (a, b)
+    one = torch.ones((), dtype=torch.bfloat16, device="cuda").expand(T, H, d)
+    assert api.sla2_packed_backward(p, q, k, v, qs, ks, out, lse, one, dq, dk, dv, workspace=ws, check=False) == api.SLA2_EINVAL
+
+
 @pytest.mark.parametrize("case", [([700], [700], 4, 2, 128, True), ([300, 41], [1500, 900], 2, 2, 64, False), ([9], [5000], 2, 1, 128, False),
                                   ([1], [3000], 4, 4, 64, True), ([2500], [70], 3, 3, 128, False), ([1200], [1200], 2, 1, 64, True),
                                   ([5, 900, 1], [5, 2000, 700], 8, 2, 128, True)])

@@ -120,6 +120,42 @@ def test_packed_tensors_that_are_refused():
     assert forward(packed(), q_start=torch.zeros(4, dtype=torch.int64)) == EINVAL
 
 
+def test_dout_in_an_order_of_its_own():
+    """out head-major, dout token-major: each is held to its own strides, in what is refused and in what may overlap."""
+    for kw, status in ((dict(dout_stride=(64, 0)), EINVAL), (dict(dout_stride=(0, 256)), EINVAL), (dict(dout_stride=(-64, 256)), EINVAL),
+                       (dict(dout_stride=(68, 256)), EUNSUPPORTED), (dict(dout_stride=(64, 56)), EUNSUPPORTED),
+                       (dict(dout_stride=(64, 1 << 24)), EUNSUPPORTED)):
+        p = packed(**kw)
+        assert api.sla2_packed_workspace_bytes(p, True) == 0 and backward(p) == status, kw
+    size = 10 * 4 * 64 * 2
+    p = packed(out_stride=(10 * 64, 64), dout_stride=(128, 512))             # dout: 9 x 512 + 3 x 128 + 64 elements, 10,112 bytes
+    assert backward(p, ws_bytes=0) == EWORKSPACE
+    assert backward(p, dq=DO + size, ws_bytes=0) == EALIAS                     # past what it would have with the strides of out
+    assert backward(p, dq=OUT + size, ws_bytes=0) == EWORKSPACE
+    assert backward(packed(out_stride=(128, 512)), dq=DO + size, ws_bytes=0) == EALIAS        # not stated: those of out
+
+
+def test_strides_that_a_view_brings():
+    """The backward call of the binding states the strides of out and dout where they are views in another order; not those of a value or a row
+    that stands for all, which stay refused."""
+    T, H, d = 10, 4, 64
+    plain, heads = torch.zeros(T, H, d, dtype=torch.bfloat16), torch.zeros(H, T, d, dtype=torch.bfloat16).transpose(0, 1)
+    rows = torch.zeros(T, 3, H, d, dtype=torch.bfloat16)[:, 1]
+
+    def stated(out, dout):
+        p = api._with_strides_of(packed(), out, dout)
+        return tuple(p.out_stride), tuple(p.dout_stride)
+    flat = (d, H * d)
+    assert stated(heads, plain) == ((T * d, d), flat) and stated(plain, heads) == (flat, (T * d, d)) and stated(rows, heads) == ((d, 3 * H * d), (T * d, d))
+    assert stated(OUT, heads) == (flat, (T * d, d))                            # an address is taken as it is: contiguous
+    nothing = ((0, 0), (0, 0))
+    for bad in (torch.zeros((), dtype=torch.bfloat16).expand(T, H, d), torch.zeros(d, dtype=torch.bfloat16).expand(T, H, d),
+                torch.zeros(T, 1, d, dtype=torch.bfloat16).expand(T, H, d), torch.zeros(T, H, 2 * d, dtype=torch.bfloat16)[..., ::2],
+                torch.zeros(T + 1, H, 2 * d, dtype=torch.bfloat16)[..., :d], torch.zeros(T, 2 * H * d, dtype=torch.bfloat16)[:, ::2]):
+        assert stated(plain, bad) == nothing and stated(bad, plain) == nothing
+    assert not api._is_view(plain) and not api._is_view(OUT) and not api._is_view(None) and api._is_view(heads)
+
+
 # ---- cache ----
 KC, VC, SK, SV, FIRST, TABLE, LEN = (i << 28 for i in range(1, 8))
 FP8, INT8, NONE = api.SLA2_QUANT_FP8, api.SLA2_QUANT_INT8, api.SLA2_QUANT_NONE
