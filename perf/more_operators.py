@@ -154,7 +154,7 @@ def _prepare_packed(case, gen):
     if case["kind"] == "packed_bwd":
         s["dout"] = _normal(gen, (sum(nq), H, d), 0.1)
         out, s["lse"] = _attend(s)                                 # what the forward pass kept
-        s["out"] = out.to(torch.bfloat16).contiguous()
+        s["out"] = out.to(torch.bfloat16)
         s["dq"] = torch.empty_like(s["q"])
         t = torch.empty((sum(nk), 3, H_kv, d) if case["joint"] else (3, sum(nk), H_kv, d), dtype=torch.bfloat16, device="cuda")
         s["dk"], s["dv"] = (t[:, 1], t[:, 2]) if case["joint"] else (t[1], t[2])
