@@ -401,7 +401,7 @@ typedef struct sla2_cache_params {
   int H, H_kv, d;            /* as in sla2_packed_params (H: sla2_cache_attention alone) */
   int pages, page_size;      /* page_size: 16, 32, 64, 128 or 256 */
   int max_pages;             /* columns of page_table: a sequence has max_pages page_size tokens (< 2^31) at most */
-  int tokens;                /* sla2_cache_write, _read: rows of k and v; >= 0, below 2^30 */
+  int tokens;                /* sla2_cache_write, _read: rows of k and v; >= 0, at most 2^30 - 64 */
   int dtype;                 /* SLA2_BF16: of q, k, v, out */
   int quant_mode;            /* SLA2_QUANT_NONE (the cache is bf16), _FP8 or _INT8 */
   float scale;               /* of the scores; 0: 1 / sqrt(d).  Finite, not negative */

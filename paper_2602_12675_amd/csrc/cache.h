@@ -24,6 +24,10 @@ struct CacheArgs {
   float *part_o, *part_ml;
 };
 
+// Rows of a workgroup that writes or reads, one for each lane of a wave while their places are looked up, and of a call: a launch has less
+// than 2^24 workgroups of 256 threads.
+constexpr int kCacheThreads = 256, kCacheRows = 64, kMostCacheTokens = ((1 << 24) - 1) * kCacheRows;
+
 void plan_cache_attention(CacheArgs* a);
 inline size_t cache_part_floats(const CacheArgs& a) { return a.parts > 1 ? (size_t)a.parts * 2 * a.H * (a.d + 2) : 0; }
 hipError_t launch_cache_write(const CacheArgs& a, hipStream_t stream);

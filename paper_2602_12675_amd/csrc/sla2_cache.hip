@@ -12,8 +12,6 @@
 
 namespace sla2 {
 
-constexpr int kCacheThreads = 256, kCacheRows = 64;      // rows of a workgroup: one for each lane of a wave while their places are looked up
-
 // Where row i of k and v is in the cache: page and slot; page -1: nowhere, -2: the row is of no sequence.  A row a lane, the rows of a
 // wave being neighbours.  Its sequence is the number of sequences that end at or in front of it, counted 64 at a time: for all rows at
 // once where no sequence ends between them.  (Offsets that do not ascend give some sequence, whose pages bound the place.)

@@ -106,7 +106,7 @@ static int make_cache(const sla2_cache_params* p, CacheArgs* a) {
   int shift = 0;
   while (shift < 9 && 1 << shift != p->page_size) shift++;
   if (shift < 4 || shift > 8) return SLA2_EUNSUPPORTED;
-  if (p->tokens >= 1 << 30 || p->quant_mode == SLA2_QUANT_FP8_V || p->B > 65535 || (long long)p->max_pages << shift > INT_MAX) return SLA2_EUNSUPPORTED;
+  if (p->tokens > kMostCacheTokens || p->quant_mode == SLA2_QUANT_FP8_V || p->B > 65535 || (long long)p->max_pages << shift > INT_MAX) return SLA2_EUNSUPPORTED;
   *a = CacheArgs{};
   a->table_stride = p->table_stride ? p->table_stride : p->max_pages;
   if (a->table_stride < p->max_pages) return SLA2_EINVAL;

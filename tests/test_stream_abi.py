@@ -198,6 +198,13 @@ def test_bad_cache_parameters(kw, status):
     assert write(p) == status and read(p) == status and attention(p) == status
 
 
+def test_most_rows_of_a_call():
+    """64 rows a workgroup of 256 threads: below 2^32 threads, what a launch may have."""
+    assert api.sla2_cache_workspace_bytes(cache(tokens=(1 << 30) - 64)) > 0
+    p = cache(tokens=(1 << 30) - 63)
+    assert api.sla2_cache_workspace_bytes(p) == 0 and write(p) == EUNSUPPORTED and read(p) == EUNSUPPORTED
+
+
 def test_bad_cache_pointers():
     p = cache()
     for fn, names in ((write, ("k", "v")), (read, ("k", "v")), (attention, ("q", "out", "length"))):
