@@ -501,7 +501,7 @@ def _cache_sizes(content):
     p = CacheParams.from_buffer_copy(content)
     rows = p.pages * p.H_kv * p.page_size
     return (p.B, _TYPES.get(p.dtype), p.tokens * p.H_kv * p.d, p.B * p.H * p.d, p.B * p.H, p.kv_stride[1] == 0, p.q_stride[1] == 0,
-            p.out_stride[1] == 0, _CODES.get(p.quant_mode, (None,)), rows * p.d, rows, 0 if p.table_stride else p.B * p.max_pages,
+            p.out_stride[1] == 0, _CODES.get(p.quant_mode, (None,)), rows * p.d, rows, p.B * p.max_pages,
             p.cache_stride[2] == 0, p.table_stride == 0)
 
 

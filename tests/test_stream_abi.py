@@ -248,3 +248,14 @@ def test_cache_tensors_that_are_refused():
         assert attention(p, k_cache=bad) == EINVAL
     assert write(p, page_table=torch.zeros(3, 4, dtype=torch.int64)) == EINVAL
     assert write(p, page_table=torch.zeros(2, 4, dtype=torch.int32)) == EINVAL
+
+
+def test_a_page_table_of_stated_stride_has_its_elements(monkeypatch):
+    """A table with room between its rows is held to its B max_pages elements, as other strided tensors are to theirs."""
+    seen = []
+    monkeypatch.setattr(api, "_call", lambda fn, params, tensors, *rest: seen.append(tensors) or 0)
+    p, t = cache(table_stride=9), torch.zeros(3, 9, dtype=torch.int32)[:, :4]
+    for fn in (write, read, attention):
+        assert fn(p, page_table=t) == 0
+        (_, dtype, count, dense), = [x for x in seen.pop() if x[0] is t]
+        assert (dtype, count, dense) == (torch.int32, 12, False) and t.numel() == count
