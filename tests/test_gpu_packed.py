@@ -154,6 +154,45 @@ def test_offsets_that_do_not_fit_stay_inside():
         assert bool((buf[:20] == 7).all()) and bool((buf[120:] == 7).all())
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("size", [(100, 100, 2, 1), (1500, 1100, 8, 1), (41, 2604, 4, 1), (1503, 1503, 3, 3), (4303, 209, 16, 1)])
+def test_offsets_that_do_not_fit_write_nothing_else(size, causal, d):
+    """Sequences that overlap, descend, begin below 0 or end behind the tensors, grouped heads, rows and keys dealt to several workgroups and
+    launches of both kinds: nothing around out, lse, the gradients and the workspace changes."""
+    import torch
+    from paper_2602_12675_amd import api
+    Tq, Tk, H, Hkv = size
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, g = (torch.randn((Tq, H, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn((Tk, Hkv, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    p = api.make_packed_params(4, Tq, Tk, H, Hkv, d, causal=causal)
+    room = 1 << 13
+    guarded = []
+
+    def inside(shape, dtype, fill):
+        n = int(np.prod(shape))
+        buf = torch.full((n + 2 * room,), fill, dtype=dtype, device="cuda")
+        guarded.append((buf, n, fill))
+        return buf[room:room + n].view(shape)
+    out, dq = (inside((Tq, H, d), torch.bfloat16, 7.0) for _ in range(2))
+    dk, dv = (inside((Tk, Hkv, d), torch.bfloat16, 7.0) for _ in range(2))
+    lse = inside((H, Tq), torch.float32, 7.0)
+    ws = [inside((api.sla2_packed_workspace_bytes(p, x),), torch.uint8, 0x77) for x in (False, True)]
+
+    def offsets(T):
+        far = 2 ** 31 - 1
+        return [[0, T // 3, T // 4, T + 50, T], [-7, T, 0, T, far], [T // 2, T // 4, far, -far - 1, T // 8], [0, T, 0, T, 0],
+                [0, 1, T - 1, T, T], [far, -1, far, -1, far], [T, T // 2, T // 3, T // 4, 0]]
+    for qs, ks in [(a, b) for i, a in enumerate(offsets(Tq)) for j, b in enumerate(offsets(Tk)) if (i + j) % 3 == 0 or i == j]:
+        tqs, tks = dev(qs), dev(ks)
+        api.sla2_packed_forward(p, q, k, v, tqs, tks, out, lse=lse, workspace=ws[0])
+        api.sla2_packed_backward(p, q, k, v, tqs, tks, out, lse, g, dq, dk, dv, workspace=ws[1])
+        torch.cuda.synchronize()
+        for buf, n, fill in guarded:
+            assert bool((buf[:room] == fill).all()) and bool((buf[room + n:] == fill).all()), (qs, ks)
+
+
 def test_gradients_in_one_buffer_and_empty_sides():
     """dq, dk and dv as slices of the gradient of one projection, with other numbers of heads; no queries, no keys."""
     import torch
