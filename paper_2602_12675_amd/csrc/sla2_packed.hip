@@ -4,14 +4,14 @@
 // pass over the keys, 64 at a time, with the running maximum and sum of the softmax: S^T = K Q^T (keys x rows), so that a lane holds
 // scores of one row, P^T goes back into O^T += V^T P^T as it lies in the registers, and a row's maximum and sum are its lane's own and
 // one exchange with the other half of the wave.  K and V tiles go from memory into LDS past the registers: V into one of two buffers,
-// a tile ahead, K into its one buffer behind the scores.  So two workgroups (d = 64: four) fit a CU, and one's products run beside
-// another's exponentials, first reads and results.
+// a tile ahead, K into its one buffer behind the scores.  Two workgroups (d = 64: four) are on a CU, as many as their registers allow, and one's
+// products run beside another's exponentials, first reads and results.
 //
 // Bound by the vector unit beside the matrix cores: 32 keys x 32 rows take 512 cycles of products (d = 128) and some 350 of maximum,
 // exponential, sum and rounding, which only overlap as far as two waves of a SIMD happen to be in different phases (busy 45 % and 48 % of the cycles).
 // Causal, 40 heads on 8, sequences of 4,096, 2,777, 1,021, 1 and 297: 280 us for 262 GFLOP = 0.94 PFLOP/s; 12 heads of 2 x 32,760
 // queries on 512 and 131 keys: 200 us for 129 GFLOP and 410 MB, 11 steps a tile between first reads and results that nothing of the
-// same tile covers.  K and V in two buffers each, one workgroup less a CU: 295 for 280.
+// same tile covers.
 #include "packed.h"
 
 namespace sla2 {

@@ -1,11 +1,15 @@
 // Backward pass of attention over packed sequences.  With P = exp(scale Q K^T - lse) and D = rowsum(dO . O):
 //   dV = P^T dO,   dS = P . (dO V^T - D),   dQ = scale dS K,   dK = scale dS^T Q.
 //
-// Two kernels, so that every sum has one owner and a fixed order: one for each tile of rows (D and dQ), one for each tile of keys (dK
+// Two sides, so that every sum has one owner and a fixed order: a workgroup for each tile of rows (dQ), one for each tile of keys (dK
 // and dV, over the rows of all heads of the group).  Both form P and dO V^T themselves: 7 products in all for 5 that are needed, where
 // a sum of dQ over workgroups would take a d-wide row of fp32 written and read back for each tile of keys.
 //
-// In both a wave asks LDS for the operands of all products of 32 rows (keys) in one stream, some reads ahead of the products, and the
+// Where the tiles of rows fill the GPU each side is a launch, and the rows' one, which comes first, forms D for the keys'.  Where they do not,
+// a small kernel forms D and both sides are in one launch; tiles of either side may then be dealt to several workgroups (tiles of keys in
+// both forms), whose sums one more kernel for each side joins.
+//
+// On both a wave asks LDS for the operands of all products of 32 rows (keys) in one stream, some reads ahead of the products, and the
 // exponentials run beside the products of dP.  Causal, 40 heads on 8, 8,192 tokens in sequences of 4,096, 2,048, 1,026, 1,021 and 1
 // (118 GFLOP a product): rows 345 us = 1.0 PFLOP/s, keys 475 us = 1.0, sums of parts 37.  Bound by the matrix cores' and the vector
 // unit's work one behind the other (49 to 53 and 32 to 41 % busy; two waves a SIMD, their registers full) and, on the key side, by moving Q and
